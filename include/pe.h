@@ -66,6 +66,7 @@ typedef int32_t pe_status;
 /* network element types */
 #define PE_F32 0
 #define PE_BF16 1
+#define PE_F16 2 /* token operators only */
 /* pe_rollout flags */
 #define PE_ROLLOUT_DETERMINISTIC 1 /* argmax action, lowest index on ties (Sec. 4.4 evaluation) */
 
@@ -414,6 +415,123 @@ pe_status pe_fleet_windows_noalloc(const float* traces, int32_t G, int32_t L,
                                    int64_t budget_q, int32_t* counts, int32_t* peaks,
                                    void* stream);
 
+/* ------------------------------------------------------------------------
+ * Token operators: the inner calls of the post-training that the controller
+ * governs, for callers that drive a live generator beside it instead of a
+ * replayed trace.  Generation (phase 0, Sec. 4.4), per token: pe_kv_append and
+ * pe_decode_attn.  Update (phase 1): pe_token_logp and its gradient, the
+ * log-probability and entropy of step a9 over a vocabulary instead of 16
+ * actions.  Element types: PE_BF16 and PE_F16, and PE_F32 for logits; sums,
+ * maxima and statistics are held in fp32 and results are rounded once.
+ * ------------------------------------------------------------------------ */
+
+/* A paged cache of keys and values: position p of sequence s is slot
+ * p % page_size of page table[s][p / page_size].  Element d of head h of slot
+ * i of page g is at g * page_stride + i * slot_stride + h * head_stride + d
+ * elements of k and of v, so that both [pages][slots][heads][D] and
+ * [pages][heads][slots][D] are caches.  A page id outside [0, n_pages) is no
+ * page: nothing is written to its positions, and they take no part in
+ * attention (an evicted or unassigned page).
+ *  k, v: device, 16-byte aligned; strides multiples of 8 elements;
+ *  table: [n_seqs] rows of max_pages int32, table_stride apart, device;
+ *  head_dim in {64, 128, 256}; page_size in [1, 65536];
+ *  max_pages * page_size < 2^31; dtype PE_BF16 or PE_F16. */
+typedef struct pe_kv_cache {
+  void* k;
+  void* v;
+  const int32_t* table;
+  int64_t n_pages, page_stride, slot_stride, head_stride; /* strides in elements */
+  int64_t table_stride;                                   /* in int32 entries */
+  int32_t n_seqs, max_pages, page_size, n_heads, head_dim, dtype;
+} pe_kv_cache;
+
+/* New tokens for the cache, of the cache's dtype and head_dim.  Strides are
+ * in elements (token, then head); a head's elements are adjacent. */
+typedef struct pe_kv_tokens {
+  const int32_t* pos;  /* [n_tokens] position in the sequence */
+  const int32_t* seq;  /* [n_tokens] sequence (row of the table); NULL: token t is of sequence t */
+  const float* rot;    /* [max_pos][rot_dim]: rot_dim/2 cosines, then rot_dim/2 sines; NULL if rot_dim = 0 */
+  const void* q;       /* [n_tokens][n_q_heads][D] queries, or NULL: none */
+  void* q_out;         /* rotated queries; may be q itself */
+  const void* k;       /* [n_tokens][n_heads][D] */
+  const void* v;
+  int64_t n_tokens, max_pos;
+  int64_t q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride;
+  int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+  int32_t n_q_heads, rot_dim, interleaved;
+} pe_kv_tokens;
+
+/* Append keys and values to the cache, rotating queries and keys by their
+ * position on the way.  With h = rot_dim / 2, c_i = rot[p][i] and
+ * s_i = rot[p][h + i], a pair (a, b) becomes (a c_i - b s_i, b c_i + a s_i);
+ * pair i is elements (i, i + h), or (2i, 2i + 1) where interleaved is set.
+ * Elements from rot_dim on, and values, are copied.
+ * A token whose position is outside [0, max_pos) (rot_dim > 0), negative or
+ * at or beyond the table's capacity, or whose sequence is outside
+ * [0, n_seqs), is padding: nothing is written to the cache and its q_out row
+ * becomes zero.  Two tokens at one position of one sequence leave either's.
+ *  rot_dim: 0, or a multiple of 16 up to D; every pointer to vectors 16-byte
+ *  aligned and their strides multiples of 8 elements; rot 16-byte aligned.
+ * Errors: PE_EINVAL, PE_ECUDA. */
+pe_status pe_kv_append(const pe_kv_cache* cache, const pe_kv_tokens* tokens, void* stream);
+
+/* Attention of one new token per sequence over the cache.  Sequence b has
+ * n = lens[b] positions (clamped to [0, max_pages * page_size]) and attends to
+ * j in [max(0, n - window), n), or to all of [0, n) where window is 0, less
+ * the positions of absent pages.  Query head h reads key head
+ * h / (n_q_heads / n_heads):
+ *   s_j = scale * q . k_j,  out = sum_j e^(s_j) v_j / sum_j e^(s_j),
+ *   lse = log sum_j e^(s_j).
+ * Where nothing is attended to (no position, or every score -inf), out is
+ * zero and lse -inf.  What lies in cache slots that are not attended to is
+ * not used, whatever it holds.
+ *  q, out: [n_seqs][n_q_heads][D] in the cache's dtype, strides in elements
+ *  (multiples of 8, 16-byte aligned); lens: [n_seqs] int32; lse:
+ *  [n_seqs][n_q_heads] fp32 or NULL; n_q_heads a multiple of n_heads.
+ *  workspace: >= pe_decode_attn_workspace_bytes(...) bytes of device memory,
+ *  256-byte aligned; its contents need not be kept between calls.
+ * Errors: PE_EINVAL, PE_ECUDA. */
+int64_t pe_decode_attn_workspace_bytes(const pe_kv_cache* cache, int32_t n_q_heads);
+pe_status pe_decode_attn(const pe_kv_cache* cache, const void* q, int64_t q_seq_stride, int64_t q_head_stride,
+                         int32_t n_q_heads, const int32_t* lens, float scale, int32_t window, void* out,
+                         int64_t out_seq_stride, int64_t out_head_stride, float* lse, void* workspace,
+                         int64_t workspace_bytes, void* stream);
+
+/* Log-probabilities of given tokens, with the entropy and the top_k most
+ * likely tokens of each row.  With z_j = scale * logits[r][j] (scale is an
+ * inverse temperature), m = max_j z_j and S = sum_j e^(z_j - m):
+ *   lse = m + ln S,  logp = z_t - lse,  entropy = ln S - sum_j e^(z_j - m) (z_j - m) / S.
+ * A token outside [0, V) is no target (padding): logp 0.  A logit of -inf is a
+ * forbidden token: probability 0, and log-probability -inf where it is the
+ * target.  A row of -inf alone has logp -inf (0 without a target), entropy 0
+ * and lse -inf.  A row with a NaN or +inf gives NaN.
+ *  logits: [n] rows of V elements (PE_F32, PE_BF16 or PE_F16), row_stride
+ *  elements apart, element-aligned; tokens: [n] int32;
+ *  logp, entropy, lse: [n] fp32, each may be NULL (logp needs tokens);
+ *  top_logp, top_id: [n][top_k] fp32 / int32, most likely first, equal logits
+ *  lowest index first (a NaN counts as the highest); top_k in [0, min(32, V)];
+ *  scale in [1e-4, 1e4].
+ * Errors: PE_EINVAL, PE_ECUDA. */
+pe_status pe_token_logp(const void* logits, int32_t dtype, int64_t n, int32_t V, int64_t row_stride,
+                        const int32_t* tokens, float scale, float* logp, float* entropy, float* lse, int32_t top_k,
+                        float* top_logp, int32_t* top_id, void* stream);
+
+/* Gradient of sum_r g_logp[r] logp[r] + g_entropy[r] entropy[r] in the logits,
+ * from pe_token_logp's lse and entropy of the same rows, with
+ * p_j = e^(z_j - lse):
+ *   dlogits_j = scale (g_logp (1[j = t] - p_j) - g_entropy p_j (ln p_j + entropy)).
+ * A row without a target has no g_logp term.  Forbidden tokens (-inf) get 0
+ * but for the target's own g_logp; a row of -inf alone (lse = -inf) gets 0.
+ *  g_logp, g_entropy: [n] fp32, either may be NULL (its term is absent;
+ *  tokens are then not needed, or entropy is not).
+ *  dlogits: [n] rows of V elements of the logits' dtype, d_row_stride apart;
+ *  may be the logits themselves (same pointer and stride).
+ * Errors: PE_EINVAL, PE_ECUDA. */
+pe_status pe_token_logp_grad(const void* logits, int32_t dtype, int64_t n, int32_t V, int64_t row_stride,
+                             const int32_t* tokens, float scale, const float* lse, const float* entropy,
+                             const float* g_logp, const float* g_entropy, void* dlogits, int64_t d_row_stride,
+                             void* stream);
+
 /* Launch profiling (off by default).  When enabled, every kernel launch of
  * the library is bracketed by a pair of CUDA events recorded on the launch's
  * stream; pe_profile_read waits for the recorded events of one kernel kind,
@@ -430,7 +548,11 @@ pe_status pe_fleet_windows_noalloc(const float* traces, int32_t G, int32_t L,
 #define PE_PROF_FLEET_WINDOWS 8
 #define PE_PROF_MLP_POLICY 9  /* tensor-core policy network launches (bf16 rollout) */
 #define PE_PROF_MLP_VALUE 10  /* tensor-core value network launches */
-#define PE_PROF_KINDS 11
+#define PE_PROF_KV_APPEND 11
+#define PE_PROF_DECODE_ATTN 12
+#define PE_PROF_TOKEN_LOGP 13
+#define PE_PROF_TOKEN_LOGP_GRAD 14
+#define PE_PROF_KINDS 15
 pe_status pe_profile_enable(int32_t on);
 pe_status pe_profile_read(int32_t kind, double* total_ms, int64_t* launches);
 const char* pe_profile_kind_name(int32_t kind);

@@ -20,13 +20,14 @@ LIB_PATH = os.path.join(_HERE, "_build", "libpe.so")
 _lib = None
 
 PE_OK, PE_EINVAL, PE_ENOMEM, PE_ECUDA, PE_EOVERFLOW, PE_ETIMEOUT, PE_ESTATE = range(7)
-PE_F32, PE_BF16 = 0, 1
+PE_F32, PE_BF16, PE_F16 = 0, 1, 2
 PE_ROLLOUT_DETERMINISTIC = 1
 MAX_LEVELS, MAX_CH = 32, 4
 (PE_PROF_ROLLOUT, PE_PROF_VALUE, PE_PROF_GAE, PE_PROF_PPO_GRAD, PE_PROF_PPO_REDUCE,
  PE_PROF_PPO_ADAM, PE_PROF_PPO_OTHER, PE_PROF_FLEET_PREP, PE_PROF_FLEET_WINDOWS,
- PE_PROF_MLP_POLICY, PE_PROF_MLP_VALUE) = range(11)
-PE_PROF_KINDS = 11
+ PE_PROF_MLP_POLICY, PE_PROF_MLP_VALUE, PE_PROF_KV_APPEND, PE_PROF_DECODE_ATTN, PE_PROF_TOKEN_LOGP,
+ PE_PROF_TOKEN_LOGP_GRAD) = range(15)
+PE_PROF_KINDS = 15
 
 
 class PEError(RuntimeError):
@@ -73,6 +74,20 @@ class PPOConfig(C.Structure):
         ("seed", C.c_uint64), ("iteration", C.c_uint32)]
 
 
+class KVCacheDesc(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "table")] + [
+        (n, C.c_int64) for n in ("n_pages", "page_stride", "slot_stride", "head_stride", "table_stride")] + [
+        (n, C.c_int32) for n in ("n_seqs", "max_pages", "page_size", "n_heads", "head_dim", "dtype")]
+
+
+class KVTokens(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("pos", "seq", "rot", "q", "q_out", "k", "v")] + [
+        (n, C.c_int64) for n in ("n_tokens", "max_pos", "q_token_stride", "q_head_stride", "q_out_token_stride",
+                                 "q_out_head_stride", "k_token_stride", "k_head_stride", "v_token_stride",
+                                 "v_head_stride")] + [
+        (n, C.c_int32) for n in ("n_q_heads", "rot_dim", "interleaved")]
+
+
 EXPORTS = (
     "pe_env_create", "pe_env_destroy", "pe_env_state_bytes", "pe_env_save", "pe_env_load",
     "pe_param_count", "pe_rollout_workspace_bytes", "pe_rollout", "pe_value_workspace_bytes",
@@ -80,6 +95,7 @@ EXPORTS = (
     "pe_ppo_update", "pe_fleet_workspace_bytes", "pe_fleet_windows", "pe_fleet_windows_noalloc",
     "pe_fleet_stagger_workspace_bytes", "pe_fleet_stagger", "pe_env_set_offsets", "pe_rollout_rule", "pe_rollout_replay", "pe_wait_selftest",
     "pe_dual_ascent", "pe_roof_probe",
+    "pe_kv_append", "pe_decode_attn_workspace_bytes", "pe_decode_attn", "pe_token_logp", "pe_token_logp_grad",
     "pe_profile_enable",
     "pe_profile_read", "pe_profile_kind_name", "pe_last_error")
 
@@ -122,6 +138,11 @@ def lib():
             "pe_fleet_windows_noalloc": (i32, [vp, i32, i32, vp, i32, vp, i64, i32, vp, i32, i64,
                                                vp, vp, vp]),
             "pe_roof_probe": (i32, [i32, vp, i64, i64, C.POINTER(C.c_double), C.POINTER(C.c_double), vp]),
+            "pe_kv_append": (i32, [vp, vp, vp]),
+            "pe_decode_attn_workspace_bytes": (i64, [vp, i32]),
+            "pe_decode_attn": (i32, [vp, vp, i64, i64, i32, vp, C.c_float, i32, vp, i64, i64, vp, vp, i64, vp]),
+            "pe_token_logp": (i32, [vp, i32, i64, i32, i64, vp, C.c_float, vp, vp, vp, i32, vp, vp, vp]),
+            "pe_token_logp_grad": (i32, [vp, i32, i64, i32, i64, vp, C.c_float, vp, vp, vp, vp, vp, i64, vp]),
             "pe_profile_enable": (i32, [i32]),
             "pe_profile_read": (i32, [i32, C.POINTER(C.c_double), C.POINTER(C.c_int64)]),
             "pe_profile_kind_name": (C.c_char_p, [i32]),
@@ -410,6 +431,156 @@ def fleet_windows_noalloc(traces, job_of_gpu, J: int, offsets, H: int, windows: 
     _check(lib().pe_fleet_windows_noalloc(_ptr(traces), G, L, _ptr(job_of_gpu), J, _ptr(offsets), N,
                                           H, w, len(windows), budget_q, _ptr(counts), _ptr(peaks),
                                           _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# token operators: generation over a paged cache, and scoring with its gradient
+# ---------------------------------------------------------------------------
+_DTYPE = {torch.float32: PE_F32, torch.bfloat16: PE_BF16, torch.float16: PE_F16}
+
+
+def _want(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _vec(name: str, t: torch.Tensor, n: int, dtype: torch.dtype) -> int:
+    """Device pointer of a contiguous vector of n elements."""
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{name} must be a contiguous {dtype} device tensor of {n} elements")
+    return t.data_ptr()
+
+
+def _heads(name: str, t: torch.Tensor, n: int, heads: int, like: torch.Tensor):
+    """(pointer, row stride, head stride) of an [n][heads][head_dim] tensor of the cache's dtype."""
+    sh, st = t.shape, t.stride()
+    if len(sh) != 3 or sh[0] != n or (heads and sh[1] != heads) or sh[2] != like.shape[3] or t.dtype != like.dtype \
+            or st[2] != 1 or not t.is_cuda:
+        raise ValueError(f"{name} must be a {like.dtype} device tensor of [{n}, {heads or 'heads'}, {like.shape[3]}] "
+                         "with adjacent elements")
+    return t.data_ptr(), st[0] if sh[0] > 1 else 0, st[1] if sh[1] > 1 else 0
+
+
+class KVCache:
+    """A paged cache of keys and values (pe_kv_cache): k and v are
+    [pages, slots, heads, head_dim] tensors of bf16 or fp16 with equal strides
+    (a transposed view of [pages, heads, slots, head_dim] storage will do),
+    table is [sequences, pages of a sequence] int32.  Holds the tensors; the
+    table's entries may change between calls."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor):
+        _want(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype
+              and k.dtype in (torch.bfloat16, torch.float16) and k.is_cuda and v.is_cuda and k.stride(3) == 1,
+              "k and v must be bf16 or fp16 device tensors of [pages, slots, heads, head_dim] with equal strides and "
+              "adjacent elements")
+        _want(table.dim() == 2 and table.dtype == torch.int32 and table.is_cuda and (table.shape[1] < 2 or table.stride(1) == 1),
+              "table must be an int32 device tensor of [sequences, pages] with adjacent entries")
+        self.k, self.v, self.table = k, v, table
+        st = [k.stride(i) if k.shape[i] > 1 else 0 for i in range(3)]
+        self.n_seqs, self.n_heads, self.head_dim, self.page_size = table.shape[0], k.shape[2], k.shape[3], k.shape[1]
+        self._desc = KVCacheDesc(k.data_ptr(), v.data_ptr(), table.data_ptr(), k.shape[0], st[0], st[1], st[2],
+                                 max(table.stride(0), table.shape[1]), table.shape[0], table.shape[1], k.shape[1],
+                                 k.shape[2], k.shape[3], _DTYPE[k.dtype])
+        self._ref = C.byref(self._desc)
+
+
+def rot_table(max_pos: int, rot_dim: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
+    """Rotation table of kv_append: row p holds cos(p f_i), then sin(p f_i),
+    with f_i = base^(-2 i / rot_dim), evaluated in fp64 and rounded to fp32."""
+    f = base ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64) / rot_dim)
+    ang = torch.arange(max_pos, dtype=torch.float64)[:, None] * f
+    return torch.cat([torch.cos(ang), torch.sin(ang)], 1).float().to(device)
+
+
+def kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor,
+              seqs: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+              q_out: Optional[torch.Tensor] = None, rot: Optional[torch.Tensor] = None, interleaved: bool = False,
+              stream=None):
+    """Append keys and values of new tokens ([tokens, heads, head_dim]) at
+    their positions (int32), rotating q (into q_out, default in place) and k
+    by position with rot ([positions, rot_dim], see rot_table); token t is of
+    sequence seqs[t], or t where seqs is None."""
+    n = positions.numel()
+    t = KVTokens(pos=_vec("positions", positions, n, torch.int32), n_tokens=n)
+    if seqs is not None:
+        t.seq = _vec("seqs", seqs, n, torch.int32)
+    t.k, t.k_token_stride, t.k_head_stride = _heads("k", k, n, cache.n_heads, cache.k)
+    t.v, t.v_token_stride, t.v_head_stride = _heads("v", v, n, cache.n_heads, cache.k)
+    if q is not None:
+        t.n_q_heads = q.shape[1]
+        t.q, t.q_token_stride, t.q_head_stride = _heads("q", q, n, 0, cache.k)
+        t.q_out, t.q_out_token_stride, t.q_out_head_stride = _heads("q_out", q if q_out is None else q_out, n, t.n_q_heads, cache.k)
+    if rot is not None:
+        _want(rot.dim() == 2 and rot.dtype == torch.float32 and rot.is_cuda and rot.is_contiguous(),
+              "rot must be a contiguous float32 device tensor of [positions, rot_dim]")
+        t.rot, t.max_pos, t.rot_dim, t.interleaved = rot.data_ptr(), rot.shape[0], rot.shape[1], int(interleaved)
+    _check(lib().pe_kv_append(cache._ref, C.byref(t), _stream(stream)))
+
+
+def decode_attn_workspace_bytes(cache: KVCache, n_q_heads: int) -> int:
+    return int(lib().pe_decode_attn_workspace_bytes(cache._ref, n_q_heads))
+
+
+def decode_attn(cache: KVCache, q: torch.Tensor, lens: torch.Tensor, out: torch.Tensor, scale: Optional[float] = None,
+                window: int = 0, lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                stream=None):
+    """out[b] = attention of q[b] ([sequences, query heads, head_dim]) over the
+    lens[b] (int32) positions of sequence b; scale defaults to head_dim^-1/2."""
+    n, hq = cache.n_seqs, q.shape[1]
+    qp, qs, qh = _heads("q", q, n, 0, cache.k)
+    op, os_, oh = _heads("out", out, n, hq, cache.k)
+    lp = _vec("lens", lens, n, torch.int32)
+    sp = None if lse is None else _vec("lse", lse, n * hq, torch.float32)
+    if workspace is None:
+        workspace = alloc_workspace(decode_attn_workspace_bytes(cache, hq))
+        if stream is not None:
+            workspace.record_stream(stream)  # used there, allocated here
+    _check(lib().pe_decode_attn(cache._ref, qp, qs, qh, hq, lp, cache.head_dim ** -0.5 if scale is None else scale,
+                                window, op, os_, oh, sp, workspace.data_ptr(), workspace.numel(), _stream(stream)))
+
+
+def _rows(name: str, t: torch.Tensor):
+    """(pointer, dtype, rows, columns, row stride) of a matrix of logits."""
+    if t.dim() != 2 or t.dtype not in _DTYPE or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a float32, bf16 or fp16 device tensor of [rows, V] with adjacent elements")
+    n, V = t.shape
+    return t.data_ptr(), _DTYPE[t.dtype], n, V, t.stride(0) if n > 1 else V
+
+
+def token_logp(logits: torch.Tensor, tokens: Optional[torch.Tensor], logp: Optional[torch.Tensor],
+               entropy: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+               top_logp: Optional[torch.Tensor] = None, top_id: Optional[torch.Tensor] = None, scale: float = 1.0,
+               stream=None):
+    """Log-probabilities (fp32) of tokens (int32, negative: no target) under
+    softmax(scale * logits), with the rows' entropies, log sums and top
+    alternatives (top_logp fp32 and top_id int32, [rows, k]) where asked for."""
+    p, dt, n, V, rs = _rows("logits", logits)
+    f = torch.float32
+    k = 0
+    if top_id is not None or top_logp is not None:
+        _want(top_id is not None and top_logp is not None and top_id.dim() == 2, "top_logp and top_id go together, [rows, k]")
+        k = top_id.shape[1]
+    _check(lib().pe_token_logp(
+        p, dt, n, V, rs, None if tokens is None else _vec("tokens", tokens, n, torch.int32), scale,
+        None if logp is None else _vec("logp", logp, n, f), None if entropy is None else _vec("entropy", entropy, n, f),
+        None if lse is None else _vec("lse", lse, n, f), k, None if not k else _vec("top_logp", top_logp, n * k, f),
+        None if not k else _vec("top_id", top_id, n * k, torch.int32), _stream(stream)))
+
+
+def token_logp_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor], lse: torch.Tensor, dlogits: torch.Tensor,
+                    g_logp: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                    g_entropy: Optional[torch.Tensor] = None, scale: float = 1.0, stream=None):
+    """dlogits = gradient of sum(g_logp logp) + sum(g_entropy entropy) in the
+    logits, from token_logp's lse and entropy; dlogits may be logits itself."""
+    p, dt, n, V, rs = _rows("logits", logits)
+    dp, ddt, dn, dV, ds = _rows("dlogits", dlogits)
+    _want(ddt == dt and dn == n and dV == V, "dlogits must have the logits' shape and dtype")
+    f = torch.float32
+    _check(lib().pe_token_logp_grad(
+        p, dt, n, V, rs, None if tokens is None else _vec("tokens", tokens, n, torch.int32), scale,
+        _vec("lse", lse, n, f), None if entropy is None else _vec("entropy", entropy, n, f),
+        None if g_logp is None else _vec("g_logp", g_logp, n, f),
+        None if g_entropy is None else _vec("g_entropy", g_entropy, n, f), dp, ds, _stream(stream)))
 
 
 def profile_enable(on: bool):
