@@ -484,7 +484,8 @@ pe_status pe_kv_append(const pe_kv_cache* cache, const pe_kv_tokens* tokens, voi
  *   lse = log sum_j e^(s_j).
  * Where nothing is attended to (no position, or every score -inf), out is
  * zero and lse -inf.  What lies in cache slots that are not attended to is
- * not used, whatever it holds.
+ * not used, whatever it holds.  An infinite value that is attended to makes
+ * its element infinite or NaN; a NaN or +inf score makes the head NaN.
  *  q, out: [n_seqs][n_q_heads][D] in the cache's dtype, strides in elements
  *  (multiples of 8, 16-byte aligned); lens: [n_seqs] int32; lse:
  *  [n_seqs][n_q_heads] fp32 or NULL; n_q_heads a multiple of n_heads.
