@@ -73,16 +73,14 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // hi and lo parts of two weights, packed
 template <typename T>
 __device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
-  const T ha = from_f32<T>(a), hb = from_f32<T>(b);
-  const T la = from_f32<T>(a - to_f32(ha)), lb = from_f32<T>(b - to_f32(hb));
-  hi = (uint32_t)__builtin_bit_cast(uint16_t, ha) | ((uint32_t)__builtin_bit_cast(uint16_t, hb) << 16);
-  lo = (uint32_t)__builtin_bit_cast(uint16_t, la) | ((uint32_t)__builtin_bit_cast(uint16_t, lb) << 16);
+  hi = pack2<T>(a, b);
+  const float2 h = unpack2<T>(hi);
+  lo = pack2<T>(a - h.x, b - h.y);
 }
 
 template <typename T>
 __device__ __forceinline__ void store2(T* p, float a, float b) {
-  *reinterpret_cast<uint32_t*>(p) = (uint32_t)__builtin_bit_cast(uint16_t, from_f32<T>(a)) |
-                                    ((uint32_t)__builtin_bit_cast(uint16_t, from_f32<T>(b)) << 16);
+  *reinterpret_cast<uint32_t*>(p) = pack2<T>(a, b);
 }
 
 // a segment crossing CTAs, as the joining kernel finds it at its first inner
