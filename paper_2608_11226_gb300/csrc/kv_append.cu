@@ -1,73 +1,121 @@
 // Keys and values of new tokens into a paged cache; queries and keys are
-// rotated by their position on the way (formulas: pe.h).  One thread per
-// element pair; HBM-bound: each row is read and written once.
+// rotated by their position on the way (formulas: pe.h).  HBM-bound: each row
+// is read and written once, two FMAs an element.
+//
+// A lane holds one item of a head, two 16-byte chunks whose elements pair up
+// under the rotation, and keeps its cosines and sines while it goes through
+// the token's heads (query heads, key heads, value heads in one line); the
+// chunks of kAhead heads are in flight at a time.
 #include "tokens.cuh"
 
 namespace pe {
 
-template <typename T>
-__global__ void __launch_bounds__(256) kv_append_kernel(pe_kv_cache c, pe_kv_tokens t) {
-  const int64_t tok = blockIdx.x;
-  const int D = c.head_dim, rot = t.rot_dim, half = rot / 2;
-  const int nq = t.q ? t.n_q_heads : 0;
-  const int s = t.seq ? t.seq[tok] : (int)tok;
+constexpr int kAppendWarps = 4, kAhead = 4;
+
+template <typename T, int D>
+__global__ void __launch_bounds__(32 * kAppendWarps) kv_append_kernel(pe_kv_cache c, pe_kv_tokens t, int steps) {
+  constexpr int kItems = D / 16, kHeads = 32 / kItems;  // items of a head; heads of a step
+  const int lane = threadIdx.x & 31, item = lane % kItems, sub = lane / kItems;
+  const int64_t tok = (int64_t)blockIdx.x * kAppendWarps + threadIdx.x / 32;
+  if (tok >= t.n_tokens) return;
+  const int nq = t.q ? t.n_q_heads : 0, nk = c.n_heads, heads = nq + 2 * nk;
   const int p = t.pos[tok];
-  const int64_t cap = (int64_t)c.max_pages * c.page_size;
-  const bool live = p >= 0 && p < cap && (rot == 0 || p < t.max_pos) && s >= 0 && s < c.n_seqs;
+  const int s = t.seq ? t.seq[tok] : (int)tok;
+  const int rot = t.rot_dim;
+  // chunks of the item, and whether they turn: pairs (i, i + rot/2) or neighbours
+  const bool turn = item < rot / 16;
+  const int c0 = t.interleaved || !turn ? 2 * item : item;
+  const int c1 = t.interleaved || !turn ? c0 + 1 : item + rot / 16;
+
+  const bool live = p >= 0 && p < c.max_pages * c.page_size && (rot == 0 || p < t.max_pos) && s >= 0 && s < c.n_seqs;
   int64_t slot = -1;
   if (live) {
     const int page = c.table[(int64_t)s * c.table_stride + p / c.page_size];
     if (page >= 0 && page < c.n_pages) slot = kv_page_offset(c, page) + (int64_t)(p % c.page_size) * c.slot_stride;
   }
-  const float* cs = t.rot + (int64_t)(live ? p : 0) * rot;
-  const int work = (nq + 2 * c.n_heads) * (D / 2);
-  for (int i = threadIdx.x; i < work; i += blockDim.x) {
-    const int head = i / (D / 2), j = i % (D / 2);
-    const T* src;
-    T* dst;
-    bool turn = true;
-    if (head < nq) {
-      src = (const T*)t.q + tok * t.q_token_stride + head * t.q_head_stride;
-      dst = (T*)t.q_out + tok * t.q_out_token_stride + head * t.q_out_head_stride;
-    } else if (head < nq + c.n_heads) {
-      src = (const T*)t.k + tok * t.k_token_stride + (head - nq) * t.k_head_stride;
-      dst = slot < 0 ? nullptr : (T*)c.k + slot + (head - nq) * c.head_stride;
-    } else {
-      const int h = head - nq - c.n_heads;
-      src = (const T*)t.v + tok * t.v_token_stride + h * t.v_head_stride;
-      dst = slot < 0 ? nullptr : (T*)c.v + slot + h * c.head_stride;
-      turn = false;
-    }
-    if (!dst) continue;
-    int e0, e1;  // pair j: rotated ones first, then the copied rest
-    if (j < half) {
-      e0 = t.interleaved ? 2 * j : j;
-      e1 = t.interleaved ? 2 * j + 1 : j + half;
-    } else {
-      e0 = 2 * j;
-      e1 = 2 * j + 1;
-      turn = false;
-    }
-    T a = src[e0], b = src[e1];
-    if (head < nq && !live) {
-      a = from_f32<T>(0.0f);
-      b = a;
-    } else if (turn) {
-      const float x = to_f32(a), y = to_f32(b), co = cs[j], si = cs[half + j];
-      a = from_f32<T>(x * co - y * si);
-      b = from_f32<T>(y * co + x * si);
-    }
-    dst[e0] = a;
-    dst[e1] = b;
+  float co[8], si[8];
+  if (live && turn) {
+    const float4* r = reinterpret_cast<const float4*>(t.rot + (int64_t)p * rot + 8 * item);
+    const float4 a = __ldg(r), b = __ldg(r + 1), x = __ldg(r + rot / 8), y = __ldg(r + rot / 8 + 1);
+    co[0] = a.x, co[1] = a.y, co[2] = a.z, co[3] = a.w, co[4] = b.x, co[5] = b.y, co[6] = b.z, co[7] = b.w;
+    si[0] = x.x, si[1] = x.y, si[2] = x.z, si[3] = x.w, si[4] = y.x, si[5] = y.y, si[6] = y.z, si[7] = y.w;
   }
+
+  const int begin = blockIdx.y * steps * kHeads + sub, end = min(heads, (int)(blockIdx.y + 1) * steps * kHeads);
+  for (int h0 = begin; h0 < end; h0 += kAhead * kHeads) {
+    uint4 x[kAhead], y[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int h = h0 + u * kHeads;
+      if (h >= end) break;
+      const T* src = h < nq        ? (const T*)t.q + tok * t.q_token_stride + h * t.q_head_stride
+                     : h < nq + nk ? (const T*)t.k + tok * t.k_token_stride + (h - nq) * t.k_head_stride
+                                   : (const T*)t.v + tok * t.v_token_stride + (h - nq - nk) * t.v_head_stride;
+      x[u] = *reinterpret_cast<const uint4*>(src + c0 * 8);
+      y[u] = *reinterpret_cast<const uint4*>(src + c1 * 8);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int h = h0 + u * kHeads;
+      if (h >= end) break;
+      T* dst;
+      if (h < nq)
+        dst = (T*)t.q_out + tok * t.q_out_token_stride + h * t.q_out_head_stride;
+      else if (slot < 0)
+        continue;
+      else
+        dst = h < nq + nk ? (T*)c.k + slot + (h - nq) * c.head_stride : (T*)c.v + slot + (h - nq - nk) * c.head_stride;
+      if (!live) {
+        x[u] = y[u] = make_uint4(0, 0, 0, 0);
+      } else if (turn && h < nq + nk) {
+        uint32_t* a = reinterpret_cast<uint32_t*>(&x[u]);
+        uint32_t* b = reinterpret_cast<uint32_t*>(&y[u]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 f = unpack2<T>(a[i]), g = unpack2<T>(b[i]);
+          if (t.interleaved) {
+            a[i] = pack2<T>(f.x * co[i] - f.y * si[i], f.y * co[i] + f.x * si[i]);
+            b[i] = pack2<T>(g.x * co[4 + i] - g.y * si[4 + i], g.y * co[4 + i] + g.x * si[4 + i]);
+          } else {
+            a[i] = pack2<T>(f.x * co[2 * i] - g.x * si[2 * i], f.y * co[2 * i + 1] - g.y * si[2 * i + 1]);
+            b[i] = pack2<T>(g.x * co[2 * i] + f.x * si[2 * i], g.y * co[2 * i + 1] + f.y * si[2 * i + 1]);
+          }
+        }
+      }
+      *reinterpret_cast<uint4*>(dst + c0 * 8) = x[u];
+      *reinterpret_cast<uint4*>(dst + c1 * 8) = y[u];
+    }
+  }
+}
+
+template <typename T, int D>
+static void go(const pe_kv_cache& c, const pe_kv_tokens& t, cudaStream_t st) {
+  constexpr int kHeads = 32 / (D / 16);
+  const int heads = (t.q ? t.n_q_heads : 0) + 2 * c.n_heads;
+  const int all = ceil_div(heads, kHeads);  // steps of a token
+  // a warp takes whole tokens where there are enough of them for 16 warps on
+  // each SM; fewer tokens are split by heads
+  const int64_t want = ceil_div(152 * 16, t.n_tokens);
+  const int parts = (int)(want < all ? want : all), steps = ceil_div(all, parts);
+  kv_append_kernel<T, D><<<dim3((unsigned)ceil_div(t.n_tokens, kAppendWarps), ceil_div(all, steps)), 32 * kAppendWarps, 0, st>>>(c, t, steps);
+}
+
+template <typename T>
+static void go_dim(const pe_kv_cache& c, const pe_kv_tokens& t, cudaStream_t st) {
+  if (c.head_dim == 64)
+    go<T, 64>(c, t, st);
+  else if (c.head_dim == 128)
+    go<T, 128>(c, t, st);
+  else
+    go<T, 256>(c, t, st);
 }
 
 pe_status kv_append_launch(const pe_kv_cache& c, const pe_kv_tokens& t, cudaStream_t st) {
   ProfScope ps(PE_PROF_KV_APPEND, st);
   if (c.dtype == PE_BF16)
-    kv_append_kernel<__nv_bfloat16><<<(unsigned)t.n_tokens, 256, 0, st>>>(c, t);
+    go_dim<__nv_bfloat16>(c, t, st);
   else
-    kv_append_kernel<__half><<<(unsigned)t.n_tokens, 256, 0, st>>>(c, t);
+    go_dim<__half>(c, t, st);
   PE_CHECK_LAUNCH("kv_append");
   return PE_OK;
 }

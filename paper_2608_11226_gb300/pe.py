@@ -439,6 +439,12 @@ def fleet_windows_noalloc(traces, job_of_gpu, J: int, offsets, H: int, windows: 
 _DTYPE = {torch.float32: PE_F32, torch.bfloat16: PE_BF16, torch.float16: PE_F16}
 
 
+def _stream_of(t: torch.Tensor, stream=None) -> int:
+    """The given stream, or the current one of the tensor's device (by its
+    handle alone: building a Stream object costs more than the launch)."""
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(t.get_device())
+
+
 def _want(ok: bool, what: str):
     if not ok:
         raise ValueError(what)
@@ -514,7 +520,7 @@ def kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, positions: torch
         _want(rot.dim() == 2 and rot.dtype == torch.float32 and rot.is_cuda and rot.is_contiguous(),
               "rot must be a contiguous float32 device tensor of [positions, rot_dim]")
         t.rot, t.max_pos, t.rot_dim, t.interleaved = rot.data_ptr(), rot.shape[0], rot.shape[1], int(interleaved)
-    _check(lib().pe_kv_append(cache._ref, C.byref(t), _stream(stream)))
+    _check(lib().pe_kv_append(cache._ref, C.byref(t), _stream_of(k, stream)))
 
 
 def decode_attn_workspace_bytes(cache: KVCache, n_q_heads: int) -> int:
@@ -536,7 +542,7 @@ def decode_attn(cache: KVCache, q: torch.Tensor, lens: torch.Tensor, out: torch.
         if stream is not None:
             workspace.record_stream(stream)  # used there, allocated here
     _check(lib().pe_decode_attn(cache._ref, qp, qs, qh, hq, lp, cache.head_dim ** -0.5 if scale is None else scale,
-                                window, op, os_, oh, sp, workspace.data_ptr(), workspace.numel(), _stream(stream)))
+                                window, op, os_, oh, sp, workspace.data_ptr(), workspace.numel(), _stream_of(q, stream)))
 
 
 def _rows(name: str, t: torch.Tensor):
@@ -564,7 +570,7 @@ def token_logp(logits: torch.Tensor, tokens: Optional[torch.Tensor], logp: Optio
         p, dt, n, V, rs, None if tokens is None else _vec("tokens", tokens, n, torch.int32), scale,
         None if logp is None else _vec("logp", logp, n, f), None if entropy is None else _vec("entropy", entropy, n, f),
         None if lse is None else _vec("lse", lse, n, f), k, None if not k else _vec("top_logp", top_logp, n * k, f),
-        None if not k else _vec("top_id", top_id, n * k, torch.int32), _stream(stream)))
+        None if not k else _vec("top_id", top_id, n * k, torch.int32), _stream_of(logits, stream)))
 
 
 def token_logp_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor], lse: torch.Tensor, dlogits: torch.Tensor,
@@ -580,7 +586,7 @@ def token_logp_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor], lse: t
         p, dt, n, V, rs, None if tokens is None else _vec("tokens", tokens, n, torch.int32), scale,
         _vec("lse", lse, n, f), None if entropy is None else _vec("entropy", entropy, n, f),
         None if g_logp is None else _vec("g_logp", g_logp, n, f),
-        None if g_entropy is None else _vec("g_entropy", g_entropy, n, f), dp, ds, _stream(stream)))
+        None if g_entropy is None else _vec("g_entropy", g_entropy, n, f), dp, ds, _stream_of(logits, stream)))
 
 
 def profile_enable(on: bool):
