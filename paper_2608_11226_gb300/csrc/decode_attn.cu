@@ -24,8 +24,8 @@
 
 namespace pe {
 
-constexpr int kDecodeWarps = 4, kUnit = 16;
-constexpr int kDecodeCtas = 152 * 2;  // CTAs of the split: two on each SM
+constexpr int kUnit = 16;  // positions of a stage
+constexpr int kDecodeCtas = 152 * 2;  // CTAs of the split at most: two on each SM
 
 template <typename T> struct Mma;
 template <> struct Mma<__nv_bfloat16> {
@@ -91,7 +91,10 @@ struct SegMeta {
 
 template <int D, int NT, int HT>
 struct DecodeShape {
-  static constexpr int kTeams = kDecodeWarps / HT;
+  // eight warps where wide heads leave one CTA on an SM and its teams have several warps
+  static constexpr int kWarps = D == 256 && HT > 1 ? 8 : 4;
+  static constexpr int kTeams = kWarps / HT;
+  static constexpr int kCtas = D == 256 ? kDecodeCtas / 2 : kDecodeCtas;
   static constexpr int kTile = kTeams * kUnit;           // positions of a tile
   static constexpr int kHeads = 8 * NT * HT;             // query heads of a segment
   static constexpr int kUnitBytes = 2 * kUnit * D * 2;   // keys and values of a unit
@@ -103,7 +106,7 @@ struct DecodeShape {
   static constexpr int kRing = kTeams * kStages * kUnitBytes;
   static constexpr int kMerge = kTeams * kHeads * kPitch * 4;
   static constexpr int kSmem = kRing + kMerge + 2 * kTeams * kHeads * 4;
-  static_assert(kMerge >= 32 * kDecodeWarps * 8, "the prefix sums of the lengths lie there first");
+  static_assert(kMerge >= 32 * kWarps * 8, "the prefix sums of the lengths lie there first");
   static_assert(D == 256 ? kSmem <= 231000 : 2 * (kSmem + 1024 + 256) <= 233472, "shared memory of an SM");
 };
 
@@ -122,11 +125,11 @@ __device__ __forceinline__ void seq_range(const DecodeArgs& a, int b, int tile, 
 }
 
 template <typename T, int D, int NT, int HT>
-__global__ void __launch_bounds__(32 * kDecodeWarps, D == 256 ? 1 : 2)
+__global__ void __launch_bounds__(32 * DecodeShape<D, NT, HT>::kWarps, D == 256 ? 1 : 2)
     decode_attn_kernel(DecodeArgs a, int groups, int per_head, float* part, SegMeta* meta) {
   using S = DecodeShape<D, NT, HT>;
   using M = Mma<T>;
-  constexpr int kTeams = S::kTeams, kStages = S::kStages, kChunks = D / 8;
+  constexpr int kDecodeWarps = S::kWarps, kTeams = S::kTeams, kStages = S::kStages, kChunks = D / 8;
   extern __shared__ __align__(128) unsigned char smem[];
   int64_t* s_sum = reinterpret_cast<int64_t*>(smem + S::kRing);
   __shared__ int s_where[3];
@@ -251,6 +254,15 @@ __global__ void __launch_bounds__(32 * kDecodeWarps, D == 256 ? 1 : 2)
   for (int i = 0; i < kStages - 1; ++i) load();
 
   // -- computing
+  // ldmatrix places of the lane: row, and 16-byte column under the ring's
+  // swizzle, whose three bits repeat every 128 bytes of a row
+  uint32_t kat[4], vat[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int kr = lane & 15, vr = (lane & 7) + 8 * (lane / 16);
+    kat[i] = kr * (D * 2) + (((i * 2 + lane / 16) ^ (kr & 7)) << 4);
+    vat[i] = kUnit * D * 2 + vr * (D * 2) + (((i * 2 + ((lane >> 3) & 1)) ^ (vr & 7)) << 4);
+  }
   const float qscale = a.scale * 1.4426950408889634f;  // scores in powers of two
   uint32_t qf[D / 16][NT][2];
   float o[D / 16][NT][4], m[NT][2], l[NT][2];
@@ -283,23 +295,29 @@ __global__ void __launch_bounds__(32 * kDecodeWarps, D == 256 ? 1 : 2)
     else
       asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(32 * HT) : "memory");
     load();
-    const uint32_t kt = ring + stage * S::kUnitBytes, vt = kt + kUnit * D * 2;
+    const uint32_t unit = ring + stage * S::kUnitBytes;
     const uint32_t mask = s_mask[team][stage];
     stage = stage + 1 == kStages ? 0 : stage + 1;
     if (mask) {
-      float s[NT][4];
+      // two chains of products where one head tile gives only one
+      constexpr int kChains = NT == 1 ? 2 : 1;
+      float s[NT][4], s2[kChains][4];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.0f;
-      {
-        const int row = lane & 15;
+      for (int i = 0; i < 4; ++i) {
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          uint32_t f[4];
-          ldsm(f, kt + row * (D * 2) + (((kk * 2 + lane / 16) ^ (row & 7)) << 4));
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) M::mma(s[nt], f, qf[kk][nt][0], qf[kk][nt][1]);
-        }
+        for (int nt = 0; nt < NT; ++nt) s[nt][i] = 0.0f;
+        s2[kChains - 1][i] = 0.0f;
       }
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) {
+        uint32_t f[4];
+        ldsm(f, unit + kat[kk & 3] + (kk >> 2) * 128);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) M::mma(kChains == 2 && (kk & 1) ? s2[1] : s[nt], f, qf[kk][nt][0], qf[kk][nt][1]);
+      }
+      if (kChains == 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[0][i] += s2[kChains - 1][i];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -356,17 +374,14 @@ __global__ void __launch_bounds__(32 * kDecodeWarps, D == 256 ? 1 : 2)
           pl[nt][i] = transpose8(pl[nt][i]);
         }
       }
-      {
-        const int row = (lane & 7) + 8 * (lane / 16);
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          uint32_t f[4];
-          ldsm_t(f, vt + row * (D * 2) + (((kk * 2 + ((lane >> 3) & 1)) ^ (row & 7)) << 4));
+      for (int kk = 0; kk < D / 16; ++kk) {
+        uint32_t f[4];
+        ldsm_t(f, unit + vat[kk & 3] + (kk >> 2) * 128);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            M::mma(o[kk][nt], f, ph[nt][0], ph[nt][1]);
-            M::mma(o[kk][nt], f, pl[nt][0], pl[nt][1]);
-          }
+        for (int nt = 0; nt < NT; ++nt) {
+          M::mma(o[kk][nt], f, ph[nt][0], ph[nt][1]);
+          M::mma(o[kk][nt], f, pl[nt][0], pl[nt][1]);
         }
       }
     }
@@ -486,17 +501,12 @@ __global__ void __launch_bounds__(D / 2) decode_join_kernel(DecodeArgs a, int pe
 
 constexpr int64_t kMetaBytes = (kDecodeCtas * (int64_t)sizeof(SegMeta) + 255) / 256 * 256;
 
-// heads of a segment for a group of query heads: 8, 16, 32 (two warps of a
-// team share each unit), 64 (four do); wide heads take 8 per warp, for the
-// accumulators of 16 would not stay in registers
-static int seg_heads(int D, int group) {
-  if (group <= 8) return 8;
-  if (group <= 16) return 16;
-  return D == 256 || group > 32 ? (D == 256 ? 32 : 64) : 32;
-}
+// heads of a segment for a group of query heads: 8, or 16 in one warp; 32 and
+// 64 in the two or four warps of a team, which share each unit
+static int seg_heads(int group) { return group <= 8 ? 8 : group <= 16 ? 16 : group <= 32 ? 32 : 64; }
 
 int64_t decode_attn_ws_bytes(const pe_kv_cache& c, int n_q_heads) {
-  return kMetaBytes + 2 * kDecodeCtas * (int64_t)seg_heads(c.head_dim, n_q_heads / c.n_heads) * (c.head_dim + 2) * 4;
+  return kMetaBytes + 2 * kDecodeCtas * (int64_t)seg_heads(n_q_heads / c.n_heads) * (c.head_dim + 2) * 4;
 }
 
 template <typename T, int D, int NT, int HT>
@@ -508,25 +518,20 @@ static pe_status go(const DecodeArgs& a, void* ws, cudaStream_t st) {
   const int per_head = (group + S::kHeads - 1) / S::kHeads;
   SegMeta* meta = reinterpret_cast<SegMeta*>(ws);
   float* part = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + kMetaBytes);
-  kern<<<kDecodeCtas, 32 * kDecodeWarps, S::kSmem, st>>>(a, a.c.n_heads * per_head, per_head, part, meta);
+  kern<<<S::kCtas, 32 * S::kWarps, S::kSmem, st>>>(a, a.c.n_heads * per_head, per_head, part, meta);
   PE_CHECK_LAUNCH("decode_attn");
-  decode_join_kernel<T, D><<<dim3(kDecodeCtas, S::kHeads < group ? S::kHeads : group), D / 2, 0, st>>>(a, per_head, S::kHeads, part, meta);
+  decode_join_kernel<T, D><<<dim3(S::kCtas, S::kHeads < group ? S::kHeads : group), D / 2, 0, st>>>(a, per_head, S::kHeads, part, meta);
   PE_CHECK_LAUNCH("decode_join");
   return PE_OK;
 }
 
 template <typename T, int D>
 static pe_status go_heads(const DecodeArgs& a, void* ws, cudaStream_t st) {
-  const int n = seg_heads(D, a.n_q_heads / a.c.n_heads);
+  const int n = seg_heads(a.n_q_heads / a.c.n_heads);
   if (n == 8) return go<T, D, 1, 1>(a, ws, st);
-  if constexpr (D == 256) {
-    if (n == 16) return go<T, D, 1, 2>(a, ws, st);
-    return go<T, D, 1, 4>(a, ws, st);
-  } else {
-    if (n == 16) return go<T, D, 2, 1>(a, ws, st);
-    if (n == 32) return go<T, D, 2, 2>(a, ws, st);
-    return go<T, D, 2, 4>(a, ws, st);
-  }
+  if (n == 16) return go<T, D, 2, 1>(a, ws, st);
+  if (n == 32) return go<T, D, 2, 2>(a, ws, st);
+  return go<T, D, 2, 4>(a, ws, st);
 }
 
 template <typename T>
