@@ -435,7 +435,7 @@ pe_status pe_fleet_windows_noalloc(const float* traces, int32_t G, int32_t L,
  *  k, v: device, 16-byte aligned; strides multiples of 8 elements;
  *  table: [n_seqs] rows of max_pages int32, table_stride apart, device;
  *  head_dim in {64, 128, 256}; page_size in [1, 65536];
- *  max_pages * page_size < 2^31; dtype PE_BF16 or PE_F16. */
+ *  max_pages * page_size <= 2^30; dtype PE_BF16 or PE_F16. */
 typedef struct pe_kv_cache {
   void* k;
   void* v;

@@ -19,8 +19,8 @@ static pe_status check_cache(const pe_kv_cache* c) {
   if (c->page_size < 1 || c->page_size > 65536) return fail(PE_EINVAL, "page_size must be in [1, 65536]");
   if (c->n_pages < 1 || c->n_pages > INT32_MAX) return fail(PE_EINVAL, "n_pages must be in [1, 2^31)");
   if (c->n_seqs < 0 || c->n_seqs > (1 << 20)) return fail(PE_EINVAL, "n_seqs must be in [0, 2^20]");
-  if (c->max_pages < 1 || (int64_t)c->max_pages * c->page_size > INT32_MAX)
-    return fail(PE_EINVAL, "max_pages >= 1 and max_pages * page_size < 2^31 required");
+  if (c->max_pages < 1 || (int64_t)c->max_pages * c->page_size > (1 << 30))
+    return fail(PE_EINVAL, "max_pages >= 1 and max_pages * page_size <= 2^30 required");
   if (c->table_stride < 0 || (c->n_seqs > 1 && c->table_stride < c->max_pages))
     return fail(PE_EINVAL, "table_stride must be at least max_pages");
   if (bad_stride(c->page_stride) || bad_stride(c->slot_stride) || bad_stride(c->head_stride))
