@@ -92,8 +92,8 @@ struct SegMeta {
 
 template <int D, int NT, int HT>
 struct DecodeShape {
-  // eight warps where wide heads leave one CTA on an SM and its teams have several warps
-  static constexpr int kWarps = D == 256 && HT > 1 ? 8 : 4;
+  // wide heads leave one CTA on an SM: more warps where its teams have several
+  static constexpr int kWarps = D == 256 && HT > 1 ? (HT == 3 ? 12 : 8) : 4;
   static constexpr int kThreads = 32 * kWarps;
   static constexpr int kTeams = kWarps / HT;
   static constexpr int kCtas = D == 256 ? kDecodeCtas / 2 : kDecodeCtas;
@@ -107,7 +107,8 @@ struct DecodeShape {
   static constexpr int kPiece = 8 * NT * (D + 2);       // floats of a warp's piece: output, maxima, sums
   static constexpr int kTiles = NT * (D / 16);          // 16 x 8 tiles of its output
   // the teams join `kRound` tiles of each warp at a time
-  static constexpr int kRound = kTeams == 1 ? 0 : 32 / kWarps < kTiles ? 32 / kWarps : kTiles;
+  static constexpr int kAtOnce = NT > 2 || kWarps > 4 ? 4 : 8;
+  static constexpr int kRound = kTeams == 1 ? 0 : kAtOnce < kTiles ? kAtOnce : kTiles;
   static constexpr int kMerge = kWarps * (kRound * 512 + 2 * 8 * NT * 4);
   static constexpr int kWeights = kMaxRanks * kTeams * kHeads * 8;
   static constexpr int kExtra = kMerge > kWeights ? kMerge : kWeights;
@@ -365,9 +366,9 @@ __global__ void __launch_bounds__(DecodeShape<D, NT, HT>::kThreads, D == 256 ? 1
   };
   auto load = [&]() {
     if (lleft > 0) {
-      constexpr int kRows = 32 / kChunks;  // rows of one copy instruction
-      constexpr int kMine = kUnit / HT;    // rows that this warp copies
-      const int row0 = hw * kMine + lane / kChunks, ch = lane % kChunks;
+      constexpr int kRows = 32 / kChunks * HT;                 // rows of one copy instruction of each warp
+      constexpr int kCopies = (kUnit + kRows - 1) / kRows;
+      const int row0 = lane / kChunks * HT + hw, ch = lane % kChunks;
       const uint32_t dst = ring + lstage * S::kUnitBytes + row0 * (D * 2);
       const bool ok = lpage >= 0 && lpage < c.n_pages;
       int64_t off = ok ? kv_page_offset(c, lpage) + (int64_t)lslot * c.slot_stride + ls.hk * c.head_stride : 0;
@@ -384,7 +385,8 @@ __global__ void __launch_bounds__(DecodeShape<D, NT, HT>::kThreads, D == 256 ? 1
         const T* k = (const T*)c.k + off + row0 * c.slot_stride + ch * 8;
         const T* v = (const T*)c.v + off + row0 * c.slot_stride + ch * 8;
 #pragma unroll
-        for (int i = 0; i < kMine / kRows; ++i) {
+        for (int i = 0; i < kCopies; ++i) {
+          if (kUnit % kRows != 0 && row0 + i * kRows >= kUnit) break;
           const uint32_t d = dst + i * kRows * (D * 2) + ((ch ^ ((row0 + i * kRows) & 7)) << 4);
           copy16(d, k + i * kRows * c.slot_stride, true);
           copy16(d + kUnit * D * 2, v + i * kRows * c.slot_stride, true);
@@ -392,9 +394,10 @@ __global__ void __launch_bounds__(DecodeShape<D, NT, HT>::kThreads, D == 256 ? 1
       } else {
         if (one_page && lane & (kUnit - 1)) off += (lane & (kUnit - 1)) * c.slot_stride;
 #pragma unroll
-        for (int i = 0; i < kMine / kRows; ++i) {
+        for (int i = 0; i < kCopies; ++i) {
           const int row = row0 + i * kRows;
-          const int64_t o = __shfl_sync(0xffffffffu, off, row) + ch * 8;
+          const int64_t o = __shfl_sync(0xffffffffu, off, row & 31) + ch * 8;
+          if (kUnit % kRows != 0 && row >= kUnit) continue;
           const bool in = (mask >> row) & 1;
           const uint32_t d = dst + i * kRows * (D * 2) + ((ch ^ (row & 7)) << 4);
           copy16(d, (const T*)c.k + (in ? o : 0), in);
@@ -785,12 +788,18 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
 
 constexpr int64_t kMetaBytes = (kDecodeCtas * (int64_t)sizeof(SegMeta) + 255) / 256 * 256;
 
-// heads of a segment for a group of query heads: 8, or 16 in one warp; 32 and
-// 64 in the two or four warps of a team, which share each unit
-static int seg_heads(int group) { return group <= 8 ? 8 : group <= 16 ? 16 : group <= 32 ? 32 : 64; }
+// Heads of a segment for a group of query heads: up to 24 (head_dim 64: 32) in
+// one warp, whose registers hold their accumulators, more in the two or four
+// warps of a team, which share each unit.  Measured with 20 heads, 256 x 2,048
+// positions of 2 key heads: 104 us in one warp of three head tiles, 129 in two
+// of two; with 32 heads 131 us in two warps of two, 147 in one of four, which spills.
+static int seg_heads(int D, int group) {
+  if (group <= 16) return group <= 8 ? 8 : 16;
+  return group <= 24 ? 24 : group <= 32 ? 32 : 64;
+}
 
 int64_t decode_attn_ws_bytes(const pe_kv_cache& c, int n_q_heads) {
-  const int n = seg_heads(n_q_heads / c.n_heads), D = c.head_dim;
+  const int D = c.head_dim, n = seg_heads(D, n_q_heads / c.n_heads);
   const int64_t ctas = D == 256 ? kDecodeCtas / 2 : kDecodeCtas;
   return kMetaBytes + 2 * ctas * n * (D + 2) * 4;  // two pieces for each CTA
 }
@@ -855,11 +864,12 @@ static pe_status go(const DecodeArgs& a, void* ws, cudaStream_t st) {
 
 template <typename T, int D>
 static pe_status go_heads(const DecodeArgs& a, void* ws, cudaStream_t st) {
-  const int n = seg_heads(a.n_q_heads / a.c.n_heads);
+  const int n = seg_heads(D, a.n_q_heads / a.c.n_heads);
   if (n == 8) return go<T, D, 1, 1>(a, ws, st);
-  if (n == 16) return go<T, D, 2, 1>(a, ws, st);
-  if (n == 32) return go<T, D, 2, 2>(a, ws, st);
-  return go<T, D, 2, 4>(a, ws, st);
+  if (n == 16) return go<T, D, D == 256 ? 1 : 2, D == 256 ? 2 : 1>(a, ws, st);
+  if (n == 24) return go<T, D, D == 256 ? 1 : 3, D == 256 ? 3 : 1>(a, ws, st);
+  if (n == 32) return go<T, D, D == 64 ? 4 : 2, D == 64 ? 1 : 2>(a, ws, st);
+  return go<T, D, D == 64 ? 4 : 2, D == 64 ? 2 : 4>(a, ws, st);
 }
 
 template <typename T>

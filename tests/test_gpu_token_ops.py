@@ -226,6 +226,15 @@ DECODE = [
     (BF16, [20011], 4, 1, 128, 16, 0, "slot"),
     (F16, [9000, 70000], 16, 2, 64, 64, 0, "head"),
     (BF16, [4097, 8193], 16, 2, 256, 256, 0, "slot"),
+    # every number of query heads that one warp, or a team of warps, takes together
+    (BF16, [700, 0, 33], 40, 1, 128, 16, 0, "slot"),
+    (F16, [129, 5000], 33, 1, 256, 16, 0, "head"),
+    (BF16, [300, 1, 9000], 130, 1, 64, 16, 0, "slot"),
+    (BF16, [90, 2577], 24, 1, 256, 48, 0, "slot"),
+    (F16, [1000, 3333], 32, 1, 64, 100, 0, "head"),
+    (BF16, [4097, 100], 70, 1, 256, 16, 300, "slot"),
+    (BF16, [5001, 6], 34, 2, 256, 16, 0, "slot"),
+    (F16, [7000, 65], 46, 2, 128, 16, 0, "slot"),
 ]
 
 
