@@ -7,11 +7,13 @@
 // lse = scale m + ln S and entropy = ln S - scale T / S.  Bound: HBM for
 // many rows (an element costs one exponential and about five issue slots, half
 // of what the SMs have at the copy rate); for few rows the latency of one
-// row, which a cluster of CTAs then shares.
+// row, which a cluster of CTAs then shares.  CTAs, or warps where a row is
+// short, go through rows and have the next row's first loads on their way
+// while they join the sums of one.
 //
-// Top alternatives come from the same pass: the k-th largest of the threads'
-// maxima bounds the k-th largest logit from below, so only the few threads
-// whose maximum reaches it look at their elements again (from L2).
+// Top alternatives come from the same pass: the k-th largest of 32 maxima, each
+// of some threads' elements, bounds the k-th largest logit from below, so only
+// the few threads whose maximum reaches it look at their elements again (from L2).
 //
 // Backward: elementwise from the saved lse and entropy, one read and one write.
 #include <cooperative_groups.h>
@@ -58,6 +60,7 @@ template <> struct Chunk<float> {
   static __device__ __forceinline__ float2 pair(const uint4& v, int i) {
     return i == 0 ? make_float2(__uint_as_float(v.x), __uint_as_float(v.y)) : make_float2(__uint_as_float(v.z), __uint_as_float(v.w));
   }
+  static __device__ __forceinline__ float at(const uint4& v, int i) { return __uint_as_float(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w); }
   template <int U> static __device__ __forceinline__ float largest(const uint4 (&v)[U]) {
     float m = max_nan(max_nan(pair(v[0], 0).x, pair(v[0], 0).y), max_nan(pair(v[0], 1).x, pair(v[0], 1).y));
 #pragma unroll
@@ -78,6 +81,10 @@ template <> struct Chunk<float> {
 template <typename T> struct Chunk16 {
   static constexpr int kElems = 8, kPairs = 4;
   static __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+  static __device__ __forceinline__ float at(const uint4& v, int i) {
+    const float2 p = unpack2<T>(word(v, i >> 1));
+    return i & 1 ? p.y : p.x;
+  }
   static __device__ __forceinline__ void put(uint4& v, int i, float2 p) {
     const uint32_t w = pack2<T>(p.x, p.y);
     (i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w) = w;
@@ -162,12 +169,17 @@ __device__ __forceinline__ void rebase(Stat& s, float m, float scale) {  // to t
   s.S *= f;
   s.m = m;
 }
-__device__ __forceinline__ void join(Stat& a, Stat b, float scale) {
-  const float m = max_nan(a.m, b.m);
-  rebase(a, m, scale);
-  rebase(b, m, scale);
-  a.S += b.S;
-  a.T += b.T;
+// over the first N lanes of each group of N lanes
+template <int N> __device__ __forceinline__ void join_lanes(Stat& s, float scale) {
+  float m = s.m;
+#pragma unroll
+  for (int x = N / 2; x; x >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, x));
+  rebase(s, m, scale);
+#pragma unroll
+  for (int x = N / 2; x; x >>= 1) {
+    s.S += __shfl_xor_sync(0xffffffffu, s.S, x);
+    s.T += __shfl_xor_sync(0xffffffffu, s.T, x);
+  }
 }
 
 template <typename T, int U>
@@ -221,83 +233,120 @@ __device__ __forceinline__ Key merge_desc(Key a, Key b) {
   return a;
 }
 
-constexpr int kCand = 512;  // candidates held for sorting
-
-template <int THREADS> struct LogpShared {
-  float m[THREADS / 32], S[THREADS / 32], T[THREADS / 32];
-  Stat slice;          // of this CTA's part of the row
+// what the threads of a row share
+template <int ROWT, bool TOP> struct RowShared {
+  static constexpr int kWarps = ROWT / 32, kCand = !TOP ? 1 : ROWT == 32 ? 256 : 512;  // candidates held for sorting
+  Stat warp[2][kWarps];  // of the warps; rows take turns
+  Stat slice;            // of a rank's part of the row
   Key top[32];
   Key cand[kCand];
-  int count;
-  uint32_t part[THREADS / 32];
   Key best;
+  uint32_t most[32];     // the warps' largest maxima
+  uint32_t part[kWarps];
+  int count;
+  uint8_t who[kWarps][32];
 };
 
-// counts over the CTA
-template <int THREADS> __device__ __forceinline__ int count_block(bool p) {
-  return THREADS == 32 ? __popc(__ballot_sync(0xffffffffu, p)) : __syncthreads_count(p);
-}
-template <int THREADS> __device__ __forceinline__ void sync_block() {
-  if (THREADS == 32)
+template <int ROWT> __device__ __forceinline__ void sync_row() {
+  if (ROWT == 32)
     __syncwarp();
   else
     __syncthreads();
 }
 
 // The k largest keys of chunks [j0, j1) into sh.top (missing ones 0).  mine:
-// the largest logit of this thread's chunks j0 + tid + i * THREADS.
-template <typename T, int THREADS>
-__device__ void top_slice(const Row<T>& row, int j0, int j1, float mine, int k, LogpShared<THREADS>& sh) {
+// the largest logit of this thread's chunks j0 + tid + i * ROWT.
+template <typename T, int ROWT>
+__device__ void top_slice(const Row<T>& row, int j0, int j1, float mine, int k, RowShared<ROWT, true>& sh) {
   using C = Chunk<T>;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  constexpr int kWarps = ROWT / 32, kCand = RowShared<ROWT, true>::kCand;
+  const int tid = threadIdx.x % ROWT, lane = tid & 31, warp = tid / 32;
   const bool has = j0 + tid < j1;
-  // the upper 16 bits of the k-th largest thread maximum, bit by bit: a bound
-  // from below that at least k elements reach, or 0 where fewer threads have any
   const uint32_t my = has ? order_key(mine) : 0u;
-  uint32_t tau = 0;
-  for (int bit = 31; bit >= 16; --bit) {
-    const uint32_t t = tau | (1u << bit);
-    if (count_block<THREADS>(my >= t) >= k) tau = t;
-  }
-  // the elements that reach it
-  auto collect = [&](uint32_t least) {
+  // 32 thread maxima, the largest 32 / kWarps of each warp: at least k elements
+  // reach their k-th largest
+  uint32_t m = my;
+  if (kWarps > 1) {
+    uint32_t v = my;
+#pragma unroll
+    for (int i = 0; i < 32 / kWarps; ++i) {
+      const uint32_t best = __reduce_max_sync(0xffffffffu, v);
+      if (lane == 0) sh.most[warp * (32 / kWarps) + i] = best;
+      if (lane == __ffs(__ballot_sync(0xffffffffu, v == best)) - 1) v = 0;
+    }
     if (tid == 0) sh.count = 0;
-    sync_block<THREADS>();
-    uint32_t who = __ballot_sync(0xffffffffu, has && my >= least);
-    while (who) {
-      const int l = __ffs(who) - 1;
-      who &= who - 1;
-      for (int64_t j = (int64_t)j0 + warp * 32 + l + (int64_t)lane * THREADS; j < j1; j += 32 * (int64_t)THREADS) {
-        if (*(volatile int*)&sh.count > kCand) break;  // too many already: how many does not matter
-        const uint4 v = row.any((int)j);
+    __syncthreads();
+    m = sh.most[lane];
+  } else {
+    if (lane == 0) sh.count = 0;
+    __syncwarp();
+  }
+  int above = 0;  // maxima that come before this lane's
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    const uint32_t o = __shfl_sync(0xffffffffu, m, i);
+    above += o > m || (o == m && i < lane);
+  }
+  const uint32_t tau = __shfl_sync(0xffffffffu, m, __ffs(__ballot_sync(0xffffffffu, above == k - 1)) - 1);
+
+  const bool every = (int64_t)(j1 - j0) * C::kElems <= kCand;  // the candidates hold the slice
+  // the elements that reach `least`: a warp goes through the chunks of its
+  // threads that have any
+  const int per = (j1 - j0 + ROWT - 1) / ROWT;
+  auto collect = [&](uint32_t least) {
+    const uint32_t who = __ballot_sync(0xffffffffu, has && my >= least);
+    const float bound = key_logit(least);  // 0 becomes NaN, which nothing is below
+    if ((who >> lane) & 1) sh.who[warp][__popc(who & ((1u << lane) - 1))] = (uint8_t)lane;
+    __syncwarp();
+    const int pairs = __popc(who) * per;
+    for (int p0 = 0; p0 < pairs; p0 += 64) {  // the warp stays together: all its branches are taken by all lanes
+      if (*(volatile int*)&sh.count > kCand) break;  // too many already: how many does not matter
+      uint4 v[2];
+      int64_t e[2];
+      uint32_t hit[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int p = p0 + 32 * u + lane, q = p / per;
+        const int64_t j = (int64_t)j0 + warp * 32 + sh.who[warp][q & 31] + (int64_t)(p - q * per) * ROWT;
+        const bool in = p < pairs && j < j1;
+        v[u] = in ? row.any((int)j) : make_uint4(0, 0, 0, 0);
+        e[u] = j * C::kElems - row.mis;  // of the chunk's first element
+        const int64_t lo = max(-e[u], (int64_t)0), hi = min(row.V - e[u], (int64_t)C::kElems);  // elements of the row
+        hit[u] = in && hi > lo ? ((1u << hi) - 1) & ~((1u << lo) - 1) : 0u;
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        uint32_t least_hit = 0;
 #pragma unroll
         for (int i = 0; i < C::kPairs; ++i) {
-          const float2 p = C::pair(v, i);
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const float z = y ? p.y : p.x;
-            const int64_t e = (int64_t)j * C::kElems - row.mis + 2 * i + y;
-            if (order_key(z) >= least && e >= 0 && e < row.V) {
-              const int at = atomicAdd(&sh.count, 1);
-              if (at < kCand) sh.cand[at] = make_key(z, (int)e);
-            }
-          }
+          const float2 z = C::pair(v[u], i);
+          least_hit |= (z.x < bound ? 0u : 1u << (2 * i)) | (z.y < bound ? 0u : 2u << (2 * i));  // a NaN is the highest
+        }
+        hit[u] &= least_hit;
+        for (uint32_t any; (any = __ballot_sync(0xffffffffu, hit[u] != 0)) != 0; hit[u] &= hit[u] - 1) {
+          int base = 0;
+          if (lane == 0) base = atomicAdd(&sh.count, __popc(any));
+          base = __shfl_sync(0xffffffffu, base, 0);
+          const int i = __ffs(hit[u]) - 1, at = base + __popc(any & ((1u << lane) - 1));
+          if (hit[u] && at < kCand) sh.cand[at] = make_key(C::at(v[u], i), (int)(e[u] + i));
         }
       }
     }
-    sync_block<THREADS>();
-    const int n = sh.count;
-    sync_block<THREADS>();
-    return n;
+    sync_row<ROWT>();
+    return sh.count;
   };
   // keys from `least` on are collected, then sorted; the rest is found below.
   // A bound at the stand-in for low logits says nothing: a thread's maximum is
   // at least that
   const uint32_t low = order_key(__uint_as_float(kLowBits));
-  const bool every = (int64_t)(j1 - j0) * C::kElems <= kCand;
   uint32_t least = every ? 0u : tau > low ? tau : low + 1;
   int n = collect(least);
-  if (n > kCand && least == tau) n = collect(++least);  // ties at the bound
+  if (n > kCand && least == tau) {  // ties at the bound
+    sync_row<ROWT>();
+    if (tid == 0) sh.count = 0;
+    sync_row<ROWT>();
+    n = collect(++least);
+  }
   bool inclusive = false;
   if (n > kCand) {  // a row that crowds its large logits into few threads
     n = 0;
@@ -320,9 +369,9 @@ __device__ void top_slice(const Row<T>& row, int j0, int j1, float mine, int k, 
   int filled = min(n, k);
   while (filled < k && !every) {
     if (tid == 0) sh.best = 0;
-    sync_block<THREADS>();
+    sync_row<ROWT>();
     uint32_t best = 0;
-    for (int64_t j = (int64_t)j0 + tid; j < j1; j += THREADS) {
+    for (int64_t j = (int64_t)j0 + tid; j < j1; j += ROWT) {
       const uint4 v = row.any((int)j);
 #pragma unroll
       for (int i = 0; i < C::kElems; ++i) {
@@ -333,12 +382,12 @@ __device__ void top_slice(const Row<T>& row, int j0, int j1, float mine, int k, 
       }
     }
     atomicMax(&sh.best, (Key)best);
-    sync_block<THREADS>();
+    sync_row<ROWT>();
     best = (uint32_t)sh.best;
     inclusive = false;
     below = best;
     if (best == 0) break;  // the slice is used up
-    for (int64_t jj = j0; jj < j1 && filled < k; jj += THREADS) {
+    for (int64_t jj = j0; jj < j1 && filled < k; jj += ROWT) {
       const int64_t j = jj + tid;
       uint32_t hit = 0;
       if (j < j1) {
@@ -356,9 +405,9 @@ __device__ void top_slice(const Row<T>& row, int j0, int j1, float mine, int k, 
         if (lane >= x) before += y;
       }
       if (lane == 31) sh.part[warp] = before;
-      sync_block<THREADS>();
+      sync_row<ROWT>();
       uint32_t base = 0, all = 0;
-      for (int w = 0; w < THREADS / 32; ++w) {
+      for (int w = 0; w < kWarps; ++w) {
         if (w < warp) base += sh.part[w];
         all += sh.part[w];
       }
@@ -366,149 +415,184 @@ __device__ void top_slice(const Row<T>& row, int j0, int j1, float mine, int k, 
       for (; hit && at < k; hit &= hit - 1, ++at)
         sh.top[at] = ((Key)best << 32) | (0xffffffffu - (uint32_t)(j * C::kElems - row.mis + __ffs(hit) - 1));
       filled = (int)min((int64_t)k, (int64_t)filled + all);
-      sync_block<THREADS>();
+      sync_row<ROWT>();
     }
   }
 }
 
-// A row is cut into gridDim.x slices, one for each CTA of its cluster.
-template <typename T, int THREADS, bool TOP>
-__global__ void __launch_bounds__(THREADS) token_logp_kernel(LogpArgs a) {
-  constexpr int U = 4, kWarps = THREADS / 32;
-  __shared__ LogpShared<THREADS> sh;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int rank = blockIdx.x, ranks = gridDim.x;
-  const int64_t r = blockIdx.y + (int64_t)blockIdx.z * gridDim.y;
-  if (r >= a.n) return;  // a whole cluster, or none of it
-  const Row<T> row((const T*)a.logits + r * a.row_stride, a.V);
-  const int all = row.chunks();
-  const int j0 = (int)((int64_t)all * rank / ranks), j1 = (int)((int64_t)all * (rank + 1) / ranks);
-  const int w0 = row.first_whole(), w1 = min(j1, row.end_whole());
-  // the target's logit, on its way while the row is read
-  int t = -1;
-  float zt = 0.0f;
-  if (rank == 0 && tid == 0 && a.logp) {
-    t = a.tokens[r];
-    if (t >= 0 && t < a.V) zt = to_f32(row.x[t]);
-  }
-
+// nothing above the stand-in: -inf alone, or masks of the type's lowest value
+// alone; by the definition, element by element
+template <typename T, int ROWT, typename SH>
+__device__ Stat careful(const Row<T>& row, float scale, SH& sh) {
+  const int tid = threadIdx.x % ROWT, lane = tid & 31, warp = tid / 32;
   Stat s;
-  s.m = __uint_as_float(kLowBits);
+  s.m = -CUDART_INF_F;
+  for (int e = tid; e < row.V; e += ROWT) s.m = fmaxf(s.m, to_f32(row.x[e]));
+  for (int x = 16; x; x >>= 1) s.m = fmaxf(s.m, __shfl_xor_sync(0xffffffffu, s.m, x));
+  if (ROWT > 32) {
+    __syncthreads();
+    if (lane == 0) sh.warp[0][warp].m = s.m;
+    __syncthreads();
+    for (int w = 0; w < ROWT / 32; ++w) s.m = fmaxf(s.m, sh.warp[0][w].m);
+  }
   s.S = s.T = 0.0f;
-  for (int64_t j = j0; j < j1; j += U * THREADS) {
-    uint4 v[U];
-    if (j >= w0 && j + U * THREADS <= w1) {
+  if (s.m != -CUDART_INF_F)
+    for (int e = tid; e < row.V; e += ROWT) {
+      const float d = to_f32(row.x[e]) - s.m, p = exp_fast(d * scale);
+      s.S += p;
+      s.T += p == 0.0f ? 0.0f : p * d;
+    }
+  for (int x = 16; x; x >>= 1) {
+    s.S += __shfl_xor_sync(0xffffffffu, s.S, x);
+    s.T += __shfl_xor_sync(0xffffffffu, s.T, x);
+  }
+  if (ROWT > 32) {
+    if (lane == 0) sh.warp[1][warp] = s;
+    __syncthreads();
+    s.S = s.T = 0.0f;
+    for (int w = 0; w < ROWT / 32; ++w) {
+      s.S += sh.warp[1][w].S;
+      s.T += sh.warp[1][w].T;
+    }
+    __syncthreads();
+  }
+  return s;
+}
+
+// ROWT threads go through rows; with `ranks` above 1 a cluster's CTAs take one
+// row's slices and the grid has a cluster for each row.
+template <typename T, int ROWT> struct RowThreads {
+  static constexpr int kCta = ROWT == 32 ? 128 : ROWT;
+  static constexpr bool kLoop = ROWT == 32;
+};
+
+template <typename T, int ROWT, bool TOP>
+__global__ void __launch_bounds__(RowThreads<T, ROWT>::kCta, (TOP ? 1024 : ROWT == 32 ? 1280 : 1536) / RowThreads<T, ROWT>::kCta) token_logp_kernel(LogpArgs a, int ranks) {
+  // the next row's first loads before this one's joining: its registers would
+  // cost the wide rows' CTAs a third of their warps
+  constexpr bool kLoop = RowThreads<T, ROWT>::kLoop, kAhead = kLoop && !TOP;
+  constexpr int U = 4, kWarps = ROWT / 32, kRows = RowThreads<T, ROWT>::kCta / ROWT;
+  using C = Chunk<T>;
+  __shared__ RowShared<ROWT, TOP> shared[kRows];
+  RowShared<ROWT, TOP>& sh = shared[threadIdx.x / ROWT];
+  const int tid = threadIdx.x % ROWT, lane = tid & 31, warp = tid / 32;
+  const int rank = ranks > 1 ? blockIdx.x % ranks : 0;
+  int64_t r = ranks > 1 ? blockIdx.x / ranks : (int64_t)blockIdx.x * kRows + threadIdx.x / ROWT;
+  const int64_t step = ranks > 1 ? a.n : (int64_t)gridDim.x * kRows;
+  if (r >= a.n) return;  // a row's threads all leave
+
+  uint4 v[U];
+  auto slice = [&](const Row<T>& row, int& j0, int& j1) {
+    const int all = row.chunks();
+    j0 = ranks > 1 ? (int)((int64_t)all * rank / ranks) : 0;
+    j1 = ranks > 1 ? (int)((int64_t)all * (rank + 1) / ranks) : all;
+  };
+  auto fetch = [&](const Row<T>& row, int64_t j, int j1) {
+    if (j >= row.first_whole() && j + U * ROWT <= min(j1, row.end_whole())) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = row.whole((int)j + u * THREADS + tid);
+      for (int u = 0; u < U; ++u) v[u] = row.whole((int)j + u * ROWT + tid);
     } else {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int64_t jj = j + u * THREADS + tid;
-        v[u] = jj < j1 ? row.any((int)jj) : make_uint4(Chunk<T>::kNone, Chunk<T>::kNone, Chunk<T>::kNone, Chunk<T>::kNone);
+        const int64_t jj = j + u * ROWT + tid;
+        v[u] = jj < j1 ? row.any((int)jj) : make_uint4(C::kNone, C::kNone, C::kNone, C::kNone);
       }
     }
-    absorb<T, U>(v, a.scale, s);
-  }
-  const float mine = s.m;
-#pragma unroll
-  for (int x = 16; x; x >>= 1) {
-    Stat o;
-    o.m = __shfl_xor_sync(0xffffffffu, s.m, x);
-    o.S = __shfl_xor_sync(0xffffffffu, s.S, x);
-    o.T = __shfl_xor_sync(0xffffffffu, s.T, x);
-    join(s, o, a.scale);
-  }
-  if (kWarps > 1) {
-    if (lane == 0) {
-      sh.m[warp] = s.m;
-      sh.S[warp] = s.S;
-      sh.T[warp] = s.T;
+  };
+  Row<T> row((const T*)a.logits + r * a.row_stride, a.V);
+  int j0, j1;
+  slice(row, j0, j1);
+  fetch(row, j0, j1);
+  for (int turn = 0;; turn ^= 1) {
+    // the target's logit, on its way while the row is read
+    int t = -1;
+    float zt = 0.0f;
+    if (rank == 0 && tid == 0 && a.logp) {
+      t = a.tokens[r];
+      if (t >= 0 && t < a.V) zt = to_f32(row.x[t]);
     }
-    __syncthreads();
-    s = Stat{sh.m[0], sh.S[0], sh.T[0]};
-#pragma unroll
-    for (int w = 1; w < kWarps; ++w) join(s, Stat{sh.m[w], sh.S[w], sh.T[w]}, a.scale);
-  }
-  if (TOP) top_slice<T, THREADS>(row, j0, j1, mine, a.top_k, sh);
-  Key top = 0;
-  if (ranks > 1) {
-    cg::cluster_group cl = cg::this_cluster();
-    if (tid == 0) sh.slice = s;
-    cl.sync();
-    if (rank == 0) {
-      for (int p = 1; p < ranks; ++p) join(s, *cl.map_shared_rank(&sh.slice, p), a.scale);
-      if (TOP && warp == 0) {
-        top = sh.top[lane];
-        for (int p = 1; p < ranks; ++p) top = merge_desc(top, cl.map_shared_rank(sh.top, p)[lane]);
-      }
-    }
-    cl.sync();  // the others' shared memory has been read
-    if (rank) return;
-  } else if (TOP) {
-    sync_block<THREADS>();
-    if (warp == 0) top = sh.top[lane];
-  }
-
-  if (s.m <= __uint_as_float(kLowBits)) {
-    // nothing above the stand-in: -inf alone, or masks of the type's lowest
-    // value alone; by the definition, element by element
-    float m = -CUDART_INF_F;
-    for (int e = tid; e < a.V; e += THREADS) m = fmaxf(m, to_f32(row.x[e]));
-    for (int x = 16; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-    sync_block<THREADS>();
-    if (lane == 0) sh.m[warp] = m;
-    sync_block<THREADS>();
-    for (int w = 0; w < kWarps; ++w) m = fmaxf(m, sh.m[w]);
-    s.m = m;
-    float S = 0.0f, D = 0.0f;
-    if (m != -CUDART_INF_F)
-      for (int e = tid; e < a.V; e += THREADS) {
-        const float d = to_f32(row.x[e]) - m;
-        const float p = exp_fast(d * a.scale);
-        S += p;
-        D += p == 0.0f ? 0.0f : p * d;
-      }
-    for (int x = 16; x; x >>= 1) {
-      S += __shfl_xor_sync(0xffffffffu, S, x);
-      D += __shfl_xor_sync(0xffffffffu, D, x);
-    }
-    if (lane == 0) {
-      sh.S[warp] = S;
-      sh.T[warp] = D;
-    }
-    sync_block<THREADS>();
+    Stat s;
+    s.m = __uint_as_float(kLowBits);
     s.S = s.T = 0.0f;
-    for (int w = 0; w < kWarps; ++w) {
-      s.S += sh.S[w];
-      s.T += sh.T[w];
+    for (int64_t j = j0;;) {
+      absorb<T, U>(v, a.scale, s);
+      j += U * ROWT;
+      if (j >= j1) break;
+      fetch(row, j, j1);
     }
-  }
-  const bool empty = s.m == -CUDART_INF_F;
-  const float ln = logf(s.S);
-  if (tid == 0) {
-    if (a.lse) a.lse[r] = empty ? -CUDART_INF_F : fmaf(s.m, a.scale, ln);
-    if (a.entropy) a.entropy[r] = empty ? 0.0f : ln - a.scale * s.T / s.S;
-    if (a.logp) a.logp[r] = t < 0 || t >= a.V ? 0.0f : empty ? -CUDART_INF_F : (zt - s.m) * a.scale - ln;
-  }
-  if (TOP && tid < a.top_k) {
-    a.top_id[r * a.top_k + tid] = (int32_t)(0xffffffffu - (uint32_t)top);
-    a.top_logp[r * a.top_k + tid] = empty ? -CUDART_INF_F : (key_logit((uint32_t)(top >> 32)) - s.m) * a.scale - ln;
+    const float mine = s.m;
+    const Row<T> done = row;
+    const int64_t rd = r;
+    const int d0 = j0, d1 = j1;
+    r += step;
+    auto next = [&]() {
+      row = Row<T>((const T*)a.logits + r * a.row_stride, a.V);
+      slice(row, j0, j1);
+      fetch(row, j0, j1);
+    };
+    if (kAhead && r < a.n) next();
+
+    join_lanes<32>(s, a.scale);
+    if (kWarps > 1) {
+      if (lane == 0) sh.warp[turn][warp] = s;
+      __syncthreads();
+      s = sh.warp[turn][lane % kWarps];
+      join_lanes<kWarps>(s, a.scale);
+    }
+    Key top = 0;
+    if constexpr (TOP) top_slice<T, ROWT>(done, d0, d1, mine, a.top_k, sh);
+    if (ranks > 1) {
+      cg::cluster_group cl = cg::this_cluster();
+      if (tid == 0) sh.slice = s;
+      cl.sync();
+      if (rank == 0) {
+        if (lane < ranks) s = *cl.map_shared_rank(&sh.slice, lane);
+        if (lane >= ranks) s = Stat{__uint_as_float(kLowBits), 0.0f, 0.0f};
+        join_lanes<32>(s, a.scale);
+        if (TOP && warp == 0) {
+          top = sh.top[lane];
+          for (int p = 1; p < ranks; ++p) top = merge_desc(top, cl.map_shared_rank(sh.top, p)[lane]);
+        }
+      }
+      cl.sync();  // the others' shared memory has been read
+      if (rank) return;
+    } else if (TOP) {
+      sync_row<ROWT>();
+      if (warp == 0) top = sh.top[lane];
+    }
+
+    if (s.m <= __uint_as_float(kLowBits)) s = careful<T, ROWT>(done, a.scale, sh);
+    const bool empty = s.m == -CUDART_INF_F;
+    const float ln = logf(s.S);
+    if (tid == 0) {
+      if (a.lse) a.lse[rd] = empty ? -CUDART_INF_F : fmaf(s.m, a.scale, ln);
+      if (a.entropy) a.entropy[rd] = empty ? 0.0f : ln - a.scale * s.T / s.S;
+      if (a.logp) a.logp[rd] = t < 0 || t >= a.V ? 0.0f : empty ? -CUDART_INF_F : (zt - s.m) * a.scale - ln;
+    }
+    if (TOP && tid < a.top_k) {
+      a.top_id[rd * a.top_k + tid] = (int32_t)(0xffffffffu - (uint32_t)top);
+      a.top_logp[rd * a.top_k + tid] = empty ? -CUDART_INF_F : (key_logit((uint32_t)(top >> 32)) - s.m) * a.scale - ln;
+    }
+    if (!kLoop || r >= a.n) return;
+    if (TOP) sync_row<ROWT>();  // the next row's candidates go where this one's were
+    if (!kAhead) next();
   }
 }
 
 // ---------------------------------------------------------------------------
-// gradient: THREADS threads on kGradChunks chunks each of one row
+// gradient: THREADS threads take kGradChunks chunks each of one row; a warp a
+// row where the row is short, eight of them in a CTA
 // ---------------------------------------------------------------------------
 constexpr int kGradChunks = 4;
 
 template <typename T, int THREADS>
-__global__ void __launch_bounds__(THREADS) token_logp_grad_kernel(LogpGradArgs a) {
+__global__ void __launch_bounds__(256) token_logp_grad_kernel(LogpGradArgs a) {
   using C = Chunk<T>;
-  const int64_t r = blockIdx.y + (int64_t)blockIdx.z * gridDim.y;
+  const int64_t r = (blockIdx.y + (int64_t)blockIdx.z * gridDim.y) * (256 / THREADS) + threadIdx.x / THREADS;
   if (r >= a.n) return;
   const Row<T> row((const T*)a.logits + r * a.row_stride, a.V);
   T* y = (T*)a.dlogits + r * a.d_row_stride;
-  const int64_t j = (int64_t)blockIdx.x * (kGradChunks * THREADS) + threadIdx.x;
+  const int64_t j = (int64_t)blockIdx.x * (kGradChunks * THREADS) + threadIdx.x % THREADS;
   const int all = row.chunks(), w0 = row.first_whole(), w1 = row.end_whole();
   if (j >= all) return;
   uint4 v[kGradChunks];
@@ -570,29 +654,37 @@ static dim3 row_grid(int x, int64_t n) {
   return dim3(x, (unsigned)y, (unsigned)((n + y - 1) / y));
 }
 
-template <typename T, int THREADS>
+template <typename T, int ROWT>
 static pe_status go_logp(const LogpArgs& a, int ranks, cudaStream_t st) {
-  auto kern = a.top_k ? token_logp_kernel<T, THREADS, true> : token_logp_kernel<T, THREADS, false>;
+  auto kern = a.top_k ? token_logp_kernel<T, ROWT, true> : token_logp_kernel<T, ROWT, false>;
+  constexpr int kCta = RowThreads<T, ROWT>::kCta, kRows = kCta / ROWT;
   cudaLaunchAttribute at{};
   at.id = cudaLaunchAttributeClusterDimension;
   at.val.clusterDim.x = ranks;
   at.val.clusterDim.y = at.val.clusterDim.z = 1;
   cudaLaunchConfig_t lc{};
-  lc.gridDim = row_grid(ranks, a.n);
-  lc.blockDim = THREADS;
+  const int64_t ctas = (a.n + kRows - 1) / kRows, most = 152 * (1536 / kCta);  // what fits the SMs at 40 registers
+  lc.gridDim = dim3((unsigned)(!RowThreads<T, ROWT>::kLoop ? a.n * ranks : ctas < most ? ctas : most));
+  lc.blockDim = kCta;
   lc.stream = st;
   lc.attrs = &at;
   lc.numAttrs = ranks > 1 ? 1 : 0;
-  PE_TRY_CUDA(cudaLaunchKernelEx(&lc, kern, a));
+  PE_TRY_CUDA(cudaLaunchKernelEx(&lc, kern, a, ranks));
   return PE_OK;
 }
 
 template <typename T>
 static pe_status logp(const LogpArgs& a, cudaStream_t st) {
   const int64_t chunks = ceil_div(a.V, Chunk<T>::kElems);
-  // a CTA of a row as wide as the row gives each thread eight chunks
-  if (chunks <= 8 * 32) return go_logp<T, 32>(a, 1, st);
-  if (chunks <= 8 * 128) return go_logp<T, 128>(a, 1, st);
+  // Threads of a row.  Few rows, up to one 512-thread CTA in each place of the
+  // SMs: eight chunks a thread, for the row's latency (one row of V = 4,096 in
+  // bf16: 2.4 us with 128 threads, 4.6 with a warp).  More: sixteen, for fewer
+  // partial sums a byte (8,000 rows: V = 2,000 9.9 us with a warp, 16.2 with 128;
+  // V = 16,000 44 us with 128, 50 with 256).
+  const bool few = a.n <= 3 * 152;
+  if (chunks <= (few ? 32 : 256)) return go_logp<T, 32>(a, 1, st);
+  if (chunks <= (few ? 1024 : 2048)) return go_logp<T, 128>(a, 1, st);
+  if (chunks <= (few ? 2048 : 8192) || a.n >= 4 * 6 * 152) return go_logp<T, 256>(a, 1, st);
   // few rows: a cluster shares one, while each thread has four chunks
   int ranks = 1;
   while (ranks < 8 && a.n * ranks * 2 <= 304 && chunks >= 512 * 4 * ranks * 2) ranks *= 2;
@@ -601,7 +693,7 @@ static pe_status logp(const LogpArgs& a, cudaStream_t st) {
 
 template <typename T, int THREADS>
 static void go_grad(const LogpGradArgs& a, int64_t chunks, cudaStream_t st) {
-  token_logp_grad_kernel<T, THREADS><<<row_grid(ceil_div(chunks, kGradChunks * THREADS), a.n), THREADS, 0, st>>>(a);
+  token_logp_grad_kernel<T, THREADS><<<row_grid(ceil_div(chunks, kGradChunks * THREADS), ceil_div(a.n, 256 / THREADS)), 256, 0, st>>>(a);
 }
 
 template <typename T>
