@@ -452,19 +452,17 @@ def _want(ok: bool, what: str):
 
 def _vec(name: str, t: torch.Tensor, n: int, dtype: torch.dtype) -> int:
     """Device pointer of a contiguous vector of n elements."""
-    if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+    if t.dtype is not dtype or t.numel() != n or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} device tensor of {n} elements")
     return t.data_ptr()
 
 
-def _heads(name: str, t: torch.Tensor, n: int, heads: int, like: torch.Tensor):
-    """(pointer, row stride, head stride) of an [n][heads][head_dim] tensor of the cache's dtype."""
-    sh, st = t.shape, t.stride()
-    if len(sh) != 3 or sh[0] != n or (heads and sh[1] != heads) or sh[2] != like.shape[3] or t.dtype != like.dtype \
-            or st[2] != 1 or not t.is_cuda:
-        raise ValueError(f"{name} must be a {like.dtype} device tensor of [{n}, {heads or 'heads'}, {like.shape[3]}] "
-                         "with adjacent elements")
-    return t.data_ptr(), st[0] if sh[0] > 1 else 0, st[1] if sh[1] > 1 else 0
+def _heads(name: str, t: torch.Tensor, shape: tuple, dtype: torch.dtype):
+    """(pointer, row stride, head stride) of an [n][heads][head_dim] tensor."""
+    s0, s1, s2 = t.stride() if t.dim() == 3 else (0, 0, 0)
+    if t.shape != shape or t.dtype is not dtype or s2 != 1 or not t.is_cuda:
+        raise ValueError(f"{name} must be a {dtype} device tensor of {list(shape)} with adjacent elements")
+    return t.data_ptr(), s0 if shape[0] > 1 else 0, s1 if shape[1] > 1 else 0
 
 
 class KVCache:
@@ -484,6 +482,7 @@ class KVCache:
         self.k, self.v, self.table = k, v, table
         st = [k.stride(i) if k.shape[i] > 1 else 0 for i in range(3)]
         self.n_seqs, self.n_heads, self.head_dim, self.page_size = table.shape[0], k.shape[2], k.shape[3], k.shape[1]
+        self.dtype = k.dtype
         self._desc = KVCacheDesc(k.data_ptr(), v.data_ptr(), table.data_ptr(), k.shape[0], st[0], st[1], st[2],
                                  max(table.stride(0), table.shape[1]), table.shape[0], table.shape[1], k.shape[1],
                                  k.shape[2], k.shape[3], _DTYPE[k.dtype])
@@ -506,20 +505,21 @@ def kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, positions: torch
     their positions (int32), rotating q (into q_out, default in place) and k
     by position with rot ([positions, rot_dim], see rot_table); token t is of
     sequence seqs[t], or t where seqs is None."""
-    n = positions.numel()
-    t = KVTokens(pos=_vec("positions", positions, n, torch.int32), n_tokens=n)
-    if seqs is not None:
-        t.seq = _vec("seqs", seqs, n, torch.int32)
-    t.k, t.k_token_stride, t.k_head_stride = _heads("k", k, n, cache.n_heads, cache.k)
-    t.v, t.v_token_stride, t.v_head_stride = _heads("v", v, n, cache.n_heads, cache.k)
+    n, D, dt = positions.numel(), cache.head_dim, cache.dtype
+    kp, ks, kh = _heads("k", k, (n, cache.n_heads, D), dt)
+    vp, vs, vh = _heads("v", v, (n, cache.n_heads, D), dt)
+    qp = qs = qh = op = os_ = oh = hq = rp = max_pos = rot_dim = 0
     if q is not None:
-        t.n_q_heads = q.shape[1]
-        t.q, t.q_token_stride, t.q_head_stride = _heads("q", q, n, 0, cache.k)
-        t.q_out, t.q_out_token_stride, t.q_out_head_stride = _heads("q_out", q if q_out is None else q_out, n, t.n_q_heads, cache.k)
+        hq = q.shape[1]
+        qp, qs, qh = _heads("q", q, (n, hq, D), dt)
+        op, os_, oh = (qp, qs, qh) if q_out is None else _heads("q_out", q_out, (n, hq, D), dt)
     if rot is not None:
-        _want(rot.dim() == 2 and rot.dtype == torch.float32 and rot.is_cuda and rot.is_contiguous(),
-              "rot must be a contiguous float32 device tensor of [positions, rot_dim]")
-        t.rot, t.max_pos, t.rot_dim, t.interleaved = rot.data_ptr(), rot.shape[0], rot.shape[1], int(interleaved)
+        if rot.dim() != 2 or rot.dtype is not torch.float32 or not rot.is_cuda or not rot.is_contiguous():
+            raise ValueError("rot must be a contiguous float32 device tensor of [positions, rot_dim]")
+        rp = rot.data_ptr()
+        max_pos, rot_dim = rot.shape
+    t = KVTokens(_vec("positions", positions, n, torch.int32), None if seqs is None else _vec("seqs", seqs, n, torch.int32),
+                 rp, qp, op, kp, vp, n, max_pos, qs, qh, os_, oh, ks, kh, vs, vh, hq, rot_dim, interleaved)
     _check(lib().pe_kv_append(cache._ref, C.byref(t), _stream_of(k, stream)))
 
 
@@ -533,8 +533,9 @@ def decode_attn(cache: KVCache, q: torch.Tensor, lens: torch.Tensor, out: torch.
     """out[b] = attention of q[b] ([sequences, query heads, head_dim]) over the
     lens[b] (int32) positions of sequence b; scale defaults to head_dim^-1/2."""
     n, hq = cache.n_seqs, q.shape[1]
-    qp, qs, qh = _heads("q", q, n, 0, cache.k)
-    op, os_, oh = _heads("out", out, n, hq, cache.k)
+    shape = (n, hq, cache.head_dim)
+    qp, qs, qh = _heads("q", q, shape, cache.dtype)
+    op, os_, oh = _heads("out", out, shape, cache.dtype)
     lp = _vec("lens", lens, n, torch.int32)
     sp = None if lse is None else _vec("lse", lse, n * hq, torch.float32)
     if workspace is None:
