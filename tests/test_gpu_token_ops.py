@@ -641,3 +641,19 @@ def test_generation_loop_matches_whole_sequence():
     for i in range(steps):
         r, _, ds, ab = plain_decode(kc, vc, table, qs[i], torch.full((B,), i + 1), D ** -0.5, 0)
         close(outs[i], r, 2.0 ** -8 * r.abs() + (2.0 ** -19 * ds + 2.0 ** -14)[..., None] * ab)
+
+
+def test_example_learns():
+    """The example's loop: the log-probabilities of sampling and scoring agree, and the reward rises."""
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "grpo_tokens.py")
+    spec = importlib.util.spec_from_file_location("grpo_tokens", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    rows = ex.main(batches=12, tokens=24)
+    assert len({r["sequences"] for r in rows}) > 1
+    assert all(r["drift"] < 0.05 and r["entropy"] >= 0.0 for r in rows)
+    first, last = (sum(r["reward"] for r in x) / 3 for x in (rows[:3], rows[-3:]))
+    assert last > first + 0.05, (first, last)
