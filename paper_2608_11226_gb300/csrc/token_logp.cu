@@ -467,7 +467,7 @@ template <typename T, int ROWT> struct RowThreads {
 };
 
 template <typename T, int ROWT, bool TOP>
-__global__ void __launch_bounds__(RowThreads<T, ROWT>::kCta, (TOP ? 1024 : ROWT == 32 ? 1280 : 1536) / RowThreads<T, ROWT>::kCta) token_logp_kernel(LogpArgs a, int ranks) {
+__global__ void __launch_bounds__(RowThreads<T, ROWT>::kCta, (ROWT > 32 ? 1536 : TOP ? 1024 : 1280) / RowThreads<T, ROWT>::kCta) token_logp_kernel(LogpArgs a, int ranks) {
   // the next row's first loads before this one's joining: its registers would
   // cost the wide rows' CTAs a third of their warps
   constexpr bool kLoop = RowThreads<T, ROWT>::kLoop, kAhead = kLoop && !TOP;
@@ -684,7 +684,9 @@ static pe_status logp(const LogpArgs& a, cudaStream_t st) {
   const bool few = a.n <= 3 * 152;
   if (chunks <= (few ? 32 : 256)) return go_logp<T, 32>(a, 1, st);
   if (chunks <= (few ? 1024 : 2048)) return go_logp<T, 128>(a, 1, st);
-  if (chunks <= (few ? 2048 : 8192) || a.n >= 4 * 6 * 152) return go_logp<T, 256>(a, 1, st);
+  // Longer rows of 256 threads where all rows fit the SMs at once (six CTAs each)
+  // or fill them several times; in between 512, whose last round is shorter.
+  if (chunks <= (few ? 2048 : 8192) || (!few && a.n <= 6 * 152) || a.n >= 4 * 6 * 152) return go_logp<T, 256>(a, 1, st);
   // few rows: a cluster shares one, while each thread has four chunks
   int ranks = 1;
   while (ranks < 8 && a.n * ranks * 2 <= 304 && chunks >= 512 * 4 * ranks * 2) ranks *= 2;
