@@ -29,6 +29,23 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 5) kv_append_kernel(pe_kv_c
   const int c0 = t.interleaved || !turn ? 2 * item : item;
   const int c1 = t.interleaved || !turn ? c0 + 1 : item + rot / 16;
 
+  // the first heads are on their way before the position is known
+  const int begin = blockIdx.y * steps * kHeads + sub, end = min(heads, (int)(blockIdx.y + 1) * steps * kHeads);
+  uint4 x[kAhead], y[kAhead];
+  auto fetch = [&](int h0) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int h = h0 + u * kHeads;
+      if (h >= end) break;
+      const T* src = h < nq        ? (const T*)t.q + tok * t.q_token_stride + h * t.q_head_stride
+                     : h < nq + nk ? (const T*)t.k + tok * t.k_token_stride + (h - nq) * t.k_head_stride
+                                   : (const T*)t.v + tok * t.v_token_stride + (h - nq - nk) * t.v_head_stride;
+      x[u] = *reinterpret_cast<const uint4*>(src + c0 * 8);
+      y[u] = *reinterpret_cast<const uint4*>(src + c1 * 8);
+    }
+  };
+  fetch(begin);
+
   const bool live = p >= 0 && p < c.max_pages * c.page_size && (rot == 0 || p < t.max_pos) && s >= 0 && s < c.n_seqs;
   int64_t slot = -1;
   if (live) {
@@ -43,19 +60,8 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 5) kv_append_kernel(pe_kv_c
     si[0] = x.x, si[1] = x.y, si[2] = x.z, si[3] = x.w, si[4] = y.x, si[5] = y.y, si[6] = y.z, si[7] = y.w;
   }
 
-  const int begin = blockIdx.y * steps * kHeads + sub, end = min(heads, (int)(blockIdx.y + 1) * steps * kHeads);
   for (int h0 = begin; h0 < end; h0 += kAhead * kHeads) {
-    uint4 x[kAhead], y[kAhead];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int h = h0 + u * kHeads;
-      if (h >= end) break;
-      const T* src = h < nq        ? (const T*)t.q + tok * t.q_token_stride + h * t.q_head_stride
-                     : h < nq + nk ? (const T*)t.k + tok * t.k_token_stride + (h - nq) * t.k_head_stride
-                                   : (const T*)t.v + tok * t.v_token_stride + (h - nq - nk) * t.v_head_stride;
-      x[u] = *reinterpret_cast<const uint4*>(src + c0 * 8);
-      y[u] = *reinterpret_cast<const uint4*>(src + c1 * 8);
-    }
+    if (h0 != begin) fetch(h0);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int h = h0 + u * kHeads;
