@@ -603,13 +603,23 @@ __global__ void __launch_bounds__(256) token_logp_grad_kernel(LogpGradArgs a) {
   }
   const float lse = a.lse[r];
   const int t = a.g_logp ? a.tokens[r] : -1;
-  const float g = t >= 0 && t < a.V ? a.g_logp[r] : 0.0f;
-  const float ge = a.g_entropy ? a.g_entropy[r] : 0.0f, H = a.g_entropy ? a.entropy[r] : 0.0f;
+  const bool empty = lse == -CUDART_INF_F;  // no distribution: all zeros
+  const float g = t >= 0 && t < a.V && !empty ? a.g_logp[r] : 0.0f;
+  const float ge = a.g_entropy && !empty ? a.g_entropy[r] : 0.0f, H = a.g_entropy ? a.entropy[r] : 0.0f;
   // dz = p (A + B ln p)
-  const float A = -a.scale * fmaf(ge, H, g), B = -a.scale * ge;
-  const bool empty = lse == -CUDART_INF_F;
+  const float A = empty ? 0.0f : -a.scale * fmaf(ge, H, g), B = empty ? 0.0f : -a.scale * ge;
   const bool same = ((reinterpret_cast<uintptr_t>(row.x) ^ reinterpret_cast<uintptr_t>(y)) & 15) == 0;
-  const float2 sc = both2(a.scale), L = both2(-lse), l2 = both2(kLog2e), A2 = both2(A), B2 = both2(B);
+  const float2 sc = both2(a.scale), L = both2(empty ? 0.0f : -lse), l2 = both2(kLog2e), A2 = both2(A), B2 = both2(B);
+  auto gradient = [&](float2 x) {
+    float2 d = __ffma2_rn(x, sc, L);
+    // ln p of a forbidden token, kept finite: p is 0 there.  NaN stays
+    d = make_float2(max_nan(d.x, -1000.0f), max_nan(d.y, -1000.0f));
+    const float2 e = __fmul2_rn(d, l2);
+    float2 p;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(p.x) : "f"(e.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(p.y) : "f"(e.y));
+    return __fmul2_rn(p, __ffma2_rn(B2, d, A2));
+  };
 #pragma unroll
   for (int u = 0; u < kGradChunks; ++u) {
     const int64_t c = j + u * THREADS;
@@ -618,22 +628,19 @@ __global__ void __launch_bounds__(256) token_logp_grad_kernel(LogpGradArgs a) {
     const uint4 in = whole ? v[u] : row.any((int)c);
     uint4 out;
 #pragma unroll
-    for (int i = 0; i < C::kPairs; ++i) {
-      float2 d = __ffma2_rn(C::pair(in, i), sc, L);
-      // ln p of a forbidden token, kept finite: p is 0 there.  NaN stays
-      d.x = d.x < -1000.0f ? -1000.0f : d.x;
-      d.y = d.y < -1000.0f ? -1000.0f : d.y;
-      const float2 x = __fmul2_rn(d, l2);
-      float2 p;
-      asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(p.x) : "f"(x.x));
-      asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(p.y) : "f"(x.y));
-      float2 z = __fmul2_rn(p, __ffma2_rn(B2, d, A2));
-      const int e = (int)(c * C::kElems - row.mis) + 2 * i;
-      if (e == t) z.x = fmaf(a.scale, g, z.x);  // the target's own term
-      if (e + 1 == t) z.y = fmaf(a.scale, g, z.y);
-      if (empty) z = both2(0.0f);
-      C::put(out, i, z);
-    }
+    for (int i = 0; i < C::kPairs; ++i) C::put(out, i, gradient(C::pair(in, i)));
+    const int place = t - (int)(c * C::kElems - row.mis);  // of the target in the chunk, which adds its own term
+    if (place >= 0 && place < C::kElems)
+#pragma unroll
+      for (int i = 0; i < C::kPairs; ++i)
+        if (i == place >> 1) {
+          float2 z = gradient(C::pair(in, i));
+          if (place & 1)
+            z.y = fmaf(a.scale, g, z.y);
+          else
+            z.x = fmaf(a.scale, g, z.x);
+          C::put(out, i, z);
+        }
     if (whole && same) {
       __stcs(reinterpret_cast<uint4*>(y + (c * C::kElems - row.mis)), out);
     } else {
@@ -700,7 +707,9 @@ static void go_grad(const LogpGradArgs& a, int64_t chunks, cudaStream_t st) {
 
 template <typename T>
 static void grad(const LogpGradArgs& a, cudaStream_t st) {
-  const int64_t chunks = (int64_t)ceil_div(a.V, Chunk<T>::kElems) + 1;  // one more where the row is not aligned
+  // one more where rows do not start on 16 bytes
+  const bool aligned = reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 && (a.n == 1 || a.row_stride % Chunk<T>::kElems == 0);
+  const int64_t chunks = (int64_t)ceil_div(a.V, Chunk<T>::kElems) + (aligned ? 0 : 1);
   if (chunks <= 4 * 32)
     go_grad<T, 32>(a, chunks, st);
   else
