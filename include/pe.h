@@ -12,6 +12,10 @@
  *   pe_ppo_update   -- epochs x minibatches of clipped-loss PPO with Adam  (Sec. 4.2, 4.5)
  *   pe_fleet_windows-- composed fleet traces, window violation counts and
  *                      peaks over 0.5 s / 30 s / 5 min windows             (Sec. 7, 8, Eqs. 1-2)
+ * and, for a live generator in place of a replayed trace, the inner calls of
+ * the two phases that the controller governs (Sec. 4.1, 4.4):
+ *   pe_kv_append, pe_decode_attn          -- generation over a paged cache
+ *   pe_token_logp, pe_token_logp_grad     -- scoring of tokens and its gradient
  *
  * Conventions
  *  - Every buffer argument is a DEVICE pointer owned by the caller, unless

@@ -100,12 +100,13 @@ struct DecodeShape {
   static constexpr int kWarps = D == 256 && HT > 1 ? (HT == 3 ? 12 : 8) : 4;
   static constexpr int kThreads = 32 * kWarps;
   static constexpr int kTeams = kWarps / HT;
-  static constexpr int kCtas = D == 256 ? kDecodeCtas / 2 : kDecodeCtas;
+  static constexpr int kBlocks = D == 256 ? 1 : 2;  // CTAs on an SM
+  static constexpr int kCtas = 152 * kBlocks;
   static constexpr int kHeads = 8 * NT * HT;            // query heads of a segment
-  static constexpr int kUnit = D == 64 ? 32 : 16;       // positions of a stage
+  static constexpr int kUnit = D == 64 || (D == 128 && HT > 1) || (D == 256 && HT == 4) ? 32 : 16;  // positions of a stage
   static constexpr int kUnitBytes = 2 * kUnit * D * 2;  // its keys and values
   // a ring of 96 KB (two CTAs on an SM) or, for wide heads, 192 KB; at most 8 stages
-  static constexpr int kFit = (D == 256 ? 196608 : 98304) / (kTeams * kUnitBytes);
+  static constexpr int kFit = (kBlocks == 1 ? 196608 : 98304) / (kTeams * kUnitBytes);
   static constexpr int kStages = kFit > 8 ? 8 : kFit;
   static constexpr int kRing = kTeams * kStages * kUnitBytes;
   static constexpr int kPiece = 8 * NT * (D + 2);       // floats of a warp's piece: output, maxima, sums
@@ -118,7 +119,7 @@ struct DecodeShape {
   static constexpr int kExtra = kMerge > kWeights ? kMerge : kWeights;
   static constexpr int kSmem = kRing + kExtra;  // prefix sums at first, then what joins the teams, or the cluster
   static_assert(HT * kPiece * 4 <= kStages * kUnitBytes, "a team's piece in place of its ring");
-  static_assert(D == 256 ? kSmem <= 231000 : 2 * (kSmem + 1024 + 512) <= 233472, "shared memory of an SM");
+  static_assert(kBlocks == 1 ? kSmem <= 231000 : 2 * (kSmem + 1024 + 512) <= 233472, "shared memory of an SM");
 };
 
 struct Segment {
@@ -251,7 +252,7 @@ __device__ __forceinline__ void finish(const DecodeArgs& a, int seq, int64_t hea
 // least `least` to each.  by_seg: the joining kernel goes by segments and not
 // by CTAs.
 template <typename T, int D, int NT, int HT, bool CL>
-__global__ void __launch_bounds__(DecodeShape<D, NT, HT>::kThreads, D == 256 ? 1 : 2)
+__global__ void __launch_bounds__(DecodeShape<D, NT, HT>::kThreads, DecodeShape<D, NT, HT>::kBlocks)
     decode_attn_kernel(DecodeArgs a, int groups, int per_head, int page_shift, int ranks, int least, bool by_seg, float* part, SegMeta* meta) {
   using S = DecodeShape<D, NT, HT>;
   using M = Mma<T>;

@@ -539,9 +539,8 @@ def decode_attn(cache: KVCache, q: torch.Tensor, lens: torch.Tensor, out: torch.
     lp = _vec("lens", lens, n, torch.int32)
     sp = None if lse is None else _vec("lse", lse, n * hq, torch.float32)
     if workspace is None:
-        workspace = alloc_workspace(decode_attn_workspace_bytes(cache, hq))
-        if stream is not None:
-            workspace.record_stream(stream)  # used there, allocated here
+        with torch.cuda.stream(stream):  # of the stream that uses it (None: the current one)
+            workspace = alloc_workspace(decode_attn_workspace_bytes(cache, hq))
     _check(lib().pe_decode_attn(cache._ref, qp, qs, qh, hq, lp, cache.head_dim ** -0.5 if scale is None else scale,
                                 window, op, os_, oh, sp, workspace.data_ptr(), workspace.numel(), _stream_of(q, stream)))
 
