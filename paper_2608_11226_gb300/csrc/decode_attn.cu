@@ -4,7 +4,7 @@
 // Up to 16 query heads a key head run at 83% (head_dim 64) to 97% of the copy
 // rate on long caches (one sequence of 262,143 positions: 162 us, 6.6 TB/s);
 // beyond that the warps' chains of products and shuffles set the pace: 20 heads
-// 61-76%, 32 heads 51-65%, 64 heads 31-36%.
+// 61-76%, 32 heads 51-66%, 64 heads 34-41%.
 //
 // Work is cut into units of 16 (head_dim 64: 32) positions.  A team of HT warps
 // takes a unit at a time through its own ring of cp.async stages, and a CTA's
@@ -793,11 +793,13 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
 
 constexpr int64_t kMetaBytes = (kDecodeCtas * (int64_t)sizeof(SegMeta) + 255) / 256 * 256;
 
-// Heads of a segment for a group of query heads: up to 24 (head_dim 64: 32) in
-// one warp, whose registers hold their accumulators, more in the two or four
-// warps of a team, which share each unit.  Measured with 20 heads, 256 x 2,048
-// positions of 2 key heads: 104 us in one warp of three head tiles, 129 in two
-// of two; with 32 heads 131 us in two warps of two, 147 in one of four, which spills.
+// Heads of a segment for a group of query heads: up to 24 (head_dim 64: 32; 256:
+// 8) in one warp, whose registers hold their accumulators, more in the warps of a
+// team, which share each unit.  Measured with 256 x 2,048 positions of 2 key heads
+// of 128: 20 heads 104 us in one warp of three head tiles, 112 in three warps of
+// one; 16 heads 92 us in one warp, 94 in two; 32 heads 120 us in two warps of two,
+// 133 in four of one, 147 in one of four, which spills.  head_dim 256, 1,024
+// positions: 20 heads 130 us in three warps of one, 152 in two of two.
 static int seg_heads(int D, int group) {
   if (group <= 16) return group <= 8 ? 8 : 16;
   return group <= 24 ? 24 : group <= 32 ? 32 : 64;
@@ -811,17 +813,21 @@ int64_t decode_attn_ws_bytes(const pe_kv_cache& c, int n_q_heads) {
 
 // Ranks of the cluster that takes a segment, or 0 for the line of tiles.  The
 // positions that a segment can have at most and the segments' number decide.
-// Measured with 8 key heads of 128, cluster against line: 8 sequences of 512 7.6
-// against 9.5 us, 32 of 512 14.5 against 20.2, 1 of 4,096 11.0 against 10.0 (and
-// a launch less on the host); beyond the bounds 128 of 256 32.4 against 30.6, 1 of
-// 16,384 29.8 against 20.4.
+// Measured with 8 key heads of 128, cluster against line: 8 sequences of 512 6.8
+// against 9.5 us, 32 of 512 14.6 against 20.2, 1 of 4,096 11.0 against 10.0 (and
+// a launch less on the host); beyond the bounds 128 of 256 32.4 against 30.6, 128
+// of 64 16.8 against 13.5, 1 of 16,384 29.8 against 20.4.
 static int cluster_ranks(const DecodeArgs& a, int64_t segments, int tile) {
   int64_t most = (int64_t)a.c.max_pages * a.c.page_size;
   if (a.window > 0 && a.window + 32 < most) most = a.window + 32;
   const int64_t tiles = (most + tile - 1) / tile;
-  if (tiles * segments > 2048 || tiles > 64) return 0;
+  if (tiles * segments > 2048 || tiles > 64 || segments > 4 * 152) return 0;
+  // A larger cluster starts and joins later.  One sequence, 8 key heads, in 2, 4
+  // and 8 ranks: 200 positions 5.1, 5.8, 5.8 us; 700 7.5, 6.8, 7.5; 1,500 10.5,
+  // 8.5, 8.6; 3,000 16.7, 11.5, 10.1 (sixteen cost 13.0).
+  const int ranks = tiles < 3 ? 1 : tiles < 10 ? 2 : tiles < 24 ? 4 : kMaxRanks;
   int r = 1;
-  while (r < kMaxRanks && segments * r * 2 <= 2 * 152 && tiles >= 2 * r) r *= 2;
+  while (r < ranks && segments * r * 2 <= 2 * 152) r *= 2;
   return r;
 }
 
