@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Dict, Optional, Sequence
 
 import torch
@@ -86,6 +87,11 @@ class KVTokens(C.Structure):
                                  "q_out_head_stride", "k_token_stride", "k_head_stride", "v_token_stride",
                                  "v_head_stride")] + [
         (n, C.c_int32) for n in ("n_q_heads", "rot_dim", "interleaved")]
+
+
+# the same bytes at once: filling the structure's fields costs four times as much
+_KV_TOKENS = struct.Struct("17q3i4x").pack
+assert struct.calcsize("17q3i4x") == C.sizeof(KVTokens)
 
 
 EXPORTS = (
@@ -459,10 +465,11 @@ def _vec(name: str, t: torch.Tensor, n: int, dtype: torch.dtype) -> int:
 
 def _heads(name: str, t: torch.Tensor, shape: tuple, dtype: torch.dtype):
     """(pointer, row stride, head stride) of an [n][heads][head_dim] tensor."""
-    s0, s1, s2 = t.stride() if t.dim() == 3 else (0, 0, 0)
-    if t.shape != shape or t.dtype is not dtype or s2 != 1 or not t.is_cuda:
-        raise ValueError(f"{name} must be a {dtype} device tensor of {list(shape)} with adjacent elements")
-    return t.data_ptr(), s0 if shape[0] > 1 else 0, s1 if shape[1] > 1 else 0
+    if t.shape == shape and t.dtype is dtype and t.is_cuda:
+        s0, s1, s2 = t.stride()
+        if s2 == 1:
+            return t.data_ptr(), s0 if shape[0] > 1 else 0, s1 if shape[1] > 1 else 0
+    raise ValueError(f"{name} must be a {dtype} device tensor of {list(shape)} with adjacent elements")
 
 
 class KVCache:
@@ -518,9 +525,9 @@ def kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, positions: torch
             raise ValueError("rot must be a contiguous float32 device tensor of [positions, rot_dim]")
         rp = rot.data_ptr()
         max_pos, rot_dim = rot.shape
-    t = KVTokens(_vec("positions", positions, n, torch.int32), None if seqs is None else _vec("seqs", seqs, n, torch.int32),
-                 rp, qp, op, kp, vp, n, max_pos, qs, qh, os_, oh, ks, kh, vs, vh, hq, rot_dim, interleaved)
-    _check(lib().pe_kv_append(cache._ref, C.byref(t), _stream_of(k, stream)))
+    t = _KV_TOKENS(_vec("positions", positions, n, torch.int32), 0 if seqs is None else _vec("seqs", seqs, n, torch.int32),
+                   rp, qp, op, kp, vp, n, max_pos, qs, qh, os_, oh, ks, kh, vs, vh, hq, rot_dim, interleaved)
+    _check(lib().pe_kv_append(cache._ref, t, _stream_of(k, stream)))
 
 
 def decode_attn_workspace_bytes(cache: KVCache, n_q_heads: int) -> int:
@@ -547,10 +554,12 @@ def decode_attn(cache: KVCache, q: torch.Tensor, lens: torch.Tensor, out: torch.
 
 def _rows(name: str, t: torch.Tensor):
     """(pointer, dtype, rows, columns, row stride) of a matrix of logits."""
-    if t.dim() != 2 or t.dtype not in _DTYPE or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name} must be a float32, bf16 or fp16 device tensor of [rows, V] with adjacent elements")
-    n, V = t.shape
-    return t.data_ptr(), _DTYPE[t.dtype], n, V, t.stride(0) if n > 1 else V
+    dt = _DTYPE.get(t.dtype)
+    if dt is not None and t.is_cuda and t.ndim == 2:
+        (n, V), (rs, cs) = t.shape, t.stride()
+        if cs == 1 or V < 2:
+            return t.data_ptr(), dt, n, V, rs if n > 1 else V
+    raise ValueError(f"{name} must be a float32, bf16 or fp16 device tensor of [rows, V] with adjacent elements")
 
 
 def token_logp(logits: torch.Tensor, tokens: Optional[torch.Tensor], logp: Optional[torch.Tensor],
