@@ -19,6 +19,7 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 5) kv_append_kernel(pe_kv_c
   constexpr int kItems = D / 16, kHeads = 32 / kItems;  // items of a head; heads of a step
   const int lane = threadIdx.x & 31, item = lane % kItems, sub = lane / kItems;
   const int64_t tok = (int64_t)blockIdx.x * kAppendWarps + threadIdx.x / 32;
+  pdl_enter();
   if (tok >= t.n_tokens) return;
   const int nq = t.q ? t.n_q_heads : 0, nk = c.n_heads, heads = nq + 2 * nk;
   const int p = t.pos[tok];
@@ -97,7 +98,7 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 5) kv_append_kernel(pe_kv_c
 }
 
 template <typename T, int D>
-static void go(const pe_kv_cache& c, const pe_kv_tokens& t, cudaStream_t st) {
+static pe_status go(const pe_kv_cache& c, const pe_kv_tokens& t, cudaStream_t st) {
   constexpr int kHeads = 32 / (D / 16);
   const int heads = (t.q ? t.n_q_heads : 0) + 2 * c.n_heads;
   const int all = ceil_div(heads, kHeads);  // steps of a token
@@ -105,27 +106,21 @@ static void go(const pe_kv_cache& c, const pe_kv_tokens& t, cudaStream_t st) {
   // each SM; fewer tokens are split by heads
   const int64_t want = ceil_div(152 * 16, t.n_tokens);
   const int parts = (int)(want < all ? want : all), steps = ceil_div(all, parts);
-  kv_append_kernel<T, D><<<dim3((unsigned)ceil_div(t.n_tokens, kAppendWarps), ceil_div(all, steps)), 32 * kAppendWarps, 0, st>>>(c, t, steps);
+  PE_TRY_CUDA(launch_pdl(kv_append_kernel<T, D>, dim3((unsigned)ceil_div(t.n_tokens, kAppendWarps), ceil_div(all, steps)),
+                         dim3(32 * kAppendWarps), 0, st, true, c, t, steps));
+  return PE_OK;
 }
 
 template <typename T>
-static void go_dim(const pe_kv_cache& c, const pe_kv_tokens& t, cudaStream_t st) {
-  if (c.head_dim == 64)
-    go<T, 64>(c, t, st);
-  else if (c.head_dim == 128)
-    go<T, 128>(c, t, st);
-  else
-    go<T, 256>(c, t, st);
+static pe_status go_dim(const pe_kv_cache& c, const pe_kv_tokens& t, cudaStream_t st) {
+  if (c.head_dim == 64) return go<T, 64>(c, t, st);
+  if (c.head_dim == 128) return go<T, 128>(c, t, st);
+  return go<T, 256>(c, t, st);
 }
 
 pe_status kv_append_launch(const pe_kv_cache& c, const pe_kv_tokens& t, cudaStream_t st) {
   ProfScope ps(PE_PROF_KV_APPEND, st);
-  if (c.dtype == PE_BF16)
-    go_dim<__nv_bfloat16>(c, t, st);
-  else
-    go_dim<__half>(c, t, st);
-  PE_CHECK_LAUNCH("kv_append");
-  return PE_OK;
+  return c.dtype == PE_BF16 ? go_dim<__nv_bfloat16>(c, t, st) : go_dim<__half>(c, t, st);
 }
 
 }  // namespace pe
