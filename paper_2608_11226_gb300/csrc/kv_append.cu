@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 5) kv_append_kernel(pe_kv_c
   float co[8], si[8];
   if (live && turn) {
     const float4* r = reinterpret_cast<const float4*>(t.rot + (int64_t)p * rot + 8 * item);
-    const float4 a = __ldg(r), b = __ldg(r + 1), x = __ldg(r + rot / 8), y = __ldg(r + rot / 8 + 1);
+    const float4 a = r[0], b = r[1], x = r[rot / 8], y = r[rot / 8 + 1];
     co[0] = a.x, co[1] = a.y, co[2] = a.z, co[3] = a.w, co[4] = b.x, co[5] = b.y, co[6] = b.z, co[7] = b.w;
     si[0] = x.x, si[1] = x.y, si[2] = x.z, si[3] = x.w, si[4] = y.x, si[5] = y.y, si[6] = y.z, si[7] = y.w;
   }

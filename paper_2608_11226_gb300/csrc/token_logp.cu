@@ -140,7 +140,8 @@ template <typename T> struct Row {
   __device__ __forceinline__ int chunks() const { return (int)(((int64_t)mis + V + E - 1) / E); }
   __device__ __forceinline__ int first_whole() const { return mis ? 1 : 0; }
   __device__ __forceinline__ int end_whole() const { return (int)(((int64_t)mis + V) / E); }
-  __device__ __forceinline__ uint4 whole(int j) const { return __ldg(reinterpret_cast<const uint4*>(x + ((int64_t)j * E - mis))); }
+  // coherent: the kernel may be set up before the one that writes the logits has ended
+  __device__ __forceinline__ uint4 whole(int j) const { return __ldcg(reinterpret_cast<const uint4*>(x + ((int64_t)j * E - mis))); }
   // read once, and perhaps written in place: not through the read-only path
   __device__ __forceinline__ uint4 once(int j) const { return __ldcs(reinterpret_cast<const uint4*>(x + ((int64_t)j * E - mis))); }
   __device__ __forceinline__ uint4 any(int j) const {

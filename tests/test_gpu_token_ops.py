@@ -657,3 +657,24 @@ def test_example_learns():
     assert all(r["drift"] < 0.05 and r["entropy"] >= 0.0 for r in rows)
     first, last = (sum(r["reward"] for r in x) / 3 for x in (rows[:3], rows[-3:]))
     assert last > first + 0.05, (first, last)
+
+
+@pytest.mark.parametrize("n,V", [(3, 40000), (500, 1000), (64, 9001)])
+def test_chain_of_calls_needs_no_wait(n, V):
+    """Scoring and gradient in place, over and over, without a wait in between: each sees what the last one wrote."""
+    def chain(wait):
+        x, t = logits(n, V, F32, 3, 31, spread=1.0), targets(n, V, 31)
+        logp, ent, lse = (torch.empty(n, device="cuda") for _ in range(3))
+        gl, ge = torch.full((n,), 3.0, device="cuda"), torch.full((n,), 0.5, device="cuda")
+        for _ in range(12):
+            pe.token_logp(x, t, logp, entropy=ent, lse=lse)
+            if wait:
+                torch.cuda.synchronize()
+            pe.token_logp_grad(x, t, lse, x, g_logp=gl, entropy=ent, g_entropy=ge)
+            if wait:
+                torch.cuda.synchronize()
+        return x, logp, ent, lse
+
+    a = chain(True)
+    for _ in range(3):
+        assert all(torch.equal(p, q) for p, q in zip(chain(False), a))
