@@ -6,8 +6,8 @@
 // under the rotation, and keeps its cosines and sines while it goes through
 // the token's heads (query heads, key heads, value heads in one line); the
 // chunks of kAhead heads are in flight at a time: three, with five CTAs on an
-// SM (32,768 tokens of 64 + 16 heads of 128: 204 us, 98% of the copy rate; four
-// with four CTAs 206, two with eight 210).
+// SM (32,768 tokens of 64 + 16 heads of 128: 201 us, the copy rate; four with four
+// CTAs took 1% longer, two with eight 3%).
 #include "tokens.cuh"
 
 namespace pe {
