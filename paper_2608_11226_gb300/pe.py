@@ -486,12 +486,13 @@ class KVCache:
               "adjacent elements")
         _want(table.dim() == 2 and table.dtype == torch.int32 and table.is_cuda and (table.shape[1] < 2 or table.stride(1) == 1),
               "table must be an int32 device tensor of [sequences, pages] with adjacent entries")
+        _want(table.shape[0] < 2 or table.stride(0) >= table.shape[1], "table's rows must not overlap (an expanded row is no table)")
         self.k, self.v, self.table = k, v, table
         st = [k.stride(i) if k.shape[i] > 1 else 0 for i in range(3)]
         self.n_seqs, self.n_heads, self.head_dim, self.page_size = table.shape[0], k.shape[2], k.shape[3], k.shape[1]
         self.dtype = k.dtype
         self._desc = KVCacheDesc(k.data_ptr(), v.data_ptr(), table.data_ptr(), k.shape[0], st[0], st[1], st[2],
-                                 max(table.stride(0), table.shape[1]), table.shape[0], table.shape[1], k.shape[1],
+                                 table.stride(0) if table.shape[0] > 1 else table.shape[1], table.shape[0], table.shape[1], k.shape[1],
                                  k.shape[2], k.shape[3], _DTYPE[k.dtype])
         self._ref = C.byref(self._desc)
 
