@@ -301,7 +301,12 @@ __device__ void top_slice(const Row<T>& row, int j0, int j1, float mine, int k, 
     __syncwarp();
     const int pairs = __popc(who) * per;
     for (int p0 = 0; p0 < pairs; p0 += 64) {  // the warp stays together: all its branches are taken by all lanes
-      if (*(volatile int*)&sh.count > kCand) break;  // too many already: how many does not matter
+      // Too many already: how many does not matter.  Other warps change the
+      // count, so one lane reads it for all: lanes that saw different counts
+      // would part, and the warp's collectives below wait for every lane.
+      int seen = 0;
+      if (lane == 0) seen = *(volatile int*)&sh.count;
+      if (__shfl_sync(0xffffffffu, seen, 0) > kCand) break;
       uint4 v[2];
       int64_t e[2];
       uint32_t hit[2];
