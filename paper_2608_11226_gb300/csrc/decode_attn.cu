@@ -819,7 +819,7 @@ int64_t decode_attn_ws_bytes(const pe_kv_cache& c, int n_q_heads) {
 // of 64 16.8 against 13.5, 1 of 16,384 29.8 against 20.4.
 static int cluster_ranks(const DecodeArgs& a, int64_t segments, int tile) {
   int64_t most = (int64_t)a.c.max_pages * a.c.page_size;
-  if (a.window > 0 && a.window + 32 < most) most = a.window + 32;
+  if (a.window > 0 && (int64_t)a.window + 32 < most) most = (int64_t)a.window + 32;
   const int64_t tiles = (most + tile - 1) / tile;
   if (tiles * segments > 2048 || tiles > 64 || segments > 4 * 152) return 0;
   // A larger cluster starts and joins later.  One sequence, 8 key heads, in 2, 4

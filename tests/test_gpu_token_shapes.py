@@ -24,3 +24,16 @@ def test_logp_more_candidates_than_are_held(dtype, n, V):
         rows[torch.rand(rows.shape, generator=g, device="cuda") < share] = 4.0
     x[0, V // 2] = 5.0
     ops.check_logp(x.to(dtype), ops.targets(n, V, V), k=20)
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 32, 2 ** 31 - 33])
+@pytest.mark.parametrize("n", [40, 3000, 100003])
+def test_decode_window_beyond_any_length(n, window):
+    """A window that no length reaches is no window, bit for bit."""
+    g = ops.gen(n)
+    kc, vc, table = ops.make_cache([n, n // 3], 2, 64, 16, BF16, "slot", g)
+    q = torch.randn((2, 8, 64), generator=g, device="cuda").to(BF16)
+    lens = torch.tensor([n, n // 3], dtype=torch.int32, device="cuda")
+    want, want_lse = ops.check_decode(kc, vc, table, q, lens)
+    got, lse = ops.check_decode(kc, vc, table, q, lens, window=window)
+    assert torch.equal(got, want) and torch.equal(lse, want_lse)
