@@ -725,6 +725,7 @@ __global__ void __launch_bounds__(DecodeShape<D, NT, HT>::kThreads, DecodeShape<
       for (int p = 0; p < pieces; ++p) sum += piece_weight(wm[p * S::kHeads + tid], mm) * wl[p * S::kHeads + tid];
       const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
       for (int p = 0; p < pieces; ++p) wm[p * S::kHeads + tid] = piece_weight(wm[p * S::kHeads + tid], mm) * inv;
+      wl[tid] = sum == 0.0f ? 0.0f : 1.0f;  // 0: nothing attended to, whatever the values are (0 times inf is no 0)
       if (a.lse && blockIdx.x % ranks == 0 && h0 + tid < group) a.lse[(int64_t)cs.b * a.n_q_heads + head + tid] = log_sum<T>(mm, sum);
     }
     __syncthreads();
@@ -743,7 +744,8 @@ __global__ void __launch_bounds__(DecodeShape<D, NT, HT>::kThreads, DecodeShape<
         x.z = fmaf(f.x, v.z, x.z);
         x.w = fmaf(f.y, v.w, x.w);
       }
-      store_tile<T>((T*)a.out + cs.b * a.o_seq + (head + h) * a.o_head, a.o_head, group - h0 - h, in % (D / 16), x, 1.0f, 1.0f);
+      const float2 any = *reinterpret_cast<const float2*>(wl + h + 2 * (lane & 3));
+      store_tile<T>((T*)a.out + cs.b * a.o_seq + (head + h) * a.o_head, a.o_head, group - h0 - h, in % (D / 16), x, any.x, any.y);
     }
     if (ranks > 1) cl.sync();  // the others have read this rank's pieces
   }

@@ -37,3 +37,25 @@ def test_decode_window_beyond_any_length(n, window):
     want, want_lse = ops.check_decode(kc, vc, table, q, lens)
     got, lse = ops.check_decode(kc, vc, table, q, lens, window=window)
     assert torch.equal(got, want) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("n,spare", [(200, 0), (200, 9000), (9000, 0)])
+@pytest.mark.parametrize("D,group", [(64, 2), (64, 20), (128, 12), (128, 40), (256, 3), (256, 40)])
+def test_decode_nothing_but_minus_infinity(D, group, n, spare, dtype):
+    """Every score -inf: zero and -inf, whatever the values are, in small batches and in the line of tiles."""
+    g = ops.gen(n + D + group)
+    kc, vc, table = ops.make_cache([n, n], 1, D, 16, dtype, "slot", g, slack=1 + spare // 16)
+    at = table[0].long()[:-(-n // 16)]
+    kc[at, :, 0, 0] = -INF
+    vc[at[0], 3, 0, 5], vc[at[-1], 1, 0, 6], vc[at[2]] = INF, NAN, -INF
+    q = torch.randn((2, group, D), generator=g, device="cuda").to(dtype)
+    q[:, :, 0] = 1.0
+    lens = torch.tensor([n, n], dtype=torch.int32, device="cuda")
+    out, lse = torch.full_like(q, NAN), torch.full((2, group), NAN, device="cuda")
+    pe.decode_attn(pe.KVCache(kc, vc, table), q, lens, out, lse=lse)
+    assert bool((out[0] == 0).all()) and bool((lse[0] == -INF).all())
+    r, rl, ds, ab = (t[1] for t in ops.plain_decode(kc, vc, table, q, lens, D ** -0.5, 0))
+    ds = ds * 2.0 ** -20
+    ops.close(out[1], r, ops.U[dtype] * r.abs() + (2 * ds + 2.0 ** -14)[:, None] * ab + ops.TINY[dtype])
+    ops.close(lse[1], rl, ds + 2.0 ** -18 + 2.0 ** -22 * rl.abs())
