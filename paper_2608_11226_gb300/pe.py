@@ -445,10 +445,22 @@ def fleet_windows_noalloc(traces, job_of_gpu, J: int, offsets, H: int, windows: 
 _DTYPE = {torch.float32: PE_F32, torch.bfloat16: PE_BF16, torch.float16: PE_F16}
 
 
-def _stream_of(t: torch.Tensor, stream=None) -> int:
-    """The given stream, or the current one of the tensor's device (by its
-    handle alone: building a Stream object costs more than the launch)."""
-    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(t.get_device())
+_current_device = torch._C._cuda_getDevice
+
+
+def _stream_of(dev: int, stream=None) -> int:
+    """The given stream, or the device's current one (by its handle alone:
+    building a Stream object costs more than the launch)."""
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _launch_device(name: str, t: torch.Tensor) -> int:
+    """Device of a call: that of its tensors, which has to be the current one,
+    where the library launches."""
+    dev = t.get_device()
+    if dev < 0 or dev != _current_device():
+        raise ValueError(f"{name} must be on the current CUDA device")
+    return dev
 
 
 def _want(ok: bool, what: str):
@@ -456,20 +468,20 @@ def _want(ok: bool, what: str):
         raise ValueError(what)
 
 
-def _vec(name: str, t: torch.Tensor, n: int, dtype: torch.dtype) -> int:
+def _vec(name: str, t: torch.Tensor, n: int, dtype: torch.dtype, dev: int) -> int:
     """Device pointer of a contiguous vector of n elements."""
-    if t.dtype is not dtype or t.numel() != n or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} device tensor of {n} elements")
+    if t.dtype is not dtype or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements on device {dev}")
     return t.data_ptr()
 
 
-def _heads(name: str, t: torch.Tensor, shape: tuple, dtype: torch.dtype):
+def _heads(name: str, t: torch.Tensor, shape: tuple, dtype: torch.dtype, dev: int):
     """(pointer, row stride, head stride) of an [n][heads][head_dim] tensor."""
-    if t.shape == shape and t.dtype is dtype and t.is_cuda:
+    if t.shape == shape and t.dtype is dtype and t.get_device() == dev:
         s0, s1, s2 = t.stride()
         if s2 == 1:
             return t.data_ptr(), s0 if shape[0] > 1 else 0, s1 if shape[1] > 1 else 0
-    raise ValueError(f"{name} must be a {dtype} device tensor of {list(shape)} with adjacent elements")
+    raise ValueError(f"{name} must be a {dtype} tensor of {list(shape)} on device {dev} with adjacent elements")
 
 
 class KVCache:
@@ -477,7 +489,8 @@ class KVCache:
     [pages, slots, heads, head_dim] tensors of bf16 or fp16 with equal strides
     (a transposed view of [pages, heads, slots, head_dim] storage will do),
     table is [sequences, pages of a sequence] int32.  Holds the tensors; the
-    table's entries may change between calls."""
+    table's entries may change between calls.  The calls below run on the
+    current device, where all of their tensors have to be."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor):
         _want(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype
@@ -487,6 +500,7 @@ class KVCache:
         _want(table.dim() == 2 and table.dtype == torch.int32 and table.is_cuda and (table.shape[1] < 2 or table.stride(1) == 1),
               "table must be an int32 device tensor of [sequences, pages] with adjacent entries")
         _want(table.shape[0] < 2 or table.stride(0) >= table.shape[1], "table's rows must not overlap (an expanded row is no table)")
+        _want(k.get_device() == v.get_device() == table.get_device(), "k, v and table must be on one device")
         self.k, self.v, self.table = k, v, table
         st = [k.stride(i) if k.shape[i] > 1 else 0 for i in range(3)]
         self.n_seqs, self.n_heads, self.head_dim, self.page_size = table.shape[0], k.shape[2], k.shape[3], k.shape[1]
@@ -513,22 +527,23 @@ def kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, positions: torch
     their positions (int32), rotating q (into q_out, default in place) and k
     by position with rot ([positions, rot_dim], see rot_table); token t is of
     sequence seqs[t], or t where seqs is None."""
-    n, D, dt = positions.numel(), cache.head_dim, cache.dtype
-    kp, ks, kh = _heads("k", k, (n, cache.n_heads, D), dt)
-    vp, vs, vh = _heads("v", v, (n, cache.n_heads, D), dt)
+    n, D, dt, dev = positions.numel(), cache.head_dim, cache.dtype, _launch_device("the cache", cache.k)
+    kp, ks, kh = _heads("k", k, (n, cache.n_heads, D), dt, dev)
+    vp, vs, vh = _heads("v", v, (n, cache.n_heads, D), dt, dev)
     qp = qs = qh = op = os_ = oh = hq = rp = max_pos = rot_dim = 0
     if q is not None:
         hq = q.shape[1]
-        qp, qs, qh = _heads("q", q, (n, hq, D), dt)
-        op, os_, oh = (qp, qs, qh) if q_out is None else _heads("q_out", q_out, (n, hq, D), dt)
+        qp, qs, qh = _heads("q", q, (n, hq, D), dt, dev)
+        op, os_, oh = (qp, qs, qh) if q_out is None else _heads("q_out", q_out, (n, hq, D), dt, dev)
     if rot is not None:
-        if rot.dim() != 2 or rot.dtype is not torch.float32 or not rot.is_cuda or not rot.is_contiguous():
-            raise ValueError("rot must be a contiguous float32 device tensor of [positions, rot_dim]")
+        if rot.dim() != 2 or rot.dtype is not torch.float32 or rot.get_device() != dev or not rot.is_contiguous():
+            raise ValueError(f"rot must be a contiguous float32 tensor of [positions, rot_dim] on device {dev}")
         rp = rot.data_ptr()
         max_pos, rot_dim = rot.shape
-    t = _KV_TOKENS(_vec("positions", positions, n, torch.int32), 0 if seqs is None else _vec("seqs", seqs, n, torch.int32),
-                   rp, qp, op, kp, vp, n, max_pos, qs, qh, os_, oh, ks, kh, vs, vh, hq, rot_dim, interleaved)
-    _check(lib().pe_kv_append(cache._ref, t, _stream_of(k, stream)))
+    t = _KV_TOKENS(_vec("positions", positions, n, torch.int32, dev),
+                   0 if seqs is None else _vec("seqs", seqs, n, torch.int32, dev), rp, qp, op, kp, vp, n, max_pos,
+                   qs, qh, os_, oh, ks, kh, vs, vh, hq, rot_dim, interleaved)
+    _check(lib().pe_kv_append(cache._ref, t, _stream_of(dev, stream)))
 
 
 def decode_attn_workspace_bytes(cache: KVCache, n_q_heads: int) -> int:
@@ -540,27 +555,29 @@ def decode_attn(cache: KVCache, q: torch.Tensor, lens: torch.Tensor, out: torch.
                 stream=None):
     """out[b] = attention of q[b] ([sequences, query heads, head_dim]) over the
     lens[b] (int32) positions of sequence b; scale defaults to head_dim^-1/2."""
-    n, hq = cache.n_seqs, q.shape[1]
+    n, hq, dev = cache.n_seqs, q.shape[1], _launch_device("the cache", cache.k)
     shape = (n, hq, cache.head_dim)
-    qp, qs, qh = _heads("q", q, shape, cache.dtype)
-    op, os_, oh = _heads("out", out, shape, cache.dtype)
-    lp = _vec("lens", lens, n, torch.int32)
-    sp = None if lse is None else _vec("lse", lse, n * hq, torch.float32)
+    qp, qs, qh = _heads("q", q, shape, cache.dtype, dev)
+    op, os_, oh = _heads("out", out, shape, cache.dtype, dev)
+    lp = _vec("lens", lens, n, torch.int32, dev)
+    sp = None if lse is None else _vec("lse", lse, n * hq, torch.float32, dev)
     if workspace is None:
         with torch.cuda.stream(stream):  # of the stream that uses it (None: the current one)
             workspace = alloc_workspace(decode_attn_workspace_bytes(cache, hq))
+    elif workspace.get_device() != dev:
+        raise ValueError(f"workspace must be on device {dev}")
     _check(lib().pe_decode_attn(cache._ref, qp, qs, qh, hq, lp, cache.head_dim ** -0.5 if scale is None else scale,
-                                window, op, os_, oh, sp, workspace.data_ptr(), workspace.numel(), _stream_of(q, stream)))
+                                window, op, os_, oh, sp, workspace.data_ptr(), workspace.numel(), _stream_of(dev, stream)))
 
 
-def _rows(name: str, t: torch.Tensor):
+def _rows(name: str, t: torch.Tensor, dev: int):
     """(pointer, dtype, rows, columns, row stride) of a matrix of logits."""
     dt = _DTYPE.get(t.dtype)
-    if dt is not None and t.is_cuda and t.ndim == 2:
+    if dt is not None and t.get_device() == dev and t.ndim == 2:
         (n, V), (rs, cs) = t.shape, t.stride()
         if cs == 1 or V < 2:
             return t.data_ptr(), dt, n, V, rs if n > 1 else V
-    raise ValueError(f"{name} must be a float32, bf16 or fp16 device tensor of [rows, V] with adjacent elements")
+    raise ValueError(f"{name} must be a float32, bf16 or fp16 tensor of [rows, V] on device {dev} with adjacent elements")
 
 
 def token_logp(logits: torch.Tensor, tokens: Optional[torch.Tensor], logp: Optional[torch.Tensor],
@@ -570,17 +587,18 @@ def token_logp(logits: torch.Tensor, tokens: Optional[torch.Tensor], logp: Optio
     """Log-probabilities (fp32) of tokens (int32, negative: no target) under
     softmax(scale * logits), with the rows' entropies, log sums and top
     alternatives (top_logp fp32 and top_id int32, [rows, k]) where asked for."""
-    p, dt, n, V, rs = _rows("logits", logits)
+    dev = _launch_device("logits", logits)
+    p, dt, n, V, rs = _rows("logits", logits, dev)
     f = torch.float32
     k = 0
     if top_id is not None or top_logp is not None:
         _want(top_id is not None and top_logp is not None and top_id.dim() == 2, "top_logp and top_id go together, [rows, k]")
         k = top_id.shape[1]
     _check(lib().pe_token_logp(
-        p, dt, n, V, rs, None if tokens is None else _vec("tokens", tokens, n, torch.int32), scale,
-        None if logp is None else _vec("logp", logp, n, f), None if entropy is None else _vec("entropy", entropy, n, f),
-        None if lse is None else _vec("lse", lse, n, f), k, None if not k else _vec("top_logp", top_logp, n * k, f),
-        None if not k else _vec("top_id", top_id, n * k, torch.int32), _stream_of(logits, stream)))
+        p, dt, n, V, rs, None if tokens is None else _vec("tokens", tokens, n, torch.int32, dev), scale,
+        None if logp is None else _vec("logp", logp, n, f, dev), None if entropy is None else _vec("entropy", entropy, n, f, dev),
+        None if lse is None else _vec("lse", lse, n, f, dev), k, None if not k else _vec("top_logp", top_logp, n * k, f, dev),
+        None if not k else _vec("top_id", top_id, n * k, torch.int32, dev), _stream_of(dev, stream)))
 
 
 def token_logp_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor], lse: torch.Tensor, dlogits: torch.Tensor,
@@ -588,15 +606,16 @@ def token_logp_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor], lse: t
                     g_entropy: Optional[torch.Tensor] = None, scale: float = 1.0, stream=None):
     """dlogits = gradient of sum(g_logp logp) + sum(g_entropy entropy) in the
     logits, from token_logp's lse and entropy; dlogits may be logits itself."""
-    p, dt, n, V, rs = _rows("logits", logits)
-    dp, ddt, dn, dV, ds = _rows("dlogits", dlogits)
+    dev = _launch_device("logits", logits)
+    p, dt, n, V, rs = _rows("logits", logits, dev)
+    dp, ddt, dn, dV, ds = _rows("dlogits", dlogits, dev)
     _want(ddt == dt and dn == n and dV == V, "dlogits must have the logits' shape and dtype")
     f = torch.float32
     _check(lib().pe_token_logp_grad(
-        p, dt, n, V, rs, None if tokens is None else _vec("tokens", tokens, n, torch.int32), scale,
-        _vec("lse", lse, n, f), None if entropy is None else _vec("entropy", entropy, n, f),
-        None if g_logp is None else _vec("g_logp", g_logp, n, f),
-        None if g_entropy is None else _vec("g_entropy", g_entropy, n, f), dp, ds, _stream_of(logits, stream)))
+        p, dt, n, V, rs, None if tokens is None else _vec("tokens", tokens, n, torch.int32, dev), scale,
+        _vec("lse", lse, n, f, dev), None if entropy is None else _vec("entropy", entropy, n, f, dev),
+        None if g_logp is None else _vec("g_logp", g_logp, n, f, dev),
+        None if g_entropy is None else _vec("g_entropy", g_entropy, n, f, dev), dp, ds, _stream_of(dev, stream)))
 
 
 def profile_enable(on: bool):
