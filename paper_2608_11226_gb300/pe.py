@@ -564,8 +564,8 @@ def decode_attn(cache: KVCache, q: torch.Tensor, lens: torch.Tensor, out: torch.
     if workspace is None:
         with torch.cuda.stream(stream):  # of the stream that uses it (None: the current one)
             workspace = alloc_workspace(decode_attn_workspace_bytes(cache, hq))
-    elif workspace.get_device() != dev:
-        raise ValueError(f"workspace must be on device {dev}")
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous, on device {dev}")
     _check(lib().pe_decode_attn(cache._ref, qp, qs, qh, hq, lp, cache.head_dim ** -0.5 if scale is None else scale,
                                 window, op, os_, oh, sp, workspace.data_ptr(), workspace.numel(), _stream_of(dev, stream)))
 

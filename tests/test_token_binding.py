@@ -126,3 +126,11 @@ def test_a_cache_lies_on_one_device(part, where):
     t[part] = t[part].as_subclass(where)
     with pytest.raises(ValueError):
         pe.KVCache(*t)
+
+
+@pytest.mark.parametrize("ws", [torch.zeros(1, dtype=torch.uint8).expand(1 << 20), torch.zeros(1 << 20, dtype=torch.uint8)[::2]],
+                         ids=["expanded", "strided"])
+def test_a_workspace_is_contiguous(on_device_0, ws):
+    f, make = CALLS["decode"]
+    with pytest.raises(ValueError):
+        f(**dict(make(), workspace=dev(ws)))
