@@ -446,6 +446,7 @@ _DTYPE = {torch.float32: PE_F32, torch.bfloat16: PE_BF16, torch.float16: PE_F16}
 
 
 _current_device = torch._C._cuda_getDevice
+_INT32 = 2 ** 31 - 1  # the largest size of an int32 argument; ctypes drops what is above
 
 
 def _stream_of(dev: int, stream=None) -> int:
@@ -499,6 +500,7 @@ class KVCache:
               "adjacent elements")
         _want(table.dim() == 2 and table.dtype == torch.int32 and table.is_cuda and (table.shape[1] < 2 or table.stride(1) == 1),
               "table must be an int32 device tensor of [sequences, pages] with adjacent entries")
+        _want(max(table.shape) <= _INT32 and max(k.shape[1:]) <= _INT32, "sizes must be below 2^31")
         _want(table.shape[0] < 2 or table.stride(0) >= table.shape[1], "table's rows must not overlap (an expanded row is no table)")
         _want(k.get_device() == v.get_device() == table.get_device(), "k, v and table must be on one device")
         self.k, self.v, self.table = k, v, table
@@ -561,6 +563,8 @@ def decode_attn(cache: KVCache, q: torch.Tensor, lens: torch.Tensor, out: torch.
     op, os_, oh = _heads("out", out, shape, cache.dtype, dev)
     lp = _vec("lens", lens, n, torch.int32, dev)
     sp = None if lse is None else _vec("lse", lse, n * hq, torch.float32, dev)
+    if abs(window) > _INT32:
+        raise ValueError("window must be in [0, 2^31)")
     if workspace is None:
         with torch.cuda.stream(stream):  # of the stream that uses it (None: the current one)
             workspace = alloc_workspace(decode_attn_workspace_bytes(cache, hq))
@@ -575,7 +579,7 @@ def _rows(name: str, t: torch.Tensor, dev: int):
     dt = _DTYPE.get(t.dtype)
     if dt is not None and t.get_device() == dev and t.ndim == 2:
         (n, V), (rs, cs) = t.shape, t.stride()
-        if cs == 1 or V < 2:
+        if (cs == 1 or V < 2) and V <= _INT32:
             return t.data_ptr(), dt, n, V, rs if n > 1 else V
     raise ValueError(f"{name} must be a float32, bf16 or fp16 tensor of [rows, V] on device {dev} with adjacent elements")
 

@@ -134,3 +134,28 @@ def test_a_workspace_is_contiguous(on_device_0, ws):
     f, make = CALLS["decode"]
     with pytest.raises(ValueError):
         f(**dict(make(), workspace=dev(ws)))
+
+
+# ---------------------------------------------------------------------------
+# sizes that a 32-bit argument does not hold
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("window", [2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 63 - 1, -2 ** 32, -2 ** 32 + 5])
+def test_a_window_that_passes_32_bits_is_refused(on_device_0, window):
+    f, make = CALLS["decode"]
+    with pytest.raises(ValueError):
+        f(**make(), window=window)
+
+
+@pytest.mark.parametrize("V", [2 ** 31, 2 ** 32 + 9])
+@pytest.mark.parametrize("call", ["logp", "grad"])
+def test_rows_that_pass_32_bits_are_refused(on_device_0, call, V):
+    f, make = CALLS[call]
+    a = {k: t[:0] for k, t in make().items()}
+    a.update({k: z(0, V) for k in ("logits", "dlogits") if k in a})
+    with pytest.raises(ValueError):
+        f(**a)
+
+
+def test_a_table_that_passes_32_bits_is_refused():
+    with pytest.raises(ValueError):
+        pe.KVCache(pages(), pages(), dev(torch.empty((0, 2 ** 32 + 2), dtype=I32)))
