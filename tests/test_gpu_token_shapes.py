@@ -59,3 +59,52 @@ def test_decode_nothing_but_minus_infinity(D, group, n, spare, dtype):
     ds = ds * 2.0 ** -20
     ops.close(out[1], r, ops.U[dtype] * r.abs() + (2 * ds + 2.0 ** -14)[:, None] * ab + ops.TINY[dtype])
     ops.close(lse[1], rl, ds + 2.0 ** -18 + 2.0 ** -22 * rl.abs())
+
+
+def wide_cache(lens, Hkv, D, page, dtype, capacity, g):
+    """A cache whose table has room for `capacity` positions of each sequence, as a server's has for the model's
+    context; the entries beyond a length name a page of NaN."""
+    kc, vc, exact = ops.make_cache(lens, Hkv, D, page, dtype, "slot", g, slack=0, spare=1)
+    unused = torch.ones(kc.shape[0], dtype=torch.bool, device="cuda")
+    unused[exact.long().flatten()] = False
+    table = torch.full((len(lens), capacity // page + 3), int(torch.nonzero(unused)[0]), dtype=torch.int32, device="cuda")
+    for b, n in enumerate(lens):
+        table[b, :-(-n // page)] = exact[b, :-(-n // page)]
+    return kc, vc, table[:, :capacity // page]
+
+
+# Every number of query heads at which a warp, or a team of warps, takes another number of them together, in the three
+# ways in which sequences come: few and short (clusters), long ones in a line of tiles, more of them than CTAs.
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("way", ["short", "long", "many"])
+@pytest.mark.parametrize("group", [1, 8, 9, 16, 17, 24, 25, 32, 33, 64, 65])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_decode_heads(D, group, way, dtype):
+    g = ops.gen(D + group)
+    lens, Hkv, capacity = {"short": ([37, 0, 300], 2, 304), "long": ([2100, 5, 700], 2, 16384),
+                           "many": ([(i * 37) % 601 for i in range(44)], 8, 16384)}[way]
+    kc, vc, table = wide_cache(lens, Hkv, D, 16, dtype, capacity, g)
+    q = (2 * torch.randn((len(lens), Hkv * group, D), generator=g, device="cuda")).to(dtype)
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    for window in (0, 130):
+        ops.check_decode(kc, vc, table, q, n, window=window)
+
+
+def test_decode_on_two_streams_at_once():
+    """Calls on two streams, each with a workspace of its own, over one cache."""
+    g = ops.gen(40)
+    lens = [9000, 1, 4000, 333]
+    kc, vc, table = wide_cache(lens, 2, 128, 16, BF16, 16384, g)
+    cache, n = pe.KVCache(kc, vc, table), torch.tensor(lens, dtype=torch.int32, device="cuda")
+    qs = [torch.randn((4, 8, 128), generator=g, device="cuda").to(BF16) for _ in range(2)]
+    want = [ops.check_decode(kc, vc, table, q, n)[0] for q in qs]
+    streams = [torch.cuda.Stream() for _ in qs]
+    ws = [pe.alloc_workspace(pe.decode_attn_workspace_bytes(cache, 8)) for _ in qs]
+    outs = [[torch.full_like(q, NAN) for _ in range(20)] for q in qs]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for q, st, w, out in zip(qs, streams, ws, outs):
+            pe.decode_attn(cache, q, n, out[i], workspace=w, stream=st)
+    torch.cuda.synchronize()
+    for out, r in zip(outs, want):
+        assert all(torch.equal(o, r) for o in out)
