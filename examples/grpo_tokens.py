@@ -1,7 +1,8 @@
 """Generation and update of a small policy under the power controller.
 
 The controller (here the hysteresis rule over the 72B-shaped trace) sets the
-generation concurrency, batch by batch.  Each batch then runs both phases of
+generation concurrency, batch by batch, all of it from the replayed trace: the
+power of the batches below does not flow back.  Each batch runs both phases of
 group-relative policy optimisation on the same GPU:
 
   generation  per token: keys and values into a paged cache with the position

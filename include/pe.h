@@ -12,8 +12,8 @@
  *   pe_ppo_update   -- epochs x minibatches of clipped-loss PPO with Adam  (Sec. 4.2, 4.5)
  *   pe_fleet_windows-- composed fleet traces, window violation counts and
  *                      peaks over 0.5 s / 30 s / 5 min windows             (Sec. 7, 8, Eqs. 1-2)
- * and, for a live generator in place of a replayed trace, the inner calls of
- * the two phases that the controller governs (Sec. 4.1, 4.4):
+ * and, beside that path and not called by it, the inner calls of the two
+ * phases of the workload whose power the traces record (Sec. 4.1, 4.4):
  *   pe_kv_append, pe_decode_attn          -- generation over a paged cache
  *   pe_token_logp, pe_token_logp_grad     -- scoring of tokens and its gradient
  *
@@ -421,8 +421,8 @@ pe_status pe_fleet_windows_noalloc(const float* traces, int32_t G, int32_t L,
 
 /* ------------------------------------------------------------------------
  * Token operators: the inner calls of the post-training that the controller
- * governs, for callers that drive a live generator beside it instead of a
- * replayed trace.  Generation (phase 0, Sec. 4.4), per token: pe_kv_append and
+ * governs, for callers that run that workload themselves; nothing of the
+ * calls above uses them.  Generation (phase 0, Sec. 4.4), per token: pe_kv_append and
  * pe_decode_attn.  Update (phase 1): pe_token_logp and its gradient, the
  * log-probability and entropy of step a9 over a vocabulary instead of 16
  * actions.  Element types: PE_BF16 and PE_F16, and PE_F32 for logits; sums,
@@ -437,7 +437,8 @@ pe_status pe_fleet_windows_noalloc(const float* traces, int32_t G, int32_t L,
  * page: nothing is written to its positions, and they take no part in
  * attention (an evicted or unassigned page).
  *  k, v: device, 16-byte aligned; strides multiples of 8 elements;
- *  table: [n_seqs] rows of max_pages int32, table_stride apart, device;
+ *  table: [n_seqs] rows of max_pages int32, table_stride >= max_pages apart,
+ *  device;
  *  head_dim in {64, 128, 256}; page_size in [1, 65536];
  *  max_pages * page_size <= 2^30; dtype PE_BF16 or PE_F16. */
 typedef struct pe_kv_cache {
@@ -473,7 +474,7 @@ typedef struct pe_kv_tokens {
  * A token whose position is outside [0, max_pos) (rot_dim > 0), negative or
  * at or beyond the table's capacity, or whose sequence is outside
  * [0, n_seqs), is padding: nothing is written to the cache and its q_out row
- * becomes zero.  Two tokens at one position of one sequence leave either's.
+ * becomes zero.  Two tokens at one position of one sequence leave a mix of both.
  *  rot_dim: 0, or a multiple of 16 up to D; every pointer to vectors 16-byte
  *  aligned and their strides multiples of 8 elements; rot 16-byte aligned.
  * Errors: PE_EINVAL, PE_ECUDA. */
@@ -490,6 +491,9 @@ pe_status pe_kv_append(const pe_kv_cache* cache, const pe_kv_tokens* tokens, voi
  * zero and lse -inf.  What lies in cache slots that are not attended to is
  * not used, whatever it holds.  An infinite value that is attended to makes
  * its element infinite or NaN; a NaN or +inf score makes the head NaN.
+ * Weights enter the sum of values with 16 bits or more; with PE_F16 one below
+ * 2^-31 of the largest may count as 0 there (not in lse).  A window that no
+ * length reaches is the same as 0.
  *  q, out: [n_seqs][n_q_heads][D] in the cache's dtype, strides in elements
  *  (multiples of 8, 16-byte aligned); lens: [n_seqs] int32; lse:
  *  [n_seqs][n_q_heads] fp32 or NULL; n_q_heads a multiple of n_heads.

