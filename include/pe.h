@@ -15,6 +15,8 @@
  * and, beside that path and not called by it, the inner calls of the two
  * phases of the workload whose power the traces record (Sec. 4.1, 4.4):
  *   pe_kv_append, pe_decode_attn          -- generation over a paged cache
+ *   pe_kv_append_at, pe_decode_attn8      -- the same over a cache in 8 bits
+ *   pe_tree_attn, pe_kv_move              -- drafted tokens: attention, and the accepted ones' rows
  *   pe_token_logp, pe_token_logp_grad     -- scoring of tokens and its gradient
  *
  * Conventions
@@ -71,6 +73,7 @@ typedef int32_t pe_status;
 #define PE_F32 0
 #define PE_BF16 1
 #define PE_F16 2 /* token operators only */
+#define PE_E4M3 3 /* codes of an 8-bit cache only: sign, 4 exponent bits, 3 bits of mantissa, no infinity */
 /* pe_rollout flags */
 #define PE_ROLLOUT_DETERMINISTIC 1 /* argmax action, lowest index on ties (Sec. 4.4 evaluation) */
 
@@ -506,6 +509,90 @@ pe_status pe_decode_attn(const pe_kv_cache* cache, const void* q, int64_t q_seq_
                          int64_t out_seq_stride, int64_t out_head_stride, float* lse, void* workspace,
                          int64_t workspace_bytes, void* stream);
 
+/* Scales of an 8-bit cache (dtype PE_E4M3, one byte an element): one byte for
+ * each row (position and head) of keys and of values, at
+ * page * page_stride + slot * slot_stride + head * head_stride.  Byte b stands
+ * for 2^(b - 127); 255 for NaN; bytes below 63 count as 63, others above 247 as
+ * 247.  A row's elements are its codes times its scale.
+ * Used by the calls below, which take a 16-bit cache with NULL in its place.
+ * An 8-bit cache's k and v are 16-byte aligned and its strides multiples of
+ * 16; the calls above refuse it. */
+typedef struct pe_kv_scales {
+  uint8_t *k, *v;                                 /* device */
+  int64_t page_stride, slot_stride, head_stride;  /* in bytes, of both */
+} pe_kv_scales;
+
+/* pe_kv_append into either kind of cache, at slots that are not the tokens'
+ * positions: token t is rotated by pos[t] and written to position slots[t] of
+ * its sequence (drafted tokens of one depth share a position, not a slot).
+ * slots NULL: pos.  A token whose pos or slot is out of range is padding.
+ * A 16-bit cache (scales NULL) gets what pe_kv_append writes.  For an 8-bit
+ * cache a row x -- a key after its rotation, whose two products and sum are
+ * each rounded to fp32, or a value -- with a = max |x_d| gets
+ *   e = the least integer >= -64 with a <= 448 * 2^e,  scale byte e + 127,
+ *   codes x_d / 2^e rounded to nearest even (nothing saturates);
+ * a row with an element that is not finite gets scale 255 and codes 0.
+ *  dtype: of q, k and v (PE_BF16 or PE_F16; the cache's if that has 16 bits).
+ * Errors: PE_EINVAL, PE_ECUDA. */
+pe_status pe_kv_append_at(const pe_kv_cache* cache, const pe_kv_scales* scales, const pe_kv_tokens* tokens,
+                          const int32_t* slots, int32_t dtype, void* stream);
+
+/* pe_decode_attn over an 8-bit cache; q and out are of `dtype` (PE_BF16 or
+ * PE_F16).  A position whose key or value scale is 255 makes the heads that
+ * attend to it NaN. */
+int64_t pe_decode_attn8_workspace_bytes(const pe_kv_cache* cache, int32_t n_q_heads);
+pe_status pe_decode_attn8(const pe_kv_cache* cache, const pe_kv_scales* scales, int32_t dtype, const void* q,
+                          int64_t q_seq_stride, int64_t q_head_stride, int32_t n_q_heads, const int32_t* lens,
+                          float scale, int32_t window, void* out, int64_t out_seq_stride, int64_t out_head_stride,
+                          float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Drafted tokens of each sequence, a tree of n_nodes at most: node i of
+ * sequence b lies at position lens[b] + i of the cache (its keys and values
+ * have been appended there).  Bit a of mask[b * mask_stride + i]: node i
+ * attends to node a (its ancestors and itself; bits from n_nodes on are
+ * ignored); a mask of 0: node i is padding. */
+typedef struct pe_tree_queries {
+  const void* q;         /* [n_seqs][n_nodes][n_q_heads][D] */
+  void* out;             /* the same shape */
+  float* lse;            /* [n_seqs][n_nodes][n_q_heads], or NULL */
+  const int32_t* lens;   /* [n_seqs] positions ahead of the tree, clamped to [0, max_pages * page_size] */
+  const uint64_t* mask;  /* [n_seqs] rows of n_nodes; mask_stride 0: one tree for all */
+  int64_t q_seq_stride, q_node_stride, q_head_stride, out_seq_stride, out_node_stride, out_head_stride;
+  int64_t mask_stride;
+  int32_t n_nodes, n_q_heads, dtype; /* n_nodes in [0, 64]; dtype of q and out: PE_BF16 or PE_F16 */
+} pe_tree_queries;
+
+/* Attention of drafted tokens over either kind of cache (scales NULL: 16
+ * bits, dtype the cache's).  With n = lens[b], a node that is no padding
+ * attends to the positions [0, n) and to the nodes of its mask; with window > 0
+ * it stands at position n + c - 1, c the number of its mask's bits, and attends
+ * to the positions [max(0, n + c - window), n) and the nodes of its mask.
+ * Positions of absent pages, and nodes at or beyond the table's capacity, take
+ * no part.  Formulas, head groups, scale and what is made of empty rows and of
+ * slots that are not attended to as in pe_decode_attn, for each node by
+ * itself: a row that does not attend to a node does not see what that holds.
+ * Weights enter the sum of values rounded to 16 bits (bf16 cache: bf16, others:
+ * fp16, where one below 2^-30 of the largest may count as 0).
+ *  strides in elements, multiples of 8, 16-byte aligned; window 0 or >= 64.
+ *  workspace: >= pe_tree_attn_workspace_bytes(...) bytes of device memory,
+ *  256-byte aligned; its contents need not be kept between calls.
+ * Errors: PE_EINVAL, PE_ECUDA. */
+int64_t pe_tree_attn_workspace_bytes(const pe_kv_cache* cache, int32_t n_nodes, int32_t n_q_heads);
+pe_status pe_tree_attn(const pe_kv_cache* cache, const pe_kv_scales* scales, const pe_tree_queries* tree, float scale,
+                       int32_t window, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Move rows of a cache (keys, values, scales; every head): position dst[b][i]
+ * of sequence b gets what position src[b][i] held before the call, so that the
+ * accepted nodes of a tree end up at consecutive positions.  A move whose src
+ * or dst is outside [0, max_pages * page_size) or on an absent page is left
+ * out.  Two moves to one position leave a mix of both; so do moves of
+ * sequences that share the pages they write.
+ *  src, dst: device, [n_seqs] rows of n_moves int32, src_stride and dst_stride
+ *  (>= n_moves) apart; n_moves in [0, 64].
+ * Errors: PE_EINVAL, PE_ECUDA. */
+pe_status pe_kv_move(const pe_kv_cache* cache, const pe_kv_scales* scales, const int32_t* src, int64_t src_stride,
+                     const int32_t* dst, int64_t dst_stride, int32_t n_moves, void* stream);
+
 /* Log-probabilities of given tokens, with the entropy and the top_k most
  * likely tokens of each row.  With z_j = scale * logits[r][j] (scale is an
  * inverse temperature), m = max_j z_j and S = sum_j e^(z_j - m):
@@ -561,7 +648,9 @@ pe_status pe_token_logp_grad(const void* logits, int32_t dtype, int64_t n, int32
 #define PE_PROF_DECODE_ATTN 12
 #define PE_PROF_TOKEN_LOGP 13
 #define PE_PROF_TOKEN_LOGP_GRAD 14
-#define PE_PROF_KINDS 15
+#define PE_PROF_TREE_ATTN 15
+#define PE_PROF_KV_MOVE 16
+#define PE_PROF_KINDS 17
 pe_status pe_profile_enable(int32_t on);
 pe_status pe_profile_read(int32_t kind, double* total_ms, int64_t* launches);
 const char* pe_profile_kind_name(int32_t kind);

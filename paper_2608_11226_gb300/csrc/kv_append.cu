@@ -1,6 +1,6 @@
-// Keys and values of new tokens into a paged cache; queries and keys are
-// rotated by their position on the way (formulas: pe.h).  HBM-bound: each row
-// is read and written once, two FMAs an element.
+// Keys and values of new tokens into a paged cache of 16 or 8 bits; queries and
+// keys are rotated by their position on the way (formulas: pe.h).  HBM-bound:
+// each row is read and written once, two FMAs an element.
 //
 // A lane holds one item of a head, two 16-byte chunks whose elements pair up
 // under the rotation, and keeps its cosines and sines while it goes through
@@ -14,15 +14,25 @@ namespace pe {
 
 constexpr int kAppendWarps = 4, kAhead = 3;
 
-template <typename T, int D>
-__global__ void __launch_bounds__(32 * kAppendWarps, 5) kv_append_kernel(pe_kv_cache c, pe_kv_tokens t, int steps) {
+// codes of four elements times a power of two
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float f) {
+  uint16_t lo, hi;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b * f), "f"(a * f));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d * f), "f"(c * f));
+  return (uint32_t)lo | (uint32_t)hi << 16;
+}
+
+// E8: an 8-bit cache
+template <typename T, int D, bool E8>
+__global__ void __launch_bounds__(32 * kAppendWarps, 5)
+    kv_append_kernel(pe_kv_cache c, pe_kv_scales sc, pe_kv_tokens t, const int32_t* slots, int steps) {
   constexpr int kItems = D / 16, kHeads = 32 / kItems;  // items of a head; heads of a step
   const int lane = threadIdx.x & 31, item = lane % kItems, sub = lane / kItems;
   const int64_t tok = (int64_t)blockIdx.x * kAppendWarps + threadIdx.x / 32;
   pdl_enter();
   if (tok >= t.n_tokens) return;
   const int nq = t.q ? t.n_q_heads : 0, nk = c.n_heads, heads = nq + 2 * nk;
-  const int p = t.pos[tok];
+  const int p = t.pos[tok], at = slots ? slots[tok] : p;
   const int s = t.seq ? t.seq[tok] : (int)tok;
   const int rot = t.rot_dim;
   // chunks of the item, and whether they turn: pairs (i, i + rot/2) or neighbours
@@ -47,11 +57,14 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 5) kv_append_kernel(pe_kv_c
   };
   fetch(begin);
 
-  const bool live = p >= 0 && p < c.max_pages * c.page_size && (rot == 0 || p < t.max_pos) && s >= 0 && s < c.n_seqs;
-  int64_t slot = -1;
+  const bool live = p >= 0 && at >= 0 && at < c.max_pages * c.page_size && (rot == 0 || p < t.max_pos) && s >= 0 && s < c.n_seqs;
+  int64_t slot = -1, sslot = 0;
   if (live) {
-    const int page = c.table[(int64_t)s * c.table_stride + p / c.page_size];
-    if (page >= 0 && page < c.n_pages) slot = kv_page_offset(c, page) + (int64_t)(p % c.page_size) * c.slot_stride;
+    const int page = c.table[(int64_t)s * c.table_stride + at / c.page_size];
+    if (page >= 0 && page < c.n_pages) {
+      slot = kv_page_offset(c, page) + (int64_t)(at % c.page_size) * c.slot_stride;
+      if (E8) sslot = page * sc.page_stride + (int64_t)(at % c.page_size) * sc.slot_stride;
+    }
   }
   float co[8], si[8];
   if (live && turn) {
@@ -67,6 +80,54 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 5) kv_append_kernel(pe_kv_c
     for (int u = 0; u < kAhead; ++u) {
       const int h = h0 + u * kHeads;
       if (h >= end) break;
+      if constexpr (E8) {
+        if (h >= nq) {
+          if (slot < 0) continue;
+          const bool key = h < nq + nk;
+          const int hk = key ? h - nq : h - nq - nk;
+          float f[8], g[8];  // the item's elements, chunk by chunk
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 a = unpack2<T>(reinterpret_cast<const uint32_t*>(&x[u])[i]), b = unpack2<T>(reinterpret_cast<const uint32_t*>(&y[u])[i]);
+            f[2 * i] = a.x, f[2 * i + 1] = a.y, g[2 * i] = b.x, g[2 * i + 1] = b.y;
+          }
+          if (turn && key) {
+            // products and sums rounded one by one: codes do not depend on how they are contracted
+            auto pair = [](float& a, float& b, float co, float si) {
+              const float p = __fsub_rn(__fmul_rn(a, co), __fmul_rn(b, si));
+              b = __fadd_rn(__fmul_rn(b, co), __fmul_rn(a, si));
+              a = p;
+            };
+            if (t.interleaved) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                pair(f[2 * i], f[2 * i + 1], co[i], si[i]);
+                pair(g[2 * i], g[2 * i + 1], co[4 + i], si[4 + i]);
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) pair(f[i], g[i], co[i], si[i]);
+            }
+          }
+          uint32_t most = 0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) most = max(most, max(__float_as_uint(f[i]) & 0x7fffffffu, __float_as_uint(g[i]) & 0x7fffffffu));
+          const uint32_t members = (kItems == 32 ? 0xffffffffu : (1u << kItems) - 1) << (lane & ~(kItems - 1));  // the head's lanes
+#pragma unroll
+          for (int w = 1; w < kItems; w *= 2) most = max(most, __shfl_xor_sync(members, most, w));
+          // 448 = 1.75 * 2^8: one more than the exponent less 8 where the mantissa is above 1.75
+          const int byte = most >= 0x7f800000u ? 255 : max((int)(most >> 23) - 8 + ((most & 0x7fffffu) > 0x600000u), 63);
+          const float inv = __uint_as_float((254u - byte) << 23);  // 2^-e
+          uint8_t* to = (uint8_t*)(key ? c.k : c.v) + slot + hk * c.head_stride;
+          uint2 a = make_uint2(codes4(f[0], f[1], f[2], f[3], inv), codes4(f[4], f[5], f[6], f[7], inv));
+          uint2 b = make_uint2(codes4(g[0], g[1], g[2], g[3], inv), codes4(g[4], g[5], g[6], g[7], inv));
+          if (byte == 255) a = b = make_uint2(0, 0);
+          *reinterpret_cast<uint2*>(to + c0 * 8) = a;
+          *reinterpret_cast<uint2*>(to + c1 * 8) = b;
+          if (item == 0) (key ? sc.k : sc.v)[sslot + hk * sc.head_stride] = (uint8_t)byte;
+          continue;
+        }
+      }
       T* dst;
       if (h < nq)
         dst = (T*)t.q_out + tok * t.q_out_token_stride + h * t.q_out_head_stride;
@@ -97,8 +158,8 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 5) kv_append_kernel(pe_kv_c
   }
 }
 
-template <typename T, int D>
-static pe_status go(const pe_kv_cache& c, const pe_kv_tokens& t, cudaStream_t st) {
+template <typename T, int D, bool E8>
+static pe_status go(const pe_kv_cache& c, const pe_kv_scales& sc, const pe_kv_tokens& t, const int32_t* slots, cudaStream_t st) {
   constexpr int kHeads = 32 / (D / 16);
   const int heads = (t.q ? t.n_q_heads : 0) + 2 * c.n_heads;
   const int all = ceil_div(heads, kHeads);  // steps of a token
@@ -106,21 +167,88 @@ static pe_status go(const pe_kv_cache& c, const pe_kv_tokens& t, cudaStream_t st
   // each SM; fewer tokens are split by heads
   const int64_t want = ceil_div(152 * 16, t.n_tokens);
   const int parts = (int)(want < all ? want : all), steps = ceil_div(all, parts);
-  PE_TRY_CUDA(launch_pdl(kv_append_kernel<T, D>, dim3((unsigned)ceil_div(t.n_tokens, kAppendWarps), ceil_div(all, steps)),
-                         dim3(32 * kAppendWarps), 0, st, true, c, t, steps));
+  PE_TRY_CUDA(launch_pdl(kv_append_kernel<T, D, E8>, dim3((unsigned)ceil_div(t.n_tokens, kAppendWarps), ceil_div(all, steps)),
+                         dim3(32 * kAppendWarps), 0, st, true, c, sc, t, slots, steps));
   return PE_OK;
 }
 
-template <typename T>
-static pe_status go_dim(const pe_kv_cache& c, const pe_kv_tokens& t, cudaStream_t st) {
-  if (c.head_dim == 64) return go<T, 64>(c, t, st);
-  if (c.head_dim == 128) return go<T, 128>(c, t, st);
-  return go<T, 256>(c, t, st);
+template <typename T, bool E8>
+static pe_status go_dim(const pe_kv_cache& c, const pe_kv_scales& sc, const pe_kv_tokens& t, const int32_t* slots, cudaStream_t st) {
+  if (c.head_dim == 64) return go<T, 64, E8>(c, sc, t, slots, st);
+  if (c.head_dim == 128) return go<T, 128, E8>(c, sc, t, slots, st);
+  return go<T, 256, E8>(c, sc, t, slots, st);
 }
 
-pe_status kv_append_launch(const pe_kv_cache& c, const pe_kv_tokens& t, cudaStream_t st) {
+pe_status kv_append_launch(const pe_kv_cache& c, const pe_kv_scales& sc, const pe_kv_tokens& t, const int32_t* slots, int dtype,
+                           cudaStream_t st) {
   ProfScope ps(PE_PROF_KV_APPEND, st);
-  return c.dtype == PE_BF16 ? go_dim<__nv_bfloat16>(c, t, st) : go_dim<__half>(c, t, st);
+  if (c.dtype == PE_E4M3)
+    return dtype == PE_BF16 ? go_dim<__nv_bfloat16, true>(c, sc, t, slots, st) : go_dim<__half, true>(c, sc, t, slots, st);
+  return dtype == PE_BF16 ? go_dim<__nv_bfloat16, false>(c, sc, t, slots, st) : go_dim<__half, false>(c, sc, t, slots, st);
+}
+
+// ---------------------------------------------------------------------------
+// Rows from one position of a sequence to another.  A CTA holds all moves of one
+// sequence's head, keys or values, in registers between the reads and the
+// writes, so that a move's source may be another's target.
+// ---------------------------------------------------------------------------
+constexpr int kMoveThreads = 256, kMoveMost = 64;
+
+// R: bytes of a row
+template <int R>
+__global__ void __launch_bounds__(kMoveThreads) kv_move_kernel(MoveArgs a) {
+  constexpr int kChunks = R / 16, kRows = kMoveThreads / kChunks, kEach = (kMoveMost + kRows - 1) / kRows;
+  const pe_kv_cache& c = a.c;
+  const int b = blockIdx.x, h = blockIdx.y, row0 = threadIdx.x / kChunks, ch = threadIdx.x % kChunks;
+  const bool value = blockIdx.z != 0, eight = c.dtype == PE_E4M3;
+  const int es = eight ? 1 : 2;  // bytes of an element
+  pdl_enter();
+  char* base = (char*)(value ? c.v : c.k) + h * c.head_stride * es + ch * 16;
+  uint8_t* scales = (value ? a.sc.v : a.sc.k) + h * a.sc.head_stride;
+  const int cap = c.max_pages * c.page_size;
+  uint4 x[kEach];
+  uint8_t sx[kEach];
+  int page[kEach], slot[kEach];  // of the target; page -1: no move
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int m = row0 + i * kRows;
+    page[i] = -1;
+    slot[i] = 0;
+    x[i] = make_uint4(0, 0, 0, 0);
+    sx[i] = 0;
+    if (m >= a.n) continue;
+    const int s = a.src[b * a.src_stride + m], d = a.dst[b * a.dst_stride + m];
+    if (s < 0 || s >= cap || d < 0 || d >= cap || s == d) continue;
+    const int32_t* table = c.table + (int64_t)b * c.table_stride;
+    const int sp = table[s / c.page_size], dp = table[d / c.page_size];
+    if (sp < 0 || sp >= c.n_pages || dp < 0 || dp >= c.n_pages) continue;
+    page[i] = dp;
+    slot[i] = d % c.page_size;
+    x[i] = *reinterpret_cast<const uint4*>(base + (kv_page_offset(c, sp) + (int64_t)(s % c.page_size) * c.slot_stride) * es);
+    if (eight && ch == 0) sx[i] = scales[sp * a.sc.page_stride + (int64_t)(s % c.page_size) * a.sc.slot_stride];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    if (page[i] < 0) continue;
+    *reinterpret_cast<uint4*>(base + (kv_page_offset(c, page[i]) + (int64_t)slot[i] * c.slot_stride) * es) = x[i];
+    if (eight && ch == 0) scales[page[i] * a.sc.page_stride + (int64_t)slot[i] * a.sc.slot_stride] = sx[i];
+  }
+}
+
+pe_status kv_move_launch(const MoveArgs& a, cudaStream_t st) {
+  ProfScope ps(PE_PROF_KV_MOVE, st);
+  const dim3 grid(a.c.n_seqs, a.c.n_heads, 2), block(kMoveThreads);
+  const int row = a.c.head_dim * (a.c.dtype == PE_E4M3 ? 1 : 2);
+  if (row == 64)
+    PE_TRY_CUDA(launch_pdl(kv_move_kernel<64>, grid, block, 0, st, true, a));
+  else if (row == 128)
+    PE_TRY_CUDA(launch_pdl(kv_move_kernel<128>, grid, block, 0, st, true, a));
+  else if (row == 256)
+    PE_TRY_CUDA(launch_pdl(kv_move_kernel<256>, grid, block, 0, st, true, a));
+  else
+    PE_TRY_CUDA(launch_pdl(kv_move_kernel<512>, grid, block, 0, st, true, a));
+  return PE_OK;
 }
 
 }  // namespace pe

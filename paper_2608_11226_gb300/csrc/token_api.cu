@@ -11,9 +11,13 @@ static bool off(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t
 // a stride of vectors that are read 16 bytes at a time
 static bool bad_stride(int64_t s) { return s < 0 || (s & 7) != 0 || s > ((int64_t)1 << 44); }
 
-static pe_status check_cache(const pe_kv_cache* c) {
+static bool is16(int32_t dtype) { return dtype == PE_BF16 || dtype == PE_F16; }
+
+// `eight`: a cache of 8-bit codes will do
+static pe_status check_cache(const pe_kv_cache* c, bool eight = false) {
   if (!c) return fail(PE_EINVAL, "null cache");
-  if (c->dtype != PE_BF16 && c->dtype != PE_F16) return fail(PE_EINVAL, "cache dtype must be PE_BF16 or PE_F16");
+  if (!is16(c->dtype) && !(eight && c->dtype == PE_E4M3))
+    return fail(PE_EINVAL, eight ? "cache dtype must be PE_BF16, PE_F16 or PE_E4M3" : "cache dtype must be PE_BF16 or PE_F16");
   if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return fail(PE_EINVAL, "head_dim must be 64, 128 or 256");
   if (c->n_heads < 1 || c->n_heads > 1024) return fail(PE_EINVAL, "n_heads must be in [1, 1024]");
   if (c->page_size < 1 || c->page_size > 65536) return fail(PE_EINVAL, "page_size must be in [1, 65536]");
@@ -25,17 +29,34 @@ static pe_status check_cache(const pe_kv_cache* c) {
     return fail(PE_EINVAL, "table_stride must be at least max_pages");
   if (bad_stride(c->page_stride) || bad_stride(c->slot_stride) || bad_stride(c->head_stride))
     return fail(PE_EINVAL, "cache strides must be multiples of 8 elements");
+  if (c->dtype == PE_E4M3 && ((c->page_stride | c->slot_stride | c->head_stride) & 15) != 0)
+    return fail(PE_EINVAL, "strides of an 8-bit cache must be multiples of 16");
   if (!c->k || !c->v || (!c->table && c->n_seqs > 0)) return fail(PE_EINVAL, "null argument");
   if (off(c->k, 16) || off(c->v, 16)) return fail(PE_EINVAL, "k and v must be 16-byte aligned");
   return PE_OK;
 }
 
-extern "C" {
+static pe_status check_scales(const pe_kv_cache* c, const pe_kv_scales* sc) {
+  if (c->dtype != PE_E4M3) return sc ? fail(PE_EINVAL, "a 16-bit cache has no scales") : PE_OK;
+  if (!sc || !sc->k || !sc->v) return fail(PE_EINVAL, "an 8-bit cache needs scales");
+  const int64_t most = (int64_t)1 << 44;
+  if (sc->page_stride < 0 || sc->slot_stride < 0 || sc->head_stride < 0 || sc->page_stride > most || sc->slot_stride > most ||
+      sc->head_stride > most)
+    return fail(PE_EINVAL, "scale strides must be in [0, 2^44]");
+  return PE_OK;
+}
 
-pe_status pe_kv_append(const pe_kv_cache* cache, const pe_kv_tokens* t, void* stream) {
-  clear_error();
-  pe_status s = check_cache(cache);
+// an 8-bit cache with its scales, and the type of what goes in or comes out
+static pe_status check_pair(const pe_kv_cache* c, const pe_kv_scales* sc, int32_t dtype) {
+  const pe_status s = check_cache(c, true);
   if (s != PE_OK) return s;
+  if (!is16(dtype) || (c->dtype != PE_E4M3 && dtype != c->dtype))
+    return fail(PE_EINVAL, "dtype must be PE_BF16 or PE_F16, and a 16-bit cache's own");
+  return check_scales(c, sc);
+}
+
+static pe_status append(const pe_kv_cache* cache, const pe_kv_scales* scales, const pe_kv_tokens* t, const int32_t* slots,
+                        int32_t dtype, void* stream) {
   if (!t) return fail(PE_EINVAL, "null tokens");
   if (t->n_tokens < 0 || t->n_tokens > INT32_MAX) return fail(PE_EINVAL, "n_tokens must be in [0, 2^31)");
   if (t->rot_dim < 0 || t->rot_dim > cache->head_dim || t->rot_dim % 16 != 0)
@@ -51,7 +72,109 @@ pe_status pe_kv_append(const pe_kv_cache* cache, const pe_kv_tokens* t, void* st
     return fail(PE_EINVAL, "token strides must be multiples of 8 elements");
   if (off(t->k, 16) || off(t->v, 16) || (t->q && (off(t->q, 16) || off(t->q_out, 16))) || (t->rot_dim > 0 && off(t->rot, 16)))
     return fail(PE_EINVAL, "q, q_out, k, v and rot must be 16-byte aligned");
-  return kv_append_launch(*cache, *t, reinterpret_cast<cudaStream_t>(stream));
+  return kv_append_launch(*cache, scales ? *scales : pe_kv_scales{}, *t, slots, dtype, reinterpret_cast<cudaStream_t>(stream));
+}
+
+extern "C" {
+
+pe_status pe_kv_append(const pe_kv_cache* cache, const pe_kv_tokens* t, void* stream) {
+  clear_error();
+  const pe_status s = check_cache(cache);
+  return s != PE_OK ? s : append(cache, nullptr, t, nullptr, cache->dtype, stream);
+}
+
+pe_status pe_kv_append_at(const pe_kv_cache* cache, const pe_kv_scales* scales, const pe_kv_tokens* t, const int32_t* slots,
+                          int32_t dtype, void* stream) {
+  clear_error();
+  const pe_status s = check_pair(cache, scales, dtype);
+  return s != PE_OK ? s : append(cache, scales, t, slots, dtype, stream);
+}
+
+pe_status pe_kv_move(const pe_kv_cache* cache, const pe_kv_scales* scales, const int32_t* src, int64_t src_stride,
+                     const int32_t* dst, int64_t dst_stride, int32_t n_moves, void* stream) {
+  clear_error();
+  pe_status s = check_cache(cache, true);
+  if (s == PE_OK) s = check_scales(cache, scales);
+  if (s != PE_OK) return s;
+  if (n_moves < 0 || n_moves > 64) return fail(PE_EINVAL, "n_moves must be in [0, 64]");
+  if (cache->n_seqs > 1 && (src_stride < n_moves || dst_stride < n_moves)) return fail(PE_EINVAL, "src_stride and dst_stride must be at least n_moves");
+  if (src_stride < 0 || dst_stride < 0 || src_stride > ((int64_t)1 << 40) || dst_stride > ((int64_t)1 << 40))
+    return fail(PE_EINVAL, "src_stride and dst_stride must be in [0, 2^40]");
+  if (cache->n_seqs == 0 || n_moves == 0) return PE_OK;
+  if (!src || !dst) return fail(PE_EINVAL, "null argument");
+  MoveArgs a{*cache, scales ? *scales : pe_kv_scales{}, src, dst, src_stride, dst_stride, n_moves};
+  return kv_move_launch(a, reinterpret_cast<cudaStream_t>(stream));
+}
+
+static bool bad_group(const pe_kv_cache* c, int32_t n_q_heads) {
+  return n_q_heads < 1 || n_q_heads > 65536 || n_q_heads % c->n_heads != 0;
+}
+
+int64_t pe_tree_attn_workspace_bytes(const pe_kv_cache* cache, int32_t n_nodes, int32_t n_q_heads) {
+  if (check_cache(cache, true) != PE_OK) return -1;
+  if (bad_group(cache, n_q_heads) || n_nodes < 0 || n_nodes > 64) return -1;
+  return n_nodes == 0 ? 0 : tree_attn_ws_bytes(*cache, n_nodes, n_q_heads);
+}
+
+static pe_status check_workspace(const void* workspace, int64_t bytes, int64_t need) {
+  if (need > 0 && !workspace) return fail(PE_EINVAL, "null argument");
+  if (bytes < need) return fail(PE_EINVAL, "workspace too small (%lld < %lld bytes)", (long long)bytes, (long long)need);
+  if (need > 0 && off(workspace, 256)) return fail(PE_EINVAL, "workspace must be 256-byte aligned");
+  return PE_OK;
+}
+
+pe_status pe_tree_attn(const pe_kv_cache* cache, const pe_kv_scales* scales, const pe_tree_queries* t, float scale, int32_t window,
+                       void* workspace, int64_t workspace_bytes, void* stream) {
+  clear_error();
+  if (!t) return fail(PE_EINVAL, "null tree");
+  pe_status s = check_pair(cache, scales, t->dtype);
+  if (s != PE_OK) return s;
+  if (bad_group(cache, t->n_q_heads)) return fail(PE_EINVAL, "n_q_heads must be a multiple of n_heads in [1, 65536]");
+  if (t->n_nodes < 0 || t->n_nodes > 64) return fail(PE_EINVAL, "n_nodes must be in [0, 64]");
+  if (!std::isfinite(scale)) return fail(PE_EINVAL, "scale must be finite");
+  if (window < 0 || (window > 0 && window < 64)) return fail(PE_EINVAL, "window must be 0 or at least 64");
+  if (t->mask_stride < 0 || t->mask_stride > ((int64_t)1 << 40)) return fail(PE_EINVAL, "mask_stride must be in [0, 2^40]");
+  if (cache->n_seqs == 0 || t->n_nodes == 0) return PE_OK;
+  if (!t->q || !t->out || !t->lens || !t->mask) return fail(PE_EINVAL, "null argument");
+  if (bad_stride(t->q_seq_stride) || bad_stride(t->q_node_stride) || bad_stride(t->q_head_stride) || bad_stride(t->out_seq_stride) ||
+      bad_stride(t->out_node_stride) || bad_stride(t->out_head_stride))
+    return fail(PE_EINVAL, "q and out strides must be multiples of 8 elements");
+  if (off(t->q, 16) || off(t->out, 16)) return fail(PE_EINVAL, "q and out must be 16-byte aligned");
+  if (off(t->mask, 8)) return fail(PE_EINVAL, "mask must be 8-byte aligned");
+  s = check_workspace(workspace, workspace_bytes, tree_attn_ws_bytes(*cache, t->n_nodes, t->n_q_heads));
+  if (s != PE_OK) return s;
+  TreeArgs a{*cache, scales ? *scales : pe_kv_scales{}, t->q, t->out, t->lse, t->lens, t->mask, t->q_seq_stride, t->q_node_stride,
+             t->q_head_stride, t->out_seq_stride, t->out_node_stride, t->out_head_stride, t->mask_stride, scale, t->n_nodes,
+             t->n_q_heads, window, t->dtype};
+  return tree_attn_launch(a, workspace, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int64_t pe_decode_attn8_workspace_bytes(const pe_kv_cache* cache, int32_t n_q_heads) {
+  if (check_cache(cache, true) != PE_OK || cache->dtype != PE_E4M3 || bad_group(cache, n_q_heads)) return -1;
+  return tree_attn_ws_bytes(*cache, 1, n_q_heads);
+}
+
+pe_status pe_decode_attn8(const pe_kv_cache* cache, const pe_kv_scales* scales, int32_t dtype, const void* q,
+                          int64_t q_seq_stride, int64_t q_head_stride, int32_t n_q_heads, const int32_t* lens,
+                          float scale, int32_t window, void* out, int64_t out_seq_stride, int64_t out_head_stride,
+                          float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
+  clear_error();
+  pe_status s = check_pair(cache, scales, dtype);
+  if (s != PE_OK) return s;
+  if (cache->dtype != PE_E4M3) return fail(PE_EINVAL, "cache dtype must be PE_E4M3");
+  if (bad_group(cache, n_q_heads)) return fail(PE_EINVAL, "n_q_heads must be a multiple of n_heads in [1, 65536]");
+  if (!std::isfinite(scale)) return fail(PE_EINVAL, "scale must be finite");
+  if (window < 0) return fail(PE_EINVAL, "window must be >= 0");
+  if (cache->n_seqs == 0) return PE_OK;
+  if (!q || !out || !lens) return fail(PE_EINVAL, "null argument");
+  if (bad_stride(q_seq_stride) || bad_stride(q_head_stride) || bad_stride(out_seq_stride) || bad_stride(out_head_stride))
+    return fail(PE_EINVAL, "q and out strides must be multiples of 8 elements");
+  if (off(q, 16) || off(out, 16)) return fail(PE_EINVAL, "q and out must be 16-byte aligned");
+  s = check_workspace(workspace, workspace_bytes, tree_attn_ws_bytes(*cache, 1, n_q_heads));
+  if (s != PE_OK) return s;
+  TreeArgs a{*cache, *scales, q, out, lse, lens, nullptr, q_seq_stride, 0, q_head_stride, out_seq_stride, 0, out_head_stride, 0,
+             scale, 1, n_q_heads, window, dtype};
+  return tree_attn_launch(a, workspace, reinterpret_cast<cudaStream_t>(stream));
 }
 
 int64_t pe_decode_attn_workspace_bytes(const pe_kv_cache* cache, int32_t n_q_heads) {

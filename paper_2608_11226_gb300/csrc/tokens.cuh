@@ -57,6 +57,34 @@ struct DecodeArgs {
   int32_t n_q_heads, window;
 };
 
+// scale of a row of an 8-bit cache (pe.h: pe_kv_scales)
+__device__ __forceinline__ float scale_of(int byte) {
+  return __int_as_float(byte == 255 ? 0x7fc00000 : min(max(byte, 63), 247) << 23);
+}
+
+// Attention of one or several new tokens over either kind of cache: the tree's
+// nodes (mask), or one token (mask null, n_nodes 1) that lens counts.
+struct TreeArgs {
+  pe_kv_cache c;
+  pe_kv_scales sc;
+  const void* q;
+  void* out;
+  float* lse;
+  const int32_t* lens;
+  const uint64_t* mask;
+  int64_t q_seq, q_node, q_head, o_seq, o_node, o_head, mask_stride;
+  float scale;
+  int32_t n_nodes, n_q_heads, window, dtype;
+};
+
+struct MoveArgs {
+  pe_kv_cache c;
+  pe_kv_scales sc;
+  const int32_t *src, *dst;
+  int64_t src_stride, dst_stride;
+  int32_t n;
+};
+
 struct LogpArgs {
   const void* logits;
   const int32_t* tokens;
@@ -77,7 +105,11 @@ struct LogpGradArgs {
   float scale;
 };
 
-pe_status kv_append_launch(const pe_kv_cache& c, const pe_kv_tokens& t, cudaStream_t st);
+pe_status kv_append_launch(const pe_kv_cache& c, const pe_kv_scales& sc, const pe_kv_tokens& t, const int32_t* slots, int dtype,
+                           cudaStream_t st);
+pe_status kv_move_launch(const MoveArgs& a, cudaStream_t st);
+int64_t tree_attn_ws_bytes(const pe_kv_cache& c, int n_nodes, int n_q_heads);
+pe_status tree_attn_launch(const TreeArgs& a, void* ws, cudaStream_t st);
 int64_t decode_attn_ws_bytes(const pe_kv_cache& c, int n_q_heads);
 pe_status decode_attn_launch(const DecodeArgs& a, void* ws, cudaStream_t st);
 pe_status token_logp_launch(const LogpArgs& a, int dtype, cudaStream_t st);

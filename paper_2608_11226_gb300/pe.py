@@ -21,14 +21,14 @@ LIB_PATH = os.path.join(_HERE, "_build", "libpe.so")
 _lib = None
 
 PE_OK, PE_EINVAL, PE_ENOMEM, PE_ECUDA, PE_EOVERFLOW, PE_ETIMEOUT, PE_ESTATE = range(7)
-PE_F32, PE_BF16, PE_F16 = 0, 1, 2
+PE_F32, PE_BF16, PE_F16, PE_E4M3 = 0, 1, 2, 3
 PE_ROLLOUT_DETERMINISTIC = 1
 MAX_LEVELS, MAX_CH = 32, 4
 (PE_PROF_ROLLOUT, PE_PROF_VALUE, PE_PROF_GAE, PE_PROF_PPO_GRAD, PE_PROF_PPO_REDUCE,
  PE_PROF_PPO_ADAM, PE_PROF_PPO_OTHER, PE_PROF_FLEET_PREP, PE_PROF_FLEET_WINDOWS,
  PE_PROF_MLP_POLICY, PE_PROF_MLP_VALUE, PE_PROF_KV_APPEND, PE_PROF_DECODE_ATTN, PE_PROF_TOKEN_LOGP,
- PE_PROF_TOKEN_LOGP_GRAD) = range(15)
-PE_PROF_KINDS = 15
+ PE_PROF_TOKEN_LOGP_GRAD, PE_PROF_TREE_ATTN, PE_PROF_KV_MOVE) = range(17)
+PE_PROF_KINDS = 17
 
 
 class PEError(RuntimeError):
@@ -89,9 +89,23 @@ class KVTokens(C.Structure):
         (n, C.c_int32) for n in ("n_q_heads", "rot_dim", "interleaved")]
 
 
+class KVScales(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)] + [
+        (n, C.c_int64) for n in ("page_stride", "slot_stride", "head_stride")]
+
+
+class TreeQueries(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "out", "lse", "lens", "mask")] + [
+        (n, C.c_int64) for n in ("q_seq_stride", "q_node_stride", "q_head_stride", "out_seq_stride", "out_node_stride",
+                                 "out_head_stride", "mask_stride")] + [
+        (n, C.c_int32) for n in ("n_nodes", "n_q_heads", "dtype")]
+
+
 # the same bytes at once: filling the structure's fields costs four times as much
 _KV_TOKENS = struct.Struct("17q3i4x").pack
 assert struct.calcsize("17q3i4x") == C.sizeof(KVTokens)
+_TREE_QUERIES = struct.Struct("12q3i4x").pack
+assert struct.calcsize("12q3i4x") == C.sizeof(TreeQueries)
 
 
 EXPORTS = (
@@ -102,6 +116,8 @@ EXPORTS = (
     "pe_fleet_stagger_workspace_bytes", "pe_fleet_stagger", "pe_env_set_offsets", "pe_rollout_rule", "pe_rollout_replay", "pe_wait_selftest",
     "pe_dual_ascent", "pe_roof_probe",
     "pe_kv_append", "pe_decode_attn_workspace_bytes", "pe_decode_attn", "pe_token_logp", "pe_token_logp_grad",
+    "pe_kv_append_at", "pe_decode_attn8_workspace_bytes", "pe_decode_attn8", "pe_tree_attn_workspace_bytes",
+    "pe_tree_attn", "pe_kv_move",
     "pe_profile_enable",
     "pe_profile_read", "pe_profile_kind_name", "pe_last_error")
 
@@ -149,6 +165,12 @@ def lib():
             "pe_decode_attn": (i32, [vp, vp, i64, i64, i32, vp, C.c_float, i32, vp, i64, i64, vp, vp, i64, vp]),
             "pe_token_logp": (i32, [vp, i32, i64, i32, i64, vp, C.c_float, vp, vp, vp, i32, vp, vp, vp]),
             "pe_token_logp_grad": (i32, [vp, i32, i64, i32, i64, vp, C.c_float, vp, vp, vp, vp, vp, i64, vp]),
+            "pe_kv_append_at": (i32, [vp, vp, vp, vp, i32, vp]),
+            "pe_decode_attn8_workspace_bytes": (i64, [vp, i32]),
+            "pe_decode_attn8": (i32, [vp, vp, i32, vp, i64, i64, i32, vp, C.c_float, i32, vp, i64, i64, vp, vp, i64, vp]),
+            "pe_tree_attn_workspace_bytes": (i64, [vp, i32, i32]),
+            "pe_tree_attn": (i32, [vp, vp, vp, C.c_float, i32, vp, i64, vp]),
+            "pe_kv_move": (i32, [vp, vp, vp, i64, vp, i64, i32, vp]),
             "pe_profile_enable": (i32, [i32]),
             "pe_profile_read": (i32, [i32, C.POINTER(C.c_double), C.POINTER(C.c_int64)]),
             "pe_profile_kind_name": (C.c_char_p, [i32]),
@@ -487,30 +509,55 @@ def _heads(name: str, t: torch.Tensor, shape: tuple, dtype: torch.dtype, dev: in
 
 class KVCache:
     """A paged cache of keys and values (pe_kv_cache): k and v are
-    [pages, slots, heads, head_dim] tensors of bf16 or fp16 with equal strides
-    (a transposed view of [pages, heads, slots, head_dim] storage will do),
-    table is [sequences, pages of a sequence] int32.  Holds the tensors; the
-    table's entries may change between calls.  The calls below run on the
-    current device, where all of their tensors have to be."""
+    [pages, slots, heads, head_dim] tensors of bf16, fp16 or float8_e4m3fn with
+    equal strides (a transposed view of [pages, heads, slots, head_dim] storage
+    will do), table is [sequences, pages of a sequence] int32.  A cache of
+    float8_e4m3fn has scales (pe_kv_scales): k_scale and v_scale are
+    [pages, slots, heads] tensors of uint8 or float8_e8m0fnu with equal strides.
+    Holds the tensors; the table's entries may change between calls.  The calls
+    below run on the current device, where all of their tensors have to be."""
 
-    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor):
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
         _want(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype
-              and k.dtype in (torch.bfloat16, torch.float16) and k.is_cuda and v.is_cuda and k.stride(3) == 1,
-              "k and v must be bf16 or fp16 device tensors of [pages, slots, heads, head_dim] with equal strides and "
-              "adjacent elements")
+              and k.dtype in (torch.bfloat16, torch.float16, torch.float8_e4m3fn) and k.is_cuda and v.is_cuda and k.stride(3) == 1,
+              "k and v must be bf16, fp16 or float8_e4m3fn device tensors of [pages, slots, heads, head_dim] with equal "
+              "strides and adjacent elements")
         _want(table.dim() == 2 and table.dtype == torch.int32 and table.is_cuda and (table.shape[1] < 2 or table.stride(1) == 1),
               "table must be an int32 device tensor of [sequences, pages] with adjacent entries")
         _want(max(table.shape) <= _INT32 and max(k.shape[1:]) <= _INT32, "sizes must be below 2^31")
         _want(table.shape[0] < 2 or table.stride(0) >= table.shape[1], "table's rows must not overlap (an expanded row is no table)")
         _want(k.get_device() == v.get_device() == table.get_device(), "k, v and table must be on one device")
-        self.k, self.v, self.table = k, v, table
+        self.k, self.v, self.table, self.k_scale, self.v_scale = k, v, table, k_scale, v_scale
         st = [k.stride(i) if k.shape[i] > 1 else 0 for i in range(3)]
         self.n_seqs, self.n_heads, self.head_dim, self.page_size = table.shape[0], k.shape[2], k.shape[3], k.shape[1]
+        self.eight = k.dtype == torch.float8_e4m3fn
         self.dtype = k.dtype
         self._desc = KVCacheDesc(k.data_ptr(), v.data_ptr(), table.data_ptr(), k.shape[0], st[0], st[1], st[2],
                                  table.stride(0) if table.shape[0] > 1 else table.shape[1], table.shape[0], table.shape[1], k.shape[1],
-                                 k.shape[2], k.shape[3], _DTYPE[k.dtype])
+                                 k.shape[2], k.shape[3], PE_E4M3 if self.eight else _DTYPE[k.dtype])
         self._ref = C.byref(self._desc)
+        self._scales = None
+        if not self.eight:
+            _want(k_scale is None and v_scale is None, "a 16-bit cache has no scales")
+            return
+        _want(k_scale is not None and v_scale is not None and k_scale.shape == v_scale.shape == k.shape[:3]
+              and k_scale.stride() == v_scale.stride() and k_scale.dtype == v_scale.dtype
+              and k_scale.dtype in (torch.uint8, torch.float8_e8m0fnu)
+              and k_scale.get_device() == v_scale.get_device() == k.get_device(),
+              "an 8-bit cache needs k_scale and v_scale, uint8 or float8_e8m0fnu device tensors of [pages, slots, heads] "
+              "with equal strides")
+        ss = [k_scale.stride(i) if k.shape[i] > 1 else 0 for i in range(3)]
+        _want(all(x > 0 for x, n in zip(ss, k.shape) if n > 1), "rows of an 8-bit cache must not share a scale")
+        self._scale_desc = KVScales(k_scale.data_ptr(), v_scale.data_ptr(), *ss)
+        self._scales = C.byref(self._scale_desc)
+
+    def _type(self, name: str, t: torch.Tensor) -> torch.dtype:
+        """dtype of what goes in or comes out: the cache's, or t's where that has 8 bits."""
+        if not self.eight:
+            return self.dtype
+        _want(t.dtype in (torch.bfloat16, torch.float16), f"{name} must be bf16 or fp16")
+        return t.dtype
 
 
 def rot_table(max_pos: int, rot_dim: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
@@ -524,12 +571,14 @@ def rot_table(max_pos: int, rot_dim: int, base: float = 10000.0, device="cuda") 
 def kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor,
               seqs: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
               q_out: Optional[torch.Tensor] = None, rot: Optional[torch.Tensor] = None, interleaved: bool = False,
-              stream=None):
+              stream=None, slots: Optional[torch.Tensor] = None):
     """Append keys and values of new tokens ([tokens, heads, head_dim]) at
     their positions (int32), rotating q (into q_out, default in place) and k
     by position with rot ([positions, rot_dim], see rot_table); token t is of
-    sequence seqs[t], or t where seqs is None."""
-    n, D, dt, dev = positions.numel(), cache.head_dim, cache.dtype, _launch_device("the cache", cache.k)
+    sequence seqs[t], or t where seqs is None.  With slots (int32) token t is
+    written to position slots[t] and not where its rotation says.  An 8-bit
+    cache gets codes and scales of the rows (bf16 or fp16, like q)."""
+    n, D, dt, dev = positions.numel(), cache.head_dim, cache._type("k", k), _launch_device("the cache", cache.k)
     kp, ks, kh = _heads("k", k, (n, cache.n_heads, D), dt, dev)
     vp, vs, vh = _heads("v", v, (n, cache.n_heads, D), dt, dev)
     qp = qs = qh = op = os_ = oh = hq = rp = max_pos = rot_dim = 0
@@ -545,33 +594,108 @@ def kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, positions: torch
     t = _KV_TOKENS(_vec("positions", positions, n, torch.int32, dev),
                    0 if seqs is None else _vec("seqs", seqs, n, torch.int32, dev), rp, qp, op, kp, vp, n, max_pos,
                    qs, qh, os_, oh, ks, kh, vs, vh, hq, rot_dim, interleaved)
-    _check(lib().pe_kv_append(cache._ref, t, _stream_of(dev, stream)))
+    if cache.eight or slots is not None:
+        at = None if slots is None else _vec("slots", slots, n, torch.int32, dev)
+        _check(lib().pe_kv_append_at(cache._ref, cache._scales, t, at, _DTYPE[dt], _stream_of(dev, stream)))
+    else:
+        _check(lib().pe_kv_append(cache._ref, t, _stream_of(dev, stream)))
 
 
 def decode_attn_workspace_bytes(cache: KVCache, n_q_heads: int) -> int:
+    if cache.eight:
+        return int(lib().pe_decode_attn8_workspace_bytes(cache._ref, n_q_heads))
     return int(lib().pe_decode_attn_workspace_bytes(cache._ref, n_q_heads))
+
+
+def _workspace(workspace: Optional[torch.Tensor], nbytes, dev: int, stream) -> torch.Tensor:
+    """The caller's workspace, or one of nbytes() bytes."""
+    if workspace is None:
+        with torch.cuda.stream(stream):  # of the stream that uses it (None: the current one)
+            return alloc_workspace(nbytes())
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous, on device {dev}")
+    return workspace
 
 
 def decode_attn(cache: KVCache, q: torch.Tensor, lens: torch.Tensor, out: torch.Tensor, scale: Optional[float] = None,
                 window: int = 0, lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                 stream=None):
     """out[b] = attention of q[b] ([sequences, query heads, head_dim]) over the
-    lens[b] (int32) positions of sequence b; scale defaults to head_dim^-1/2."""
-    n, hq, dev = cache.n_seqs, q.shape[1], _launch_device("the cache", cache.k)
+    lens[b] (int32) positions of sequence b; scale defaults to head_dim^-1/2.
+    q and out are of the cache's dtype, of bf16 or fp16 over an 8-bit cache."""
+    n, hq, dev, dt = cache.n_seqs, q.shape[1], _launch_device("the cache", cache.k), cache._type("q", q)
     shape = (n, hq, cache.head_dim)
-    qp, qs, qh = _heads("q", q, shape, cache.dtype, dev)
-    op, os_, oh = _heads("out", out, shape, cache.dtype, dev)
+    qp, qs, qh = _heads("q", q, shape, dt, dev)
+    op, os_, oh = _heads("out", out, shape, dt, dev)
     lp = _vec("lens", lens, n, torch.int32, dev)
     sp = None if lse is None else _vec("lse", lse, n * hq, torch.float32, dev)
     if abs(window) > _INT32:
         raise ValueError("window must be in [0, 2^31)")
-    if workspace is None:
-        with torch.cuda.stream(stream):  # of the stream that uses it (None: the current one)
-            workspace = alloc_workspace(decode_attn_workspace_bytes(cache, hq))
-    elif workspace.get_device() != dev or not workspace.is_contiguous():
-        raise ValueError(f"workspace must be contiguous, on device {dev}")
-    _check(lib().pe_decode_attn(cache._ref, qp, qs, qh, hq, lp, cache.head_dim ** -0.5 if scale is None else scale,
-                                window, op, os_, oh, sp, workspace.data_ptr(), workspace.numel(), _stream_of(dev, stream)))
+    workspace = _workspace(workspace, lambda: decode_attn_workspace_bytes(cache, hq), dev, stream)
+    scale = cache.head_dim ** -0.5 if scale is None else scale
+    if cache.eight:
+        _check(lib().pe_decode_attn8(cache._ref, cache._scales, _DTYPE[dt], qp, qs, qh, hq, lp, scale, window, op, os_, oh, sp,
+                                     workspace.data_ptr(), workspace.numel(), _stream_of(dev, stream)))
+    else:
+        _check(lib().pe_decode_attn(cache._ref, qp, qs, qh, hq, lp, scale, window, op, os_, oh, sp, workspace.data_ptr(),
+                                    workspace.numel(), _stream_of(dev, stream)))
+
+
+def tree_attn_workspace_bytes(cache: KVCache, n_nodes: int, n_q_heads: int) -> int:
+    return int(lib().pe_tree_attn_workspace_bytes(cache._ref, n_nodes, n_q_heads))
+
+
+def _nodes(name: str, t: torch.Tensor, shape: tuple, dtype: torch.dtype, dev: int):
+    """(pointer, sequence, node and head strides) of an [n][nodes][heads][head_dim] tensor."""
+    if t.shape == shape and t.dtype is dtype and t.get_device() == dev:
+        s0, s1, s2, s3 = t.stride()
+        if s3 == 1:
+            return t.data_ptr(), s0 if shape[0] > 1 else 0, s1 if shape[1] > 1 else 0, s2 if shape[2] > 1 else 0
+    raise ValueError(f"{name} must be a {dtype} tensor of {list(shape)} on device {dev} with adjacent elements")
+
+
+def tree_attn(cache: KVCache, q: torch.Tensor, lens: torch.Tensor, mask: torch.Tensor, out: torch.Tensor,
+              scale: Optional[float] = None, window: int = 0, lse: Optional[torch.Tensor] = None,
+              workspace: Optional[torch.Tensor] = None, stream=None):
+    """Attention of drafted tokens q ([sequences, nodes, query heads, head_dim],
+    64 nodes at most): node i of sequence b, appended at position lens[b] + i,
+    attends to the lens[b] positions ahead of the tree and to the nodes whose
+    bits are set in mask[b, i] (int64 [sequences, nodes]; 0: padding).  A mask
+    expanded from one row is a tree for all.  scale defaults to head_dim^-1/2."""
+    dev = _launch_device("the cache", cache.k)
+    _want(q.dim() == 4, "q must have the dimensions [sequences, nodes, query heads, head_dim]")
+    n, nodes, hq, dt = cache.n_seqs, q.shape[1], q.shape[2], cache._type("q", q)
+    shape = (n, nodes, hq, cache.head_dim)
+    qp, qs, qn, qh = _nodes("q", q, shape, dt, dev)
+    op, os_, on, oh = _nodes("out", out, shape, dt, dev)
+    _want(mask.shape == (n, nodes) and mask.dtype is torch.int64 and mask.get_device() == dev
+          and (nodes < 2 or mask.stride(1) == 1), f"mask must be an int64 tensor of {[n, nodes]} on device {dev} with adjacent entries")
+    _want(nodes <= 64, "a tree has 64 nodes at most")
+    if abs(window) > _INT32:
+        raise ValueError("window must be in [0, 2^31)")
+    sp = 0 if lse is None else _vec("lse", lse, n * nodes * hq, torch.float32, dev)
+    t = _TREE_QUERIES(qp, op, sp, _vec("lens", lens, n, torch.int32, dev), mask.data_ptr(), qs, qn, qh, os_, on, oh,
+                      mask.stride(0) if n > 1 else 0, nodes, hq, _DTYPE[dt])
+    workspace = _workspace(workspace, lambda: tree_attn_workspace_bytes(cache, nodes, hq), dev, stream)
+    _check(lib().pe_tree_attn(cache._ref, cache._scales, t, cache.head_dim ** -0.5 if scale is None else scale, window,
+                              workspace.data_ptr(), workspace.numel(), _stream_of(dev, stream)))
+
+
+def _moves(name: str, t: torch.Tensor, shape, dev: int):
+    if t.shape == shape and t.dtype is torch.int32 and t.get_device() == dev and (shape[1] < 2 or t.stride(1) == 1):
+        return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1]
+    raise ValueError(f"{name} must be an int32 tensor of {list(shape)} on device {dev} with adjacent entries")
+
+
+def kv_move(cache: KVCache, src: torch.Tensor, dst: torch.Tensor, stream=None):
+    """Position dst[b, i] of sequence b gets what position src[b, i] held before
+    the call (int32 [sequences, moves], 64 moves at most; out of range: no move)."""
+    dev = _launch_device("the cache", cache.k)
+    _want(src.dim() == 2 and src.shape[0] == cache.n_seqs and src.shape[1] <= 64, "src must be [sequences, moves], 64 moves at most")
+    shape = src.shape
+    sp, ss = _moves("src", src, shape, dev)
+    dp, ds = _moves("dst", dst, shape, dev)
+    _check(lib().pe_kv_move(cache._ref, cache._scales, sp, ss, dp, ds, shape[1], _stream_of(dev, stream)))
 
 
 def _rows(name: str, t: torch.Tensor, dev: int):
