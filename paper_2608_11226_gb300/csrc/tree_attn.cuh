@@ -1,0 +1,1055 @@
+// Attention of one or several new tokens over a paged cache of 16 or 8 bits on
+// tcgen05 (formulas: pe.h).
+//
+// A sequence's new tokens and the query heads of a key head are the rows of one
+// matrix, so keys and values are read once for all of them: S = Q K^T and
+// O += P V are products of 128 rows with tiles of kKeys positions.  Up to 128
+// rows the cache's bytes bound it (bf16, head_dim 128: 512 clk of products against
+// 2,790 of HBM for 128 positions), beyond 256 the products do.
+//
+// One CTA on an SM.  Tiles of all (sequence, key head, block of rows) segments
+// form one line that is dealt out evenly to the CTAs; a segment that crosses CTAs
+// leaves pieces (unnormalised output, maxima, sums) that a second kernel joins in
+// the order of the CTAs.
+//
+// Roles: producer warps bring keys and values into a ring of swizzled entries
+// (cp.async from whatever pages; 8-bit codes go through registers and become
+// fp16), one thread issues the products, two warpgroups take the softmax: a
+// thread reads its row of S from TMEM and puts the weights P back as the second
+// product's operand.
+//   Wide (more than 128 rows in a block): each warpgroup has 128 rows of its own,
+//     whose products run while the other works on its weights; P replaces S.
+//   Narrow: both warpgroups share one tile of 128 rows, half of the tile's columns
+//     each (they exchange the maxima), and S and P have two buffers.
+//
+// An 8-bit row is its codes times 2^e.  Within a tile the codes become fp16 as
+// code * 2^(e - E), E the tile's largest exponent (exact down to e - E = -15; the
+// rest is below 2^-24 of the largest scale), and 2^E goes into the exponentials'
+// argument.  Queries become fp16 with a power of two of their own, which is exact
+// for all that fp32 would keep.
+//
+// Weights are relative to a running maximum that follows only when it is passed
+// by 8 (a factor of 256), so the output is seldom rescaled.
+#pragma once
+
+#include <math_constants.h>
+
+#include "tc.cuh"
+#include "tokens.cuh"
+
+namespace pe {
+namespace tree {
+
+constexpr int kCtas = 152;
+constexpr int kInfos = 8;  // tiles whose description is kept: more than the ring holds
+
+struct SegMeta {
+  int32_t seq, group, pieces, first_slot;  // pieces 0: nothing to join
+};
+
+template <int D, bool E8, bool WIDE>
+struct Shape {
+  static_assert(!(WIDE && D == 256), "two outputs of 256 columns leave no room for scores");
+  static constexpr int kKeys = D == 256 ? 64 : 128;
+  static constexpr int kRows = WIDE ? 256 : 128;  // of a block
+  static constexpr int kProducers = E8 ? 8 : 4;   // warps
+  static constexpr int kThreads = 32 * (9 + kProducers);
+  static constexpr int kEntry = kKeys * D * 2;
+  static constexpr int kEntries = D == 64 ? 8 : (WIDE || D == 256) ? 4 : 5;
+  static constexpr int kLag = kEntries >= 5 ? 3 : 2;  // entries whose copies are in flight
+  static constexpr int kQBytes = kRows * D * 2;
+  static constexpr int kSmem = kQBytes + kEntries * kEntry + 1024;
+  static constexpr int kCols = WIDE ? kKeys : kKeys / 2;  // columns of a thread
+  // TMEM columns
+  static constexpr int kO = 0, kOStep = 128, kS = 256, kSStep = WIDE ? 128 : kKeys;
+  static constexpr int kP = WIDE ? 256 : D == 256 ? 384 : 128, kPStep = WIDE ? 128 : kKeys / 2;
+  static_assert(kSmem > kPdlTmemSmem, "no second kernel with tensor memory beside it");
+  static_assert(kSmem + 14000 <= 232448, "shared memory of an SM");
+};
+
+struct Info {  // a tile
+  uint32_t valid[4];  // its positions that exist: in the sequence's range, on present pages
+  int p0, n, lo, flags;  // first position; the sequence's length and lowest position; 1: rows attend to it differently
+  float ek, ev;       // exponents of an 8-bit tile's factors
+};
+
+struct Control {
+  uint64_t full[8], empty[8], info[kInfos], q_full, q_empty, s_full[2], p_full[2], pv_done[2], fin;
+  Info tile[kInfos];
+  unsigned long long bad[8][2];  // per segment: nodes, and positions from lo on, with values that are not finite
+  int64_t off[2][128];           // element offsets of a tile's rows, -1: none
+  int64_t sum[32];
+  float mx[2][2][128], l[2][128], qf[4][256];
+  uint32_t fac[2][2][128];
+  int wmax[2][8];
+  int where[4];
+  uint32_t tmem;
+  int err;
+};
+
+struct Args {
+  TreeArgs a;
+  int groups, blocks, page_shift;  // groups: key heads x blocks of rows
+  float* part;
+  SegMeta* meta;
+  int32_t* error;
+};
+
+struct Seg {
+  int b, grp, nt, n, lo, end, base;
+};
+
+template <int KEYS>
+__device__ __forceinline__ void seg_range(const TreeArgs& a, int len, Seg& s) {
+  const int cap = a.c.max_pages * a.c.page_size;
+  s.n = min(max(len, 0), cap);
+  s.lo = a.window > 0 ? max(0, s.n + (a.mask ? 1 : 0) - a.window) : 0;
+  s.end = a.mask ? min(cap, s.n + a.n_nodes) : s.n;
+  s.base = s.lo & ~(KEYS - 1);
+  s.nt = max(1, (s.end - s.base + KEYS - 1) / KEYS);  // an empty sequence has one empty tile
+}
+
+// The line of `total` tiles dealt out to `workers` CTAs: the first `more` get one
+// more than the others.
+struct Deal {
+  int64_t each;
+  int more;
+  __device__ __forceinline__ Deal(int64_t total, int workers) : each(total / workers), more((int)(total % workers)) {}
+  __device__ __forceinline__ int64_t start(int w) const { return w * each + min(w, more); }
+  __device__ __forceinline__ int worker(int64_t tile) const {
+    const int64_t cut = more * (each + 1);
+    return tile < cut ? (int)(tile / (each + 1)) : more + (int)((tile - cut) / each);
+  }
+};
+
+// the CTA's share of the line, segment by segment; every role walks it
+template <int KEYS>
+struct Walk {
+  const Args& g;
+  Seg s;
+  int ct, cnt, ahead, index;  // first tile and tiles of this CTA in the segment; the next sequence's length; segments behind
+  int64_t left;
+  __device__ __forceinline__ Walk(const Args& g, const int* where, int64_t tiles) : g(g) {
+    s.b = where[0], s.grp = where[1], ct = where[2], index = 0;
+    seg_range<KEYS>(g.a, where[3], s);
+    ahead = g.a.lens[min(s.b + 1, g.a.c.n_seqs - 1)];
+    left = tiles;
+    cnt = (int)min((int64_t)(s.nt - ct), left);
+  }
+  __device__ __forceinline__ bool next() {
+    left -= cnt;
+    if (left <= 0) return false;
+    ct = 0;
+    ++index;
+    if (++s.grp == g.groups) {
+      s.grp = 0;
+      ++s.b;
+      seg_range<KEYS>(g.a, ahead, s);
+      ahead = g.a.lens[min(s.b + 1, g.a.c.n_seqs - 1)];
+    }
+    cnt = (int)min((int64_t)s.nt, left);
+    return true;
+  }
+};
+
+// ---------------------------------------------------------------- PTX
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool ok) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
+// A (16-bit, K-major) from TMEM
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+      "}\n" ::"r"(d), "r"(a), "l"(db), "r"(idesc), "r"(accumulate));
+}
+template <typename T> constexpr uint32_t idesc(int M, int N, int b_mn) {
+  const uint32_t fmt = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+  return (1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)b_mn << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+// 32 columns of the thread's lane, without waiting
+__device__ __forceinline__ void ld32(uint32_t at, float (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
+      "%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
+        "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]),
+        "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]),
+        "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+      : "r"(at));
+}
+__device__ __forceinline__ void ld_wait(float (&v)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]),
+                 "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]), "+f"(v[16]), "+f"(v[17]),
+                 "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]),
+                 "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void st16(uint32_t at, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at), "r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+      "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// a bounded wait; once one has given up, the others do not wait either
+__device__ __forceinline__ void wait(Control& c, uint64_t* b, uint32_t parity) {
+  if (tc::mbar_try_wait(b, parity)) return;
+  const long long t0 = clock64();
+  while (!tc::mbar_try_wait(b, parity)) {
+    if (*(volatile int*)&c.err) return;
+    if (clock64() - t0 > 4000000000LL) {
+      atomicExch(&c.err, 1);
+      return;
+    }
+  }
+}
+
+// the weight of a piece with maximum m where the largest is mm; a piece that
+// met nothing has m = -inf, sum 0
+__device__ __forceinline__ float piece_weight(float m, float mm) {
+  return m == -CUDART_INF_F ? (mm == -CUDART_INF_F ? 1.0f : 0.0f) : exp2_fast(m - mm);
+}
+
+// fp16 weights are e^(s - m) 2^6, at most 2^14: what is 2^-30 of the largest is kept
+template <typename M> struct Weights;
+template <> struct Weights<__nv_bfloat16> {
+  static constexpr float kBias = 0.0f;
+};
+template <> struct Weights<__half> {
+  static constexpr float kBias = 6.0f;
+};
+template <typename M> __device__ __forceinline__ float log_sum(float m, float l) {
+  return l == 0.0f ? -CUDART_INF_F : (m == -CUDART_INF_F ? 0.0f : m - Weights<M>::kBias) * 0.69314718f + logf(l);
+}
+
+template <typename M> __device__ __forceinline__ bool not_finite(uint32_t w, int half) {
+  const uint32_t e = std::is_same<M, __nv_bfloat16>::value ? 0x7f80u : 0x7c00u;
+  return ((w >> (16 * half)) & e) == e;
+}
+
+// byte address of 16-byte chunk ch of row r in a swizzled tile of `rows` rows
+__device__ __forceinline__ uint32_t chunk_at(int r, int ch, int rows) {
+  return (ch >> 3) * rows * 128 + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
+}
+
+// ---------------------------------------------------------------- the kernel
+// T: type of queries and output; E8: an 8-bit cache
+template <typename T, bool E8, int D, bool WIDE>
+__global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(Args g) {
+  using S = Shape<D, E8, WIDE>;
+  using M = typename std::conditional<E8, __half, T>::type;  // type of the products
+  constexpr int kKeys = S::kKeys, kChunks = D / 8, kEntries = S::kEntries;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ __align__(16) Control ctl;
+  const TreeArgs& a = g.a;
+  const pe_kv_cache& c = a.c;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  const uint32_t qs = tc::smem_u32(smem), ring = qs + S::kQBytes;
+  const int G = a.n_q_heads / c.n_heads, R = a.n_nodes * G, B = c.n_seqs;
+
+  if (warp == 8) tc::tmem_alloc(&ctl.tmem, 512);
+  if (tid == 0) {
+    for (int i = 0; i < 8; ++i) {
+      tc::mbar_init(&ctl.full[i], S::kProducers);
+      tc::mbar_init(&ctl.empty[i], 1);
+      tc::mbar_init(&ctl.info[i], S::kProducers);
+    }
+    tc::mbar_init(&ctl.q_full, S::kProducers);
+    tc::mbar_init(&ctl.q_empty, 1);
+    tc::mbar_init(&ctl.fin, 1);
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(&ctl.s_full[i], 1);
+      tc::mbar_init(&ctl.p_full[i], WIDE ? 4 : 8);
+      tc::mbar_init(&ctl.pv_done[i], 1);
+    }
+    ctl.err = 0;
+    tc::fence_mbar_init();
+  }
+  cudaGridDependencySynchronize();
+  cudaTriggerProgrammaticLaunchCompletion();
+
+  // -- a prefix sum of the sequences' tiles finds where this CTA's share starts
+  const int chunk = (B + S::kThreads - 1) / S::kThreads;
+  int64_t sum = 0;
+  Seg s0;
+  for (int b = tid * chunk; b < min(B, (tid + 1) * chunk); ++b) {
+    seg_range<kKeys>(a, a.lens[b], s0);
+    sum += s0.nt;
+  }
+  int64_t incl = sum;
+  for (int x = 1; x < 32; x <<= 1) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, incl, x);
+    if (lane >= x) incl += y;
+  }
+  if (lane == 31) ctl.sum[warp] = incl;
+  tc::fence_before();
+  __syncthreads();
+  tc::fence_after();
+  int64_t before = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < S::kThreads / 32; ++w) {
+    if (w < warp) before += ctl.sum[w];
+    total += ctl.sum[w];
+  }
+  total *= g.groups;
+  const int workers = (int)min(total, (int64_t)gridDim.x);
+  const Deal deal(total, workers);
+  const int64_t start = (int)blockIdx.x < workers ? deal.start(blockIdx.x) : 0;
+  const int64_t tiles = (int)blockIdx.x < workers ? deal.start(blockIdx.x + 1) - start : 0;
+  const int64_t lo = (before + incl - sum) * g.groups, hi = (before + incl) * g.groups;
+  if (start >= lo && start < hi) {
+    int64_t at = lo;
+    int b = tid * chunk, len = 0;
+    for (;; ++b) {
+      len = a.lens[b];
+      seg_range<kKeys>(a, len, s0);
+      if (start < at + (int64_t)s0.nt * g.groups) break;
+      at += (int64_t)s0.nt * g.groups;
+    }
+    ctl.where[0] = b;
+    ctl.where[1] = (int)((start - at) / s0.nt);
+    ctl.where[2] = (int)((start - at) % s0.nt);
+    ctl.where[3] = len;
+  }
+  __syncthreads();
+  const uint32_t tmem = ctl.tmem;
+  if (tid == 0) {
+    // the boundary at this CTA's start joins the segment if it is the first inside it
+    SegMeta m{0, 0, 0, 0};
+    if (tiles > 0) {
+      Walk<kKeys> w(g, ctl.where, tiles);
+      const int64_t g0 = start - w.ct, prev = blockIdx.x ? deal.start((int)blockIdx.x - 1) : 0;
+      m.seq = w.s.b, m.group = w.s.grp;
+      if (w.ct > 0 && prev <= g0) {
+        m.pieces = deal.worker(g0 + w.s.nt - 1) - blockIdx.x + 2;
+        m.first_slot = 2 * (blockIdx.x - 1) + (prev < g0 ? 1 : 0);
+      }
+    }
+    g.meta[blockIdx.x] = m;
+  }
+
+  if (tiles == 0) {
+    // nothing to do
+  } else if (warp < 8) {
+    // ================================================== softmax
+    const int wg = warp >> 2, row = (warp & 3) * 32 + lane;  // row of the tile, lane of TMEM
+    const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const float qlog = fabsf(a.scale) * 1.4426950408889634f;
+    uint32_t sp[2] = {0, 0}, pp[2] = {0, 0}, ip = 0;  // phases: scores, outputs, tiles seen
+    Walk<kKeys> w(g, ctl.where, tiles);
+    do {
+      const Seg& s = w.s;
+      const int hk = s.grp / g.blocks, r0 = s.grp % g.blocks * S::kRows, rows = min(R - r0, S::kRows);
+      const int rr = r0 + (WIDE ? wg * 128 : 0) + row;  // row of the sequence and key head
+      const bool exists = rr < R && (WIDE ? wg * 128 + row < rows : row < rows);
+      const int node = exists ? rr / G : 0, head = hk * G + (exists ? rr % G : 0);
+      uint64_t bits = 0;
+      int row_lo = s.lo;
+      bool live = exists;
+      if (a.mask) {
+        if (exists) bits = a.mask[s.b * a.mask_stride + node] & (0xffffffffffffffffull >> (64 - a.n_nodes));
+        live = bits != 0;
+        if (a.window > 0) row_lo = max(0, s.n + __popcll(bits) - a.window);
+      }
+      const int lo_hi = a.mask && a.window > 0 ? max(0, s.n + 64 - a.window) : s.lo;
+      const bool warp_live = __any_sync(0xffffffffu, exists);
+      const bool both = !WIDE || rows > 128;  // the second warpgroup has work
+      float m = -CUDART_INF_F, l = 0.0f, qf = 1.0f;
+      if (WIDE && wg == 1 && !both) {
+        ip += w.cnt;
+        continue;
+      }
+      for (int t = 0; t < w.cnt; ++t, ++ip) {
+        const int buf = WIDE ? wg : t & 1;
+        wait(ctl, &ctl.info[ip % kInfos], (ip / kInfos) & 1);
+        const Info& f = ctl.tile[ip % kInfos];
+        wait(ctl, &ctl.s_full[buf], sp[buf] & 1);
+        ++sp[buf];
+        __syncwarp();
+        tc::fence_after();
+        if (E8 && t == 0) qf = ctl.qf[w.index & 3][(WIDE ? wg * 128 : 0) + row];
+        const float ev = E8 ? f.ev : 0.0f;
+        const float cf = E8 ? qlog * qf * exp2f(f.ek) : qlog;
+        if (warp_live) {
+          const uint32_t sc = lanes + S::kS + buf * S::kSStep + (WIDE ? 0 : wg * S::kCols);
+          const uint32_t pc = lanes + S::kP + buf * S::kPStep + (WIDE ? 0 : wg * S::kCols / 2);
+          const bool whole = f.p0 >= lo_hi && f.p0 + kKeys <= f.n && (f.valid[0] & f.valid[1] & f.valid[2] & f.valid[3]) == 0xffffffffu;
+          uint32_t keep[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};  // of the thread's columns
+          if (!whole) {
+#pragma unroll
+            for (int i = 0; i < S::kCols / 32; ++i) {
+              const int at = i + (WIDE ? 0 : wg * (S::kCols / 32)), pw = f.p0 + 32 * at;
+              const int below = min(max(f.n - pw, 0), 32), skip = min(max(row_lo - pw, 0), 32);
+              uint32_t ctx = below == 32 ? 0xffffffffu : (1u << below) - 1;
+              ctx &= skip == 32 ? 0u : 0xffffffffu << skip;
+              const int sh = pw - f.n;
+              const uint32_t nodes = sh >= 64 || sh <= -32 ? 0u : sh >= 0 ? (uint32_t)(bits >> sh) : (uint32_t)(bits << -sh);
+              keep[i] = live ? f.valid[at] & (ctx | nodes) : 0u;
+            }
+          }
+          // the row's largest score
+          float top = -CUDART_INF_F;
+          float v[32];
+#pragma unroll
+          for (int i = 0; i < S::kCols / 32; ++i) {
+            ld32(sc + 32 * i, v);
+            ld_wait(v);
+            if (!whole) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[j] = (keep[i] >> j) & 1 ? v[j] : -CUDART_INF_F;
+            }
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) top = fmaxf(top, fmaxf(v[j], v[j + 1]));
+          }
+          if (!WIDE) {
+            ctl.mx[ip & 1][wg][row] = top;
+            bar_sync(1 + (warp & 3), 64);
+            top = fmaxf(top, ctl.mx[ip & 1][wg ^ 1][row]);
+          }
+          top = top == -CUDART_INF_F ? top : fmaf(top, cf, ev);
+          const bool over = top > m + 8.0f;
+          if (__any_sync(0xffffffffu, over)) {
+            const float x = over ? top : m;
+            const float fr = over ? (m == -CUDART_INF_F ? 0.0f : exp2_fast(m - x)) : 1.0f;
+            m = x;
+            l *= fr;
+            if (t > 0) {
+              if (!WIDE) wait(ctl, &ctl.pv_done[0], (pp[0] - 1) & 1);  // the last product into the output
+              __syncwarp();
+              tc::fence_after();
+              const uint32_t oc = lanes + S::kO + (WIDE ? wg * S::kOStep : wg * (D / 2));
+#pragma unroll 1
+              for (int i = 0; i < (WIDE ? D : D / 2) / 32; ++i) {
+                ld32(oc + 32 * i, v);
+                ld_wait(v);
+                uint32_t lo16[16], hi16[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                  lo16[j] = __float_as_uint(v[j] * fr);
+                  hi16[j] = __float_as_uint(v[j + 16] * fr);
+                }
+                st16(oc + 32 * i, lo16);
+                st16(oc + 32 * i + 16, hi16);
+              }
+            }
+          }
+          const float off = ev + Weights<M>::kBias - (m == -CUDART_INF_F ? 0.0f : m);
+          float part[2] = {0.0f, 0.0f};
+#pragma unroll
+          for (int i = 0; i < S::kCols / 32; ++i) {
+            ld32(sc + 32 * i, v);
+            ld_wait(v);
+            uint32_t pk[16];
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+              const float2 e = __ffma2_rn(make_float2(v[j], v[j + 1]), make_float2(cf, cf), make_float2(off, off));
+              float p0 = exp2_fast(e.x), p1 = exp2_fast(e.y);
+              if (!whole) {
+                p0 = (keep[i] >> j) & 1 ? p0 : 0.0f;
+                p1 = (keep[i] >> (j + 1)) & 1 ? p1 : 0.0f;
+              }
+              part[0] += p0;
+              part[1] += p1;
+              pk[j / 2] = pack2<M>(p0, p1);
+            }
+            st16(pc + 16 * i, pk);
+          }
+          l = E8 ? fmaf(part[0] + part[1], exp2f(-ev), l) : l + (part[0] + part[1]);
+          st_wait();
+        } else if (!WIDE) {
+          bar_sync(1 + (warp & 3), 64);
+        }
+        tc::fence_before();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&ctl.p_full[buf]);
+        ++pp[WIDE ? wg : 0];
+      }
+      // -- the segment, or this CTA's part of it, ends
+      // (the last scores say that all products but two, or one, are done: no phase is skipped)
+      if (!WIDE && w.cnt > 1) wait(ctl, &ctl.pv_done[0], pp[0] & 1);
+      wait(ctl, &ctl.pv_done[WIDE ? wg : 0], (pp[WIDE ? wg : 0] - 1) & 1);
+      __syncwarp();
+      tc::fence_after();
+      if (!live) m = -CUDART_INF_F, l = 0.0f;
+      if (!WIDE) {
+        ctl.l[wg][row] = l;
+        bar_sync(1 + (warp & 3), 64);
+        l += ctl.l[wg ^ 1][row];
+      }
+      if (warp_live) {
+        const bool whole = w.ct == 0 && w.cnt == s.nt;
+        const uint64_t bad_node = ctl.bad[w.index & 7][0] & bits;
+        uint64_t bad_pos = ctl.bad[w.index & 7][1];
+        if (row_lo > s.lo) bad_pos &= row_lo - s.lo >= 64 ? 0 : 0xffffffffffffffffull << (row_lo - s.lo);
+        const bool spoilt = live && (bad_node | bad_pos) != 0;
+        constexpr int kMine = WIDE ? D : D / 2;  // elements of the thread
+        const int d0 = WIDE ? 0 : wg * kMine;
+        const uint32_t oc = lanes + S::kO + (WIDE ? wg * S::kOStep : d0);
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        T* out = (T*)a.out + s.b * a.o_seq + node * a.o_node + head * a.o_head + d0;
+        // a CTA has two slots: its first segment's, and that of a segment it starts and does not end
+        const int64_t slot = 2 * (int64_t)blockIdx.x + (w.index > 0 ? 1 : 0);
+        float* piece = g.part + slot * S::kRows * (D + 2);
+        const int prow = (WIDE ? wg * 128 : 0) + row;
+        float v[32];
+#pragma unroll 1
+        for (int i = 0; i < kMine / 32; ++i) {
+          ld32(oc + 32 * i, v);
+          ld_wait(v);
+          if (spoilt) {  // an attended value that is not finite makes its element NaN
+#pragma unroll 1
+            for (int k = 0; k < 128; ++k) {
+              if (!((k < 64 ? bad_node >> k : bad_pos >> (k - 64)) & 1)) continue;
+              const int p = k < 64 ? s.n + k : s.lo + k - 64;
+              const int page = c.table[(int64_t)s.b * c.table_stride + p / c.page_size], sl = p % c.page_size;
+              const int64_t at = kv_page_offset(c, page) + (int64_t)sl * c.slot_stride + hk * c.head_stride + d0 + 32 * i;
+              const bool row_bad = E8 && a.sc.v[page * a.sc.page_stride + (int64_t)sl * a.sc.slot_stride + hk * a.sc.head_stride] == 255;
+#pragma unroll
+              for (int j = 0; j < 32; ++j) {
+                const bool x = E8 ? row_bad || (((const uint8_t*)c.v)[at + j] & 0x7f) == 0x7f : not_finite<T>(((const uint16_t*)c.v)[at + j], 0);
+                if (x) v[j] = CUDART_NAN_F;
+              }
+            }
+          }
+          if (exists && whole) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 8) {
+              uint4 o;
+              o.x = pack2<T>(v[j] * inv, v[j + 1] * inv), o.y = pack2<T>(v[j + 2] * inv, v[j + 3] * inv);
+              o.z = pack2<T>(v[j + 4] * inv, v[j + 5] * inv), o.w = pack2<T>(v[j + 6] * inv, v[j + 7] * inv);
+              if (l == 0.0f) o = make_uint4(0, 0, 0, 0);  // nothing attended to, whatever the values are
+              *reinterpret_cast<uint4*>(out + 32 * i + j) = o;
+            }
+          } else if (exists) {
+            float* to = piece + (int64_t)prow * D + d0 + 32 * i;
+#pragma unroll
+            for (int j = 0; j < 32; j += 4)
+              *reinterpret_cast<float4*>(to + j) = l == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+          }
+          __syncwarp();
+        }
+        if (exists && (WIDE || wg == 0)) {
+          if (whole) {
+            if (a.lse) a.lse[((int64_t)s.b * a.n_nodes + node) * a.n_q_heads + head] = log_sum<M>(m, l);
+          } else {
+            piece[S::kRows * D + prow] = m;
+            piece[S::kRows * (D + 1) + prow] = l;
+          }
+        }
+      }
+      tc::fence_before();
+    } while (w.next());
+  } else if (warp == 8) {
+    // ================================================== products
+    if (lane == 0) {
+      constexpr uint32_t kIdS = idesc<M>(128, kKeys, 0), kIdO = idesc<M>(128, D, 1);
+      uint32_t fe = 0, pf[2] = {0, 0}, qi = 0;  // next ring entry to see; phases of the weights; of the queries
+      auto entry = [&](uint32_t e) { return ring + (e % kEntries) * S::kEntry; };
+      auto seen = [&](uint32_t e) {  // entries come in order
+        while (fe <= e) {
+          wait(ctl, &ctl.full[fe % kEntries], (fe / kEntries) & 1);
+          ++fe;
+        }
+        tc::fence_after();
+      };
+      auto qk = [&](uint32_t e, int rt, int buf) {
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)
+          tc::mma_bf16(tmem + S::kS + buf * S::kSStep,
+                       tc::desc_kmajor(qs + rt * 128 * 128 * (D / 64) + (kk >> 2) * 128 * 128 + (kk & 3) * 32, 1024, tc::kLayoutSW128),
+                       tc::desc_kmajor(entry(e) + (kk >> 2) * kKeys * 128 + (kk & 3) * 32, 1024, tc::kLayoutSW128), kIdS, kk > 0);
+        tc::mma_commit(&ctl.s_full[buf]);
+      };
+      auto pv = [&](uint32_t e, int rt, int buf, bool first) {
+        wait(ctl, &ctl.p_full[buf], pf[buf] & 1);
+        ++pf[buf];
+        tc::fence_after();
+#pragma unroll
+        for (int kk = 0; kk < kKeys / 16; ++kk)
+          mma_ts(tmem + S::kO + rt * S::kOStep, tmem + S::kP + buf * S::kPStep + 8 * kk,
+                 tc::desc_strided(entry(e) + kk * 2048, kKeys * 128, 1024, tc::kLayoutSW128), kIdO, !(first && kk == 0));
+        tc::mma_commit(&ctl.pv_done[rt]);
+      };
+      uint32_t e0 = 0;  // entry of the segment's first keys
+      Walk<kKeys> w(g, ctl.where, tiles);
+      do {
+        const int rows = min(R - w.s.grp % g.blocks * S::kRows, S::kRows), nt = w.cnt;
+        wait(ctl, &ctl.q_full, qi & 1);
+        ++qi;
+        if (WIDE) {
+          const bool both = rows > 128;
+          seen(e0);
+          qk(e0, 0, 0);
+          if (both) qk(e0, 1, 1);
+          tc::mma_commit(&ctl.empty[e0 % kEntries]);
+          if (nt == 1) tc::mma_commit(&ctl.q_empty);
+          for (int t = 0; t < nt; ++t) {
+            const uint32_t ke = e0 + 2 * t + 2, ve = e0 + 2 * t + 1;
+            seen(ve);
+            pv(ve, 0, 0, t == 0);
+            if (!both) tc::mma_commit(&ctl.empty[ve % kEntries]);
+            if (t + 1 < nt) {
+              seen(ke);
+              qk(ke, 0, 0);
+            }
+            if (both) {
+              pv(ve, 1, 1, t == 0);
+              tc::mma_commit(&ctl.empty[ve % kEntries]);
+              if (t + 1 < nt) qk(ke, 1, 1);
+            }
+            if (t + 1 < nt) tc::mma_commit(&ctl.empty[ke % kEntries]);
+            if (t + 2 == nt) tc::mma_commit(&ctl.q_empty);
+          }
+        } else {
+          for (int t = 0; t < min(nt, 2); ++t) {
+            const uint32_t ke = e0 + 2 * t;
+            seen(ke);
+            qk(ke, 0, t);
+            tc::mma_commit(&ctl.empty[ke % kEntries]);
+          }
+          if (nt <= 2) tc::mma_commit(&ctl.q_empty);
+          for (int t = 0; t < nt; ++t) {
+            const uint32_t ve = e0 + 2 * t + 1, ke = e0 + 2 * t + 4;
+            seen(ve);
+            pv(ve, 0, t & 1, t == 0);
+            tc::mma_commit(&ctl.empty[ve % kEntries]);
+            if (t + 2 < nt) {
+              seen(ke);
+              qk(ke, 0, t & 1);
+              tc::mma_commit(&ctl.empty[ke % kEntries]);
+              if (t + 3 == nt) tc::mma_commit(&ctl.q_empty);
+            }
+          }
+        }
+        e0 += 2 * nt;
+      } while (w.next());
+      tc::mma_commit(&ctl.fin);
+      if (!tc::mbar_wait(&ctl.fin, 0)) atomicExch(&ctl.err, 1);
+    }
+  } else {
+    // ================================================== producers
+    constexpr int kN = 32 * S::kProducers;
+    const int pt = tid - 32 * 9;
+    auto sync = [&]() { bar_sync(5, kN); };
+    auto arrive = [&](uint64_t* b) {
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(b);
+    };
+    // queries of a segment's block of rows
+    auto load_q = [&](const Walk<kKeys>& w) {
+      const Seg& s = w.s;
+      const int hk = s.grp / g.blocks, r0 = s.grp % g.blocks * S::kRows, rows = min(R - r0, S::kRows);
+      if (w.index > 0) wait(ctl, &ctl.q_empty, (w.index - 1) & 1);
+      const T* q = (const T*)a.q + s.b * a.q_seq + (int64_t)hk * G * a.q_head;
+      constexpr int kStep = kN / kChunks;
+      const int ch = pt % kChunks;
+#pragma unroll 1
+      for (int r1 = 0; r1 < rows; r1 += 4 * kStep) {
+        uint4 x[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int r = r1 + pt / kChunks + u * kStep, rr = r0 + r;
+          x[u] = make_uint4(0, 0, 0, 0);
+          if (r < rows) x[u] = *reinterpret_cast<const uint4*>(q + (rr / G) * a.q_node + (rr % G) * a.q_head + ch * 8);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int r = r1 + pt / kChunks + u * kStep;
+          uint32_t* y = reinterpret_cast<uint32_t*>(&x[u]);
+          if (E8) {
+            // fp16 with the row's largest in [2^14, 2^15)
+            uint32_t most = 0;
+            float2 f[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              f[i] = unpack2<T>(y[i]);
+              most = max(most, max(__float_as_uint(f[i].x) & 0x7fffffffu, __float_as_uint(f[i].y) & 0x7fffffffu));
+            }
+#pragma unroll
+            for (int x = 1; x < kChunks; x *= 2) most = max(most, __shfl_xor_sync(0xffffffffu, most, x));
+            const int ex = (int)(most >> 23);
+            const int up = ex == 255 || most == 0 ? 127 : min(268 - ex, 253);  // exponent field of the factor
+            const float fac = __uint_as_float((uint32_t)up << 23);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = pack2<__half>(f[i].x * fac, f[i].y * fac);
+            if (ch == 0 && r < rows) ctl.qf[w.index & 3][r] = __uint_as_float((uint32_t)(254 - up) << 23);
+          }
+          if (a.scale < 0.0f)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] ^= 0x80008000u;
+          if (r < rows)
+            *reinterpret_cast<uint4*>(smem + (r >> 7) * (128 * 128 * (D / 64)) + chunk_at(r & 127, ch, 128)) = x[u];
+        }
+      }
+      tc::fence_async_smem();
+      arrive(&ctl.q_full);
+    };
+    // the page of position p of the sequence, or -1
+    auto page_of = [&](const Seg& s, int p) {
+      if (p < s.lo || p >= s.end) return -1;
+      const int i = g.page_shift >= 0 ? p >> g.page_shift : p / c.page_size;
+      const int page = c.table[(int64_t)s.b * c.table_stride + i];
+      return page >= 0 && page < c.n_pages ? page : -1;
+    };
+    auto slot_of = [&](int p) { return g.page_shift >= 0 ? p & (c.page_size - 1) : p % c.page_size; };
+    // bits of the values that rows attend to differently: (nodes, positions from lo on)
+    auto apart = [&](const Info& f, int r, int& which) -> uint64_t {
+      const int p = f.p0 + r, node = p - f.n;
+      which = 0;
+      if (node >= 0) return node < a.n_nodes ? 1ull << node : 0;
+      which = 1;
+      return a.window > 0 && p >= f.lo && p - f.lo < 64 ? 1ull << (p - f.lo) : 0;
+    };
+    Walk<kKeys> w(g, ctl.where, tiles);
+    uint32_t tile = 0;  // tiles behind
+    const int orow = pt % 128;  // the row whose place the thread finds
+    const bool owner = orow < kKeys && pt < 128;
+    int64_t my_off = -1;
+
+    if constexpr (!E8) {
+      constexpr int kPass = kN / kChunks;  // rows of a pass
+      const int row0 = pt / kChunks, ch = pt % kChunks;
+      uint32_t issued = 0, told = 0;
+      auto tell = [&]() {  // the oldest entry in flight has landed
+        if (a.mask && (told & 1)) {
+          const Info& f = ctl.tile[(told >> 1) % kInfos];
+          if (f.flags) {
+            const uint32_t at = ring + (told % kEntries) * S::kEntry;
+            unsigned long long* bad = ctl.bad[f.flags >> 1];
+#pragma unroll 1
+            for (int r = row0; r < kKeys; r += kPass) {
+              int which;
+              const uint64_t bit = apart(f, r, which);
+              if (!bit || !((f.valid[r >> 5] >> (r & 31)) & 1)) continue;
+              uint4* p = reinterpret_cast<uint4*>(smem + (at - qs) + chunk_at(r, ch, kKeys));
+              uint4 x = *p;
+              uint32_t* y = reinterpret_cast<uint32_t*>(&x);
+              bool any = false;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                if (not_finite<T>(y[i], 0)) y[i] &= 0xffff0000u, any = true;
+                if (not_finite<T>(y[i], 1)) y[i] &= 0x0000ffffu, any = true;
+              }
+              if (any) {
+                *p = x;
+                atomicOr(&bad[which], bit);
+              }
+            }
+          }
+        }
+        tc::fence_async_smem();
+        arrive(&ctl.full[told % kEntries]);
+        ++told;
+      };
+      int page = owner ? page_of(w.s, w.s.base + w.ct * kKeys + orow) : -1;
+      do {
+        const Seg& s = w.s;
+        const int hk = s.grp / g.blocks;
+        for (int t = 0; t < w.cnt; ++t, ++tile) {
+          const int p0 = s.base + (w.ct + t) * kKeys;
+          const int64_t* offs = ctl.off[tile & 1];
+          Info& f = ctl.tile[tile % kInfos];
+          if (t == 0 && pt < 2) ctl.bad[w.index & 7][pt] = 0;
+          if (pt < 128) {
+            my_off = page < 0 ? -1 : kv_page_offset(c, page) + (int64_t)slot_of(p0 + orow) * c.slot_stride + hk * c.head_stride;
+            if (owner) ctl.off[tile & 1][orow] = my_off;
+            const uint32_t ok = __ballot_sync(0xffffffffu, my_off >= 0);
+            if (lane == 0) f.valid[pt / 32] = orow < kKeys ? ok : 0xffffffffu;
+            if (pt == 0) {
+              f.p0 = p0, f.n = s.n, f.lo = s.lo;
+              const bool differ = a.mask && (p0 + kKeys > s.n || (a.window > 0 && p0 < s.lo + 64));
+              f.flags = differ ? 1 | (w.index & 7) << 1 : 0;
+            }
+          }
+          sync();
+          arrive(&ctl.info[tile % kInfos]);
+          if (t + 1 < w.cnt && owner) page = page_of(s, p0 + kKeys + orow);
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv) {
+            if (issued >= kEntries) wait(ctl, &ctl.empty[issued % kEntries], (issued / kEntries - 1) & 1);
+            const uint32_t dst = ring + (issued % kEntries) * S::kEntry;
+            const T* src = (const T*)(kv ? c.v : c.k) + ch * 8;
+#pragma unroll 8
+            for (int i = 0; i < kKeys / kPass; ++i) {
+              const int r = row0 + i * kPass;
+              const int64_t o = offs[r];
+              copy16(dst + chunk_at(r, ch, kKeys), src + (o < 0 ? 0 : o), o >= 0);
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            if (++issued > S::kLag) {
+              asm volatile("cp.async.wait_group %0;" ::"n"(S::kLag) : "memory");
+              tell();
+            }
+          }
+          // the first tile is under way before the last segment's queries are done with; all that
+          // this waits for has been told: kLag entries are in flight at most, two of them the tile's
+          if (t == 0) load_q(w);
+        }
+        if (w.left > w.cnt && owner) {  // the next segment's first page
+          Walk<kKeys> x = w;
+          x.next();
+          page = page_of(x.s, x.s.base + orow);
+        }
+      } while (w.next());
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+      while (told < issued) tell();
+    } else {
+      constexpr int kCh = D / 16, kPass = kN / kCh, kEach = kKeys / kPass;  // 16-code chunks of a row; rows of a pass; of a thread
+      const int row0 = pt / kCh, ch = pt % kCh;
+      const int which = pt / 128;  // the thread finds its row's place (0) and keys' scale, or (1) its values' scale
+      uint4 raw[2][kEach];
+      auto fetch = [&](uint4 (&x)[kEach], const void* base, const int64_t* offs) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          const int64_t o = offs[row0 + i * kPass];
+          x[i] = o < 0 ? make_uint4(0, 0, 0, 0) : __ldcg(reinterpret_cast<const uint4*>((const uint8_t*)base + o + ch * 16));
+        }
+      };
+      uint32_t issued = 0;
+      auto put = [&](const uint4 (&x)[kEach], const uint32_t* fac, bool check, const Info& f, unsigned long long* bad) {
+        if (issued >= kEntries) wait(ctl, &ctl.empty[issued % kEntries], (issued / kEntries - 1) & 1);
+        unsigned char* dst = smem + S::kQBytes + (issued % kEntries) * S::kEntry;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          const int r = row0 + i * kPass;
+          uint32_t fr = fac[r];
+          uint4 z = x[i];
+          uint32_t* y = reinterpret_cast<uint32_t*>(&z);
+          if (check) {
+            int k;
+            const uint64_t bit = apart(f, r, k);
+            if (bit && ((f.valid[r >> 5] >> (r & 31)) & 1)) {
+              bool any = (fr & 0x7fffu) > 0x7c00u;
+              if (any) fr = 0, z = make_uint4(0, 0, 0, 0);
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int b = 0; b < 32; b += 8)
+                  if (((y[j] >> b) & 0x7f) == 0x7f) y[j] &= ~(0xffu << b), any = true;
+              if (any) atomicOr(&bad[k], bit);
+            }
+          }
+          uint4 h[2];
+          uint32_t* hw = reinterpret_cast<uint32_t*>(h);
+          const __half2 ff = *reinterpret_cast<const __half2*>(&fr);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            uint32_t v;
+            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(v) : "h"((uint16_t)(y[j / 2] >> (16 * (j & 1)))));
+            const __half2 p = __hmul2(*reinterpret_cast<const __half2*>(&v), ff);
+            hw[j] = *reinterpret_cast<const uint32_t*>(&p);
+          }
+          // lanes of a row's second half store their halves the other way round: no two in one bank
+          const int flip = (ch >> 2) & 1;
+          *reinterpret_cast<uint4*>(dst + chunk_at(r, 2 * ch + flip, kKeys)) = flip ? h[1] : h[0];
+          *reinterpret_cast<uint4*>(dst + chunk_at(r, 2 * ch + 1 - flip, kKeys)) = flip ? h[0] : h[1];
+        }
+        tc::fence_async_smem();
+        arrive(&ctl.full[issued % kEntries]);
+        ++issued;
+      };
+      // places of tile x's rows, and the scale byte of the thread's own (-1: no row)
+      auto place = [&](int buf, const Seg& s, int p0, int page) {
+        const int hk = s.grp / g.blocks;
+        int64_t off = -1;
+        int byte = -1;
+        if (orow < kKeys && page >= 0) {
+          const int sl = slot_of(p0 + orow);
+          off = kv_page_offset(c, page) + (int64_t)sl * c.slot_stride + hk * c.head_stride;
+          byte = (which ? a.sc.v : a.sc.k)[page * a.sc.page_stride + (int64_t)sl * a.sc.slot_stride + hk * a.sc.head_stride];
+        }
+        if (which == 0 && orow < kKeys) ctl.off[buf][orow] = off;
+        return byte;
+      };
+      // the tile after (s, t): its sequence's range and first position; false at the end
+      Walk<kKeys> nx = w;  // one tile ahead
+      int nt = 0;
+      bool more = true;
+      auto step = [&]() {
+        if (++nt < nx.cnt) return;
+        nt = 0;
+        more = nx.next();
+      };
+      auto pos_of = [&]() { return nx.s.base + (nx.ct + nt) * kKeys; };
+      int byte = place(0, nx.s, pos_of(), page_of(nx.s, pos_of() + orow));
+      sync();
+      fetch(raw[0], c.k, ctl.off[0]);
+      fetch(raw[1], c.v, ctl.off[0]);
+      step();
+      int page = more ? page_of(nx.s, pos_of() + orow) : -1;
+      do {
+        const Seg& s = w.s;
+        for (int t = 0; t < w.cnt; ++t, ++tile) {
+          const int p0 = s.base + (w.ct + t) * kKeys, buf = tile & 1;
+          Info& f = ctl.tile[tile % kInfos];
+          const int own = byte;
+          if (t == 0 && pt < 2) ctl.bad[w.index & 7][pt] = 0;
+          const uint32_t ok = __ballot_sync(0xffffffffu, own >= 0);
+          // bytes in [63, 247]; 255 takes no part in the largest
+          const int fit = own < 0 || own == 255 ? -1 : min(max(own, 63), 247);
+          const int wm = __reduce_max_sync(0xffffffffu, fit);
+          if (lane == 0) {
+            ctl.wmax[buf][pt / 32] = wm;
+            if (pt < 128) f.valid[pt / 32] = orow < kKeys ? ok : 0xffffffffu;
+          }
+          if (pt == 0) {
+            f.p0 = p0, f.n = s.n, f.lo = s.lo;
+            const bool differ = a.mask && (p0 + kKeys > s.n || (a.window > 0 && p0 < s.lo + 64));
+            f.flags = differ ? 1 | (w.index & 7) << 1 : 0;
+          }
+          if (more) byte = place(buf ^ 1, nx.s, pos_of(), page);
+          sync();
+          int big = ctl.wmax[buf][4 * which];
+#pragma unroll
+          for (int i = 1; i < 4; ++i) big = max(big, ctl.wmax[buf][4 * which + i]);
+          if (big < 0) big = 127;
+          if (orow < kKeys) {
+            const int d = fit - big;  // at most 0; a factor below 2^-24 is 0
+            const uint32_t h = own < 0 ? 0u : own == 255 ? 0x7e00u : d >= -14 ? (uint32_t)(15 + d) << 10 : d >= -24 ? 1u << (24 + d) : 0u;
+            ctl.fac[buf][which][orow] = h | h << 16;
+          }
+          if (orow == 0) (which ? f.ev : f.ek) = (float)(big - 127);
+          sync();
+          arrive(&ctl.info[tile % kInfos]);
+          const bool check = f.flags != 0;
+          put(raw[0], ctl.fac[buf][0], false, f, ctl.bad[0]);
+          if (more) fetch(raw[0], c.k, ctl.off[buf ^ 1]);
+          put(raw[1], ctl.fac[buf][1], check, f, ctl.bad[w.index & 7]);
+          if (t == 0) load_q(w);
+          if (more) {
+            fetch(raw[1], c.v, ctl.off[buf ^ 1]);
+            step();
+            page = more ? page_of(nx.s, pos_of() + orow) : -1;
+          }
+        }
+      } while (w.next());
+    }
+  }
+  __syncwarp();
+  tc::fence_before();
+  __syncthreads();
+  tc::fence_after();
+  if (warp == 8) tc::tmem_dealloc(tmem, 512);
+  if (tid == 0 && ctl.err) atomicExch(g.error, 1);
+}
+
+// Joins the pieces of a segment in the order of the CTAs.  A warp takes a row;
+// its lanes hold the pieces' maxima and sums, then the output's elements.
+constexpr int kJoinRows = 8;
+template <typename T, typename M, int D>
+__global__ void __launch_bounds__(32 * kJoinRows) join_kernel(Args g, int block_rows) {
+  cudaGridDependencySynchronize();
+  cudaTriggerProgrammaticLaunchCompletion();
+  const TreeArgs& a = g.a;
+  const SegMeta s = g.meta[blockIdx.x];
+  if (s.pieces == 0) return;
+  const int lane = threadIdx.x & 31, G = a.n_q_heads / a.c.n_heads, R = a.n_nodes * G;
+  const int hk = s.group / g.blocks, r0 = s.group % g.blocks * block_rows, row = blockIdx.y * kJoinRows + threadIdx.x / 32;
+  if (row >= min(R - r0, block_rows)) return;
+  const int64_t slot = (int64_t)block_rows * (D + 2);
+  // piece 0 is in first_slot, the others in the first slots of the CTAs after it
+  auto at = [&](int i) { return g.part + (i ? (int64_t)((s.first_slot & ~1) + 2 * i) : (int64_t)s.first_slot) * slot; };
+  float mm = -CUDART_INF_F, sum = 0.0f;
+  for (int i = lane; i < s.pieces; i += 32) mm = fmaxf(mm, at(i)[block_rows * D + row]);
+  for (int x = 16; x; x >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, x));
+  constexpr int kV = D / 128 > 0 ? D / 128 : 1;  // float4s of a lane (head_dim 64: of half the lanes)
+  float4 o[kV];
+#pragma unroll
+  for (int v = 0; v < kV; ++v) o[v] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int i0 = 0; i0 < s.pieces; i0 += 32) {
+    float f = 0.0f, fl = 0.0f;
+    if (i0 + lane < s.pieces) {
+      const float* p = at(i0 + lane);
+      f = piece_weight(p[block_rows * D + row], mm);
+      fl = f * p[block_rows * (D + 1) + row];
+    }
+    float all = fl;
+    for (int x = 16; x; x >>= 1) all += __shfl_xor_sync(0xffffffffu, all, x);
+    sum += all;
+    const int n = min(32, s.pieces - i0);
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+      const float wgt = __shfl_sync(0xffffffffu, f, i);
+      const float4* p = reinterpret_cast<const float4*>(at(i0 + i) + (int64_t)row * D);
+#pragma unroll
+      for (int v = 0; v < kV; ++v) {
+        if (D == 64 && lane >= 16) continue;
+        const float4 x = p[lane + 32 * v];
+        o[v].x = fmaf(wgt, x.x, o[v].x), o[v].y = fmaf(wgt, x.y, o[v].y), o[v].z = fmaf(wgt, x.z, o[v].z), o[v].w = fmaf(wgt, x.w, o[v].w);
+      }
+    }
+  }
+  const int rr = r0 + row, node = rr / G, head = hk * G + rr % G;
+  T* out = (T*)a.out + s.seq * a.o_seq + node * a.o_node + head * a.o_head;
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+  for (int v = 0; v < kV; ++v) {
+    if (D == 64 && lane >= 16) continue;
+    uint2 x = make_uint2(pack2<T>(o[v].x * inv, o[v].y * inv), pack2<T>(o[v].z * inv, o[v].w * inv));
+    if (sum == 0.0f) x = make_uint2(0, 0);
+    *reinterpret_cast<uint2*>(out + 4 * (lane + 32 * v)) = x;
+  }
+  if (a.lse && lane == 0) a.lse[((int64_t)s.seq * a.n_nodes + node) * a.n_q_heads + head] = log_sum<M>(mm, sum);
+}
+
+constexpr int64_t kMetaBytes = (kCtas * (int64_t)sizeof(SegMeta) + 255) / 256 * 256;
+
+static inline bool wide(int D, int rows) { return D < 256 && rows > 128; }
+
+template <typename T, bool E8, int D, bool WIDE>
+static pe_status go(const TreeArgs& a, void* ws, int32_t* error, cudaStream_t st) {
+  using S = Shape<D, E8, WIDE>;
+  using M = typename std::conditional<E8, __half, T>::type;
+  const int rows = a.n_nodes * (a.n_q_heads / a.c.n_heads);
+  Args g{};
+  g.a = a;
+  g.blocks = ceil_div(rows, S::kRows);
+  g.groups = a.c.n_heads * g.blocks;
+  g.page_shift = -1;  // of a page size that is a power of two
+  if ((a.c.page_size & (a.c.page_size - 1)) == 0)
+    while (a.c.page_size >> (g.page_shift + 1)) ++g.page_shift;
+  g.meta = reinterpret_cast<SegMeta*>(ws);
+  g.part = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + kMetaBytes);
+  g.error = error;
+  // a CTA's tiles are counted in 31 bits
+  if ((double)a.c.n_seqs * g.groups * ((double)a.c.max_pages * a.c.page_size / S::kKeys + 2) / kCtas >= 2147483000.0)
+    return fail(PE_EINVAL, "n_seqs * n_heads * max_pages * page_size too large");
+  auto kern = attn_kernel<T, E8, D, WIDE>;
+  PE_TRY_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
+  PE_TRY_CUDA(launch_pdl(kern, dim3(kCtas), dim3(S::kThreads), S::kSmem, st, true, g));
+  PE_TRY_CUDA(launch_pdl(join_kernel<T, M, D>, dim3(kCtas, ceil_div(rows < S::kRows ? rows : S::kRows, kJoinRows)), dim3(32 * kJoinRows), 0, st,
+                         true, g, (int)S::kRows));
+  return PE_OK;
+}
+
+template <typename T, bool E8>
+static pe_status go_dim(const TreeArgs& a, void* ws, int32_t* error, cudaStream_t st) {
+  const int rows = a.n_nodes * (a.n_q_heads / a.c.n_heads);
+  if (a.c.head_dim == 64) return wide(64, rows) ? go<T, E8, 64, true>(a, ws, error, st) : go<T, E8, 64, false>(a, ws, error, st);
+  if (a.c.head_dim == 128) return wide(128, rows) ? go<T, E8, 128, true>(a, ws, error, st) : go<T, E8, 128, false>(a, ws, error, st);
+  return go<T, E8, 256, false>(a, ws, error, st);
+}
+
+// the flag that a wait of this translation unit's kernels sets when it gives up
+static inline pe_status flag_address(const void* symbol, int32_t** p) {
+  PE_TRY_CUDA(cudaGetSymbolAddress(reinterpret_cast<void**>(p), symbol));
+  return PE_OK;
+}
+
+}  // namespace tree
+}  // namespace pe
