@@ -34,6 +34,8 @@
 
 #include <math_constants.h>
 
+#include <type_traits>
+
 #include "tc.cuh"
 #include "tokens.cuh"
 
@@ -52,13 +54,13 @@ struct Shape {
   static_assert(!(WIDE && D == 256), "two outputs of 256 columns leave no room for scores");
   static constexpr int kKeys = D == 256 ? 64 : 128;
   static constexpr int kRows = WIDE ? 256 : 128;  // of a block
-  static constexpr int kProducers = E8 ? 8 : 4;   // warps
+  static constexpr int kProducers = 4;            // warps
   static constexpr int kThreads = 32 * (9 + kProducers);
   static constexpr int kEntry = kKeys * D * 2;
-  static constexpr int kEntries = D == 64 ? 8 : (WIDE || D == 256) ? 4 : 5;
-  static constexpr int kLag = kEntries >= 5 ? 3 : 2;  // entries whose copies are in flight
+  static constexpr int kEntries = E8 ? (D == 64 ? 6 : 3) : D == 64 ? 8 : (WIDE || D == 256) ? 4 : 5;
+  static constexpr int kStages = !E8 ? 0 : (WIDE || D == 256) ? 3 : 4;  // entries of codes on their way (8 bits)
   static constexpr int kQBytes = kRows * D * 2;
-  static constexpr int kSmem = kQBytes + kEntries * kEntry + 1024;
+  static constexpr int kSmem = kQBytes + kEntries * kEntry + kStages * kEntry / 2 + 1024;
   static constexpr int kCols = WIDE ? kKeys : kKeys / 2;  // columns of a thread
   // TMEM columns
   static constexpr int kO = 0, kOStep = 128, kS = 256, kSStep = WIDE ? 128 : kKeys;
@@ -77,11 +79,11 @@ struct Control {
   uint64_t full[8], empty[8], info[kInfos], q_full, q_empty, s_full[2], p_full[2], pv_done[2], fin;
   Info tile[kInfos];
   unsigned long long bad[8][2];  // per segment: nodes, and positions from lo on, with values that are not finite
-  int64_t off[2][128];           // element offsets of a tile's rows, -1: none
+  int64_t off[4][128];           // element offsets of a tile's rows, -1: none
   int64_t sum[32];
   float mx[2][2][128], l[2][128], qf[4][256];
   uint32_t fac[2][2][128];
-  int wmax[2][8];
+  int wmax[2][2][4];
   int where[4];
   uint32_t tmem;
   int err;
@@ -265,7 +267,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
   if (warp == 8) tc::tmem_alloc(&ctl.tmem, 512);
   if (tid == 0) {
     for (int i = 0; i < 8; ++i) {
-      tc::mbar_init(&ctl.full[i], S::kProducers);
+      tc::mbar_init(&ctl.full[i], E8 ? S::kProducers : 32 * S::kProducers);
       tc::mbar_init(&ctl.empty[i], 1);
       tc::mbar_init(&ctl.info[i], S::kProducers);
     }
@@ -389,87 +391,124 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           const uint32_t sc = lanes + S::kS + buf * S::kSStep + (WIDE ? 0 : wg * S::kCols);
           const uint32_t pc = lanes + S::kP + buf * S::kPStep + (WIDE ? 0 : wg * S::kCols / 2);
           const bool whole = f.p0 >= lo_hi && f.p0 + kKeys <= f.n && (f.valid[0] & f.valid[1] & f.valid[2] & f.valid[3]) == 0xffffffffu;
-          uint32_t keep[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};  // of the thread's columns
-          if (!whole) {
+          auto tile = [&](auto masked) {
+            constexpr bool kMasked = decltype(masked)::value;
+            constexpr int kChunks32 = S::kCols / 32, kHeld = WIDE ? (kMasked ? 1 : 2) : kChunks32;  // chunks of columns; of those in registers
+            uint32_t keep[kChunks32];
+            if (kMasked) {
 #pragma unroll
-            for (int i = 0; i < S::kCols / 32; ++i) {
-              const int at = i + (WIDE ? 0 : wg * (S::kCols / 32)), pw = f.p0 + 32 * at;
-              const int below = min(max(f.n - pw, 0), 32), skip = min(max(row_lo - pw, 0), 32);
-              uint32_t ctx = below == 32 ? 0xffffffffu : (1u << below) - 1;
-              ctx &= skip == 32 ? 0u : 0xffffffffu << skip;
-              const int sh = pw - f.n;
-              const uint32_t nodes = sh >= 64 || sh <= -32 ? 0u : sh >= 0 ? (uint32_t)(bits >> sh) : (uint32_t)(bits << -sh);
-              keep[i] = live ? f.valid[at] & (ctx | nodes) : 0u;
+              for (int i = 0; i < kChunks32; ++i) {
+                const int at = i + (WIDE ? 0 : wg * kChunks32), pw = f.p0 + 32 * at;
+                const int below = min(max(f.n - pw, 0), 32), skip = min(max(row_lo - pw, 0), 32);
+                uint32_t ctx = below == 32 ? 0xffffffffu : (1u << below) - 1;
+                ctx &= skip == 32 ? 0u : 0xffffffffu << skip;
+                const int sh = pw - f.n;
+                const uint32_t nodes = sh >= 64 || sh <= -32 ? 0u : sh >= 0 ? (uint32_t)(bits >> sh) : (uint32_t)(bits << -sh);
+                keep[i] = live ? f.valid[at] & (ctx | nodes) : 0u;
+              }
             }
-          }
-          // the row's largest score
-          float top = -CUDART_INF_F;
-          float v[32];
+            // the row's largest score
+            float v[kHeld][32];
+            float top = -CUDART_INF_F, top2 = -CUDART_INF_F;
+            auto largest = [&](float (&x)[32], int i) {
+              if (kMasked) {
 #pragma unroll
-          for (int i = 0; i < S::kCols / 32; ++i) {
-            ld32(sc + 32 * i, v);
-            ld_wait(v);
-            if (!whole) {
+                for (int j = 0; j < 32; ++j) x[j] = (keep[i] >> j) & 1 ? x[j] : -CUDART_INF_F;
+              }
 #pragma unroll
-              for (int j = 0; j < 32; ++j) v[j] = (keep[i] >> j) & 1 ? v[j] : -CUDART_INF_F;
+              for (int j = 0; j < 32; j += 4) {
+                top = fmaxf(top, fmaxf(x[j], x[j + 1]));
+                top2 = fmaxf(top2, fmaxf(x[j + 2], x[j + 3]));
+              }
+            };
+            if constexpr (!WIDE) {
+#pragma unroll
+              for (int i = 0; i < kChunks32; ++i) ld32(sc + 32 * i, v[i]);
+#pragma unroll
+              for (int i = 0; i < kChunks32; ++i) {
+                ld_wait(v[i]);
+                largest(v[i], i);
+              }
+            } else {
+              ld32(sc, v[0]);
+#pragma unroll
+              for (int i = 0; i < kChunks32; ++i) {
+                ld_wait(v[i % kHeld]);
+                const uint32_t next = sc + 32 * (i + 1 < kChunks32 ? i + 1 : 0);  // at last the first again
+                if (kHeld == 2) ld32(next, v[(i + 1) % kHeld]);
+                largest(v[i % kHeld], i);
+                if (kHeld == 1) ld32(next, v[0]);
+              }
             }
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) top = fmaxf(top, fmaxf(v[j], v[j + 1]));
-          }
-          if (!WIDE) {
-            ctl.mx[ip & 1][wg][row] = top;
-            bar_sync(1 + (warp & 3), 64);
-            top = fmaxf(top, ctl.mx[ip & 1][wg ^ 1][row]);
-          }
-          top = top == -CUDART_INF_F ? top : fmaf(top, cf, ev);
-          const bool over = top > m + 8.0f;
-          if (__any_sync(0xffffffffu, over)) {
-            const float x = over ? top : m;
-            const float fr = over ? (m == -CUDART_INF_F ? 0.0f : exp2_fast(m - x)) : 1.0f;
-            m = x;
-            l *= fr;
-            if (t > 0) {
-              if (!WIDE) wait(ctl, &ctl.pv_done[0], (pp[0] - 1) & 1);  // the last product into the output
-              __syncwarp();
-              tc::fence_after();
-              const uint32_t oc = lanes + S::kO + (WIDE ? wg * S::kOStep : wg * (D / 2));
+            top = fmaxf(top, top2);
+            if (!WIDE) {
+              ctl.mx[ip & 1][wg][row] = top;
+              bar_sync(1 + (warp & 3), 64);
+              top = fmaxf(top, ctl.mx[ip & 1][wg ^ 1][row]);
+            }
+            top = top == -CUDART_INF_F ? top : fmaf(top, cf, ev);
+            const bool over = top > m + 8.0f;
+            if (__any_sync(0xffffffffu, over)) {
+              const float x = over ? top : m;
+              const float fr = over ? (m == -CUDART_INF_F ? 0.0f : exp2_fast(m - x)) : 1.0f;
+              m = x;
+              l *= fr;
+              if (t > 0) {
+                if (!WIDE) wait(ctl, &ctl.pv_done[0], (pp[0] - 1) & 1);  // the last product into the output
+                __syncwarp();
+                tc::fence_after();
+                const uint32_t oc = lanes + S::kO + (WIDE ? wg * S::kOStep : wg * (D / 2));
 #pragma unroll 1
-              for (int i = 0; i < (WIDE ? D : D / 2) / 32; ++i) {
-                ld32(oc + 32 * i, v);
-                ld_wait(v);
-                uint32_t lo16[16], hi16[16];
+                for (int i = 0; i < (WIDE ? D : D / 2) / 16; ++i) {
+                  float o[16];
+                  tc::tmem_ld16(oc + 16 * i, o);
+                  uint32_t r[16];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                  lo16[j] = __float_as_uint(v[j] * fr);
-                  hi16[j] = __float_as_uint(v[j + 16] * fr);
+                  for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(o[j] * fr);
+                  st16(oc + 16 * i, r);
                 }
-                st16(oc + 32 * i, lo16);
-                st16(oc + 32 * i + 16, hi16);
               }
             }
-          }
-          const float off = ev + Weights<M>::kBias - (m == -CUDART_INF_F ? 0.0f : m);
-          float part[2] = {0.0f, 0.0f};
+            const float off = ev + Weights<M>::kBias - (m == -CUDART_INF_F ? 0.0f : m);
+            const float2 cf2 = make_float2(cf, cf), off2 = make_float2(off, off);
+            float2 part = make_float2(0.0f, 0.0f);
+            auto weights = [&](float (&x)[32], int i) {
+              uint32_t pk[16];
 #pragma unroll
-          for (int i = 0; i < S::kCols / 32; ++i) {
-            ld32(sc + 32 * i, v);
-            ld_wait(v);
-            uint32_t pk[16];
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-              const float2 e = __ffma2_rn(make_float2(v[j], v[j + 1]), make_float2(cf, cf), make_float2(off, off));
-              float p0 = exp2_fast(e.x), p1 = exp2_fast(e.y);
-              if (!whole) {
-                p0 = (keep[i] >> j) & 1 ? p0 : 0.0f;
-                p1 = (keep[i] >> (j + 1)) & 1 ? p1 : 0.0f;
+              for (int j = 0; j < 32; j += 2) {
+                const float2 e = __ffma2_rn(make_float2(x[j], x[j + 1]), cf2, off2);
+                float2 p = make_float2(exp2_fast(e.x), exp2_fast(e.y));
+                if (kMasked) {
+                  p.x = (keep[i] >> j) & 1 ? p.x : 0.0f;
+                  p.y = (keep[i] >> (j + 1)) & 1 ? p.y : 0.0f;
+                }
+                part = __fadd2_rn(part, p);
+                pk[j / 2] = pack2<M>(p.x, p.y);
               }
-              part[0] += p0;
-              part[1] += p1;
-              pk[j / 2] = pack2<M>(p0, p1);
+              st16(pc + 16 * i, pk);
+            };
+            if constexpr (!WIDE) {
+#pragma unroll
+              for (int i = 0; i < kChunks32; ++i) weights(v[i], i);
+            } else {
+#pragma unroll
+              for (int i = 0; i < kChunks32; ++i) {
+                ld_wait(v[i % kHeld]);
+                if (kHeld == 2 && i + 1 < kChunks32) ld32(sc + 32 * (i + 1), v[(i + 1) % kHeld]);
+                if (kMasked) {
+#pragma unroll
+                  for (int j = 0; j < 32; ++j) v[i % kHeld][j] = (keep[i] >> j) & 1 ? v[i % kHeld][j] : -CUDART_INF_F;
+                }
+                weights(v[i % kHeld], i);
+                if (kHeld == 1 && i + 1 < kChunks32) ld32(sc + 32 * (i + 1), v[0]);
+              }
             }
-            st16(pc + 16 * i, pk);
-          }
-          l = E8 ? fmaf(part[0] + part[1], exp2f(-ev), l) : l + (part[0] + part[1]);
+            l = E8 ? fmaf(part.x + part.y, exp2f(-ev), l) : l + (part.x + part.y);
+          };
+          if (whole)
+            tile(std::false_type{});
+          else
+            tile(std::true_type{});
           st_wait();
         } else if (!WIDE) {
           bar_sync(1 + (warp & 3), 64);
@@ -565,6 +604,8 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           wait(ctl, &ctl.full[fe % kEntries], (fe / kEntries) & 1);
           ++fe;
         }
+        // copies write as ordinary stores do, products read through the asynchronous proxy
+        if (!E8) tc::fence_async_smem();
         tc::fence_after();
       };
       auto qk = [&](uint32_t e, int rt, int buf) {
@@ -724,37 +765,31 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     if constexpr (!E8) {
       constexpr int kPass = kN / kChunks;  // rows of a pass
       const int row0 = pt / kChunks, ch = pt % kChunks;
-      uint32_t issued = 0, told = 0;
-      auto tell = [&]() {  // the oldest entry in flight has landed
-        if (a.mask && (told & 1)) {
-          const Info& f = ctl.tile[(told >> 1) % kInfos];
-          if (f.flags) {
-            const uint32_t at = ring + (told % kEntries) * S::kEntry;
-            unsigned long long* bad = ctl.bad[f.flags >> 1];
+      uint32_t issued = 0;
+      // values that are not finite, where rows attend to them differently, become zeros and a mark
+      auto spoils = [&](const Info& f) {
+        const uint32_t at = S::kQBytes + (issued % kEntries) * S::kEntry;
+        unsigned long long* bad = ctl.bad[f.flags >> 1];
+        asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll 1
-            for (int r = row0; r < kKeys; r += kPass) {
-              int which;
-              const uint64_t bit = apart(f, r, which);
-              if (!bit || !((f.valid[r >> 5] >> (r & 31)) & 1)) continue;
-              uint4* p = reinterpret_cast<uint4*>(smem + (at - qs) + chunk_at(r, ch, kKeys));
-              uint4 x = *p;
-              uint32_t* y = reinterpret_cast<uint32_t*>(&x);
-              bool any = false;
+        for (int r = row0; r < kKeys; r += kPass) {
+          int which;
+          const uint64_t bit = apart(f, r, which);
+          if (!bit || !((f.valid[r >> 5] >> (r & 31)) & 1)) continue;
+          uint4* p = reinterpret_cast<uint4*>(smem + at + chunk_at(r, ch, kKeys));
+          uint4 x = *p;
+          uint32_t* y = reinterpret_cast<uint32_t*>(&x);
+          bool any = false;
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                if (not_finite<T>(y[i], 0)) y[i] &= 0xffff0000u, any = true;
-                if (not_finite<T>(y[i], 1)) y[i] &= 0x0000ffffu, any = true;
-              }
-              if (any) {
-                *p = x;
-                atomicOr(&bad[which], bit);
-              }
-            }
+          for (int i = 0; i < 4; ++i) {
+            if (not_finite<T>(y[i], 0)) y[i] &= 0xffff0000u, any = true;
+            if (not_finite<T>(y[i], 1)) y[i] &= 0x0000ffffu, any = true;
+          }
+          if (any) {
+            *p = x;
+            atomicOr(&bad[which], bit);
           }
         }
-        tc::fence_async_smem();
-        arrive(&ctl.full[told % kEntries]);
-        ++told;
       };
       int page = owner ? page_of(w.s, w.s.base + w.ct * kKeys + orow) : -1;
       do {
@@ -790,14 +825,17 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
               const int64_t o = offs[r];
               copy16(dst + chunk_at(r, ch, kKeys), src + (o < 0 ? 0 : o), o >= 0);
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            if (++issued > S::kLag) {
-              asm volatile("cp.async.wait_group %0;" ::"n"(S::kLag) : "memory");
-              tell();
+            if (kv && f.flags) {
+              spoils(f);
+              tc::fence_async_smem();
+              tc::mbar_arrive(&ctl.full[issued % kEntries]);
+            } else {
+              // the thread arrives when its copies have landed
+              asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tc::smem_u32(&ctl.full[issued % kEntries])) : "memory");
             }
+            ++issued;
           }
-          // the first tile is under way before the last segment's queries are done with; all that
-          // this waits for has been told: kLag entries are in flight at most, two of them the tile's
+          // the first tile is under way before the last segment's queries are done with
           if (t == 0) load_q(w);
         }
         if (w.left > w.cnt && owner) {  // the next segment's first page
@@ -806,29 +844,42 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           page = page_of(x.s, x.s.base + orow);
         }
       } while (w.next());
-      asm volatile("cp.async.wait_group 0;" ::: "memory");
-      while (told < issued) tell();
+      asm volatile("cp.async.wait_all;" ::: "memory");
     } else {
+      // Codes are copied to a stage of their own, kStages entries ahead, where the thread that copied
+      // a chunk finds it again; as fp16 they go to the ring.
       constexpr int kCh = D / 16, kPass = kN / kCh, kEach = kKeys / kPass;  // 16-code chunks of a row; rows of a pass; of a thread
+      constexpr int kStages = S::kStages;
       const int row0 = pt / kCh, ch = pt % kCh;
-      const int which = pt / 128;  // the thread finds its row's place (0) and keys' scale, or (1) its values' scale
-      uint4 raw[2][kEach];
-      auto fetch = [&](uint4 (&x)[kEach], const void* base, const int64_t* offs) {
+      unsigned char* stages = smem + S::kQBytes + kEntries * S::kEntry + pt * 16;
+      const uint32_t stages_at = tc::smem_u32(stages);
+      // entry e (keys and values in turn), of a tile whose rows have been placed
+      auto copy = [&](uint32_t e, bool there) {
+        if (there) {
+          const int64_t* offs = ctl.off[(e >> 1) & 3];
+          const uint8_t* base = (const uint8_t*)(e & 1 ? c.v : c.k) + ch * 16;
+          const uint32_t dst = stages_at + (e % kStages) * (S::kEntry / 2);
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-          const int64_t o = offs[row0 + i * kPass];
-          x[i] = o < 0 ? make_uint4(0, 0, 0, 0) : __ldcg(reinterpret_cast<const uint4*>((const uint8_t*)base + o + ch * 16));
+          for (int i = 0; i < kEach; ++i) {
+            const int64_t o = offs[row0 + i * kPass];
+            copy16(dst + i * kN * 16, base + (o < 0 ? 0 : o), o >= 0);
+          }
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
       };
-      uint32_t issued = 0;
-      auto put = [&](const uint4 (&x)[kEach], const uint32_t* fac, bool check, const Info& f, unsigned long long* bad) {
-        if (issued >= kEntries) wait(ctl, &ctl.empty[issued % kEntries], (issued / kEntries - 1) & 1);
-        unsigned char* dst = smem + S::kQBytes + (issued % kEntries) * S::kEntry;
+      auto put = [&](uint32_t e, const uint32_t* fac, bool check, const Info& f, unsigned long long* bad) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        if (e >= kEntries) wait(ctl, &ctl.empty[e % kEntries], (e / kEntries - 1) & 1);
+        __syncwarp();
+        const unsigned char* from = stages + (e % kStages) * (S::kEntry / 2);
+        unsigned char* dst = smem + S::kQBytes + (e % kEntries) * S::kEntry;
+        // lanes of a row's second half store their halves the other way round: no two in one bank
+        const int flip = (ch >> 2) & 1;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
           const int r = row0 + i * kPass;
           uint32_t fr = fac[r];
-          uint4 z = x[i];
+          uint4 z = *reinterpret_cast<const uint4*>(from + i * kN * 16);
           uint32_t* y = reinterpret_cast<uint32_t*>(&z);
           if (check) {
             int k;
@@ -854,90 +905,92 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             const __half2 p = __hmul2(*reinterpret_cast<const __half2*>(&v), ff);
             hw[j] = *reinterpret_cast<const uint32_t*>(&p);
           }
-          // lanes of a row's second half store their halves the other way round: no two in one bank
-          const int flip = (ch >> 2) & 1;
           *reinterpret_cast<uint4*>(dst + chunk_at(r, 2 * ch + flip, kKeys)) = flip ? h[1] : h[0];
           *reinterpret_cast<uint4*>(dst + chunk_at(r, 2 * ch + 1 - flip, kKeys)) = flip ? h[0] : h[1];
         }
         tc::fence_async_smem();
-        arrive(&ctl.full[issued % kEntries]);
-        ++issued;
+        arrive(&ctl.full[e % kEntries]);
       };
-      // places of tile x's rows, and the scale byte of the thread's own (-1: no row)
-      auto place = [&](int buf, const Seg& s, int p0, int page) {
-        const int hk = s.grp / g.blocks;
-        int64_t off = -1;
-        int byte = -1;
-        if (orow < kKeys && page >= 0) {
-          const int sl = slot_of(p0 + orow);
-          off = kv_page_offset(c, page) + (int64_t)sl * c.slot_stride + hk * c.head_stride;
-          byte = (which ? a.sc.v : a.sc.k)[page * a.sc.page_stride + (int64_t)sl * a.sc.slot_stride + hk * a.sc.head_stride];
-        }
-        if (which == 0 && orow < kKeys) ctl.off[buf][orow] = off;
-        return byte;
-      };
-      // the tile after (s, t): its sequence's range and first position; false at the end
-      Walk<kKeys> nx = w;  // one tile ahead
-      int nt = 0;
+      // the walk two tiles ahead: places of a tile's rows, and the scale bytes of the thread's own (-1: no row)
+      Walk<kKeys> nx = w;
+      int nt = 0, page = -1;
       bool more = true;
-      auto step = [&]() {
-        if (++nt < nx.cnt) return;
-        nt = 0;
-        more = nx.next();
+      auto look = [&]() { page = more && owner ? page_of(nx.s, nx.s.base + (nx.ct + nt) * kKeys + orow) : -1; };
+      auto place = [&](uint32_t tile, int2& bytes) {
+        bytes = make_int2(-1, -1);
+        if (more) {
+          int64_t off = -1;
+          if (page >= 0) {
+            const int sl = slot_of(nx.s.base + (nx.ct + nt) * kKeys + orow), hk = nx.s.grp / g.blocks;
+            off = kv_page_offset(c, page) + (int64_t)sl * c.slot_stride + hk * c.head_stride;
+            const int64_t so = page * a.sc.page_stride + (int64_t)sl * a.sc.slot_stride + hk * a.sc.head_stride;
+            bytes = make_int2(a.sc.k[so], a.sc.v[so]);
+          }
+          if (owner) ctl.off[tile & 3][orow] = off;
+          if (++nt == nx.cnt) {
+            nt = 0;
+            more = nx.next();
+          }
+        }
       };
-      auto pos_of = [&]() { return nx.s.base + (nx.ct + nt) * kKeys; };
-      int byte = place(0, nx.s, pos_of(), page_of(nx.s, pos_of() + orow));
+      const uint32_t entries = (uint32_t)(2 * tiles);
+      int2 b0, b1, b2;
+      look();
+      place(0, b0);
+      look();
+      place(1, b1);
       sync();
-      fetch(raw[0], c.k, ctl.off[0]);
-      fetch(raw[1], c.v, ctl.off[0]);
-      step();
-      int page = more ? page_of(nx.s, pos_of() + orow) : -1;
+      look();
+#pragma unroll
+      for (int e = 0; e < kStages; ++e) copy(e, e < entries);
       do {
         const Seg& s = w.s;
         for (int t = 0; t < w.cnt; ++t, ++tile) {
           const int p0 = s.base + (w.ct + t) * kKeys, buf = tile & 1;
           Info& f = ctl.tile[tile % kInfos];
-          const int own = byte;
+          place(tile + 2, b2);
           if (t == 0 && pt < 2) ctl.bad[w.index & 7][pt] = 0;
-          const uint32_t ok = __ballot_sync(0xffffffffu, own >= 0);
           // bytes in [63, 247]; 255 takes no part in the largest
-          const int fit = own < 0 || own == 255 ? -1 : min(max(own, 63), 247);
-          const int wm = __reduce_max_sync(0xffffffffu, fit);
+          auto fit = [](int b) { return b < 0 || b == 255 ? -1 : min(max(b, 63), 247); };
+          const uint32_t ok = __ballot_sync(0xffffffffu, b0.x >= 0);
+          const int km = __reduce_max_sync(0xffffffffu, fit(b0.x)), vm = __reduce_max_sync(0xffffffffu, fit(b0.y));
           if (lane == 0) {
-            ctl.wmax[buf][pt / 32] = wm;
-            if (pt < 128) f.valid[pt / 32] = orow < kKeys ? ok : 0xffffffffu;
+            ctl.wmax[buf][0][pt / 32] = km;
+            ctl.wmax[buf][1][pt / 32] = vm;
+            f.valid[pt / 32] = orow < kKeys ? ok : 0xffffffffu;
           }
           if (pt == 0) {
             f.p0 = p0, f.n = s.n, f.lo = s.lo;
             const bool differ = a.mask && (p0 + kKeys > s.n || (a.window > 0 && p0 < s.lo + 64));
             f.flags = differ ? 1 | (w.index & 7) << 1 : 0;
           }
-          if (more) byte = place(buf ^ 1, nx.s, pos_of(), page);
           sync();
-          int big = ctl.wmax[buf][4 * which];
 #pragma unroll
-          for (int i = 1; i < 4; ++i) big = max(big, ctl.wmax[buf][4 * which + i]);
-          if (big < 0) big = 127;
-          if (orow < kKeys) {
-            const int d = fit - big;  // at most 0; a factor below 2^-24 is 0
-            const uint32_t h = own < 0 ? 0u : own == 255 ? 0x7e00u : d >= -14 ? (uint32_t)(15 + d) << 10 : d >= -24 ? 1u << (24 + d) : 0u;
-            ctl.fac[buf][which][orow] = h | h << 16;
+          for (int x = 0; x < 2; ++x) {
+            const int own = x ? b0.y : b0.x;
+            int big = max(max(ctl.wmax[buf][x][0], ctl.wmax[buf][x][1]), max(ctl.wmax[buf][x][2], ctl.wmax[buf][x][3]));
+            if (big < 0) big = 127;
+            if (orow < kKeys) {
+              const int d = fit(own) - big;  // at most 0; a factor below 2^-24 is 0
+              const uint32_t h = own < 0 ? 0u : own == 255 ? 0x7e00u : d >= -14 ? (uint32_t)(15 + d) << 10 : d >= -24 ? 1u << (24 + d) : 0u;
+              ctl.fac[buf][x][orow] = h | h << 16;
+            }
+            if (pt == 0) (x ? f.ev : f.ek) = (float)(big - 127);
           }
-          if (orow == 0) (which ? f.ev : f.ek) = (float)(big - 127);
           sync();
           arrive(&ctl.info[tile % kInfos]);
+          look();
           const bool check = f.flags != 0;
-          put(raw[0], ctl.fac[buf][0], false, f, ctl.bad[0]);
-          if (more) fetch(raw[0], c.k, ctl.off[buf ^ 1]);
-          put(raw[1], ctl.fac[buf][1], check, f, ctl.bad[w.index & 7]);
+          put(2 * tile, ctl.fac[buf][0], false, f, ctl.bad[0]);
+          copy(2 * tile + kStages, 2 * tile + kStages < entries);
+          put(2 * tile + 1, ctl.fac[buf][1], check, f, ctl.bad[w.index & 7]);
+          copy(2 * tile + 1 + kStages, 2 * tile + 1 + kStages < entries);
           if (t == 0) load_q(w);
-          if (more) {
-            fetch(raw[1], c.v, ctl.off[buf ^ 1]);
-            step();
-            page = more ? page_of(nx.s, pos_of() + orow) : -1;
-          }
+          b0 = b1;
+          b1 = b2;
         }
       } while (w.next());
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
     }
   }
   __syncwarp();
