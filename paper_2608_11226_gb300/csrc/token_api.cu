@@ -149,9 +149,16 @@ pe_status pe_tree_attn(const pe_kv_cache* cache, const pe_kv_scales* scales, con
   return tree_attn_launch(a, workspace, reinterpret_cast<cudaStream_t>(stream));
 }
 
+// whether one token's heads of a key head are enough for tiles of 128 rows
+static bool many_heads(const pe_kv_cache& c, int n_q_heads) { return n_q_heads / c.n_heads > 24; }
+
+static int64_t decode8_ws_bytes(const pe_kv_cache& c, int n_q_heads) {
+  return many_heads(c, n_q_heads) ? tree_attn_ws_bytes(c, 1, n_q_heads) : decode_attn8_ws_bytes(c, n_q_heads);
+}
+
 int64_t pe_decode_attn8_workspace_bytes(const pe_kv_cache* cache, int32_t n_q_heads) {
   if (check_cache(cache, true) != PE_OK || cache->dtype != PE_E4M3 || bad_group(cache, n_q_heads)) return -1;
-  return tree_attn_ws_bytes(*cache, 1, n_q_heads);
+  return decode8_ws_bytes(*cache, n_q_heads);
 }
 
 pe_status pe_decode_attn8(const pe_kv_cache* cache, const pe_kv_scales* scales, int32_t dtype, const void* q,
@@ -170,8 +177,12 @@ pe_status pe_decode_attn8(const pe_kv_cache* cache, const pe_kv_scales* scales, 
   if (bad_stride(q_seq_stride) || bad_stride(q_head_stride) || bad_stride(out_seq_stride) || bad_stride(out_head_stride))
     return fail(PE_EINVAL, "q and out strides must be multiples of 8 elements");
   if (off(q, 16) || off(out, 16)) return fail(PE_EINVAL, "q and out must be 16-byte aligned");
-  s = check_workspace(workspace, workspace_bytes, tree_attn_ws_bytes(*cache, 1, n_q_heads));
+  s = check_workspace(workspace, workspace_bytes, decode8_ws_bytes(*cache, n_q_heads));
   if (s != PE_OK) return s;
+  if (!many_heads(*cache, n_q_heads)) {
+    DecodeArgs a{*cache, *scales, q, out, lse, lens, q_seq_stride, q_head_stride, out_seq_stride, out_head_stride, scale, n_q_heads, window};
+    return decode_attn8_launch(a, dtype, workspace, reinterpret_cast<cudaStream_t>(stream));
+  }
   TreeArgs a{*cache, *scales, q, out, lse, lens, nullptr, q_seq_stride, 0, q_head_stride, out_seq_stride, 0, out_head_stride, 0,
              scale, 1, n_q_heads, window, dtype};
   return tree_attn_launch(a, workspace, reinterpret_cast<cudaStream_t>(stream));
@@ -203,7 +214,7 @@ pe_status pe_decode_attn(const pe_kv_cache* cache, const void* q, int64_t q_seq_
   if (workspace_bytes < need)
     return fail(PE_EINVAL, "workspace too small (%lld < %lld bytes)", (long long)workspace_bytes, (long long)need);
   if (need > 0 && off(workspace, 256)) return fail(PE_EINVAL, "workspace must be 256-byte aligned");
-  DecodeArgs a{*cache, q, out, lse, lens, q_seq_stride, q_head_stride, out_seq_stride, out_head_stride, scale, n_q_heads, window};
+  DecodeArgs a{*cache, pe_kv_scales{}, q, out, lse, lens, q_seq_stride, q_head_stride, out_seq_stride, out_head_stride, scale, n_q_heads, window};
   return decode_attn_launch(a, workspace, reinterpret_cast<cudaStream_t>(stream));
 }
 

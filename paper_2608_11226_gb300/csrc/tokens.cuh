@@ -48,6 +48,7 @@ __device__ __forceinline__ int64_t kv_page_offset(const pe_kv_cache& c, int page
 
 struct DecodeArgs {
   pe_kv_cache c;
+  pe_kv_scales sc;
   const void* q;
   void* out;
   float* lse;
@@ -112,6 +113,8 @@ int64_t tree_attn_ws_bytes(const pe_kv_cache& c, int n_nodes, int n_q_heads);
 pe_status tree_attn_launch(const TreeArgs& a, void* ws, cudaStream_t st);
 int64_t decode_attn_ws_bytes(const pe_kv_cache& c, int n_q_heads);
 pe_status decode_attn_launch(const DecodeArgs& a, void* ws, cudaStream_t st);
+int64_t decode_attn8_ws_bytes(const pe_kv_cache& c, int n_q_heads);
+pe_status decode_attn8_launch(const DecodeArgs& a, int dtype, void* ws, cudaStream_t st);
 pe_status token_logp_launch(const LogpArgs& a, int dtype, cudaStream_t st);
 pe_status token_logp_grad_launch(const LogpGradArgs& a, int dtype, cudaStream_t st);
 
