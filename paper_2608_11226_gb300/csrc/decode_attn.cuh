@@ -399,6 +399,7 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + team * kStages * S::kUnitBytes;
   const int at0 = CL ? 0 : team * kUnit;                // place of the team's unit in a tile
   const bool one_page = c.page_size % kUnit == 0;  // no unit crosses a page
+  const bool two_pages = E8 && c.page_size % 16 == 0;  // no half of one does
   // place of a 16-byte chunk in its row, so that ldmatrix' eight rows meet no bank twice
   auto swizzle = [](int row, int ch) { return E8 && D == 64 ? ch ^ ((row >> 1) & 3) : ch ^ (row & 7); };
   Segment ls = cs;
@@ -456,6 +457,23 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
           const uint32_t d = dst + i * kRows * kRow + (swizzle(row0 + i * kRows, ch) << 4);
           copy16(d, k + i * kRows * c.slot_stride, true);
           copy16(d + kUnit * kRow, v + i * kRows * c.slot_stride, true);
+        }
+      } else if (two_pages && mask == kAll) {
+        const E* base[2][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int64_t o = __shfl_sync(0xffffffffu, off, 16 * h) + (int64_t)(row0 - 16 * h) * c.slot_stride + ch * kPer;
+          base[h][0] = (const E*)c.k + o;
+          base[h][1] = (const E*)c.v + o;
+        }
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+          const int row = row0 + i * kRows;
+          if (kUnit % kRows != 0 && row >= kUnit) break;
+          const bool h = 16 % kRows == 0 ? i * kRows >= 16 : row >= 16;
+          const uint32_t d = dst + i * kRows * kRow + (swizzle(row, ch) << 4);
+          copy16(d, (h ? base[1][0] : base[0][0]) + i * kRows * c.slot_stride, true);
+          copy16(d + kUnit * kRow, (h ? base[1][1] : base[0][1]) + i * kRows * c.slot_stride, true);
         }
       } else {
         if (one_page && lane & (kUnit - 1)) off += (lane & (kUnit - 1)) * c.slot_stride;
