@@ -43,7 +43,7 @@ namespace pe {
 namespace tree {
 
 constexpr int kCtas = 152;
-constexpr int kInfos = 8;  // tiles whose description is kept: more than the ring holds
+constexpr int kInfos = 16;  // tiles whose description is kept: what the ring holds, and what is placed ahead
 
 struct SegMeta {
   int32_t seq, group, pieces, first_slot;  // pieces 0: nothing to join
@@ -55,18 +55,20 @@ struct Shape {
   static constexpr int kKeys = D == 256 ? 64 : 128;
   static constexpr int kRows = WIDE ? 256 : 128;  // of a block
   static constexpr int kProducers = 4;            // warps
-  static constexpr int kThreads = 32 * (9 + kProducers);
+  static constexpr int kThreads = 512;
   static constexpr int kEntry = kKeys * D * 2;
-  static constexpr int kEntries = E8 ? (D == 64 ? 6 : 3) : D == 64 ? 8 : (WIDE || D == 256) ? 4 : 5;
-  static constexpr int kStages = !E8 ? 0 : (WIDE || D == 256) ? 3 : 4;  // entries of codes on their way (8 bits)
+  // queries of two segments where there is room, so that the next one's are there in time
+  static constexpr int kQs = WIDE || D == 256 ? 1 : 2;
+  static constexpr int kEntries = D == 64 ? 6 : E8 ? 3 : 4;
+  static constexpr int kStages = E8 ? 3 : 0;  // entries of codes on their way
   static constexpr int kQBytes = kRows * D * 2;
-  static constexpr int kSmem = kQBytes + kEntries * kEntry + kStages * kEntry / 2 + 1024;
+  static constexpr int kSmem = kQs * kQBytes + kEntries * kEntry + kStages * kEntry / 2 + 1024;
   static constexpr int kCols = WIDE ? kKeys : kKeys / 2;  // columns of a thread
   // TMEM columns
   static constexpr int kO = 0, kOStep = 128, kS = 256, kSStep = WIDE ? 128 : kKeys;
   static constexpr int kP = WIDE ? 256 : D == 256 ? 384 : 128, kPStep = WIDE ? 128 : kKeys / 2;
   static_assert(kSmem > kPdlTmemSmem, "no second kernel with tensor memory beside it");
-  static_assert(kSmem + 14000 <= 232448, "shared memory of an SM");
+  static_assert(kSmem + 17000 <= 232448, "shared memory of an SM");
 };
 
 struct Info {  // a tile
@@ -76,14 +78,13 @@ struct Info {  // a tile
 };
 
 struct Control {
-  uint64_t full[8], empty[8], info[kInfos], q_full, q_empty, s_full[2], p_full[2], pv_done[2], fin;
+  uint64_t full[8], empty[8], info[kInfos], placed[4], taken[4], q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2], fin;
   Info tile[kInfos];
-  unsigned long long bad[8][2];  // per segment: nodes, and positions from lo on, with values that are not finite
+  unsigned long long bad[16][2];  // per segment: nodes, and positions from lo on, with values that are not finite
   int64_t off[4][128];           // element offsets of a tile's rows, -1: none
-  int64_t sum[32];
+  int64_t sum[16];
   float mx[2][2][128], l[2][128], qf[4][256];
-  uint32_t fac[2][2][128];
-  int wmax[2][2][4];
+  uint32_t fac[4][2][128];
   int where[4];
   uint32_t tmem;
   int err;
@@ -207,6 +208,19 @@ __device__ __forceinline__ void st16(uint32_t at, const uint32_t (&r)[16]) {
 }
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+__device__ __forceinline__ bool mbar_test(uint64_t* b, uint32_t parity) {  // without suspending
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t"
+      "}\n"
+      : "=r"(ok)
+      : "r"(tc::smem_u32(b)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
 // a bounded wait; once one has given up, the others do not wait either
 __device__ __forceinline__ void wait(Control& c, uint64_t* b, uint32_t parity) {
   if (tc::mbar_try_wait(b, parity)) return;
@@ -261,7 +275,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
   const pe_kv_cache& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  const uint32_t qs = tc::smem_u32(smem), ring = qs + S::kQBytes;
+  const uint32_t qs = tc::smem_u32(smem), ring = qs + S::kQs * S::kQBytes;
   const int G = a.n_q_heads / c.n_heads, R = a.n_nodes * G, B = c.n_seqs;
 
   if (warp == 8) tc::tmem_alloc(&ctl.tmem, 512);
@@ -269,12 +283,16 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     for (int i = 0; i < 8; ++i) {
       tc::mbar_init(&ctl.full[i], E8 ? S::kProducers : 32 * S::kProducers);
       tc::mbar_init(&ctl.empty[i], 1);
-      tc::mbar_init(&ctl.info[i], S::kProducers);
     }
-    tc::mbar_init(&ctl.q_full, S::kProducers);
-    tc::mbar_init(&ctl.q_empty, 1);
+    for (int i = 0; i < kInfos; ++i) tc::mbar_init(&ctl.info[i], 1);
+    for (int i = 0; i < 4; ++i) {
+      tc::mbar_init(&ctl.placed[i], 1);
+      tc::mbar_init(&ctl.taken[i], S::kProducers);
+    }
     tc::mbar_init(&ctl.fin, 1);
     for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(&ctl.q_full[i], E8 ? S::kProducers : 32 * S::kProducers);
+      tc::mbar_init(&ctl.q_empty[i], 1);
       tc::mbar_init(&ctl.s_full[i], 1);
       tc::mbar_init(&ctl.p_full[i], WIDE ? 4 : 8);
       tc::mbar_init(&ctl.pv_done[i], 1);
@@ -349,6 +367,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     // nothing to do
   } else if (warp < 8) {
     // ================================================== softmax
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");  // 256 threads of 160 and 256 of 96: what 512 of 128 had
     const int wg = warp >> 2, row = (warp & 3) * 32 + lane;  // row of the tile, lane of TMEM
     const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const float qlog = fabsf(a.scale) * 1.4426950408889634f;
@@ -386,129 +405,104 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         tc::fence_after();
         if (E8 && t == 0) qf = ctl.qf[w.index & 3][(WIDE ? wg * 128 : 0) + row];
         const float ev = E8 ? f.ev : 0.0f;
-        const float cf = E8 ? qlog * qf * exp2f(f.ek) : qlog;
+        // (a scale of 0 as the least there is: what is masked stays -inf)
+        const float cf = fmaxf(E8 ? qlog * qf * exp2f(f.ek) : qlog, 1e-37f);
         if (warp_live) {
           const uint32_t sc = lanes + S::kS + buf * S::kSStep + (WIDE ? 0 : wg * S::kCols);
           const uint32_t pc = lanes + S::kP + buf * S::kPStep + (WIDE ? 0 : wg * S::kCols / 2);
           const bool whole = f.p0 >= lo_hi && f.p0 + kKeys <= f.n && (f.valid[0] & f.valid[1] & f.valid[2] & f.valid[3]) == 0xffffffffu;
-          auto tile = [&](auto masked) {
-            constexpr bool kMasked = decltype(masked)::value;
-            constexpr int kChunks32 = S::kCols / 32, kHeld = WIDE ? (kMasked ? 1 : 2) : kChunks32;  // chunks of columns; of those in registers
-            uint32_t keep[kChunks32];
-            if (kMasked) {
+          // 64 columns at a time (head_dim 256: 32); code is kept short, for the roles share the instruction cache
+          constexpr int kHalves = S::kCols >= 64 ? 2 : 1, kTurns = S::kCols / (32 * kHalves);
+          uint32_t keep[S::kCols / 32];
+          if (!whole) {
 #pragma unroll
-              for (int i = 0; i < kChunks32; ++i) {
-                const int at = i + (WIDE ? 0 : wg * kChunks32), pw = f.p0 + 32 * at;
-                const int below = min(max(f.n - pw, 0), 32), skip = min(max(row_lo - pw, 0), 32);
-                uint32_t ctx = below == 32 ? 0xffffffffu : (1u << below) - 1;
-                ctx &= skip == 32 ? 0u : 0xffffffffu << skip;
-                const int sh = pw - f.n;
-                const uint32_t nodes = sh >= 64 || sh <= -32 ? 0u : sh >= 0 ? (uint32_t)(bits >> sh) : (uint32_t)(bits << -sh);
-                keep[i] = live ? f.valid[at] & (ctx | nodes) : 0u;
+            for (int i = 0; i < S::kCols / 32; ++i) {
+              const int at = i + (WIDE ? 0 : wg * (S::kCols / 32)), pw = f.p0 + 32 * at;
+              const int below = min(max(f.n - pw, 0), 32), skip = min(max(row_lo - pw, 0), 32);
+              uint32_t ctx = below == 32 ? 0xffffffffu : (1u << below) - 1;
+              ctx &= skip == 32 ? 0u : 0xffffffffu << skip;
+              const int sh = pw - f.n;
+              const uint32_t nodes = sh >= 64 || sh <= -32 ? 0u : sh >= 0 ? (uint32_t)(bits >> sh) : (uint32_t)(bits << -sh);
+              keep[i] = live ? f.valid[at] & (ctx | nodes) : 0u;
+            }
+          }
+          float v[kHalves][32];
+          auto fetch = [&](int turn) {
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) ld32(sc + 64 * turn + 32 * h, v[h]);
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) ld_wait(v[h]);
+            if (!whole) {
+#pragma unroll
+              for (int h = 0; h < kHalves; ++h) {
+                const uint32_t k = kTurns == 1 ? keep[h] : turn ? keep[(kTurns - 1) * kHalves + h] : keep[h];
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[h][j] = (k >> j) & 1 ? v[h][j] : -CUDART_INF_F;
               }
             }
-            // the row's largest score
-            float v[kHeld][32];
-            float top = -CUDART_INF_F, top2 = -CUDART_INF_F;
-            auto largest = [&](float (&x)[32], int i) {
-              if (kMasked) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j) x[j] = (keep[i] >> j) & 1 ? x[j] : -CUDART_INF_F;
-              }
-#pragma unroll
-              for (int j = 0; j < 32; j += 4) {
-                top = fmaxf(top, fmaxf(x[j], x[j + 1]));
-                top2 = fmaxf(top2, fmaxf(x[j + 2], x[j + 3]));
-              }
-            };
-            if constexpr (!WIDE) {
-#pragma unroll
-              for (int i = 0; i < kChunks32; ++i) ld32(sc + 32 * i, v[i]);
-#pragma unroll
-              for (int i = 0; i < kChunks32; ++i) {
-                ld_wait(v[i]);
-                largest(v[i], i);
-              }
-            } else {
-              ld32(sc, v[0]);
-#pragma unroll
-              for (int i = 0; i < kChunks32; ++i) {
-                ld_wait(v[i % kHeld]);
-                const uint32_t next = sc + 32 * (i + 1 < kChunks32 ? i + 1 : 0);  // at last the first again
-                if (kHeld == 2) ld32(next, v[(i + 1) % kHeld]);
-                largest(v[i % kHeld], i);
-                if (kHeld == 1) ld32(next, v[0]);
-              }
-            }
-            top = fmaxf(top, top2);
-            if (!WIDE) {
-              ctl.mx[ip & 1][wg][row] = top;
-              bar_sync(1 + (warp & 3), 64);
-              top = fmaxf(top, ctl.mx[ip & 1][wg ^ 1][row]);
-            }
-            top = top == -CUDART_INF_F ? top : fmaf(top, cf, ev);
-            const bool over = top > m + 8.0f;
-            if (__any_sync(0xffffffffu, over)) {
-              const float x = over ? top : m;
-              const float fr = over ? (m == -CUDART_INF_F ? 0.0f : exp2_fast(m - x)) : 1.0f;
-              m = x;
-              l *= fr;
-              if (t > 0) {
-                if (!WIDE) wait(ctl, &ctl.pv_done[0], (pp[0] - 1) & 1);  // the last product into the output
-                __syncwarp();
-                tc::fence_after();
-                const uint32_t oc = lanes + S::kO + (WIDE ? wg * S::kOStep : wg * (D / 2));
+          };
+          // the row's largest score
+          float top = -CUDART_INF_F;
 #pragma unroll 1
-                for (int i = 0; i < (WIDE ? D : D / 2) / 16; ++i) {
-                  float o[16];
-                  tc::tmem_ld16(oc + 16 * i, o);
-                  uint32_t r[16];
+          for (int turn = 0; turn < kTurns; ++turn) {
+            fetch(turn);
+            float most[4] = {top, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
-                  for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(o[j] * fr);
-                  st16(oc + 16 * i, r);
-                }
+            for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+              for (int j = 0; j < 32; j += 8)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) most[i] = fmaxf(most[i], fmaxf(v[h][j + 2 * i], v[h][j + 2 * i + 1]));
+            top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+          }
+          if (!WIDE) {
+            ctl.mx[ip & 1][wg][row] = top;
+            bar_sync(1 + (warp & 3), 64);
+            top = fmaxf(top, ctl.mx[ip & 1][wg ^ 1][row]);
+          }
+          top = top == -CUDART_INF_F ? top : fmaf(top, cf, ev);
+          const bool over = top > m + 8.0f;
+          if (__any_sync(0xffffffffu, over)) {
+            const float x = over ? top : m;
+            const float fr = over ? (m == -CUDART_INF_F ? 0.0f : exp2_fast(m - x)) : 1.0f;
+            m = x;
+            l *= fr;
+            if (t > 0) {
+              if (!WIDE) wait(ctl, &ctl.pv_done[0], (pp[0] - 1) & 1);  // the last product into the output
+              __syncwarp();
+              tc::fence_after();
+              const uint32_t oc = lanes + S::kO + (WIDE ? wg * S::kOStep : wg * (D / 2));
+#pragma unroll 1
+              for (int i = 0; i < (WIDE ? D : D / 2) / 16; ++i) {
+                float o[16];
+                tc::tmem_ld16(oc + 16 * i, o);
+                uint32_t r[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(o[j] * fr);
+                st16(oc + 16 * i, r);
               }
             }
-            const float off = ev + Weights<M>::kBias - (m == -CUDART_INF_F ? 0.0f : m);
-            const float2 cf2 = make_float2(cf, cf), off2 = make_float2(off, off);
-            float2 part = make_float2(0.0f, 0.0f);
-            auto weights = [&](float (&x)[32], int i) {
+          }
+          const float off = ev + Weights<M>::kBias - (m == -CUDART_INF_F ? 0.0f : m);
+          const float2 cf2 = make_float2(cf, cf), off2 = make_float2(off, off);
+          float2 part = make_float2(0.0f, 0.0f);
+#pragma unroll 1
+          for (int turn = 0; turn < kTurns; ++turn) {
+            if (kTurns > 1) fetch(turn);
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
               uint32_t pk[16];
 #pragma unroll
               for (int j = 0; j < 32; j += 2) {
-                const float2 e = __ffma2_rn(make_float2(x[j], x[j + 1]), cf2, off2);
-                float2 p = make_float2(exp2_fast(e.x), exp2_fast(e.y));
-                if (kMasked) {
-                  p.x = (keep[i] >> j) & 1 ? p.x : 0.0f;
-                  p.y = (keep[i] >> (j + 1)) & 1 ? p.y : 0.0f;
-                }
+                const float2 e = __ffma2_rn(make_float2(v[h][j], v[h][j + 1]), cf2, off2);
+                const float2 p = make_float2(exp2_fast(e.x), exp2_fast(e.y));
                 part = __fadd2_rn(part, p);
                 pk[j / 2] = pack2<M>(p.x, p.y);
               }
-              st16(pc + 16 * i, pk);
-            };
-            if constexpr (!WIDE) {
-#pragma unroll
-              for (int i = 0; i < kChunks32; ++i) weights(v[i], i);
-            } else {
-#pragma unroll
-              for (int i = 0; i < kChunks32; ++i) {
-                ld_wait(v[i % kHeld]);
-                if (kHeld == 2 && i + 1 < kChunks32) ld32(sc + 32 * (i + 1), v[(i + 1) % kHeld]);
-                if (kMasked) {
-#pragma unroll
-                  for (int j = 0; j < 32; ++j) v[i % kHeld][j] = (keep[i] >> j) & 1 ? v[i % kHeld][j] : -CUDART_INF_F;
-                }
-                weights(v[i % kHeld], i);
-                if (kHeld == 1 && i + 1 < kChunks32) ld32(sc + 32 * (i + 1), v[0]);
-              }
+              st16(pc + 32 * turn + 16 * h, pk);
             }
-            l = E8 ? fmaf(part.x + part.y, exp2f(-ev), l) : l + (part.x + part.y);
-          };
-          if (whole)
-            tile(std::false_type{});
-          else
-            tile(std::true_type{});
+          }
+          l = E8 ? fmaf(part.x + part.y, exp2f(-ev), l) : l + (part.x + part.y);
           st_wait();
         } else if (!WIDE) {
           bar_sync(1 + (warp & 3), 64);
@@ -532,8 +526,8 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       }
       if (warp_live) {
         const bool whole = w.ct == 0 && w.cnt == s.nt;
-        const uint64_t bad_node = ctl.bad[w.index & 7][0] & bits;
-        uint64_t bad_pos = ctl.bad[w.index & 7][1];
+        const uint64_t bad_node = ctl.bad[w.index & 15][0] & bits;
+        uint64_t bad_pos = ctl.bad[w.index & 15][1];
         if (row_lo > s.lo) bad_pos &= row_lo - s.lo >= 64 ? 0 : 0xffffffffffffffffull << (row_lo - s.lo);
         const bool spoilt = live && (bad_node | bad_pos) != 0;
         constexpr int kMine = WIDE ? D : D / 2;  // elements of the thread
@@ -545,42 +539,74 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         const int64_t slot = 2 * (int64_t)blockIdx.x + (w.index > 0 ? 1 : 0);
         float* piece = g.part + slot * S::kRows * (D + 2);
         const int prow = (WIDE ? wg * 128 : 0) + row;
-        float v[32];
+        // 16-byte parts of a row change lanes, so that eight lanes store 128 bytes of a row together
+        char* to = whole ? reinterpret_cast<char*>(out) : reinterpret_cast<char*>(piece + (int64_t)prow * D + d0);
+        const int per = whole ? (kMine >= 64 ? 64 : 32) : 32;  // elements of a turn
 #pragma unroll 1
-        for (int i = 0; i < kMine / 32; ++i) {
-          ld32(oc + 32 * i, v);
-          ld_wait(v);
-          if (spoilt) {  // an attended value that is not finite makes its element NaN
+        for (int i = 0; i < kMine; i += per) {
+          uint4 u[8];
+          float v[32];
+          auto take = [&](int d) {
+            ld32(oc + d, v);
+            ld_wait(v);
+            if (spoilt) {  // an attended value that is not finite makes its element NaN
 #pragma unroll 1
-            for (int k = 0; k < 128; ++k) {
-              if (!((k < 64 ? bad_node >> k : bad_pos >> (k - 64)) & 1)) continue;
-              const int p = k < 64 ? s.n + k : s.lo + k - 64;
-              const int page = c.table[(int64_t)s.b * c.table_stride + p / c.page_size], sl = p % c.page_size;
-              const int64_t at = kv_page_offset(c, page) + (int64_t)sl * c.slot_stride + hk * c.head_stride + d0 + 32 * i;
-              const bool row_bad = E8 && a.sc.v[page * a.sc.page_stride + (int64_t)sl * a.sc.slot_stride + hk * a.sc.head_stride] == 255;
+              for (int k = 0; k < 128; ++k) {
+                if (!((k < 64 ? bad_node >> k : bad_pos >> (k - 64)) & 1)) continue;
+                const int p = k < 64 ? s.n + k : s.lo + k - 64;
+                const int page = c.table[(int64_t)s.b * c.table_stride + p / c.page_size], sl = p % c.page_size;
+                const int64_t at = kv_page_offset(c, page) + (int64_t)sl * c.slot_stride + hk * c.head_stride + d0 + d;
+                const bool row_bad = E8 && a.sc.v[page * a.sc.page_stride + (int64_t)sl * a.sc.slot_stride + hk * a.sc.head_stride] == 255;
 #pragma unroll
-              for (int j = 0; j < 32; ++j) {
-                const bool x = E8 ? row_bad || (((const uint8_t*)c.v)[at + j] & 0x7f) == 0x7f : not_finite<T>(((const uint16_t*)c.v)[at + j], 0);
-                if (x) v[j] = CUDART_NAN_F;
+                for (int j = 0; j < 32; ++j) {
+                  const bool x = E8 ? row_bad || (((const uint8_t*)c.v)[at + j] & 0x7f) == 0x7f : not_finite<T>(((const uint16_t*)c.v)[at + j], 0);
+                  if (x) v[j] = CUDART_NAN_F;
+                }
               }
             }
-          }
-          if (exists && whole) {
+            __syncwarp();
+          };
+          if (whole) {
 #pragma unroll
-            for (int j = 0; j < 32; j += 8) {
-              uint4 o;
-              o.x = pack2<T>(v[j] * inv, v[j + 1] * inv), o.y = pack2<T>(v[j + 2] * inv, v[j + 3] * inv);
-              o.z = pack2<T>(v[j + 4] * inv, v[j + 5] * inv), o.w = pack2<T>(v[j + 6] * inv, v[j + 7] * inv);
-              if (l == 0.0f) o = make_uint4(0, 0, 0, 0);  // nothing attended to, whatever the values are
-              *reinterpret_cast<uint4*>(out + 32 * i + j) = o;
+            for (int h = 0; h < (kMine >= 64 ? 2 : 1); ++h) {
+              take(i + 32 * h);
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                u[4 * h + j] = make_uint4(pack2<T>(v[8 * j] * inv, v[8 * j + 1] * inv), pack2<T>(v[8 * j + 2] * inv, v[8 * j + 3] * inv),
+                                          pack2<T>(v[8 * j + 4] * inv, v[8 * j + 5] * inv), pack2<T>(v[8 * j + 6] * inv, v[8 * j + 7] * inv));
             }
-          } else if (exists) {
-            float* to = piece + (int64_t)prow * D + d0 + 32 * i;
+          } else {
+            take(i);
 #pragma unroll
-            for (int j = 0; j < 32; j += 4)
-              *reinterpret_cast<float4*>(to + j) = l == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            for (int j = 0; j < 8; ++j)
+              u[j] = make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3]));
           }
-          __syncwarp();
+          if (l == 0.0f)  // nothing attended to, whatever the values are
+#pragma unroll
+            for (int j = 0; j < 8; ++j) u[j] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+          for (int x = 1; x < 8; x *= 2)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              if (j & x) continue;
+              const bool up = lane & x;
+              uint4 send = up ? u[j] : u[j + x];
+              send.x = __shfl_xor_sync(0xffffffffu, send.x, x), send.y = __shfl_xor_sync(0xffffffffu, send.y, x);
+              send.z = __shfl_xor_sync(0xffffffffu, send.z, x), send.w = __shfl_xor_sync(0xffffffffu, send.w, x);
+              if (up)
+                u[j] = send;
+              else
+                u[j + x] = send;
+            }
+          const uint32_t there = __ballot_sync(0xffffffffu, exists);
+          const bool mine = !whole || kMine >= 64 || (lane & 7) < 4;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int from = (lane & 24) | j;
+            char* p = reinterpret_cast<char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(to), from));
+            if (((there >> from) & 1) && mine) *reinterpret_cast<uint4*>(p + 16 * (lane & 7)) = u[j];
+          }
+          to += whole ? per * 2 : per * 4;
         }
         if (exists && (WIDE || wg == 0)) {
           if (whole) {
@@ -593,88 +619,172 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       }
       tc::fence_before();
     } while (w.next());
-  } else if (warp == 8) {
+  } else if (warp < 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+    if (warp == 9) {
+    // ================================================== places
+      // a lane finds the places of rows lane, lane + 32, ... and, of codes, what brings their scales
+      // to the tile's largest: pages two tiles ahead, scales one
+      constexpr int kMine = kKeys / 32;
+      Walk<kKeys> nx(g, ctl.where, tiles);  // one tile ahead
+      int nt = 0;
+      bool more = true;
+      int page[kMine], kb[kMine], vb[kMine];
+      auto look = [&]() {
+#pragma unroll
+        for (int j = 0; j < kMine; ++j) {
+          const int p = nx.s.base + (nx.ct + nt) * kKeys + lane + 32 * j;
+          page[j] = -1;
+          if (more && p >= nx.s.lo && p < nx.s.end) {
+            page[j] = c.table[(int64_t)nx.s.b * c.table_stride + (g.page_shift >= 0 ? p >> g.page_shift : p / c.page_size)];
+            if (page[j] >= c.n_pages) page[j] = -1;
+          }
+        }
+      };
+      // places of tile x, whose pages have been looked up
+      auto place = [&](uint32_t x) {
+        if (!more) return;
+        if (x >= 4) wait(ctl, &ctl.taken[x & 3], ((x >> 2) - 1) & 1);
+        __syncwarp();
+        const int hk = nx.s.grp / g.blocks, p0 = nx.s.base + (nx.ct + nt) * kKeys;
+        Info& f = ctl.tile[x % kInfos];
+#pragma unroll
+        for (int j = 0; j < kMine; ++j) {
+          const int p = p0 + lane + 32 * j, sl = g.page_shift >= 0 ? p & (c.page_size - 1) : p % c.page_size;
+          const bool ok = page[j] >= 0;
+          ctl.off[x & 3][lane + 32 * j] = ok ? kv_page_offset(c, page[j]) + (int64_t)sl * c.slot_stride + hk * c.head_stride : -1;
+          if (E8) {
+            kb[j] = vb[j] = -1;
+            if (ok) {
+              const int64_t so = page[j] * a.sc.page_stride + (int64_t)sl * a.sc.slot_stride + hk * a.sc.head_stride;
+              kb[j] = a.sc.k[so];
+              vb[j] = a.sc.v[so];
+            }
+          }
+          const uint32_t word = __ballot_sync(0xffffffffu, ok);
+          if (lane == j) f.valid[j] = word;
+        }
+        if (lane >= kMine && lane < 4) f.valid[lane] = 0xffffffffu;
+        if (lane == 0) {
+          f.p0 = p0, f.n = nx.s.n, f.lo = nx.s.lo;
+          const bool differ = a.mask && (p0 + kKeys > nx.s.n || (a.window > 0 && p0 < nx.s.lo + 64));
+          f.flags = differ ? 1 | (nx.index & 15) << 1 : 0;
+          if (nt == 0) ctl.bad[nx.index & 15][0] = ctl.bad[nx.index & 15][1] = 0;
+        }
+        if (++nt == nx.cnt) {
+          nt = 0;
+          more = nx.next();
+        }
+      };
+      look();
+      place(0);
+      look();
+      for (uint32_t x = 0; x < (uint32_t)tiles; ++x) {
+        int own[2][kMine];
+#pragma unroll
+        for (int j = 0; j < kMine; ++j) own[0][j] = kb[j], own[1][j] = vb[j];
+        if (E8) {
+          Info& f = ctl.tile[x % kInfos];
+          // bytes in [63, 247]; 255 takes no part in the largest
+          auto fit = [](int b) { return b < 0 || b == 255 ? -1 : min(max(b, 63), 247); };
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            int big = -1;
+#pragma unroll
+            for (int j = 0; j < kMine; ++j) big = max(big, fit(own[i][j]));
+            big = __reduce_max_sync(0xffffffffu, big);
+            if (big < 0) big = 127;
+#pragma unroll
+            for (int j = 0; j < kMine; ++j) {
+              const int b = own[i][j], d = fit(b) - big;  // at most 0; a factor below 2^-24 is 0
+              const uint32_t h = b < 0 ? 0u : b == 255 ? 0x7e00u : d >= -14 ? (uint32_t)(15 + d) << 10 : d >= -24 ? 1u << (24 + d) : 0u;
+              ctl.fac[x & 3][i][lane + 32 * j] = h | h << 16;
+            }
+            if (lane == 0) (i ? f.ev : f.ek) = (float)(big - 127);
+          }
+        }
+        __syncwarp();
+        if (lane == 0) {
+          tc::mbar_arrive(&ctl.info[x % kInfos]);
+          tc::mbar_arrive(&ctl.placed[x & 3]);
+        }
+        place(x + 1);
+        look();
+      }
+    }
+    if (warp == 8) {
     // ================================================== products
     if (lane == 0) {
-      constexpr uint32_t kIdS = idesc<M>(128, kKeys, 0), kIdO = idesc<M>(128, D, 1);
-      uint32_t fe = 0, pf[2] = {0, 0}, qi = 0;  // next ring entry to see; phases of the weights; of the queries
+      // queries with their sign where the scale is negative
+      const uint32_t kIdS = idesc<M>(128, kKeys, 0) | (!E8 && a.scale < 0.0f ? 1u << 13 : 0u), kIdO = idesc<M>(128, D, 1);
       auto entry = [&](uint32_t e) { return ring + (e % kEntries) * S::kEntry; };
-      auto seen = [&](uint32_t e) {  // entries come in order
-        while (fe <= e) {
-          wait(ctl, &ctl.full[fe % kEntries], (fe / kEntries) & 1);
-          ++fe;
-        }
+      auto landed = [&](uint32_t e) {
+        if (!mbar_test(&ctl.full[e % kEntries], (e / kEntries) & 1)) return false;
         // copies write as ordinary stores do, products read through the asynchronous proxy
         if (!E8) tc::fence_async_smem();
-        tc::fence_after();
+        return true;
       };
-      auto qk = [&](uint32_t e, int rt, int buf) {
-#pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk)
-          tc::mma_bf16(tmem + S::kS + buf * S::kSStep,
-                       tc::desc_kmajor(qs + rt * 128 * 128 * (D / 64) + (kk >> 2) * 128 * 128 + (kk & 3) * 32, 1024, tc::kLayoutSW128),
-                       tc::desc_kmajor(entry(e) + (kk >> 2) * kKeys * 128 + (kk & 3) * 32, 1024, tc::kLayoutSW128), kIdS, kk > 0);
-        tc::mma_commit(&ctl.s_full[buf]);
-      };
-      auto pv = [&](uint32_t e, int rt, int buf, bool first) {
-        wait(ctl, &ctl.p_full[buf], pf[buf] & 1);
-        ++pf[buf];
-        tc::fence_after();
-#pragma unroll
-        for (int kk = 0; kk < kKeys / 16; ++kk)
-          mma_ts(tmem + S::kO + rt * S::kOStep, tmem + S::kP + buf * S::kPStep + 8 * kk,
-                 tc::desc_strided(entry(e) + kk * 2048, kKeys * 128, 1024, tc::kLayoutSW128), kIdO, !(first && kk == 0));
-        tc::mma_commit(&ctl.pv_done[rt]);
-      };
-      uint32_t e0 = 0;  // entry of the segment's first keys
+      uint32_t ps[2] = {0, 0};  // phases of the weights
+      uint32_t e0 = 0;          // entry of the segment's first keys
       Walk<kKeys> w(g, ctl.where, tiles);
       do {
         const int rows = min(R - w.s.grp % g.blocks * S::kRows, S::kRows), nt = w.cnt;
-        wait(ctl, &ctl.q_full, qi & 1);
-        ++qi;
-        if (WIDE) {
-          const bool both = rows > 128;
-          seen(e0);
-          qk(e0, 0, 0);
-          if (both) qk(e0, 1, 1);
-          tc::mma_commit(&ctl.empty[e0 % kEntries]);
-          if (nt == 1) tc::mma_commit(&ctl.q_empty);
-          for (int t = 0; t < nt; ++t) {
-            const uint32_t ke = e0 + 2 * t + 2, ve = e0 + 2 * t + 1;
-            seen(ve);
-            pv(ve, 0, 0, t == 0);
-            if (!both) tc::mma_commit(&ctl.empty[ve % kEntries]);
-            if (t + 1 < nt) {
-              seen(ke);
-              qk(ke, 0, 0);
+        const int tracks = WIDE && rows > 128 ? 2 : 1;  // of rows with products of their own
+        const int qb = w.index % S::kQs;
+        wait(ctl, &ctl.q_full[qb], (w.index / S::kQs) & 1);
+        if (!E8) tc::fence_async_smem();
+        int nk[2] = {0, 0}, np[2] = {0, 0}, kseen = 0, vseen = 0;  // tiles whose scores, outputs are under way; that have landed
+        long long t0 = clock64();
+        while (np[0] < nt || (tracks == 2 && np[1] < nt)) {
+          bool any = false;
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            if (x >= tracks) break;
+            // scores two tiles ahead of the outputs (narrow), or one
+            if (nk[x] < nt && nk[x] < np[x] + (WIDE ? 1 : 2)) {
+              const int t = nk[x];
+              const uint32_t e = e0 + 2 * t;
+              if (kseen > t || landed(e)) {
+                kseen = max(kseen, t + 1);
+                const int buf = WIDE ? x : t & 1;
+                tc::fence_after();
+#pragma unroll 2
+                for (int kk = 0; kk < D / 16; ++kk)
+                  tc::mma_bf16(tmem + S::kS + buf * S::kSStep,
+                               tc::desc_kmajor(qs + qb * S::kQBytes + x * 128 * 128 * (D / 64) + (kk >> 2) * 128 * 128 + (kk & 3) * 32, 1024, tc::kLayoutSW128),
+                               tc::desc_kmajor(entry(e) + (kk >> 2) * kKeys * 128 + (kk & 3) * 32, 1024, tc::kLayoutSW128), kIdS, kk > 0);
+                tc::mma_commit(&ctl.s_full[buf]);
+                ++nk[x];
+                if (tracks == 1 || nk[x ^ 1] >= nk[x]) {
+                  tc::mma_commit(&ctl.empty[e % kEntries]);
+                  if (nk[x] == nt) tc::mma_commit(&ctl.q_empty[qb]);
+                }
+                any = true;
+              }
             }
-            if (both) {
-              pv(ve, 1, 1, t == 0);
-              tc::mma_commit(&ctl.empty[ve % kEntries]);
-              if (t + 1 < nt) qk(ke, 1, 1);
+            if (np[x] < nk[x]) {
+              const int t = np[x], buf = WIDE ? x : t & 1;
+              const uint32_t e = e0 + 2 * t + 1;
+              if (mbar_test(&ctl.p_full[buf], ps[buf] & 1) && (vseen > t || landed(e))) {
+                vseen = max(vseen, t + 1);
+                ++ps[buf];
+                tc::fence_after();
+#pragma unroll 2
+                for (int kk = 0; kk < kKeys / 16; ++kk)
+                  mma_ts(tmem + S::kO + x * S::kOStep, tmem + S::kP + buf * S::kPStep + 8 * kk,
+                         tc::desc_strided(entry(e) + kk * 2048, kKeys * 128, 1024, tc::kLayoutSW128), kIdO, !(t == 0 && kk == 0));
+                tc::mma_commit(&ctl.pv_done[x]);
+                ++np[x];
+                if (tracks == 1 || np[x ^ 1] >= np[x]) tc::mma_commit(&ctl.empty[e % kEntries]);
+                any = true;
+              }
             }
-            if (t + 1 < nt) tc::mma_commit(&ctl.empty[ke % kEntries]);
-            if (t + 2 == nt) tc::mma_commit(&ctl.q_empty);
           }
-        } else {
-          for (int t = 0; t < min(nt, 2); ++t) {
-            const uint32_t ke = e0 + 2 * t;
-            seen(ke);
-            qk(ke, 0, t);
-            tc::mma_commit(&ctl.empty[ke % kEntries]);
-          }
-          if (nt <= 2) tc::mma_commit(&ctl.q_empty);
-          for (int t = 0; t < nt; ++t) {
-            const uint32_t ve = e0 + 2 * t + 1, ke = e0 + 2 * t + 4;
-            seen(ve);
-            pv(ve, 0, t & 1, t == 0);
-            tc::mma_commit(&ctl.empty[ve % kEntries]);
-            if (t + 2 < nt) {
-              seen(ke);
-              qk(ke, 0, t & 1);
-              tc::mma_commit(&ctl.empty[ke % kEntries]);
-              if (t + 3 == nt) tc::mma_commit(&ctl.q_empty);
-            }
+          if (any) {
+            t0 = clock64();
+          } else if (clock64() - t0 > 4000000000LL || *(volatile int*)&ctl.err) {
+            atomicExch(&ctl.err, 1);
+            break;
           }
         }
         e0 += 2 * nt;
@@ -682,11 +792,12 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       tc::mma_commit(&ctl.fin);
       if (!tc::mbar_wait(&ctl.fin, 0)) atomicExch(&ctl.err, 1);
     }
+    }
   } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
     // ================================================== producers
     constexpr int kN = 32 * S::kProducers;
-    const int pt = tid - 32 * 9;
-    auto sync = [&]() { bar_sync(5, kN); };
+    const int pt = tid - 384;
     auto arrive = [&](uint64_t* b) {
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(b);
@@ -695,25 +806,34 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     auto load_q = [&](const Walk<kKeys>& w) {
       const Seg& s = w.s;
       const int hk = s.grp / g.blocks, r0 = s.grp % g.blocks * S::kRows, rows = min(R - r0, S::kRows);
-      if (w.index > 0) wait(ctl, &ctl.q_empty, (w.index - 1) & 1);
+      const int qb = w.index % S::kQs;
+      if (w.index >= S::kQs) wait(ctl, &ctl.q_empty[qb], (w.index / S::kQs - 1) & 1);
+      __syncwarp();
       const T* q = (const T*)a.q + s.b * a.q_seq + (int64_t)hk * G * a.q_head;
       constexpr int kStep = kN / kChunks;
       const int ch = pt % kChunks;
+      auto row_of = [&](int r) { return q + ((r0 + r) / G) * a.q_node + ((r0 + r) % G) * a.q_head + ch * 8; };
+      auto place = [&](int r) { return qb * S::kQBytes + (r >> 7) * (128 * 128 * (D / 64)) + chunk_at(r & 127, ch, 128); };
+      if constexpr (!E8) {
+#pragma unroll 4
+        for (int r = pt / kChunks; r < rows; r += kStep) copy16(qs + place(r), row_of(r), true);
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tc::smem_u32(&ctl.q_full[qb])) : "memory");
+      } else {
+        constexpr int kAtOnce = 4;
 #pragma unroll 1
-      for (int r1 = 0; r1 < rows; r1 += 4 * kStep) {
-        uint4 x[4];
+        for (int r1 = 0; r1 < rows; r1 += kAtOnce * kStep) {
+          uint4 x[kAtOnce];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int r = r1 + pt / kChunks + u * kStep, rr = r0 + r;
-          x[u] = make_uint4(0, 0, 0, 0);
-          if (r < rows) x[u] = *reinterpret_cast<const uint4*>(q + (rr / G) * a.q_node + (rr % G) * a.q_head + ch * 8);
-        }
+          for (int u = 0; u < kAtOnce; ++u) {
+            const int r = r1 + pt / kChunks + u * kStep;
+            x[u] = make_uint4(0, 0, 0, 0);
+            if (r < rows) x[u] = *reinterpret_cast<const uint4*>(row_of(r));
+          }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int r = r1 + pt / kChunks + u * kStep;
-          uint32_t* y = reinterpret_cast<uint32_t*>(&x[u]);
-          if (E8) {
-            // fp16 with the row's largest in [2^14, 2^15)
+          for (int u = 0; u < kAtOnce; ++u) {
+            const int r = r1 + pt / kChunks + u * kStep;
+            uint32_t* y = reinterpret_cast<uint32_t*>(&x[u]);
+            // fp16 with the row's largest in [2^14, 2^15), and the scale's sign
             uint32_t most = 0;
             float2 f[4];
 #pragma unroll
@@ -722,32 +842,22 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
               most = max(most, max(__float_as_uint(f[i].x) & 0x7fffffffu, __float_as_uint(f[i].y) & 0x7fffffffu));
             }
 #pragma unroll
-            for (int x = 1; x < kChunks; x *= 2) most = max(most, __shfl_xor_sync(0xffffffffu, most, x));
+            for (int i = 1; i < kChunks; i *= 2) most = max(most, __shfl_xor_sync(0xffffffffu, most, i));
             const int ex = (int)(most >> 23);
             const int up = ex == 255 || most == 0 ? 127 : min(268 - ex, 253);  // exponent field of the factor
-            const float fac = __uint_as_float((uint32_t)up << 23);
+            const float fac = copysignf(__uint_as_float((uint32_t)up << 23), a.scale);
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[i] = pack2<__half>(f[i].x * fac, f[i].y * fac);
-            if (ch == 0 && r < rows) ctl.qf[w.index & 3][r] = __uint_as_float((uint32_t)(254 - up) << 23);
+            if (r < rows) {
+              if (ch == 0) ctl.qf[w.index & 3][r] = __uint_as_float((uint32_t)(254 - up) << 23);
+              *reinterpret_cast<uint4*>(smem + place(r)) = x[u];
+            }
           }
-          if (a.scale < 0.0f)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] ^= 0x80008000u;
-          if (r < rows)
-            *reinterpret_cast<uint4*>(smem + (r >> 7) * (128 * 128 * (D / 64)) + chunk_at(r & 127, ch, 128)) = x[u];
         }
+        tc::fence_async_smem();
+        arrive(&ctl.q_full[qb]);
       }
-      tc::fence_async_smem();
-      arrive(&ctl.q_full);
     };
-    // the page of position p of the sequence, or -1
-    auto page_of = [&](const Seg& s, int p) {
-      if (p < s.lo || p >= s.end) return -1;
-      const int i = g.page_shift >= 0 ? p >> g.page_shift : p / c.page_size;
-      const int page = c.table[(int64_t)s.b * c.table_stride + i];
-      return page >= 0 && page < c.n_pages ? page : -1;
-    };
-    auto slot_of = [&](int p) { return g.page_shift >= 0 ? p & (c.page_size - 1) : p % c.page_size; };
     // bits of the values that rows attend to differently: (nodes, positions from lo on)
     auto apart = [&](const Info& f, int r, int& which) -> uint64_t {
       const int p = f.p0 + r, node = p - f.n;
@@ -758,9 +868,10 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     };
     Walk<kKeys> w(g, ctl.where, tiles);
     uint32_t tile = 0;  // tiles behind
-    const int orow = pt % 128;  // the row whose place the thread finds
-    const bool owner = orow < kKeys && pt < 128;
-    int64_t my_off = -1;
+    auto placed = [&](uint32_t x) {
+      wait(ctl, &ctl.placed[x & 3], (x >> 2) & 1);
+      __syncwarp();
+    };
 
     if constexpr (!E8) {
       constexpr int kPass = kN / kChunks;  // rows of a pass
@@ -768,7 +879,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       uint32_t issued = 0;
       // values that are not finite, where rows attend to them differently, become zeros and a mark
       auto spoils = [&](const Info& f) {
-        const uint32_t at = S::kQBytes + (issued % kEntries) * S::kEntry;
+        const uint32_t at = S::kQs * S::kQBytes + (issued % kEntries) * S::kEntry;
         unsigned long long* bad = ctl.bad[f.flags >> 1];
         asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll 1
@@ -791,35 +902,18 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           }
         }
       };
-      int page = owner ? page_of(w.s, w.s.base + w.ct * kKeys + orow) : -1;
       do {
-        const Seg& s = w.s;
-        const int hk = s.grp / g.blocks;
         for (int t = 0; t < w.cnt; ++t, ++tile) {
-          const int p0 = s.base + (w.ct + t) * kKeys;
-          const int64_t* offs = ctl.off[tile & 1];
-          Info& f = ctl.tile[tile % kInfos];
-          if (t == 0 && pt < 2) ctl.bad[w.index & 7][pt] = 0;
-          if (pt < 128) {
-            my_off = page < 0 ? -1 : kv_page_offset(c, page) + (int64_t)slot_of(p0 + orow) * c.slot_stride + hk * c.head_stride;
-            if (owner) ctl.off[tile & 1][orow] = my_off;
-            const uint32_t ok = __ballot_sync(0xffffffffu, my_off >= 0);
-            if (lane == 0) f.valid[pt / 32] = orow < kKeys ? ok : 0xffffffffu;
-            if (pt == 0) {
-              f.p0 = p0, f.n = s.n, f.lo = s.lo;
-              const bool differ = a.mask && (p0 + kKeys > s.n || (a.window > 0 && p0 < s.lo + 64));
-              f.flags = differ ? 1 | (w.index & 7) << 1 : 0;
-            }
-          }
-          sync();
-          arrive(&ctl.info[tile % kInfos]);
-          if (t + 1 < w.cnt && owner) page = page_of(s, p0 + kKeys + orow);
-#pragma unroll
+          if (S::kQs == 2 && t == 0) load_q(w);
+          placed(tile);
+          const int64_t* offs = ctl.off[tile & 3];
+          const Info& f = ctl.tile[tile % kInfos];
+#pragma unroll 1
           for (int kv = 0; kv < 2; ++kv) {
             if (issued >= kEntries) wait(ctl, &ctl.empty[issued % kEntries], (issued / kEntries - 1) & 1);
             const uint32_t dst = ring + (issued % kEntries) * S::kEntry;
             const T* src = (const T*)(kv ? c.v : c.k) + ch * 8;
-#pragma unroll 8
+#pragma unroll 4
             for (int i = 0; i < kKeys / kPass; ++i) {
               const int r = row0 + i * kPass;
               const int64_t o = offs[r];
@@ -835,13 +929,9 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             }
             ++issued;
           }
-          // the first tile is under way before the last segment's queries are done with
-          if (t == 0) load_q(w);
-        }
-        if (w.left > w.cnt && owner) {  // the next segment's first page
-          Walk<kKeys> x = w;
-          x.next();
-          page = page_of(x.s, x.s.base + orow);
+          arrive(&ctl.taken[tile & 3]);
+          // where queries have one place, the first tile is under way before the last segment's are done with
+          if (S::kQs == 1 && t == 0) load_q(w);
         }
       } while (w.next());
       asm volatile("cp.async.wait_all;" ::: "memory");
@@ -851,7 +941,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       constexpr int kCh = D / 16, kPass = kN / kCh, kEach = kKeys / kPass;  // 16-code chunks of a row; rows of a pass; of a thread
       constexpr int kStages = S::kStages;
       const int row0 = pt / kCh, ch = pt % kCh;
-      unsigned char* stages = smem + S::kQBytes + kEntries * S::kEntry + pt * 16;
+      unsigned char* stages = smem + S::kQs * S::kQBytes + kEntries * S::kEntry + pt * 16;
       const uint32_t stages_at = tc::smem_u32(stages);
       // entry e (keys and values in turn), of a tile whose rows have been placed
       auto copy = [&](uint32_t e, bool there) {
@@ -859,7 +949,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           const int64_t* offs = ctl.off[(e >> 1) & 3];
           const uint8_t* base = (const uint8_t*)(e & 1 ? c.v : c.k) + ch * 16;
           const uint32_t dst = stages_at + (e % kStages) * (S::kEntry / 2);
-#pragma unroll
+#pragma unroll 4
           for (int i = 0; i < kEach; ++i) {
             const int64_t o = offs[row0 + i * kPass];
             copy16(dst + i * kN * 16, base + (o < 0 ? 0 : o), o >= 0);
@@ -872,10 +962,10 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         if (e >= kEntries) wait(ctl, &ctl.empty[e % kEntries], (e / kEntries - 1) & 1);
         __syncwarp();
         const unsigned char* from = stages + (e % kStages) * (S::kEntry / 2);
-        unsigned char* dst = smem + S::kQBytes + (e % kEntries) * S::kEntry;
+        unsigned char* dst = smem + S::kQs * S::kQBytes + (e % kEntries) * S::kEntry;
         // lanes of a row's second half store their halves the other way round: no two in one bank
         const int flip = (ch >> 2) & 1;
-#pragma unroll
+#pragma unroll 2
         for (int i = 0; i < kEach; ++i) {
           const int r = row0 + i * kPass;
           uint32_t fr = fac[r];
@@ -911,83 +1001,26 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         tc::fence_async_smem();
         arrive(&ctl.full[e % kEntries]);
       };
-      // the walk two tiles ahead: places of a tile's rows, and the scale bytes of the thread's own (-1: no row)
-      Walk<kKeys> nx = w;
-      int nt = 0, page = -1;
-      bool more = true;
-      auto look = [&]() { page = more && owner ? page_of(nx.s, nx.s.base + (nx.ct + nt) * kKeys + orow) : -1; };
-      auto place = [&](uint32_t tile, int2& bytes) {
-        bytes = make_int2(-1, -1);
-        if (more) {
-          int64_t off = -1;
-          if (page >= 0) {
-            const int sl = slot_of(nx.s.base + (nx.ct + nt) * kKeys + orow), hk = nx.s.grp / g.blocks;
-            off = kv_page_offset(c, page) + (int64_t)sl * c.slot_stride + hk * c.head_stride;
-            const int64_t so = page * a.sc.page_stride + (int64_t)sl * a.sc.slot_stride + hk * a.sc.head_stride;
-            bytes = make_int2(a.sc.k[so], a.sc.v[so]);
-          }
-          if (owner) ctl.off[tile & 3][orow] = off;
-          if (++nt == nx.cnt) {
-            nt = 0;
-            more = nx.next();
-          }
-        }
-      };
       const uint32_t entries = (uint32_t)(2 * tiles);
-      int2 b0, b1, b2;
-      look();
-      place(0, b0);
-      look();
-      place(1, b1);
-      sync();
-      look();
 #pragma unroll
-      for (int e = 0; e < kStages; ++e) copy(e, e < entries);
+      for (int e = 0; e < kStages; ++e) {
+        if (!(e & 1) && e < entries) placed(e >> 1);
+        copy(e, e < entries);
+      }
       do {
-        const Seg& s = w.s;
         for (int t = 0; t < w.cnt; ++t, ++tile) {
-          const int p0 = s.base + (w.ct + t) * kKeys, buf = tile & 1;
-          Info& f = ctl.tile[tile % kInfos];
-          place(tile + 2, b2);
-          if (t == 0 && pt < 2) ctl.bad[w.index & 7][pt] = 0;
-          // bytes in [63, 247]; 255 takes no part in the largest
-          auto fit = [](int b) { return b < 0 || b == 255 ? -1 : min(max(b, 63), 247); };
-          const uint32_t ok = __ballot_sync(0xffffffffu, b0.x >= 0);
-          const int km = __reduce_max_sync(0xffffffffu, fit(b0.x)), vm = __reduce_max_sync(0xffffffffu, fit(b0.y));
-          if (lane == 0) {
-            ctl.wmax[buf][0][pt / 32] = km;
-            ctl.wmax[buf][1][pt / 32] = vm;
-            f.valid[pt / 32] = orow < kKeys ? ok : 0xffffffffu;
+          const Info& f = ctl.tile[tile % kInfos];
+          const uint32_t (*fac)[128] = ctl.fac[tile & 3];
+          if (S::kQs == 2 && t == 0) load_q(w);
+#pragma unroll 1
+          for (int kv = 0; kv < 2; ++kv) {
+            const uint32_t e = 2 * tile + kv, next = e + kStages;
+            put(e, fac[kv], kv && f.flags != 0, f, ctl.bad[f.flags >> 1]);
+            if (kv) arrive(&ctl.taken[tile & 3]);
+            if (!(next & 1) && next < entries) placed(next >> 1);
+            copy(next, next < entries);
           }
-          if (pt == 0) {
-            f.p0 = p0, f.n = s.n, f.lo = s.lo;
-            const bool differ = a.mask && (p0 + kKeys > s.n || (a.window > 0 && p0 < s.lo + 64));
-            f.flags = differ ? 1 | (w.index & 7) << 1 : 0;
-          }
-          sync();
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const int own = x ? b0.y : b0.x;
-            int big = max(max(ctl.wmax[buf][x][0], ctl.wmax[buf][x][1]), max(ctl.wmax[buf][x][2], ctl.wmax[buf][x][3]));
-            if (big < 0) big = 127;
-            if (orow < kKeys) {
-              const int d = fit(own) - big;  // at most 0; a factor below 2^-24 is 0
-              const uint32_t h = own < 0 ? 0u : own == 255 ? 0x7e00u : d >= -14 ? (uint32_t)(15 + d) << 10 : d >= -24 ? 1u << (24 + d) : 0u;
-              ctl.fac[buf][x][orow] = h | h << 16;
-            }
-            if (pt == 0) (x ? f.ev : f.ek) = (float)(big - 127);
-          }
-          sync();
-          arrive(&ctl.info[tile % kInfos]);
-          look();
-          const bool check = f.flags != 0;
-          put(2 * tile, ctl.fac[buf][0], false, f, ctl.bad[0]);
-          copy(2 * tile + kStages, 2 * tile + kStages < entries);
-          put(2 * tile + 1, ctl.fac[buf][1], check, f, ctl.bad[w.index & 7]);
-          copy(2 * tile + 1 + kStages, 2 * tile + 1 + kStages < entries);
-          if (t == 0) load_q(w);
-          b0 = b1;
-          b1 = b2;
+          if (S::kQs == 1 && t == 0) load_q(w);
         }
       } while (w.next());
       asm volatile("cp.async.wait_group 0;" ::: "memory");
