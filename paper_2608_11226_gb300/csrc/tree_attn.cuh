@@ -92,11 +92,16 @@ struct Control {
 
 struct Args {
   TreeArgs a;
-  int groups, blocks, page_shift;  // groups: key heads x blocks of rows
+  int groups, blocks;             // groups: key heads x blocks of rows
+  uint32_t page_mul, page_shift;  // p / page_size = (p * page_mul >> 32) >> page_shift for p < 2^31 (page_mul 0: p >> page_shift)
   float* part;
   SegMeta* meta;
   int32_t* error;
 };
+
+__device__ __forceinline__ int page_index(const Args& g, int p) {
+  return (int)((g.page_mul ? __umulhi((uint32_t)p, g.page_mul) : (uint32_t)p) >> g.page_shift);
+}
 
 struct Seg {
   int b, grp, nt, n, lo, end, base;
@@ -222,16 +227,18 @@ __device__ __forceinline__ bool mbar_test(uint64_t* b, uint32_t parity) {  // wi
 }
 
 // a bounded wait; once one has given up, the others do not wait either
-__device__ __forceinline__ void wait(Control& c, uint64_t* b, uint32_t parity) {
-  if (tc::mbar_try_wait(b, parity)) return;
+__device__ __forceinline__ void wait_long(int* err, uint64_t* b, uint32_t parity) {
   const long long t0 = clock64();
   while (!tc::mbar_try_wait(b, parity)) {
-    if (*(volatile int*)&c.err) return;
+    if (*(volatile int*)err) return;
     if (clock64() - t0 > 4000000000LL) {
-      atomicExch(&c.err, 1);
+      atomicExch(err, 1);
       return;
     }
   }
+}
+__device__ __forceinline__ void wait(Control& c, uint64_t* b, uint32_t parity) {
+  if (__builtin_expect(!tc::mbar_try_wait(b, parity), 0)) wait_long(&c.err, b, parity);
 }
 
 // the weight of a piece with maximum m where the largest is mm; a piece that
@@ -260,6 +267,25 @@ template <typename M> __device__ __forceinline__ bool not_finite(uint32_t w, int
 // byte address of 16-byte chunk ch of row r in a swizzled tile of `rows` rows
 __device__ __forceinline__ uint32_t chunk_at(int r, int ch, int rows) {
   return (ch >> 3) * rows * 128 + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
+}
+
+// which of elements d .. d + 31 of the marked positions' values (nodes, positions from lo on) are not finite
+template <typename T, bool E8>
+__device__ __forceinline__ uint32_t spoilt_columns(const TreeArgs& a, int b, int hk, int n, int lo, uint64_t nodes, uint64_t ahead, int d) {
+  const pe_kv_cache& c = a.c;
+  uint32_t nan = 0;
+#pragma unroll 1
+  for (int k = 0; k < 128; ++k) {
+    if (!((k < 64 ? nodes >> k : ahead >> (k - 64)) & 1)) continue;
+    const int p = k < 64 ? n + k : lo + k - 64;
+    const int page = c.table[(int64_t)b * c.table_stride + p / c.page_size], sl = p % c.page_size;
+    const int64_t at = kv_page_offset(c, page) + (int64_t)sl * c.slot_stride + hk * c.head_stride + d;
+    if (E8 && a.sc.v[page * a.sc.page_stride + (int64_t)sl * a.sc.slot_stride + hk * a.sc.head_stride] == 255) return 0xffffffffu;
+#pragma unroll 1
+    for (int j = 0; j < 32; ++j)
+      if (E8 ? (((const uint8_t*)c.v)[at + j] & 0x7f) == 0x7f : not_finite<T>(((const uint16_t*)c.v)[at + j], 0)) nan |= 1u << j;
+  }
+  return nan;
 }
 
 // ---------------------------------------------------------------- the kernel
@@ -414,7 +440,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           // 64 columns at a time (head_dim 256: 32); code is kept short, for the roles share the instruction cache
           constexpr int kHalves = S::kCols >= 64 ? 2 : 1, kTurns = S::kCols / (32 * kHalves);
           uint32_t keep[S::kCols / 32];
-          if (!whole) {
+          if (__builtin_expect(!whole, 0)) {
 #pragma unroll
             for (int i = 0; i < S::kCols / 32; ++i) {
               const int at = i + (WIDE ? 0 : wg * (S::kCols / 32)), pw = f.p0 + 32 * at;
@@ -432,7 +458,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             for (int h = 0; h < kHalves; ++h) ld32(sc + 64 * turn + 32 * h, v[h]);
 #pragma unroll
             for (int h = 0; h < kHalves; ++h) ld_wait(v[h]);
-            if (!whole) {
+            if (__builtin_expect(!whole, 0)) {
 #pragma unroll
               for (int h = 0; h < kHalves; ++h) {
                 const uint32_t k = kTurns == 1 ? keep[h] : turn ? keep[(kTurns - 1) * kHalves + h] : keep[h];
@@ -462,7 +488,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           }
           top = top == -CUDART_INF_F ? top : fmaf(top, cf, ev);
           const bool over = top > m + 8.0f;
-          if (__any_sync(0xffffffffu, over)) {
+          if (__builtin_expect(__any_sync(0xffffffffu, over), 0)) {
             const float x = over ? top : m;
             const float fr = over ? (m == -CUDART_INF_F ? 0.0f : exp2_fast(m - x)) : 1.0f;
             m = x;
@@ -549,20 +575,11 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           auto take = [&](int d) {
             ld32(oc + d, v);
             ld_wait(v);
-            if (spoilt) {  // an attended value that is not finite makes its element NaN
-#pragma unroll 1
-              for (int k = 0; k < 128; ++k) {
-                if (!((k < 64 ? bad_node >> k : bad_pos >> (k - 64)) & 1)) continue;
-                const int p = k < 64 ? s.n + k : s.lo + k - 64;
-                const int page = c.table[(int64_t)s.b * c.table_stride + p / c.page_size], sl = p % c.page_size;
-                const int64_t at = kv_page_offset(c, page) + (int64_t)sl * c.slot_stride + hk * c.head_stride + d0 + d;
-                const bool row_bad = E8 && a.sc.v[page * a.sc.page_stride + (int64_t)sl * a.sc.slot_stride + hk * a.sc.head_stride] == 255;
+            if (__builtin_expect(spoilt, 0)) {  // an attended value that is not finite makes its element NaN
+              const uint32_t nan = spoilt_columns<T, E8>(a, s.b, hk, s.n, s.lo, bad_node, bad_pos, d0 + d);
 #pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                  const bool x = E8 ? row_bad || (((const uint8_t*)c.v)[at + j] & 0x7f) == 0x7f : not_finite<T>(((const uint16_t*)c.v)[at + j], 0);
-                  if (x) v[j] = CUDART_NAN_F;
-                }
-              }
+              for (int j = 0; j < 32; ++j)
+                if ((nan >> j) & 1) v[j] = CUDART_NAN_F;
             }
             __syncwarp();
           };
@@ -636,7 +653,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           const int p = nx.s.base + (nx.ct + nt) * kKeys + lane + 32 * j;
           page[j] = -1;
           if (more && p >= nx.s.lo && p < nx.s.end) {
-            page[j] = c.table[(int64_t)nx.s.b * c.table_stride + (g.page_shift >= 0 ? p >> g.page_shift : p / c.page_size)];
+            page[j] = c.table[(int64_t)nx.s.b * c.table_stride + page_index(g, p)];
             if (page[j] >= c.n_pages) page[j] = -1;
           }
         }
@@ -650,7 +667,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         Info& f = ctl.tile[x % kInfos];
 #pragma unroll
         for (int j = 0; j < kMine; ++j) {
-          const int p = p0 + lane + 32 * j, sl = g.page_shift >= 0 ? p & (c.page_size - 1) : p % c.page_size;
+          const int p = p0 + lane + 32 * j, sl = p - page_index(g, p) * c.page_size;
           const bool ok = page[j] >= 0;
           ctl.off[x & 3][lane + 32 * j] = ok ? kv_page_offset(c, page[j]) + (int64_t)sl * c.slot_stride + hk * c.head_stride : -1;
           if (E8) {
@@ -676,10 +693,10 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           more = nx.next();
         }
       };
-      look();
-      place(0);
-      look();
-      for (uint32_t x = 0; x < (uint32_t)tiles; ++x) {
+#pragma unroll 1
+      for (int64_t at = -2; at < tiles; ++at) {
+        const uint32_t x = (uint32_t)at;
+        if (at >= 0) {
         int own[2][kMine];
 #pragma unroll
         for (int j = 0; j < kMine; ++j) own[0][j] = kb[j], own[1][j] = vb[j];
@@ -697,8 +714,8 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
 #pragma unroll
             for (int j = 0; j < kMine; ++j) {
               const int b = own[i][j], d = fit(b) - big;  // at most 0; a factor below 2^-24 is 0
-              const uint32_t h = b < 0 ? 0u : b == 255 ? 0x7e00u : d >= -14 ? (uint32_t)(15 + d) << 10 : d >= -24 ? 1u << (24 + d) : 0u;
-              ctl.fac[x & 3][i][lane + 32 * j] = h | h << 16;
+              const float f = b < 0 ? 0.0f : b == 255 ? CUDART_NAN_F : __int_as_float(max(127 + d, 0) << 23);
+              ctl.fac[x & 3][i][lane + 32 * j] = pack2<__half>(f, f);
             }
             if (lane == 0) (i ? f.ev : f.ek) = (float)(big - 127);
           }
@@ -708,7 +725,8 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           tc::mbar_arrive(&ctl.info[x % kInfos]);
           tc::mbar_arrive(&ctl.placed[x & 3]);
         }
-        place(x + 1);
+        }
+        if (at >= -1) place(x + 1);
         look();
       }
     }
@@ -919,7 +937,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
               const int64_t o = offs[r];
               copy16(dst + chunk_at(r, ch, kKeys), src + (o < 0 ? 0 : o), o >= 0);
             }
-            if (kv && f.flags) {
+            if (__builtin_expect(kv && f.flags, 0)) {
               spoils(f);
               tc::fence_async_smem();
               tc::mbar_arrive(&ctl.full[issued % kEntries]);
@@ -957,34 +975,48 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
       };
-      auto put = [&](uint32_t e, const uint32_t* fac, bool check, const Info& f, unsigned long long* bad) {
+      // a value that is no number, where rows attend to it differently, becomes zero and a mark
+      auto spoils = [&](unsigned char* from, uint32_t* fac, const Info& f) {
+        unsigned long long* bad = ctl.bad[f.flags >> 1];
+#pragma unroll 1
+        for (int i = 0; i < kEach; ++i) {
+          const int r = row0 + i * kPass;
+          int k;
+          const uint64_t bit = (f.valid[r >> 5] >> (r & 31)) & 1 ? apart(f, r, k) : 0;
+          const bool none = (fac[r] & 0x7fffu) > 0x7c00u;  // the row's scale
+          __syncwarp();  // a row's lanes are in one warp
+          if (bit && none && ch == 0) fac[r] = 0;
+          if (!bit) continue;
+          uint4 z = *reinterpret_cast<const uint4*>(from + i * kN * 16);
+          uint32_t* y = reinterpret_cast<uint32_t*>(&z);
+          bool any = none;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int b = 0; b < 32; b += 8)
+              if (((y[j] >> b) & 0x7f) == 0x7f) y[j] &= ~(0xffu << b), any = true;
+          if (any) {
+            *reinterpret_cast<uint4*>(from + i * kN * 16) = z;
+            atomicOr(&bad[k], bit);
+          }
+        }
+        __syncwarp();
+      };
+      auto put = [&](uint32_t e, uint32_t* fac, bool check, const Info& f) {
         asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
         if (e >= kEntries) wait(ctl, &ctl.empty[e % kEntries], (e / kEntries - 1) & 1);
         __syncwarp();
-        const unsigned char* from = stages + (e % kStages) * (S::kEntry / 2);
+        unsigned char* from = stages + (e % kStages) * (S::kEntry / 2);
+        if (__builtin_expect(check, 0)) spoils(from, fac, f);
         unsigned char* dst = smem + S::kQs * S::kQBytes + (e % kEntries) * S::kEntry;
         // lanes of a row's second half store their halves the other way round: no two in one bank
         const int flip = (ch >> 2) & 1;
 #pragma unroll 2
         for (int i = 0; i < kEach; ++i) {
           const int r = row0 + i * kPass;
-          uint32_t fr = fac[r];
-          uint4 z = *reinterpret_cast<const uint4*>(from + i * kN * 16);
-          uint32_t* y = reinterpret_cast<uint32_t*>(&z);
-          if (check) {
-            int k;
-            const uint64_t bit = apart(f, r, k);
-            if (bit && ((f.valid[r >> 5] >> (r & 31)) & 1)) {
-              bool any = (fr & 0x7fffu) > 0x7c00u;
-              if (any) fr = 0, z = make_uint4(0, 0, 0, 0);
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int b = 0; b < 32; b += 8)
-                  if (((y[j] >> b) & 0x7f) == 0x7f) y[j] &= ~(0xffu << b), any = true;
-              if (any) atomicOr(&bad[k], bit);
-            }
-          }
+          const uint32_t fr = fac[r];
+          const uint4 z = *reinterpret_cast<const uint4*>(from + i * kN * 16);
+          const uint32_t* y = reinterpret_cast<const uint32_t*>(&z);
           uint4 h[2];
           uint32_t* hw = reinterpret_cast<uint32_t*>(h);
           const __half2 ff = *reinterpret_cast<const __half2*>(&fr);
@@ -1010,12 +1042,12 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       do {
         for (int t = 0; t < w.cnt; ++t, ++tile) {
           const Info& f = ctl.tile[tile % kInfos];
-          const uint32_t (*fac)[128] = ctl.fac[tile & 3];
+          uint32_t (*fac)[128] = ctl.fac[tile & 3];
           if (S::kQs == 2 && t == 0) load_q(w);
 #pragma unroll 1
           for (int kv = 0; kv < 2; ++kv) {
             const uint32_t e = 2 * tile + kv, next = e + kStages;
-            put(e, fac[kv], kv && f.flags != 0, f, ctl.bad[f.flags >> 1]);
+            put(e, fac[kv], kv && f.flags != 0, f);
             if (kv) arrive(&ctl.taken[tile & 3]);
             if (!(next & 1) && next < entries) placed(next >> 1);
             copy(next, next < entries);
@@ -1106,9 +1138,13 @@ static pe_status go(const TreeArgs& a, void* ws, int32_t* error, cudaStream_t st
   g.a = a;
   g.blocks = ceil_div(rows, S::kRows);
   g.groups = a.c.n_heads * g.blocks;
-  g.page_shift = -1;  // of a page size that is a power of two
-  if ((a.c.page_size & (a.c.page_size - 1)) == 0)
-    while (a.c.page_size >> (g.page_shift + 1)) ++g.page_shift;
+  // with 2^s the power of two at or above the page size d: floor(2^(31 + s) / d) + 1 (Granlund and Montgomery)
+  const uint32_t d = a.c.page_size;
+  while ((1u << g.page_shift) < d) ++g.page_shift;
+  if ((1u << g.page_shift) != d) {
+    g.page_mul = (uint32_t)(((uint64_t)1 << (31 + g.page_shift)) / d + 1);
+    g.page_shift -= 1;
+  }
   g.meta = reinterpret_cast<SegMeta*>(ws);
   g.part = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + kMetaBytes);
   g.error = error;
