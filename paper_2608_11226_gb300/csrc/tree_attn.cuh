@@ -73,7 +73,7 @@ struct Shape {
 
 struct Info {  // a tile
   uint32_t valid[4];  // its positions that exist: in the sequence's range, on present pages
-  int p0, n, lo, flags;  // first position; the sequence's length and lowest position; 1: rows attend to it differently
+  int p0, n, lo, flags;  // first position; the sequence's length and lowest position; 1: rows attend to it differently (segment from bit 1 on)
   float ek, ev;       // exponents of an 8-bit tile's factors
 };
 
@@ -766,11 +766,13 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
                 kseen = max(kseen, t + 1);
                 const int buf = WIDE ? x : t & 1;
                 tc::fence_after();
-#pragma unroll 2
+                // (addresses of 14 bits in 16 bytes: constants on top do not carry)
+                const uint64_t qd = tc::desc_kmajor(qs + qb * S::kQBytes + x * 128 * 128 * (D / 64), 1024, tc::kLayoutSW128);
+                const uint64_t kd = tc::desc_kmajor(entry(e), 1024, tc::kLayoutSW128);
+#pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk)
-                  tc::mma_bf16(tmem + S::kS + buf * S::kSStep,
-                               tc::desc_kmajor(qs + qb * S::kQBytes + x * 128 * 128 * (D / 64) + (kk >> 2) * 128 * 128 + (kk & 3) * 32, 1024, tc::kLayoutSW128),
-                               tc::desc_kmajor(entry(e) + (kk >> 2) * kKeys * 128 + (kk & 3) * 32, 1024, tc::kLayoutSW128), kIdS, kk > 0);
+                  tc::mma_bf16(tmem + S::kS + buf * S::kSStep, qd + ((kk >> 2) * 128 * 128 + (kk & 3) * 32) / 16,
+                               kd + ((kk >> 2) * kKeys * 128 + (kk & 3) * 32) / 16, kIdS, kk > 0);
                 tc::mma_commit(&ctl.s_full[buf]);
                 ++nk[x];
                 if (tracks == 1 || nk[x ^ 1] >= nk[x]) {
@@ -787,10 +789,10 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
                 vseen = max(vseen, t + 1);
                 ++ps[buf];
                 tc::fence_after();
-#pragma unroll 2
+                const uint64_t vd = tc::desc_strided(entry(e), kKeys * 128, 1024, tc::kLayoutSW128);
+#pragma unroll
                 for (int kk = 0; kk < kKeys / 16; ++kk)
-                  mma_ts(tmem + S::kO + x * S::kOStep, tmem + S::kP + buf * S::kPStep + 8 * kk,
-                         tc::desc_strided(entry(e) + kk * 2048, kKeys * 128, 1024, tc::kLayoutSW128), kIdO, !(t == 0 && kk == 0));
+                  mma_ts(tmem + S::kO + x * S::kOStep, tmem + S::kP + buf * S::kPStep + 8 * kk, vd + kk * 128, kIdO, !(t == 0 && kk == 0));
                 tc::mma_commit(&ctl.pv_done[x]);
                 ++np[x];
                 if (tracks == 1 || np[x ^ 1] >= np[x]) tc::mma_commit(&ctl.empty[e % kEntries]);
@@ -931,13 +933,17 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             if (issued >= kEntries) wait(ctl, &ctl.empty[issued % kEntries], (issued / kEntries - 1) & 1);
             const uint32_t dst = ring + (issued % kEntries) * S::kEntry;
             const T* src = (const T*)(kv ? c.v : c.k) + ch * 8;
-#pragma unroll 4
-            for (int i = 0; i < kKeys / kPass; ++i) {
-              const int r = row0 + i * kPass;
-              const int64_t o = offs[r];
-              copy16(dst + chunk_at(r, ch, kKeys), src + (o < 0 ? 0 : o), o >= 0);
+            constexpr int kAtOnce = 8;
+#pragma unroll 1
+            for (int i0 = 0; i0 < kKeys / kPass; i0 += kAtOnce) {
+              int64_t o[kAtOnce];  // read ahead of the copies, which the compiler keeps in their order
+#pragma unroll
+              for (int i = 0; i < kAtOnce; ++i) o[i] = offs[row0 + (i0 + i) * kPass];
+#pragma unroll
+              for (int i = 0; i < kAtOnce; ++i)
+                copy16(dst + chunk_at(row0 + (i0 + i) * kPass, ch, kKeys), src + (o[i] < 0 ? 0 : o[i]), o[i] >= 0);
             }
-            if (__builtin_expect(kv && f.flags, 0)) {
+            if (__builtin_expect(kv && (f.flags & 1), 0)) {
               spoils(f);
               tc::fence_async_smem();
               tc::mbar_arrive(&ctl.full[issued % kEntries]);
@@ -967,11 +973,11 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           const int64_t* offs = ctl.off[(e >> 1) & 3];
           const uint8_t* base = (const uint8_t*)(e & 1 ? c.v : c.k) + ch * 16;
           const uint32_t dst = stages_at + (e % kStages) * (S::kEntry / 2);
-#pragma unroll 4
-          for (int i = 0; i < kEach; ++i) {
-            const int64_t o = offs[row0 + i * kPass];
-            copy16(dst + i * kN * 16, base + (o < 0 ? 0 : o), o >= 0);
-          }
+          int64_t o[kEach];  // read ahead of the copies, which the compiler keeps in their order
+#pragma unroll
+          for (int i = 0; i < kEach; ++i) o[i] = offs[row0 + i * kPass];
+#pragma unroll
+          for (int i = 0; i < kEach; ++i) copy16(dst + i * kN * 16, base + (o[i] < 0 ? 0 : o[i]), o[i] >= 0);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
       };
@@ -1011,12 +1017,18 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         unsigned char* dst = smem + S::kQs * S::kQBytes + (e % kEntries) * S::kEntry;
         // lanes of a row's second half store their halves the other way round: no two in one bank
         const int flip = (ch >> 2) & 1;
-#pragma unroll 2
-        for (int i = 0; i < kEach; ++i) {
-          const int r = row0 + i * kPass;
-          const uint32_t fr = fac[r];
-          const uint4 z = *reinterpret_cast<const uint4*>(from + i * kN * 16);
-          const uint32_t* y = reinterpret_cast<const uint32_t*>(&z);
+        constexpr int kAtOnce = 4;
+#pragma unroll 1
+        for (int i0 = 0; i0 < kEach; i0 += kAtOnce) {
+        uint32_t fr4[kAtOnce];
+        uint4 z4[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) fr4[i] = fac[row0 + (i0 + i) * kPass], z4[i] = *reinterpret_cast<const uint4*>(from + (i0 + i) * kN * 16);
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+          const int r = row0 + (i0 + i) * kPass;
+          const uint32_t fr = fr4[i];
+          const uint32_t* y = reinterpret_cast<const uint32_t*>(&z4[i]);
           uint4 h[2];
           uint32_t* hw = reinterpret_cast<uint32_t*>(h);
           const __half2 ff = *reinterpret_cast<const __half2*>(&fr);
@@ -1029,6 +1041,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           }
           *reinterpret_cast<uint4*>(dst + chunk_at(r, 2 * ch + flip, kKeys)) = flip ? h[1] : h[0];
           *reinterpret_cast<uint4*>(dst + chunk_at(r, 2 * ch + 1 - flip, kKeys)) = flip ? h[0] : h[1];
+        }
         }
         tc::fence_async_smem();
         arrive(&ctl.full[e % kEntries]);
@@ -1047,7 +1060,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
 #pragma unroll 1
           for (int kv = 0; kv < 2; ++kv) {
             const uint32_t e = 2 * tile + kv, next = e + kStages;
-            put(e, fac[kv], kv && f.flags != 0, f);
+            put(e, fac[kv], kv && (f.flags & 1), f);
             if (kv) arrive(&ctl.taken[tile & 3]);
             if (!(next & 1) && next < entries) placed(next >> 1);
             copy(next, next < entries);
