@@ -77,34 +77,46 @@ struct Info {  // a tile
   float ek, ev;       // exponents of an 8-bit tile's factors
 };
 
+template <class S>
 struct Control {
   uint64_t full[8], empty[8], info[kInfos], placed[4], taken[4], q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2], fin;
   Info tile[kInfos];
   unsigned long long bad[16][2];  // per segment: nodes, and positions from lo on, with values that are not finite
-  int64_t off[4][128];           // element offsets of a tile's rows, -1: none
+  int64_t off[4][S::kKeys];      // element offsets of a tile's rows, -1: none
+  int page[2][S::kKeys];         // pages of a tile's rows; then which byte of its word a row's scales are; -1: no row
+  uint32_t word[2][2][S::kKeys];  // the words of the rows' scales
+  uint16_t fac[4][2][S::kKeys];  // 2^(e - E) in fp16
   int64_t sum[16];
-  float mx[2][2][128], l[2][128], qf[4][256];
-  uint32_t fac[4][2][128];
+  float mx[2][2][128], l[2][128], qf[4][S::kRows];
   int where[4];
   uint32_t tmem;
   int err;
 };
 
+// Division of x < 2^31 by d with a product: with 2^s the power of two at or above d,
+// m = floor(2^(31 + s) / d) + 1 (Granlund and Montgomery); m = 0: a shift alone
+struct Divisor {
+  uint32_t m, s;
+  __device__ __forceinline__ int of(int x) const { return (int)((m ? __umulhi((uint32_t)x, m) : (uint32_t)x) >> s); }
+};
+static inline Divisor divisor(uint32_t d) {
+  Divisor r{0, 0};
+  while ((1u << r.s) < d) ++r.s;
+  if ((1u << r.s) != d) r.m = (uint32_t)(((uint64_t)1 << (31 + r.s)) / d + 1), --r.s;
+  return r;
+}
+
 struct Args {
   TreeArgs a;
   int groups, blocks;             // groups: key heads x blocks of rows
-  uint32_t page_mul, page_shift;  // p / page_size = (p * page_mul >> 32) >> page_shift for p < 2^31 (page_mul 0: p >> page_shift)
+  Divisor page, group;            // by the page size, by the query heads of a key head
   float* part;
   SegMeta* meta;
   int32_t* error;
 };
 
-__device__ __forceinline__ int page_index(const Args& g, int p) {
-  return (int)((g.page_mul ? __umulhi((uint32_t)p, g.page_mul) : (uint32_t)p) >> g.page_shift);
-}
-
 struct Seg {
-  int b, grp, nt, n, lo, end, base;
+  int b, hk, blk, nt, n, lo, end, base;  // sequence, key head, block of rows; tiles; ...
 };
 
 template <int KEYS>
@@ -138,7 +150,7 @@ struct Walk {
   int ct, cnt, ahead, index;  // first tile and tiles of this CTA in the segment; the next sequence's length; segments behind
   int64_t left;
   __device__ __forceinline__ Walk(const Args& g, const int* where, int64_t tiles) : g(g) {
-    s.b = where[0], s.grp = where[1], ct = where[2], index = 0;
+    s.b = where[0], s.hk = where[1] / g.blocks, s.blk = where[1] % g.blocks, ct = where[2], index = 0;
     seg_range<KEYS>(g.a, where[3], s);
     ahead = g.a.lens[min(s.b + 1, g.a.c.n_seqs - 1)];
     left = tiles;
@@ -149,8 +161,9 @@ struct Walk {
     if (left <= 0) return false;
     ct = 0;
     ++index;
-    if (++s.grp == g.groups) {
-      s.grp = 0;
+    if (++s.blk < g.blocks) {
+    } else if (s.blk = 0, ++s.hk == g.a.c.n_heads) {
+      s.hk = 0;
       ++s.b;
       seg_range<KEYS>(g.a, ahead, s);
       ahead = g.a.lens[min(s.b + 1, g.a.c.n_seqs - 1)];
@@ -237,7 +250,8 @@ __device__ __forceinline__ void wait_long(int* err, uint64_t* b, uint32_t parity
     }
   }
 }
-__device__ __forceinline__ void wait(Control& c, uint64_t* b, uint32_t parity) {
+template <class C>
+__device__ __forceinline__ void wait(C& c, uint64_t* b, uint32_t parity) {
   if (__builtin_expect(!tc::mbar_try_wait(b, parity), 0)) wait_long(&c.err, b, parity);
 }
 
@@ -269,7 +283,7 @@ __device__ __forceinline__ uint32_t chunk_at(int r, int ch, int rows) {
   return (ch >> 3) * rows * 128 + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
 }
 
-// which of elements d .. d + 31 of the marked positions' values (nodes, positions from lo on) are not finite
+// which of elements d .. d + 15 of the marked positions' values (nodes, positions from lo on) are not finite
 template <typename T, bool E8>
 __device__ __forceinline__ uint32_t spoilt_columns(const TreeArgs& a, int b, int hk, int n, int lo, uint64_t nodes, uint64_t ahead, int d) {
   const pe_kv_cache& c = a.c;
@@ -282,7 +296,7 @@ __device__ __forceinline__ uint32_t spoilt_columns(const TreeArgs& a, int b, int
     const int64_t at = kv_page_offset(c, page) + (int64_t)sl * c.slot_stride + hk * c.head_stride + d;
     if (E8 && a.sc.v[page * a.sc.page_stride + (int64_t)sl * a.sc.slot_stride + hk * a.sc.head_stride] == 255) return 0xffffffffu;
 #pragma unroll 1
-    for (int j = 0; j < 32; ++j)
+    for (int j = 0; j < 16; ++j)
       if (E8 ? (((const uint8_t*)c.v)[at + j] & 0x7f) == 0x7f : not_finite<T>(((const uint16_t*)c.v)[at + j], 0)) nan |= 1u << j;
   }
   return nan;
@@ -296,7 +310,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
   using M = typename std::conditional<E8, __half, T>::type;  // type of the products
   constexpr int kKeys = S::kKeys, kChunks = D / 8, kEntries = S::kEntries;
   extern __shared__ unsigned char smem_raw[];
-  __shared__ __align__(16) Control ctl;
+  __shared__ __align__(16) Control<S> ctl;
   const TreeArgs& a = g.a;
   const pe_kv_cache& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -380,7 +394,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     if (tiles > 0) {
       Walk<kKeys> w(g, ctl.where, tiles);
       const int64_t g0 = start - w.ct, prev = blockIdx.x ? deal.start((int)blockIdx.x - 1) : 0;
-      m.seq = w.s.b, m.group = w.s.grp;
+      m.seq = w.s.b, m.group = w.s.hk * g.blocks + w.s.blk;
       if (w.ct > 0 && prev <= g0) {
         m.pieces = deal.worker(g0 + w.s.nt - 1) - blockIdx.x + 2;
         m.first_slot = 2 * (blockIdx.x - 1) + (prev < g0 ? 1 : 0);
@@ -398,18 +412,20 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const float qlog = fabsf(a.scale) * 1.4426950408889634f;
     uint32_t sp[2] = {0, 0}, pp[2] = {0, 0}, ip = 0;  // phases: scores, outputs, tiles seen
+    uint64_t bits = 0;  // the row's mask, of sequence last_b
+    int last_b = -1;
     Walk<kKeys> w(g, ctl.where, tiles);
     do {
       const Seg& s = w.s;
-      const int hk = s.grp / g.blocks, r0 = s.grp % g.blocks * S::kRows, rows = min(R - r0, S::kRows);
+      const int hk = s.hk, r0 = s.blk * S::kRows, rows = min(R - r0, S::kRows);
       const int rr = r0 + (WIDE ? wg * 128 : 0) + row;  // row of the sequence and key head
       const bool exists = rr < R && (WIDE ? wg * 128 + row < rows : row < rows);
-      const int node = exists ? rr / G : 0, head = hk * G + (exists ? rr % G : 0);
-      uint64_t bits = 0;
+      const int node = exists ? g.group.of(rr) : 0, head = hk * G + (exists ? rr - node * G : 0);
       int row_lo = s.lo;
       bool live = exists;
       if (a.mask) {
-        if (exists) bits = a.mask[s.b * a.mask_stride + node] & (0xffffffffffffffffull >> (64 - a.n_nodes));
+        if (s.b != last_b || g.blocks > 1) bits = exists ? a.mask[s.b * a.mask_stride + node] & (0xffffffffffffffffull >> (64 - a.n_nodes)) : 0;
+        last_b = s.b;
         live = bits != 0;
         if (a.window > 0) row_lo = max(0, s.n + __popcll(bits) - a.window);
       }
@@ -565,65 +581,32 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         const int64_t slot = 2 * (int64_t)blockIdx.x + (w.index > 0 ? 1 : 0);
         float* piece = g.part + slot * S::kRows * (D + 2);
         const int prow = (WIDE ? wg * 128 : 0) + row;
-        // 16-byte parts of a row change lanes, so that eight lanes store 128 bytes of a row together
-        char* to = whole ? reinterpret_cast<char*>(out) : reinterpret_cast<char*>(piece + (int64_t)prow * D + d0);
-        const int per = whole ? (kMine >= 64 ? 64 : 32) : 32;  // elements of a turn
+        float* to = piece + (int64_t)prow * D + d0;
+        // short code again: it is fetched anew for each segment (with the parts of a row spread over lanes, for
+        // stores of 128 bytes, it took twice as long)
 #pragma unroll 1
-        for (int i = 0; i < kMine; i += per) {
-          uint4 u[8];
-          float v[32];
-          auto take = [&](int d) {
-            ld32(oc + d, v);
-            ld_wait(v);
-            if (__builtin_expect(spoilt, 0)) {  // an attended value that is not finite makes its element NaN
-              const uint32_t nan = spoilt_columns<T, E8>(a, s.b, hk, s.n, s.lo, bad_node, bad_pos, d0 + d);
+        for (int i = 0; i < kMine; i += 16) {
+          float v[16];
+          tc::tmem_ld16(oc + i, v);
+          if (__builtin_expect(spoilt, 0)) {  // an attended value that is not finite makes its element NaN
+            const uint32_t nan = spoilt_columns<T, E8>(a, s.b, hk, s.n, s.lo, bad_node, bad_pos, d0 + i);
 #pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if ((nan >> j) & 1) v[j] = CUDART_NAN_F;
-            }
-            __syncwarp();
-          };
-          if (whole) {
-#pragma unroll
-            for (int h = 0; h < (kMine >= 64 ? 2 : 1); ++h) {
-              take(i + 32 * h);
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                u[4 * h + j] = make_uint4(pack2<T>(v[8 * j] * inv, v[8 * j + 1] * inv), pack2<T>(v[8 * j + 2] * inv, v[8 * j + 3] * inv),
-                                          pack2<T>(v[8 * j + 4] * inv, v[8 * j + 5] * inv), pack2<T>(v[8 * j + 6] * inv, v[8 * j + 7] * inv));
-            }
-          } else {
-            take(i);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              u[j] = make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3]));
+            for (int j = 0; j < 16; ++j)
+              if ((nan >> j) & 1) v[j] = CUDART_NAN_F;
           }
           if (l == 0.0f)  // nothing attended to, whatever the values are
 #pragma unroll
-            for (int j = 0; j < 8; ++j) u[j] = make_uint4(0, 0, 0, 0);
+            for (int j = 0; j < 16; ++j) v[j] = 0.0f;
+          if (exists && whole) {
 #pragma unroll
-          for (int x = 1; x < 8; x *= 2)
+            for (int j = 0; j < 16; j += 8)
+              *reinterpret_cast<uint4*>(out + i + j) = make_uint4(pack2<T>(v[j] * inv, v[j + 1] * inv), pack2<T>(v[j + 2] * inv, v[j + 3] * inv),
+                                                                  pack2<T>(v[j + 4] * inv, v[j + 5] * inv), pack2<T>(v[j + 6] * inv, v[j + 7] * inv));
+          } else if (exists) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              if (j & x) continue;
-              const bool up = lane & x;
-              uint4 send = up ? u[j] : u[j + x];
-              send.x = __shfl_xor_sync(0xffffffffu, send.x, x), send.y = __shfl_xor_sync(0xffffffffu, send.y, x);
-              send.z = __shfl_xor_sync(0xffffffffu, send.z, x), send.w = __shfl_xor_sync(0xffffffffu, send.w, x);
-              if (up)
-                u[j] = send;
-              else
-                u[j + x] = send;
-            }
-          const uint32_t there = __ballot_sync(0xffffffffu, exists);
-          const bool mine = !whole || kMine >= 64 || (lane & 7) < 4;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int from = (lane & 24) | j;
-            char* p = reinterpret_cast<char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(to), from));
-            if (((there >> from) & 1) && mine) *reinterpret_cast<uint4*>(p + 16 * (lane & 7)) = u[j];
+            for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4*>(to + i + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
           }
-          to += whole ? per * 2 : per * 4;
+          __syncwarp();
         }
         if (exists && (WIDE || wg == 0)) {
           if (whole) {
@@ -640,95 +623,106 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
     if (warp == 9) {
     // ================================================== places
-      // a lane finds the places of rows lane, lane + 32, ... and, of codes, what brings their scales
-      // to the tile's largest: pages two tiles ahead, scales one
+      // A lane finds the places of rows lane, lane + 32, ... and, of codes, what brings their scales to the
+      // tile's largest.  Table entries are copied two tiles ahead and scales one (the words they are in).
       constexpr int kMine = kKeys / 32;
-      Walk<kKeys> nx(g, ctl.where, tiles);  // one tile ahead
-      int nt = 0;
-      bool more = true;
-      int page[kMine], kb[kMine], vb[kMine];
-      auto look = [&]() {
-#pragma unroll
-        for (int j = 0; j < kMine; ++j) {
-          const int p = nx.s.base + (nx.ct + nt) * kKeys + lane + 32 * j;
-          page[j] = -1;
-          if (more && p >= nx.s.lo && p < nx.s.end) {
-            page[j] = c.table[(int64_t)nx.s.b * c.table_stride + page_index(g, p)];
-            if (page[j] >= c.n_pages) page[j] = -1;
-          }
-        }
+      Walk<kKeys> nx(g, ctl.where, tiles);  // one tile ahead of what is told
+      int nt = 0, t2 = nx.ct;
+      auto copy4 = [](void* dst, const void* src) {
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(tc::smem_u32(dst)), "l"(src) : "memory");
       };
-      // places of tile x, whose pages have been looked up
-      auto place = [&](uint32_t x) {
-        if (!more) return;
-        if (x >= 4) wait(ctl, &ctl.taken[x & 3], ((x >> 2) - 1) & 1);
-        __syncwarp();
-        const int hk = nx.s.grp / g.blocks, p0 = nx.s.base + (nx.ct + nt) * kKeys;
-        Info& f = ctl.tile[x % kInfos];
-#pragma unroll
-        for (int j = 0; j < kMine; ++j) {
-          const int p = p0 + lane + 32 * j, sl = p - page_index(g, p) * c.page_size;
-          const bool ok = page[j] >= 0;
-          ctl.off[x & 3][lane + 32 * j] = ok ? kv_page_offset(c, page[j]) + (int64_t)sl * c.slot_stride + hk * c.head_stride : -1;
-          if (E8) {
-            kb[j] = vb[j] = -1;
-            if (ok) {
-              const int64_t so = page[j] * a.sc.page_stride + (int64_t)sl * a.sc.slot_stride + hk * a.sc.head_stride;
-              kb[j] = a.sc.k[so];
-              vb[j] = a.sc.v[so];
-            }
-          }
-          const uint32_t word = __ballot_sync(0xffffffffu, ok);
-          if (lane == j) f.valid[j] = word;
-        }
-        if (lane >= kMine && lane < 4) f.valid[lane] = 0xffffffffu;
-        if (lane == 0) {
-          f.p0 = p0, f.n = nx.s.n, f.lo = nx.s.lo;
-          const bool differ = a.mask && (p0 + kKeys > nx.s.n || (a.window > 0 && p0 < nx.s.lo + 64));
-          f.flags = differ ? 1 | (nx.index & 15) << 1 : 0;
-          if (nt == 0) ctl.bad[nx.index & 15][0] = ctl.bad[nx.index & 15][1] = 0;
-        }
-        if (++nt == nx.cnt) {
-          nt = 0;
-          more = nx.next();
-        }
-      };
+      Walk<kKeys> n2 = nx;  // two
+      bool more = true, more2 = true;
 #pragma unroll 1
       for (int64_t at = -2; at < tiles; ++at) {
         const uint32_t x = (uint32_t)at;
+        asm volatile("cp.async.wait_all;" ::: "memory");
         if (at >= 0) {
-        int own[2][kMine];
-#pragma unroll
-        for (int j = 0; j < kMine; ++j) own[0][j] = kb[j], own[1][j] = vb[j];
-        if (E8) {
           Info& f = ctl.tile[x % kInfos];
-          // bytes in [63, 247]; 255 takes no part in the largest
-          auto fit = [](int b) { return b < 0 || b == 255 ? -1 : min(max(b, 63), 247); };
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            int big = -1;
-#pragma unroll
-            for (int j = 0; j < kMine; ++j) big = max(big, fit(own[i][j]));
-            big = __reduce_max_sync(0xffffffffu, big);
-            if (big < 0) big = 127;
-#pragma unroll
-            for (int j = 0; j < kMine; ++j) {
-              const int b = own[i][j], d = fit(b) - big;  // at most 0; a factor below 2^-24 is 0
-              const float f = b < 0 ? 0.0f : b == 255 ? CUDART_NAN_F : __int_as_float(max(127 + d, 0) << 23);
-              ctl.fac[x & 3][i][lane + 32 * j] = pack2<__half>(f, f);
+          if (E8) {
+#pragma unroll 1
+            for (int i = 0; i < 2; ++i) {
+              auto byte_of = [&](int r) {
+                const int w = ctl.page[x & 1][r];
+                return w < 0 ? -1 : (int)(ctl.word[x & 1][i][r] >> (8 * ((w >> (2 * i)) & 3))) & 255;
+              };
+              // bytes in [63, 247]; 255 takes no part in the largest
+              auto fit = [](int b) { return b < 0 || b == 255 ? -1 : min(max(b, 63), 247); };
+              int big = -1;
+#pragma unroll 1
+              for (int r = lane; r < kKeys; r += 32) big = max(big, fit(byte_of(r)));
+              big = __reduce_max_sync(0xffffffffu, big);
+              if (big < 0) big = 127;
+#pragma unroll 1
+              for (int r = lane; r < kKeys; r += 32) {
+                const int b = byte_of(r), d = fit(b) - big;  // at most 0; a factor below 2^-24 is 0
+                const float z = b < 0 ? 0.0f : b == 255 ? CUDART_NAN_F : __int_as_float(max(127 + d, 0) << 23);
+                ctl.fac[x & 3][i][r] = __half_as_ushort(__float2half_rn(z));
+              }
+              if (lane == 0) (i ? f.ev : f.ek) = (float)(big - 127);
             }
-            if (lane == 0) (i ? f.ev : f.ek) = (float)(big - 127);
+          }
+          __syncwarp();
+          if (lane == 0) {
+            tc::mbar_arrive(&ctl.info[x % kInfos]);
+            tc::mbar_arrive(&ctl.placed[x & 3]);
           }
         }
-        __syncwarp();
-        if (lane == 0) {
-          tc::mbar_arrive(&ctl.info[x % kInfos]);
-          tc::mbar_arrive(&ctl.placed[x & 3]);
+        if (at >= -1 && more) {  // places of tile x + 1
+          const uint32_t y = x + 1;
+          if (y >= 4) wait(ctl, &ctl.taken[y & 3], ((y >> 2) - 1) & 1);
+          __syncwarp();
+          const Seg& s = nx.s;
+          const int p0 = s.base + (nx.ct + nt) * kKeys;
+          Info& f = ctl.tile[y % kInfos];
+#pragma unroll 1
+          for (int j = 0; j < kMine; ++j) {
+            const int r = lane + 32 * j, p = p0 + r, sl = p - g.page.of(p) * c.page_size, page = ctl.page[y & 1][r];
+            const bool ok = page >= 0 && page < c.n_pages;
+            ctl.off[y & 3][r] = ok ? kv_page_offset(c, page) + (int64_t)sl * c.slot_stride + s.hk * c.head_stride : -1;
+            if (E8) {
+              int w = -1;
+              if (ok) {
+                const int64_t so = page * a.sc.page_stride + (int64_t)sl * a.sc.slot_stride + s.hk * a.sc.head_stride;
+                const uintptr_t k = reinterpret_cast<uintptr_t>(a.sc.k + so), v = reinterpret_cast<uintptr_t>(a.sc.v + so);
+                w = (int)(k & 3) | (int)(v & 3) << 2;
+                copy4(&ctl.word[y & 1][0][r], reinterpret_cast<const void*>(k & ~(uintptr_t)3));
+                copy4(&ctl.word[y & 1][1][r], reinterpret_cast<const void*>(v & ~(uintptr_t)3));
+              }
+              ctl.page[y & 1][r] = w;
+            }
+            const uint32_t word = __ballot_sync(0xffffffffu, ok);
+            if (lane == 0) f.valid[j] = word;
+          }
+          if (lane >= kMine && lane < 4) f.valid[lane] = 0xffffffffu;
+          if (lane == 0) {
+            f.p0 = p0, f.n = s.n, f.lo = s.lo;
+            const bool differ = a.mask && (p0 + kKeys > s.n || (a.window > 0 && p0 < s.lo + 64));
+            f.flags = differ ? 1 | (nx.index & 15) << 1 : 0;
+            if (nt == 0) ctl.bad[nx.index & 15][0] = ctl.bad[nx.index & 15][1] = 0;
+          }
+          if (++nt == nx.cnt) {
+            nt = 0;
+            more = nx.next();
+          }
         }
+        if (more2) {  // table entries of tile x + 2
+          const int p0 = n2.s.base + t2 * kKeys;
+#pragma unroll 1
+          for (int r = lane; r < kKeys; r += 32) {
+            const int p = p0 + r;
+            if (p >= n2.s.lo && p < n2.s.end)
+              copy4(&ctl.page[x & 1][r], c.table + (int64_t)n2.s.b * c.table_stride + g.page.of(p));
+            else
+              ctl.page[x & 1][r] = -1;
+          }
+          if (++t2 == n2.ct + n2.cnt) {
+            more2 = n2.next();
+            t2 = n2.ct;
+          }
         }
-        if (at >= -1) place(x + 1);
-        look();
       }
+      asm volatile("cp.async.wait_all;" ::: "memory");
     }
     if (warp == 8) {
     // ================================================== products
@@ -746,7 +740,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       uint32_t e0 = 0;          // entry of the segment's first keys
       Walk<kKeys> w(g, ctl.where, tiles);
       do {
-        const int rows = min(R - w.s.grp % g.blocks * S::kRows, S::kRows), nt = w.cnt;
+        const int rows = min(R - w.s.blk * S::kRows, S::kRows), nt = w.cnt;
         const int tracks = WIDE && rows > 128 ? 2 : 1;  // of rows with products of their own
         const int qb = w.index % S::kQs;
         wait(ctl, &ctl.q_full[qb], (w.index / S::kQs) & 1);
@@ -825,14 +819,17 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     // queries of a segment's block of rows
     auto load_q = [&](const Walk<kKeys>& w) {
       const Seg& s = w.s;
-      const int hk = s.grp / g.blocks, r0 = s.grp % g.blocks * S::kRows, rows = min(R - r0, S::kRows);
+      const int hk = s.hk, r0 = s.blk * S::kRows, rows = min(R - r0, S::kRows);
       const int qb = w.index % S::kQs;
       if (w.index >= S::kQs) wait(ctl, &ctl.q_empty[qb], (w.index / S::kQs - 1) & 1);
       __syncwarp();
       const T* q = (const T*)a.q + s.b * a.q_seq + (int64_t)hk * G * a.q_head;
       constexpr int kStep = kN / kChunks;
       const int ch = pt % kChunks;
-      auto row_of = [&](int r) { return q + ((r0 + r) / G) * a.q_node + ((r0 + r) % G) * a.q_head + ch * 8; };
+      auto row_of = [&](int r) {
+        const int node = g.group.of(r0 + r);
+        return q + node * a.q_node + (r0 + r - node * G) * a.q_head + ch * 8;
+      };
       auto place = [&](int r) { return qb * S::kQBytes + (r >> 7) * (128 * 128 * (D / 64)) + chunk_at(r & 127, ch, 128); };
       if constexpr (!E8) {
 #pragma unroll 4
@@ -897,11 +894,18 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       constexpr int kPass = kN / kChunks;  // rows of a pass
       const int row0 = pt / kChunks, ch = pt % kChunks;
       uint32_t issued = 0;
-      // values that are not finite, where rows attend to them differently, become zeros and a mark
-      auto spoils = [&](const Info& f) {
-        const uint32_t at = S::kQs * S::kQBytes + (issued % kEntries) * S::kEntry;
+      // Values that are not finite, where rows attend to them differently, become zeros and a mark.  The entry
+      // is looked through after the next one has been sent for.
+      int waiting = -1;
+      const Info* of = nullptr;
+      auto spoils = [&](bool last) {
+        if (last)
+          asm volatile("cp.async.wait_group 0;" ::: "memory");
+        else
+          asm volatile("cp.async.wait_group 1;" ::: "memory");
+        const Info& f = *of;
+        const uint32_t at = S::kQs * S::kQBytes + (waiting % kEntries) * S::kEntry;
         unsigned long long* bad = ctl.bad[f.flags >> 1];
-        asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll 1
         for (int r = row0; r < kKeys; r += kPass) {
           int which;
@@ -921,6 +925,9 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             atomicOr(&bad[which], bit);
           }
         }
+        tc::fence_async_smem();
+        tc::mbar_arrive(&ctl.full[waiting % kEntries]);
+        waiting = -1;
       };
       do {
         for (int t = 0; t < w.cnt; ++t, ++tile) {
@@ -943,10 +950,11 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
               for (int i = 0; i < kAtOnce; ++i)
                 copy16(dst + chunk_at(row0 + (i0 + i) * kPass, ch, kKeys), src + (o[i] < 0 ? 0 : o[i]), o[i] >= 0);
             }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            if (__builtin_expect(waiting >= 0, 0)) spoils(false);
             if (__builtin_expect(kv && (f.flags & 1), 0)) {
-              spoils(f);
-              tc::fence_async_smem();
-              tc::mbar_arrive(&ctl.full[issued % kEntries]);
+              waiting = (int)issued;
+              of = &f;
             } else {
               // the thread arrives when its copies have landed
               asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tc::smem_u32(&ctl.full[issued % kEntries])) : "memory");
@@ -958,6 +966,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           if (S::kQs == 1 && t == 0) load_q(w);
         }
       } while (w.next());
+      if (waiting >= 0) spoils(true);
       asm volatile("cp.async.wait_all;" ::: "memory");
     } else {
       // Codes are copied to a stage of their own, kStages entries ahead, where the thread that copied
@@ -982,7 +991,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         asm volatile("cp.async.commit_group;" ::: "memory");
       };
       // a value that is no number, where rows attend to it differently, becomes zero and a mark
-      auto spoils = [&](unsigned char* from, uint32_t* fac, const Info& f) {
+      auto spoils = [&](unsigned char* from, uint16_t* fac, const Info& f) {
         unsigned long long* bad = ctl.bad[f.flags >> 1];
 #pragma unroll 1
         for (int i = 0; i < kEach; ++i) {
@@ -1008,7 +1017,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         }
         __syncwarp();
       };
-      auto put = [&](uint32_t e, uint32_t* fac, bool check, const Info& f) {
+      auto put = [&](uint32_t e, uint16_t* fac, bool check, const Info& f) {
         asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
         if (e >= kEntries) wait(ctl, &ctl.empty[e % kEntries], (e / kEntries - 1) & 1);
         __syncwarp();
@@ -1027,7 +1036,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
           const int r = row0 + (i0 + i) * kPass;
-          const uint32_t fr = fr4[i];
+          const uint32_t fr = fr4[i] * 0x10001u;
           const uint32_t* y = reinterpret_cast<const uint32_t*>(&z4[i]);
           uint4 h[2];
           uint32_t* hw = reinterpret_cast<uint32_t*>(h);
@@ -1055,7 +1064,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       do {
         for (int t = 0; t < w.cnt; ++t, ++tile) {
           const Info& f = ctl.tile[tile % kInfos];
-          uint32_t (*fac)[128] = ctl.fac[tile & 3];
+          uint16_t (*fac)[kKeys] = ctl.fac[tile & 3];
           if (S::kQs == 2 && t == 0) load_q(w);
 #pragma unroll 1
           for (int kv = 0; kv < 2; ++kv) {
@@ -1151,13 +1160,8 @@ static pe_status go(const TreeArgs& a, void* ws, int32_t* error, cudaStream_t st
   g.a = a;
   g.blocks = ceil_div(rows, S::kRows);
   g.groups = a.c.n_heads * g.blocks;
-  // with 2^s the power of two at or above the page size d: floor(2^(31 + s) / d) + 1 (Granlund and Montgomery)
-  const uint32_t d = a.c.page_size;
-  while ((1u << g.page_shift) < d) ++g.page_shift;
-  if ((1u << g.page_shift) != d) {
-    g.page_mul = (uint32_t)(((uint64_t)1 << (31 + g.page_shift)) / d + 1);
-    g.page_shift -= 1;
-  }
+  g.page = divisor(a.c.page_size);
+  g.group = divisor(a.n_q_heads / a.c.n_heads);
   g.meta = reinterpret_cast<SegMeta*>(ws);
   g.part = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + kMetaBytes);
   g.error = error;
