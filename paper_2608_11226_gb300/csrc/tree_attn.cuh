@@ -54,6 +54,7 @@ struct Shape {
   static_assert(!(WIDE && D == 256), "two outputs of 256 columns leave no room for scores");
   static constexpr int kKeys = D == 256 ? 64 : 128;
   static constexpr int kRows = WIDE ? 256 : 128;  // of a block
+  static constexpr int kShared = WIDE ? 1 : 128;  // rows that two threads share
   static constexpr int kProducers = 4;            // warps
   static constexpr int kThreads = 512;
   static constexpr int kEntry = kKeys * D * 2;
@@ -68,7 +69,7 @@ struct Shape {
   static constexpr int kO = 0, kOStep = 128, kS = 256, kSStep = WIDE ? 128 : kKeys;
   static constexpr int kP = WIDE ? 256 : D == 256 ? 384 : 128, kPStep = WIDE ? 128 : kKeys / 2;
   static_assert(kSmem > kPdlTmemSmem, "no second kernel with tensor memory beside it");
-  static_assert(kSmem + 17000 <= 232448, "shared memory of an SM");
+  static_assert(kSmem + 14000 <= 232448, "shared memory of an SM");
 };
 
 struct Info {  // a tile
@@ -79,15 +80,14 @@ struct Info {  // a tile
 
 template <class S>
 struct Control {
-  uint64_t full[8], empty[8], info[kInfos], placed[4], taken[4], q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2], fin;
+  uint64_t full[8], empty[8], info[kInfos], paged[8], placed[4], taken[4], q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2], fin;
   Info tile[kInfos];
   unsigned long long bad[16][2];  // per segment: nodes, and positions from lo on, with values that are not finite
   int64_t off[4][S::kKeys];      // element offsets of a tile's rows, -1: none
-  int page[2][S::kKeys];         // pages of a tile's rows; then which byte of its word a row's scales are; -1: no row
-  uint32_t word[2][2][S::kKeys];  // the words of the rows' scales
+  int page[8][S::kKeys];         // pages of a tile's rows, -1: none
   uint16_t fac[4][2][S::kKeys];  // 2^(e - E) in fp16
   int64_t sum[16];
-  float mx[2][2][128], l[2][128], qf[4][S::kRows];
+  float mx[2][2][S::kShared], l[2][S::kShared], qf[4][S::kRows];
   int where[4];
   uint32_t tmem;
   int err;
@@ -311,6 +311,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
   constexpr int kKeys = S::kKeys, kChunks = D / 8, kEntries = S::kEntries;
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(16) Control<S> ctl;
+  static_assert(S::kSmem + sizeof(Control<S>) <= 232448, "shared memory of an SM");
   const TreeArgs& a = g.a;
   const pe_kv_cache& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -324,9 +325,11 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       tc::mbar_init(&ctl.full[i], E8 ? S::kProducers : 32 * S::kProducers);
       tc::mbar_init(&ctl.empty[i], 1);
     }
-    for (int i = 0; i < kInfos; ++i) tc::mbar_init(&ctl.info[i], 1);
+    constexpr int kPlacers = E8 ? 3 : 1;  // warps
+    for (int i = 0; i < kInfos; ++i) tc::mbar_init(&ctl.info[i], kPlacers);
+    for (int i = 0; i < 8; ++i) tc::mbar_init(&ctl.paged[i], 1);
     for (int i = 0; i < 4; ++i) {
-      tc::mbar_init(&ctl.placed[i], 1);
+      tc::mbar_init(&ctl.placed[i], kPlacers);
       tc::mbar_init(&ctl.taken[i], S::kProducers);
     }
     tc::mbar_init(&ctl.fin, 1);
@@ -623,106 +626,129 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
     if (warp == 9) {
     // ================================================== places
-      // A lane finds the places of rows lane, lane + 32, ... and, of codes, what brings their scales to the
-      // tile's largest.  Table entries are copied two tiles ahead and scales one (the words they are in).
-      constexpr int kMine = kKeys / 32;
-      Walk<kKeys> nx(g, ctl.where, tiles);  // one tile ahead of what is told
-      int nt = 0, t2 = nx.ct;
-      auto copy4 = [](void* dst, const void* src) {
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(tc::smem_u32(dst)), "l"(src) : "memory");
-      };
-      Walk<kKeys> n2 = nx;  // two
-      bool more = true, more2 = true;
+      // A lane finds the places of rows lane, lane + 32, ...; table entries are copied kAhead tiles ahead
+      constexpr int kMine = kKeys / 32, kAhead = 3;
+      Walk<kKeys> nx(g, ctl.where, tiles), far = nx;
+      int nt = 0, tf = nx.ct;
+      bool more = true;
 #pragma unroll 1
-      for (int64_t at = -2; at < tiles; ++at) {
-        const uint32_t x = (uint32_t)at;
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        if (at >= 0) {
-          Info& f = ctl.tile[x % kInfos];
-          if (E8) {
+      for (int64_t at = -kAhead; at < tiles; ++at) {
+        if (more) {  // table entries of tile at + kAhead
+          const int p0 = far.s.base + tf * kKeys;
+          int* to = ctl.page[(uint32_t)(at + kAhead) & 7];
 #pragma unroll 1
-            for (int i = 0; i < 2; ++i) {
-              auto byte_of = [&](int r) {
-                const int w = ctl.page[x & 1][r];
-                return w < 0 ? -1 : (int)(ctl.word[x & 1][i][r] >> (8 * ((w >> (2 * i)) & 3))) & 255;
-              };
-              // bytes in [63, 247]; 255 takes no part in the largest
-              auto fit = [](int b) { return b < 0 || b == 255 ? -1 : min(max(b, 63), 247); };
-              int big = -1;
-#pragma unroll 1
-              for (int r = lane; r < kKeys; r += 32) big = max(big, fit(byte_of(r)));
-              big = __reduce_max_sync(0xffffffffu, big);
-              if (big < 0) big = 127;
-#pragma unroll 1
-              for (int r = lane; r < kKeys; r += 32) {
-                const int b = byte_of(r), d = fit(b) - big;  // at most 0; a factor below 2^-24 is 0
-                const float z = b < 0 ? 0.0f : b == 255 ? CUDART_NAN_F : __int_as_float(max(127 + d, 0) << 23);
-                ctl.fac[x & 3][i][r] = __half_as_ushort(__float2half_rn(z));
-              }
-              if (lane == 0) (i ? f.ev : f.ek) = (float)(big - 127);
-            }
+          for (int r = lane; r < kKeys; r += 32) {
+            const int p = p0 + r;
+            if (p >= far.s.lo && p < far.s.end)
+              asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(tc::smem_u32(to + r)),
+                           "l"(c.table + (int64_t)far.s.b * c.table_stride + g.page.of(p))
+                           : "memory");
+            else
+              to[r] = -1;
           }
+          if (++tf == far.ct + far.cnt) {
+            more = far.next();
+            tf = far.ct;
+          }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (at < 0) continue;
+        const uint32_t x = (uint32_t)at;
+        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+        if (x >= 4) wait(ctl, &ctl.taken[x & 3], ((x >> 2) - 1) & 1);
+        __syncwarp();
+        const Seg& s = nx.s;
+        const int p0 = s.base + (nx.ct + nt) * kKeys;
+        int* pages = ctl.page[x & 7];
+        Info& f = ctl.tile[x % kInfos];
+#pragma unroll
+        for (int j = 0; j < kMine; ++j) {
+          const int r = lane + 32 * j, p = p0 + r, sl = p - g.page.of(p) * c.page_size, page = pages[r];
+          const bool ok = page >= 0 && page < c.n_pages;
+          ctl.off[x & 3][r] = ok ? kv_page_offset(c, page) + (int64_t)sl * c.slot_stride + s.hk * c.head_stride : -1;
+          if (E8 && !ok) pages[r] = -1;
+          const uint32_t word = __ballot_sync(0xffffffffu, ok);
+          if (lane == 0) f.valid[j] = word;
+        }
+        if (lane >= kMine && lane < 4) f.valid[lane] = 0xffffffffu;
+        if (lane == 0) {
+          f.p0 = p0, f.n = s.n, f.lo = s.lo;
+          const bool differ = a.mask && (p0 + kKeys > s.n || (a.window > 0 && p0 < s.lo + 64));
+          f.flags = differ ? 1 | (nx.index & 15) << 1 : 0;
+          if (nt == 0) ctl.bad[nx.index & 15][0] = ctl.bad[nx.index & 15][1] = 0;
+        }
+        __syncwarp();
+        if (lane == 0) {
+          if (E8) tc::mbar_arrive(&ctl.paged[x & 7]);
+          tc::mbar_arrive(&ctl.info[x % kInfos]);
+          tc::mbar_arrive(&ctl.placed[x & 3]);
+        }
+        if (++nt == nx.cnt) {
+          nt = 0;
+          nx.next();
+        }
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+    }
+    if (E8 && warp >= 10) {
+      // ================================================ scales: of keys, of values
+      // What brings a row's scale to the tile's largest; bytes are loaded two tiles ahead
+      constexpr int kMine = kKeys / 32;
+      const int which = warp - 10;
+      const uint8_t* base = which ? a.sc.v : a.sc.k;
+      Walk<kKeys> far(g, ctl.where, tiles);
+      int tf = far.ct, b[2][kMine];
+      bool more = true;
+      auto load = [&](int (&to)[kMine], uint32_t x) {
+        if (!more) return;
+        wait(ctl, &ctl.paged[x & 7], (x >> 3) & 1);
+        __syncwarp();
+        const int* pages = ctl.page[x & 7];
+        const uint8_t* head = base + far.s.hk * a.sc.head_stride;
+        const int p0 = far.s.base + tf * kKeys;
+#pragma unroll
+        for (int j = 0; j < kMine; ++j) {
+          const int r = lane + 32 * j, p = p0 + r, page = pages[r];
+          to[j] = page < 0 ? -1 : head[page * a.sc.page_stride + (int64_t)(p - g.page.of(p) * c.page_size) * a.sc.slot_stride];
+        }
+        if (++tf == far.ct + far.cnt) {
+          more = far.next();
+          tf = far.ct;
+        }
+      };
+      load(b[0], 0);
+      load(b[1], 1);
+#pragma unroll 1
+      for (uint32_t x0 = 0; x0 < (uint32_t)tiles; x0 += 2) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t x = x0 + i;
+          if (x >= (uint32_t)tiles) break;
+          // bytes in [63, 247]; 255 takes no part in the largest
+          auto fit = [](int b) { return b < 0 || b == 255 ? -1 : min(max(b, 63), 247); };
+          int big = -1;
+#pragma unroll
+          for (int j = 0; j < kMine; ++j) big = max(big, fit(b[i][j]));
+          big = __reduce_max_sync(0xffffffffu, big);
+          if (big < 0) big = 127;
+          if (x >= 4) wait(ctl, &ctl.taken[x & 3], ((x >> 2) - 1) & 1);
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < kMine; ++j) {
+            const int d = fit(b[i][j]) - big;  // at most 0; a factor below 2^-24 is 0
+            const float z = b[i][j] < 0 ? 0.0f : b[i][j] == 255 ? CUDART_NAN_F : __int_as_float(max(127 + d, 0) << 23);
+            ctl.fac[x & 3][which][lane + 32 * j] = __half_as_ushort(__float2half_rn(z));
+          }
+          Info& f = ctl.tile[x % kInfos];
+          if (lane == 0) (which ? f.ev : f.ek) = (float)(big - 127);
           __syncwarp();
           if (lane == 0) {
             tc::mbar_arrive(&ctl.info[x % kInfos]);
             tc::mbar_arrive(&ctl.placed[x & 3]);
           }
-        }
-        if (at >= -1 && more) {  // places of tile x + 1
-          const uint32_t y = x + 1;
-          if (y >= 4) wait(ctl, &ctl.taken[y & 3], ((y >> 2) - 1) & 1);
-          __syncwarp();
-          const Seg& s = nx.s;
-          const int p0 = s.base + (nx.ct + nt) * kKeys;
-          Info& f = ctl.tile[y % kInfos];
-#pragma unroll 1
-          for (int j = 0; j < kMine; ++j) {
-            const int r = lane + 32 * j, p = p0 + r, sl = p - g.page.of(p) * c.page_size, page = ctl.page[y & 1][r];
-            const bool ok = page >= 0 && page < c.n_pages;
-            ctl.off[y & 3][r] = ok ? kv_page_offset(c, page) + (int64_t)sl * c.slot_stride + s.hk * c.head_stride : -1;
-            if (E8) {
-              int w = -1;
-              if (ok) {
-                const int64_t so = page * a.sc.page_stride + (int64_t)sl * a.sc.slot_stride + s.hk * a.sc.head_stride;
-                const uintptr_t k = reinterpret_cast<uintptr_t>(a.sc.k + so), v = reinterpret_cast<uintptr_t>(a.sc.v + so);
-                w = (int)(k & 3) | (int)(v & 3) << 2;
-                copy4(&ctl.word[y & 1][0][r], reinterpret_cast<const void*>(k & ~(uintptr_t)3));
-                copy4(&ctl.word[y & 1][1][r], reinterpret_cast<const void*>(v & ~(uintptr_t)3));
-              }
-              ctl.page[y & 1][r] = w;
-            }
-            const uint32_t word = __ballot_sync(0xffffffffu, ok);
-            if (lane == 0) f.valid[j] = word;
-          }
-          if (lane >= kMine && lane < 4) f.valid[lane] = 0xffffffffu;
-          if (lane == 0) {
-            f.p0 = p0, f.n = s.n, f.lo = s.lo;
-            const bool differ = a.mask && (p0 + kKeys > s.n || (a.window > 0 && p0 < s.lo + 64));
-            f.flags = differ ? 1 | (nx.index & 15) << 1 : 0;
-            if (nt == 0) ctl.bad[nx.index & 15][0] = ctl.bad[nx.index & 15][1] = 0;
-          }
-          if (++nt == nx.cnt) {
-            nt = 0;
-            more = nx.next();
-          }
-        }
-        if (more2) {  // table entries of tile x + 2
-          const int p0 = n2.s.base + t2 * kKeys;
-#pragma unroll 1
-          for (int r = lane; r < kKeys; r += 32) {
-            const int p = p0 + r;
-            if (p >= n2.s.lo && p < n2.s.end)
-              copy4(&ctl.page[x & 1][r], c.table + (int64_t)n2.s.b * c.table_stride + g.page.of(p));
-            else
-              ctl.page[x & 1][r] = -1;
-          }
-          if (++t2 == n2.ct + n2.cnt) {
-            more2 = n2.next();
-            t2 = n2.ct;
-          }
+          load(b[i], x + 2);
         }
       }
-      asm volatile("cp.async.wait_all;" ::: "memory");
     }
     if (warp == 8) {
     // ================================================== products
