@@ -80,7 +80,7 @@ struct Info {  // a tile
 
 template <class S>
 struct Control {
-  uint64_t full[8], empty[8], info[kInfos], paged[8], placed[4], taken[4], q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2], fin;
+  uint64_t full[8], empty[8], info[kInfos], paged[8], placed[4], taken[4], staged[4], unstaged[4], q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2], fin;
   Info tile[kInfos];
   unsigned long long bad[16][2];  // per segment: nodes, and positions from lo on, with values that are not finite
   int64_t off[4][S::kKeys];      // element offsets of a tile's rows, -1: none
@@ -330,7 +330,9 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     for (int i = 0; i < 8; ++i) tc::mbar_init(&ctl.paged[i], 1);
     for (int i = 0; i < 4; ++i) {
       tc::mbar_init(&ctl.placed[i], kPlacers);
-      tc::mbar_init(&ctl.taken[i], S::kProducers);
+      tc::mbar_init(&ctl.taken[i], E8 ? S::kProducers + 2 : S::kProducers);
+      tc::mbar_init(&ctl.staged[i], 32);
+      tc::mbar_init(&ctl.unstaged[i], S::kProducers);
     }
     tc::mbar_init(&ctl.fin, 1);
     for (int i = 0; i < 2; ++i) {
@@ -690,14 +692,15 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
     }
-    if (E8 && warp >= 10) {
+    if constexpr (E8) if (warp >= 10) {
       // ================================================ scales: of keys, of values
-      // What brings a row's scale to the tile's largest; bytes are loaded two tiles ahead
+      // What brings a row's scale to the tile's largest; bytes are loaded a tile ahead.  Then the codes
+      // themselves, to a stage: copies wait their turn here, apart from the warps that widen them.
       constexpr int kMine = kKeys / 32;
       const int which = warp - 10;
       const uint8_t* base = which ? a.sc.v : a.sc.k;
       Walk<kKeys> far(g, ctl.where, tiles);
-      int tf = far.ct, b[2][kMine];
+      int tf = far.ct, b[kMine], next[kMine];
       bool more = true;
       auto load = [&](int (&to)[kMine], uint32_t x) {
         if (!more) return;
@@ -716,27 +719,23 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           tf = far.ct;
         }
       };
-      load(b[0], 0);
-      load(b[1], 1);
+      load(b, 0);
 #pragma unroll 1
-      for (uint32_t x0 = 0; x0 < (uint32_t)tiles; x0 += 2) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t x = x0 + i;
-          if (x >= (uint32_t)tiles) break;
+      for (uint32_t x = 0; x < (uint32_t)tiles; ++x) {
+        {
           // bytes in [63, 247]; 255 takes no part in the largest
           auto fit = [](int b) { return b < 0 || b == 255 ? -1 : min(max(b, 63), 247); };
           int big = -1;
 #pragma unroll
-          for (int j = 0; j < kMine; ++j) big = max(big, fit(b[i][j]));
+          for (int j = 0; j < kMine; ++j) big = max(big, fit(b[j]));
           big = __reduce_max_sync(0xffffffffu, big);
           if (big < 0) big = 127;
           if (x >= 4) wait(ctl, &ctl.taken[x & 3], ((x >> 2) - 1) & 1);
           __syncwarp();
 #pragma unroll
           for (int j = 0; j < kMine; ++j) {
-            const int d = fit(b[i][j]) - big;  // at most 0; a factor below 2^-24 is 0
-            const float z = b[i][j] < 0 ? 0.0f : b[i][j] == 255 ? CUDART_NAN_F : __int_as_float(max(127 + d, 0) << 23);
+            const int d = fit(b[j]) - big;  // at most 0; a factor below 2^-24 is 0
+            const float z = b[j] < 0 ? 0.0f : b[j] == 255 ? CUDART_NAN_F : __int_as_float(max(127 + d, 0) << 23);
             ctl.fac[x & 3][which][lane + 32 * j] = __half_as_ushort(__float2half_rn(z));
           }
           Info& f = ctl.tile[x % kInfos];
@@ -746,9 +745,30 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             tc::mbar_arrive(&ctl.info[x % kInfos]);
             tc::mbar_arrive(&ctl.placed[x & 3]);
           }
-          load(b[i], x + 2);
+          load(next, x + 1);
+          const uint32_t e = 2 * x + which, st = e % S::kStages;
+          if (e >= S::kStages) wait(ctl, &ctl.unstaged[st], (e / S::kStages - 1) & 1);
+          __syncwarp();
+          constexpr int kCh = D / 16, kPass = 32 / kCh, kAtOnce = 4;
+          const int64_t* offs = ctl.off[x & 3] + lane / kCh;
+          const uint8_t* codes = (const uint8_t*)(which ? c.v : c.k) + lane % kCh * 16;
+          const uint32_t dst = ring + kEntries * S::kEntry + st * (S::kEntry / 2) + lane * 16;
+#pragma unroll 1
+          for (int i0 = 0; i0 < kKeys / kPass; i0 += kAtOnce) {
+            int64_t o[kAtOnce];  // read ahead of the copies, which the compiler keeps in their order
+#pragma unroll
+            for (int y = 0; y < kAtOnce; ++y) o[y] = offs[(i0 + y) * kPass];
+#pragma unroll
+            for (int y = 0; y < kAtOnce; ++y) copy16(dst + (i0 + y) * 512, codes + (o[y] < 0 ? 0 : o[y]), o[y] >= 0);
+          }
+          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tc::smem_u32(&ctl.staged[st])) : "memory");
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(&ctl.taken[x & 3]);
+#pragma unroll
+          for (int j = 0; j < kMine; ++j) b[j] = next[j];
         }
       }
+      asm volatile("cp.async.wait_all;" ::: "memory");
     }
     if (warp == 8) {
     // ================================================== products
@@ -822,7 +842,10 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           }
           if (any) {
             t0 = clock64();
-          } else if (clock64() - t0 > 4000000000LL || *(volatile int*)&ctl.err) {
+            continue;
+          }
+          __nanosleep(20);
+          if (clock64() - t0 > 4000000000LL || *(volatile int*)&ctl.err) {
             atomicExch(&ctl.err, 1);
             break;
           }
@@ -995,27 +1018,11 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       if (waiting >= 0) spoils(true);
       asm volatile("cp.async.wait_all;" ::: "memory");
     } else {
-      // Codes are copied to a stage of their own, kStages entries ahead, where the thread that copied
-      // a chunk finds it again; as fp16 they go to the ring.
+      // Codes are widened from their stage into the ring
       constexpr int kCh = D / 16, kPass = kN / kCh, kEach = kKeys / kPass;  // 16-code chunks of a row; rows of a pass; of a thread
       constexpr int kStages = S::kStages;
       const int row0 = pt / kCh, ch = pt % kCh;
       unsigned char* stages = smem + S::kQs * S::kQBytes + kEntries * S::kEntry + pt * 16;
-      const uint32_t stages_at = tc::smem_u32(stages);
-      // entry e (keys and values in turn), of a tile whose rows have been placed
-      auto copy = [&](uint32_t e, bool there) {
-        if (there) {
-          const int64_t* offs = ctl.off[(e >> 1) & 3];
-          const uint8_t* base = (const uint8_t*)(e & 1 ? c.v : c.k) + ch * 16;
-          const uint32_t dst = stages_at + (e % kStages) * (S::kEntry / 2);
-          int64_t o[kEach];  // read ahead of the copies, which the compiler keeps in their order
-#pragma unroll
-          for (int i = 0; i < kEach; ++i) o[i] = offs[row0 + i * kPass];
-#pragma unroll
-          for (int i = 0; i < kEach; ++i) copy16(dst + i * kN * 16, base + (o[i] < 0 ? 0 : o[i]), o[i] >= 0);
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-      };
       // a value that is no number, where rows attend to it differently, becomes zero and a mark
       auto spoils = [&](unsigned char* from, uint16_t* fac, const Info& f) {
         unsigned long long* bad = ctl.bad[f.flags >> 1];
@@ -1044,66 +1051,62 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         __syncwarp();
       };
       auto put = [&](uint32_t e, uint16_t* fac, bool check, const Info& f) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        wait(ctl, &ctl.staged[e % kStages], (e / kStages) & 1);
         if (e >= kEntries) wait(ctl, &ctl.empty[e % kEntries], (e / kEntries - 1) & 1);
         __syncwarp();
         unsigned char* from = stages + (e % kStages) * (S::kEntry / 2);
-        if (__builtin_expect(check, 0)) spoils(from, fac, f);
+        if (__builtin_expect(check, 0)) spoils(from, fac, f);  // (a row's lanes are in one warp)
         unsigned char* dst = smem + S::kQs * S::kQBytes + (e % kEntries) * S::kEntry;
-        // lanes of a row's second half store their halves the other way round: no two in one bank
-        const int flip = (ch >> 2) & 1;
+        // 8 codes from each half of the row: their chunks of the ring meet no bank twice
         constexpr int kAtOnce = 4;
+        const unsigned char* own = from - pt * 16 + row0 * D + ch * 8;
 #pragma unroll 1
         for (int i0 = 0; i0 < kEach; i0 += kAtOnce) {
-        uint32_t fr4[kAtOnce];
-        uint4 z4[kAtOnce];
+          uint32_t fr[kAtOnce];
+          uint2 z[kAtOnce][2];
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) fr4[i] = fac[row0 + (i0 + i) * kPass], z4[i] = *reinterpret_cast<const uint4*>(from + (i0 + i) * kN * 16);
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-          const int r = row0 + (i0 + i) * kPass;
-          const uint32_t fr = fr4[i] * 0x10001u;
-          const uint32_t* y = reinterpret_cast<const uint32_t*>(&z4[i]);
-          uint4 h[2];
-          uint32_t* hw = reinterpret_cast<uint32_t*>(h);
-          const __half2 ff = *reinterpret_cast<const __half2*>(&fr);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            uint32_t v;
-            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(v) : "h"((uint16_t)(y[j / 2] >> (16 * (j & 1)))));
-            const __half2 p = __hmul2(*reinterpret_cast<const __half2*>(&v), ff);
-            hw[j] = *reinterpret_cast<const uint32_t*>(&p);
+          for (int i = 0; i < kAtOnce; ++i) {
+            fr[i] = fac[row0 + (i0 + i) * kPass] * 0x10001u;
+            z[i][0] = *reinterpret_cast<const uint2*>(own + (i0 + i) * kPass * D);
+            z[i][1] = *reinterpret_cast<const uint2*>(own + (i0 + i) * kPass * D + D / 2);
           }
-          *reinterpret_cast<uint4*>(dst + chunk_at(r, 2 * ch + flip, kKeys)) = flip ? h[1] : h[0];
-          *reinterpret_cast<uint4*>(dst + chunk_at(r, 2 * ch + 1 - flip, kKeys)) = flip ? h[0] : h[1];
-        }
+#pragma unroll
+          for (int i = 0; i < kAtOnce; ++i) {
+            const __half2 ff = *reinterpret_cast<const __half2*>(&fr[i]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              uint32_t y[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const uint32_t w = j < 2 ? z[i][h].x : z[i][h].y;
+                uint32_t v;
+                asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(v) : "h"((uint16_t)(w >> (16 * (j & 1)))));
+                const __half2 p = __hmul2(*reinterpret_cast<const __half2*>(&v), ff);
+                y[j] = *reinterpret_cast<const uint32_t*>(&p);
+              }
+              *reinterpret_cast<uint4*>(dst + chunk_at(row0 + (i0 + i) * kPass, ch + h * kCh, kKeys)) = make_uint4(y[0], y[1], y[2], y[3]);
+            }
+          }
         }
         tc::fence_async_smem();
-        arrive(&ctl.full[e % kEntries]);
+        __syncwarp();
+        if (lane == 0) {
+          tc::mbar_arrive(&ctl.full[e % kEntries]);
+          tc::mbar_arrive(&ctl.unstaged[e % kStages]);
+        }
       };
-      const uint32_t entries = (uint32_t)(2 * tiles);
-#pragma unroll
-      for (int e = 0; e < kStages; ++e) {
-        if (!(e & 1) && e < entries) placed(e >> 1);
-        copy(e, e < entries);
-      }
       do {
         for (int t = 0; t < w.cnt; ++t, ++tile) {
+          if (S::kQs == 2 && t == 0) load_q(w);
+          placed(tile);
           const Info& f = ctl.tile[tile % kInfos];
           uint16_t (*fac)[kKeys] = ctl.fac[tile & 3];
-          if (S::kQs == 2 && t == 0) load_q(w);
 #pragma unroll 1
-          for (int kv = 0; kv < 2; ++kv) {
-            const uint32_t e = 2 * tile + kv, next = e + kStages;
-            put(e, fac[kv], kv && (f.flags & 1), f);
-            if (kv) arrive(&ctl.taken[tile & 3]);
-            if (!(next & 1) && next < entries) placed(next >> 1);
-            copy(next, next < entries);
-          }
+          for (int kv = 0; kv < 2; ++kv) put(2 * tile + kv, fac[kv], kv && (f.flags & 1), f);
+          arrive(&ctl.taken[tile & 3]);
           if (S::kQs == 1 && t == 0) load_q(w);
         }
       } while (w.next());
-      asm volatile("cp.async.wait_group 0;" ::: "memory");
     }
   }
   __syncwarp();
