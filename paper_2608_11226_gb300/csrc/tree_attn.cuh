@@ -43,6 +43,7 @@ namespace pe {
 namespace tree {
 
 constexpr int kCtas = 152;
+constexpr int kTurn = 2;    // tiles that a segment's end is worth in the dealing (it takes 6-9 k clk, a tile 3.5 k)
 constexpr int kInfos = 16;  // tiles whose description is kept: what the ring holds, and what is placed ahead
 
 struct SegMeta {
@@ -148,28 +149,31 @@ struct Walk {
   const Args& g;
   Seg s;
   int ct, cnt, ahead, index;  // first tile and tiles of this CTA in the segment; the next sequence's length; segments behind
-  int64_t left;
-  __device__ __forceinline__ Walk(const Args& g, const int* where, int64_t tiles) : g(g) {
+  int64_t left;               // of the share, this segment's part included
+  __device__ __forceinline__ Walk(const Args& g, const int* where, int64_t share) : g(g) {
     s.b = where[0], s.hk = where[1] / g.blocks, s.blk = where[1] % g.blocks, ct = where[2], index = 0;
     seg_range<KEYS>(g.a, where[3], s);
     ahead = g.a.lens[min(s.b + 1, g.a.c.n_seqs - 1)];
-    left = tiles;
+    left = share;
     cnt = (int)min((int64_t)(s.nt - ct), left);
   }
   __device__ __forceinline__ bool next() {
-    left -= cnt;
+    left -= s.nt + kTurn - ct;
     if (left <= 0) return false;
     ct = 0;
     ++index;
-    if (++s.blk < g.blocks) {
-    } else if (s.blk = 0, ++s.hk == g.a.c.n_heads) {
-      s.hk = 0;
-      ++s.b;
-      seg_range<KEYS>(g.a, ahead, s);
-      ahead = g.a.lens[min(s.b + 1, g.a.c.n_seqs - 1)];
-    }
+    advance();
     cnt = (int)min((int64_t)s.nt, left);
     return true;
+  }
+  __device__ __forceinline__ void advance() {
+    if (++s.blk < g.blocks) return;
+    s.blk = 0;
+    if (++s.hk < g.a.c.n_heads) return;
+    s.hk = 0;
+    ++s.b;
+    seg_range<KEYS>(g.a, ahead, s);
+    ahead = g.a.lens[min(s.b + 1, g.a.c.n_seqs - 1)];
   }
 };
 
@@ -354,7 +358,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
   Seg s0;
   for (int b = tid * chunk; b < min(B, (tid + 1) * chunk); ++b) {
     seg_range<kKeys>(a, a.lens[b], s0);
-    sum += s0.nt;
+    sum += s0.nt + kTurn;
   }
   int64_t incl = sum;
   for (int x = 1; x < 32; x <<= 1) {
@@ -375,7 +379,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
   const int workers = (int)min(total, (int64_t)gridDim.x);
   const Deal deal(total, workers);
   const int64_t start = (int)blockIdx.x < workers ? deal.start(blockIdx.x) : 0;
-  const int64_t tiles = (int)blockIdx.x < workers ? deal.start(blockIdx.x + 1) - start : 0;
+  int64_t share = (int)blockIdx.x < workers ? deal.start(blockIdx.x + 1) - start : 0;
   const int64_t lo = (before + incl - sum) * g.groups, hi = (before + incl) * g.groups;
   if (start >= lo && start < hi) {
     int64_t at = lo;
@@ -383,32 +387,47 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     for (;; ++b) {
       len = a.lens[b];
       seg_range<kKeys>(a, len, s0);
-      if (start < at + (int64_t)s0.nt * g.groups) break;
-      at += (int64_t)s0.nt * g.groups;
+      if (start < at + (int64_t)(s0.nt + kTurn) * g.groups) break;
+      at += (int64_t)(s0.nt + kTurn) * g.groups;
     }
     ctl.where[0] = b;
-    ctl.where[1] = (int)((start - at) / s0.nt);
-    ctl.where[2] = (int)((start - at) % s0.nt);
+    ctl.where[1] = (int)((start - at) / (s0.nt + kTurn));
+    ctl.where[2] = (int)((start - at) % (s0.nt + kTurn));
     ctl.where[3] = len;
   }
   __syncthreads();
   const uint32_t tmem = ctl.tmem;
+  int skip = 0;  // what the share has of a segment's end
+  if (share > 0) {
+    Walk<kKeys> w(g, ctl.where, share);
+    if (w.ct >= w.s.nt) {
+      // the share starts within a segment's end: with the next segment, if it has one
+      skip = w.s.nt + kTurn - w.ct;
+      share -= skip;
+      __syncthreads();
+      if (tid == 0 && share > 0) {
+        w.advance();
+        ctl.where[0] = w.s.b, ctl.where[1] = w.s.hk * g.blocks + w.s.blk, ctl.where[2] = 0, ctl.where[3] = a.lens[w.s.b];
+      }
+      __syncthreads();
+    }
+  }
   if (tid == 0) {
     // the boundary at this CTA's start joins the segment if it is the first inside it
     SegMeta m{0, 0, 0, 0};
-    if (tiles > 0) {
-      Walk<kKeys> w(g, ctl.where, tiles);
-      const int64_t g0 = start - w.ct, prev = blockIdx.x ? deal.start((int)blockIdx.x - 1) : 0;
+    if (share > 0) {
+      Walk<kKeys> w(g, ctl.where, share);
+      const int64_t g0 = start + skip - w.ct, prev = blockIdx.x ? deal.start((int)blockIdx.x - 1) : 0;
       m.seq = w.s.b, m.group = w.s.hk * g.blocks + w.s.blk;
       if (w.ct > 0 && prev <= g0) {
         m.pieces = deal.worker(g0 + w.s.nt - 1) - blockIdx.x + 2;
-        m.first_slot = 2 * (blockIdx.x - 1) + (prev < g0 ? 1 : 0);
+        m.first_slot = 2 * (blockIdx.x - 1) + (prev < g0 - kTurn ? 1 : 0);  // (not its first segment)
       }
     }
     g.meta[blockIdx.x] = m;
   }
 
-  if (tiles == 0) {
+  if (share <= 0) {
     // nothing to do
   } else if (warp < 8) {
     // ================================================== softmax
@@ -419,7 +438,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     uint32_t sp[2] = {0, 0}, pp[2] = {0, 0}, ip = 0;  // phases: scores, outputs, tiles seen
     uint64_t bits = 0;  // the row's mask, of sequence last_b
     int last_b = -1;
-    Walk<kKeys> w(g, ctl.where, tiles);
+    Walk<kKeys> w(g, ctl.where, share);
     do {
       const Seg& s = w.s;
       const int hk = s.hk, r0 = s.blk * S::kRows, rows = min(R - r0, S::kRows);
@@ -630,11 +649,11 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     // ================================================== places
       // A lane finds the places of rows lane, lane + 32, ...; table entries are copied kAhead tiles ahead
       constexpr int kMine = kKeys / 32, kAhead = 3;
-      Walk<kKeys> nx(g, ctl.where, tiles), far = nx;
+      Walk<kKeys> nx(g, ctl.where, share), far = nx;
       int nt = 0, tf = nx.ct;
       bool more = true;
 #pragma unroll 1
-      for (int64_t at = -kAhead; at < tiles; ++at) {
+      for (int64_t at = -kAhead;; ++at) {
         if (more) {  // table entries of tile at + kAhead
           const int p0 = far.s.base + tf * kKeys;
           int* to = ctl.page[(uint32_t)(at + kAhead) & 7];
@@ -687,7 +706,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         }
         if (++nt == nx.cnt) {
           nt = 0;
-          nx.next();
+          if (!nx.next()) break;
         }
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
@@ -699,7 +718,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       constexpr int kMine = kKeys / 32;
       const int which = warp - 10;
       const uint8_t* base = which ? a.sc.v : a.sc.k;
-      Walk<kKeys> far(g, ctl.where, tiles);
+      Walk<kKeys> far(g, ctl.where, share);
       int tf = far.ct, b[kMine], next[kMine];
       bool more = true;
       auto load = [&](int (&to)[kMine], uint32_t x) {
@@ -721,7 +740,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       };
       load(b, 0);
 #pragma unroll 1
-      for (uint32_t x = 0; x < (uint32_t)tiles; ++x) {
+      for (uint32_t x = 0;; ++x) {
         {
           // bytes in [63, 247]; 255 takes no part in the largest
           auto fit = [](int b) { return b < 0 || b == 255 ? -1 : min(max(b, 63), 247); };
@@ -745,6 +764,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             tc::mbar_arrive(&ctl.info[x % kInfos]);
             tc::mbar_arrive(&ctl.placed[x & 3]);
           }
+          const bool last = !more;
           load(next, x + 1);
           const uint32_t e = 2 * x + which, st = e % S::kStages;
           if (e >= S::kStages) wait(ctl, &ctl.unstaged[st], (e / S::kStages - 1) & 1);
@@ -766,6 +786,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           if (lane == 0) tc::mbar_arrive(&ctl.taken[x & 3]);
 #pragma unroll
           for (int j = 0; j < kMine; ++j) b[j] = next[j];
+          if (last) break;
         }
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
@@ -784,7 +805,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       };
       uint32_t ps[2] = {0, 0};  // phases of the weights
       uint32_t e0 = 0;          // entry of the segment's first keys
-      Walk<kKeys> w(g, ctl.where, tiles);
+      Walk<kKeys> w(g, ctl.where, share);
       do {
         const int rows = min(R - w.s.blk * S::kRows, S::kRows), nt = w.cnt;
         const int tracks = WIDE && rows > 128 ? 2 : 1;  // of rows with products of their own
@@ -798,6 +819,24 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             if (x >= tracks) break;
+            // a track's next scores right behind its outputs: what waits for them is its softmax
+            if (np[x] < nk[x]) {
+              const int t = np[x], buf = WIDE ? x : t & 1;
+              const uint32_t e = e0 + 2 * t + 1;
+              if (mbar_test(&ctl.p_full[buf], ps[buf] & 1) && (vseen > t || landed(e))) {
+                vseen = max(vseen, t + 1);
+                ++ps[buf];
+                tc::fence_after();
+                const uint64_t vd = tc::desc_strided(entry(e), kKeys * 128, 1024, tc::kLayoutSW128);
+#pragma unroll
+                for (int kk = 0; kk < kKeys / 16; ++kk)
+                  mma_ts(tmem + S::kO + x * S::kOStep, tmem + S::kP + buf * S::kPStep + 8 * kk, vd + kk * 128, kIdO, !(t == 0 && kk == 0));
+                tc::mma_commit(&ctl.pv_done[x]);
+                ++np[x];
+                if (tracks == 1 || np[x ^ 1] >= np[x]) tc::mma_commit(&ctl.empty[e % kEntries]);
+                any = true;
+              }
+            }
             // scores two tiles ahead of the outputs (narrow), or one
             if (nk[x] < nt && nk[x] < np[x] + (WIDE ? 1 : 2)) {
               const int t = nk[x];
@@ -819,23 +858,6 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
                   tc::mma_commit(&ctl.empty[e % kEntries]);
                   if (nk[x] == nt) tc::mma_commit(&ctl.q_empty[qb]);
                 }
-                any = true;
-              }
-            }
-            if (np[x] < nk[x]) {
-              const int t = np[x], buf = WIDE ? x : t & 1;
-              const uint32_t e = e0 + 2 * t + 1;
-              if (mbar_test(&ctl.p_full[buf], ps[buf] & 1) && (vseen > t || landed(e))) {
-                vseen = max(vseen, t + 1);
-                ++ps[buf];
-                tc::fence_after();
-                const uint64_t vd = tc::desc_strided(entry(e), kKeys * 128, 1024, tc::kLayoutSW128);
-#pragma unroll
-                for (int kk = 0; kk < kKeys / 16; ++kk)
-                  mma_ts(tmem + S::kO + x * S::kOStep, tmem + S::kP + buf * S::kPStep + 8 * kk, vd + kk * 128, kIdO, !(t == 0 && kk == 0));
-                tc::mma_commit(&ctl.pv_done[x]);
-                ++np[x];
-                if (tracks == 1 || np[x ^ 1] >= np[x]) tc::mma_commit(&ctl.empty[e % kEntries]);
                 any = true;
               }
             }
@@ -932,7 +954,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       which = 1;
       return a.window > 0 && p >= f.lo && p - f.lo < 64 ? 1ull << (p - f.lo) : 0;
     };
-    Walk<kKeys> w(g, ctl.where, tiles);
+    Walk<kKeys> w(g, ctl.where, share);
     uint32_t tile = 0;  // tiles behind
     auto placed = [&](uint32_t x) {
       wait(ctl, &ctl.placed[x & 3], (x >> 2) & 1);

@@ -403,6 +403,30 @@ def test_tree(dtype, eight, lens, N, max_pages, page, Hq, Hkv, D, layout, window
     assert torch.equal(out, again)
 
 
+@pytest.mark.parametrize("eight,D,Hq,N", [(False, 64, 8, 3), (True, 64, 4, 2), (False, 128, 4, 9), (True, 128, 8, 35), (False, 256, 4, 2),
+                                          (False, 128, 12, 50), (True, 256, 8, 40)])
+@pytest.mark.parametrize("B,longest", [(90, 300), (3, 9000), (700, 2)])
+def test_many_segments(eight, D, Hq, N, B, longest):
+    """More tiles than CTAs, cut at every place: many short sequences, few long ones, nothing but trees."""
+    H, page = 4, 32
+    g = gen(B + D)
+    lens = torch.randint(0, longest + 1, (B,), generator=g, device="cuda")
+    P = Pool(B, -(-(longest + N) // page), page, H, D, BF16, eight, "slot", B)
+    masks = tree_masks(1, N, 7) * B
+    q = torch.randn((B, N, Hq, D), generator=g, device="cuda").to(BF16)
+    out, lse = torch.full_like(q, NAN), torch.full((B, N, Hq), NAN, device="cuda")
+    pe.tree_attn(P.cache, q, lens.to(torch.int32), tensor_of(masks), out, lse=lse)
+    pe.device_check()
+    some = torch.randperm(B, generator=g, device="cuda")[:6].tolist()  # the plain evaluation of a few, all rows
+    whole = P.table
+    for b in some:
+        P.table = whole[b:b + 1]
+        ro, rl, to, tl = attend(P, q[b:b + 1], [int(lens[b])], D ** -0.5, 0, masks[:1])
+        close(out[b], ro[0], to[0])
+        close(lse[b], rl[0], tl[0])
+    assert torch.isfinite(out.float()).all() and torch.isfinite(lse).all()
+
+
 @pytest.mark.parametrize("eight", [False, True])
 @pytest.mark.parametrize("Hq,N,D", [(2, 3, 64), (8, 7, 128), (8, 40, 128), (4, 20, 256), (16, 33, 64)])
 def test_what_a_row_does_not_attend_to(eight, Hq, N, D):
