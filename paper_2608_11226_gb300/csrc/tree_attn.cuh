@@ -17,8 +17,8 @@
 // fp16), one thread issues the products, two warpgroups take the softmax: a
 // thread reads its row of S from TMEM and puts the weights P back as the second
 // product's operand.
-//   Wide (more than 128 rows in a block): each warpgroup has 128 rows of its own,
-//     whose products run while the other works on its weights; P replaces S.
+//   Wide (more than 128 rows in a block): each warpgroup has 128 rows of its own;
+//     tiles of 64 positions, so that S has two buffers here as well, and P replaces S.
 //   Narrow: both warpgroups share one tile of 128 rows, half of the tile's columns
 //     each (they exchange the maxima), and S and P have two buffers.
 //
@@ -43,7 +43,6 @@ namespace pe {
 namespace tree {
 
 constexpr int kCtas = 152;
-constexpr int kTurn = 2;    // tiles that a segment's end is worth in the dealing (it takes 6-9 k clk, a tile 3.5 k)
 constexpr int kInfos = 16;  // tiles whose description is kept: what the ring holds, and what is placed ahead
 
 struct SegMeta {
@@ -53,7 +52,7 @@ struct SegMeta {
 template <int D, bool E8, bool WIDE>
 struct Shape {
   static_assert(!(WIDE && D == 256), "two outputs of 256 columns leave no room for scores");
-  static constexpr int kKeys = D == 256 ? 64 : 128;
+  static constexpr int kKeys = D == 256 || WIDE ? 64 : 128;
   static constexpr int kRows = WIDE ? 256 : 128;  // of a block
   static constexpr int kShared = WIDE ? 1 : 128;  // rows that two threads share
   static constexpr int kProducers = 4;            // warps
@@ -61,14 +60,16 @@ struct Shape {
   static constexpr int kEntry = kKeys * D * 2;
   // queries of two segments where there is room, so that the next one's are there in time
   static constexpr int kQs = WIDE || D == 256 ? 1 : 2;
-  static constexpr int kEntries = D == 64 ? 6 : E8 ? 3 : 4;
-  static constexpr int kStages = E8 ? 3 : 0;  // entries of codes on their way
+  static constexpr int kEntries = WIDE ? (E8 && D == 128 ? 6 : 8) : D == 64 ? 6 : E8 ? 3 : 4;
+  static constexpr int kStages = !E8 ? 0 : WIDE ? 4 : 3;  // entries of codes on their way
+  static constexpr int kTurn = WIDE ? 4 : 2;  // tiles that a segment's end is worth in the dealing (it takes 6-9 k clk)
   static constexpr int kQBytes = kRows * D * 2;
-  static constexpr int kSmem = kQs * kQBytes + kEntries * kEntry + kStages * kEntry / 2 + 1024;
+  static constexpr int kNeed = kQs * kQBytes + kEntries * kEntry + kStages * kEntry / 2 + 1024;
+  static constexpr int kSmem = kNeed > kPdlTmemSmem ? kNeed : kPdlTmemSmem + 1024;
   static constexpr int kCols = WIDE ? kKeys : kKeys / 2;  // columns of a thread
   // TMEM columns
-  static constexpr int kO = 0, kOStep = 128, kS = 256, kSStep = WIDE ? 128 : kKeys;
-  static constexpr int kP = WIDE ? 256 : D == 256 ? 384 : 128, kPStep = WIDE ? 128 : kKeys / 2;
+  static constexpr int kO = 0, kOStep = 128, kS = 256, kSStep = kKeys;
+  static constexpr int kP = WIDE ? 256 : D == 256 ? 384 : 128, kPStep = WIDE ? kKeys : kKeys / 2;
   static_assert(kSmem > kPdlTmemSmem, "no second kernel with tensor memory beside it");
   static_assert(kSmem + 14000 <= 232448, "shared memory of an SM");
 };
@@ -81,7 +82,7 @@ struct Info {  // a tile
 
 template <class S>
 struct Control {
-  uint64_t full[8], empty[8], info[kInfos], paged[8], placed[4], taken[4], staged[4], unstaged[4], q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2], fin;
+  uint64_t full[8], empty[8], info[kInfos], paged[8], placed[4], taken[4], staged[4], unstaged[4], q_full[2], q_empty[2], s_full[4], p_full[4], pv_done[2], fin;
   Info tile[kInfos];
   unsigned long long bad[16][2];  // per segment: nodes, and positions from lo on, with values that are not finite
   int64_t off[4][S::kKeys];      // element offsets of a tile's rows, -1: none
@@ -144,7 +145,7 @@ struct Deal {
 };
 
 // the CTA's share of the line, segment by segment; every role walks it
-template <int KEYS>
+template <int KEYS, int TURN>
 struct Walk {
   const Args& g;
   Seg s;
@@ -158,7 +159,7 @@ struct Walk {
     cnt = (int)min((int64_t)(s.nt - ct), left);
   }
   __device__ __forceinline__ bool next() {
-    left -= s.nt + kTurn - ct;
+    left -= s.nt + TURN - ct;
     if (left <= 0) return false;
     ct = 0;
     ++index;
@@ -188,13 +189,32 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 __device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
-// A (16-bit, K-major) from TMEM
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+// A whole warp runs the role that issues products, so that what goes into them stays in
+// uniform registers; one lane, the leader, issues.  (One lane in a branch of its own took 65 clk for
+// each instruction, what the tensor core takes for 128 x 128 x 16.)
+__device__ __forceinline__ bool elect() {
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  return one != 0;
+}
+__device__ __forceinline__ uint64_t desc_of(uint32_t lo, uint32_t hi) { return (uint64_t)hi << 32 | lo; }
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t leader) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
-      "}\n" ::"r"(d), "r"(a), "l"(db), "r"(idesc), "r"(accumulate));
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t"
+      "}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(leader));
+}
+// A (16-bit, K-major) from TMEM
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t leader) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+      "}\n" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(leader));
 }
 template <typename T> constexpr uint32_t idesc(int M, int N, int b_mn) {
   const uint32_t fmt = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
@@ -312,7 +332,7 @@ template <typename T, bool E8, int D, bool WIDE>
 __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(Args g) {
   using S = Shape<D, E8, WIDE>;
   using M = typename std::conditional<E8, __half, T>::type;  // type of the products
-  constexpr int kKeys = S::kKeys, kChunks = D / 8, kEntries = S::kEntries;
+  constexpr int kKeys = S::kKeys, kChunks = D / 8, kEntries = S::kEntries, kTurn = S::kTurn;
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(16) Control<S> ctl;
   static_assert(S::kSmem + sizeof(Control<S>) <= 232448, "shared memory of an SM");
@@ -335,6 +355,8 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     for (int i = 0; i < 4; ++i) {
       tc::mbar_init(&ctl.placed[i], kPlacers);
       tc::mbar_init(&ctl.taken[i], E8 ? S::kProducers + 2 : S::kProducers);
+      tc::mbar_init(&ctl.s_full[i], 1);
+      tc::mbar_init(&ctl.p_full[i], WIDE ? 4 : 8);
       tc::mbar_init(&ctl.staged[i], 32);
       tc::mbar_init(&ctl.unstaged[i], S::kProducers);
     }
@@ -342,8 +364,6 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     for (int i = 0; i < 2; ++i) {
       tc::mbar_init(&ctl.q_full[i], E8 ? S::kProducers : 32 * S::kProducers);
       tc::mbar_init(&ctl.q_empty[i], 1);
-      tc::mbar_init(&ctl.s_full[i], 1);
-      tc::mbar_init(&ctl.p_full[i], WIDE ? 4 : 8);
       tc::mbar_init(&ctl.pv_done[i], 1);
     }
     ctl.err = 0;
@@ -399,7 +419,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
   const uint32_t tmem = ctl.tmem;
   int skip = 0;  // what the share has of a segment's end
   if (share > 0) {
-    Walk<kKeys> w(g, ctl.where, share);
+    Walk<kKeys, kTurn> w(g, ctl.where, share);
     if (w.ct >= w.s.nt) {
       // the share starts within a segment's end: with the next segment, if it has one
       skip = w.s.nt + kTurn - w.ct;
@@ -416,7 +436,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     // the boundary at this CTA's start joins the segment if it is the first inside it
     SegMeta m{0, 0, 0, 0};
     if (share > 0) {
-      Walk<kKeys> w(g, ctl.where, share);
+      Walk<kKeys, kTurn> w(g, ctl.where, share);
       const int64_t g0 = start + skip - w.ct, prev = blockIdx.x ? deal.start((int)blockIdx.x - 1) : 0;
       m.seq = w.s.b, m.group = w.s.hk * g.blocks + w.s.blk;
       if (w.ct > 0 && prev <= g0) {
@@ -435,10 +455,10 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     const int wg = warp >> 2, row = (warp & 3) * 32 + lane;  // row of the tile, lane of TMEM
     const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const float qlog = fabsf(a.scale) * 1.4426950408889634f;
-    uint32_t sp[2] = {0, 0}, pp[2] = {0, 0}, ip = 0;  // phases: scores, outputs, tiles seen
+    uint32_t sp[2] = {0, 0}, pp = 0, ip = 0;  // phases: scores, outputs, tiles seen
     uint64_t bits = 0;  // the row's mask, of sequence last_b
     int last_b = -1;
-    Walk<kKeys> w(g, ctl.where, share);
+    Walk<kKeys, kTurn> w(g, ctl.where, share);
     do {
       const Seg& s = w.s;
       const int hk = s.hk, r0 = s.blk * S::kRows, rows = min(R - r0, S::kRows);
@@ -462,11 +482,11 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         continue;
       }
       for (int t = 0; t < w.cnt; ++t, ++ip) {
-        const int buf = WIDE ? wg : t & 1;
+        const int b2 = t & 1, buf = WIDE ? 2 * wg + b2 : b2;  // of scores and weights
         wait(ctl, &ctl.info[ip % kInfos], (ip / kInfos) & 1);
         const Info& f = ctl.tile[ip % kInfos];
-        wait(ctl, &ctl.s_full[buf], sp[buf] & 1);
-        ++sp[buf];
+        wait(ctl, &ctl.s_full[buf], sp[b2] & 1);
+        ++sp[b2];
         __syncwarp();
         tc::fence_after();
         if (E8 && t == 0) qf = ctl.qf[w.index & 3][(WIDE ? wg * 128 : 0) + row];
@@ -534,7 +554,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             m = x;
             l *= fr;
             if (t > 0) {
-              if (!WIDE) wait(ctl, &ctl.pv_done[0], (pp[0] - 1) & 1);  // the last product into the output
+              wait(ctl, &ctl.pv_done[WIDE ? wg : 0], (pp - 1) & 1);  // the last product into the output
               __syncwarp();
               tc::fence_after();
               const uint32_t oc = lanes + S::kO + (WIDE ? wg * S::kOStep : wg * (D / 2));
@@ -576,12 +596,12 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         tc::fence_before();
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&ctl.p_full[buf]);
-        ++pp[WIDE ? wg : 0];
+        ++pp;
       }
       // -- the segment, or this CTA's part of it, ends
-      // (the last scores say that all products but two, or one, are done: no phase is skipped)
-      if (!WIDE && w.cnt > 1) wait(ctl, &ctl.pv_done[0], pp[0] & 1);
-      wait(ctl, &ctl.pv_done[WIDE ? wg : 0], (pp[WIDE ? wg : 0] - 1) & 1);
+      // (the last scores say that all products but two are done: no phase is skipped)
+      if (w.cnt > 1) wait(ctl, &ctl.pv_done[WIDE ? wg : 0], pp & 1);
+      wait(ctl, &ctl.pv_done[WIDE ? wg : 0], (pp - 1) & 1);
       __syncwarp();
       tc::fence_after();
       if (!live) m = -CUDART_INF_F, l = 0.0f;
@@ -649,7 +669,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     // ================================================== places
       // A lane finds the places of rows lane, lane + 32, ...; table entries are copied kAhead tiles ahead
       constexpr int kMine = kKeys / 32, kAhead = 3;
-      Walk<kKeys> nx(g, ctl.where, share), far = nx;
+      Walk<kKeys, kTurn> nx(g, ctl.where, share), far = nx;
       int nt = 0, tf = nx.ct;
       bool more = true;
 #pragma unroll 1
@@ -718,7 +738,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       constexpr int kMine = kKeys / 32;
       const int which = warp - 10;
       const uint8_t* base = which ? a.sc.v : a.sc.k;
-      Walk<kKeys> far(g, ctl.where, share);
+      Walk<kKeys, kTurn> far(g, ctl.where, share);
       int tf = far.ct, b[kMine], next[kMine];
       bool more = true;
       auto load = [&](int (&to)[kMine], uint32_t x) {
@@ -793,70 +813,79 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     }
     if (warp == 8) {
     // ================================================== products
-    if (lane == 0) {
       // queries with their sign where the scale is negative
       const uint32_t kIdS = idesc<M>(128, kKeys, 0) | (!E8 && a.scale < 0.0f ? 1u << 13 : 0u), kIdO = idesc<M>(128, D, 1);
-      auto entry = [&](uint32_t e) { return ring + (e % kEntries) * S::kEntry; };
+      const uint32_t leader = elect(), tm = uniform(tmem);
+      const uint64_t k0 = tc::desc_kmajor(0, 1024, tc::kLayoutSW128), v0 = tc::desc_strided(0, kKeys * 128, 1024, tc::kLayoutSW128);
+      const uint32_t qs4 = uniform(qs) >> 4, ring4 = uniform(ring) >> 4;  // (addresses of 14 bits: offsets do not carry)
+      auto entry = [&](uint32_t e) { return ring4 + (e % kEntries) * (S::kEntry / 16); };
       auto landed = [&](uint32_t e) {
-        if (!mbar_test(&ctl.full[e % kEntries], (e / kEntries) & 1)) return false;
+        if (!__all_sync(0xffffffffu, mbar_test(&ctl.full[e % kEntries], (e / kEntries) & 1))) return false;
         // copies write as ordinary stores do, products read through the asynchronous proxy
         if (!E8) tc::fence_async_smem();
         return true;
       };
-      uint32_t ps[2] = {0, 0};  // phases of the weights
-      uint32_t e0 = 0;          // entry of the segment's first keys
-      Walk<kKeys> w(g, ctl.where, share);
+      auto commit = [&](uint64_t* b) {
+        if (leader) tc::mma_commit(b);
+      };
+      uint32_t ps[4] = {0, 0, 0, 0};  // phases of the weights
+      uint32_t e0 = 0;                // entry of the segment's first keys
+      Walk<kKeys, kTurn> w(g, ctl.where, share);
       do {
-        const int rows = min(R - w.s.blk * S::kRows, S::kRows), nt = w.cnt;
-        const int tracks = WIDE && rows > 128 ? 2 : 1;  // of rows with products of their own
-        const int qb = w.index % S::kQs;
+        const int rows = min(R - w.s.blk * S::kRows, S::kRows), nt = (int)uniform(w.cnt);
+        const int tracks = WIDE && uniform(rows > 128) ? 2 : 1;  // of rows with products of their own
+        const int qb = S::kQs == 1 ? 0 : (int)uniform(w.index & 1);
         wait(ctl, &ctl.q_full[qb], (w.index / S::kQs) & 1);
+        __syncwarp();
         if (!E8) tc::fence_async_smem();
         int nk[2] = {0, 0}, np[2] = {0, 0}, kseen = 0, vseen = 0;  // tiles whose scores, outputs are under way; that have landed
         long long t0 = clock64();
         while (np[0] < nt || (tracks == 2 && np[1] < nt)) {
           bool any = false;
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
+          for (int x = 0; x < (WIDE ? 2 : 1); ++x) {
             if (x >= tracks) break;
             // a track's next scores right behind its outputs: what waits for them is its softmax
             if (np[x] < nk[x]) {
-              const int t = np[x], buf = WIDE ? x : t & 1;
-              const uint32_t e = e0 + 2 * t + 1;
-              if (mbar_test(&ctl.p_full[buf], ps[buf] & 1) && (vseen > t || landed(e))) {
+              const int t = np[x], b2 = t & 1, buf = WIDE ? 2 * x + b2 : b2;
+              const uint32_t e = e0 + 2 * t + 1, phase = b2 ? ps[2 * x + 1] : ps[2 * x];
+              if (__all_sync(0xffffffffu, mbar_test(&ctl.p_full[buf], phase & 1)) && (vseen > t || landed(e))) {
                 vseen = max(vseen, t + 1);
-                ++ps[buf];
+                if (b2)
+                  ++ps[2 * x + 1];
+                else
+                  ++ps[2 * x];
                 tc::fence_after();
-                const uint64_t vd = tc::desc_strided(entry(e), kKeys * 128, 1024, tc::kLayoutSW128);
+                const uint32_t vd = uniform((uint32_t)v0 | entry(e)), out = tm + S::kO + x * S::kOStep, p = uniform(tm + S::kP + buf * S::kPStep);
+                const uint32_t more = uniform(t != 0);
 #pragma unroll
                 for (int kk = 0; kk < kKeys / 16; ++kk)
-                  mma_ts(tmem + S::kO + x * S::kOStep, tmem + S::kP + buf * S::kPStep + 8 * kk, vd + kk * 128, kIdO, !(t == 0 && kk == 0));
-                tc::mma_commit(&ctl.pv_done[x]);
+                  mma_ts(out, p + 8 * kk, desc_of(vd + kk * 128, (uint32_t)(v0 >> 32)), kIdO, kk > 0 ? 1u : more, leader);
+                commit(&ctl.pv_done[x]);
                 ++np[x];
-                if (tracks == 1 || np[x ^ 1] >= np[x]) tc::mma_commit(&ctl.empty[e % kEntries]);
+                if (tracks == 1 || np[x ^ 1] >= np[x]) commit(&ctl.empty[e % kEntries]);
                 any = true;
               }
             }
-            // scores two tiles ahead of the outputs (narrow), or one
-            if (nk[x] < nt && nk[x] < np[x] + (WIDE ? 1 : 2)) {
+            // (two tiles ahead of the outputs)
+            if (nk[x] < nt && nk[x] < np[x] + 2) {
               const int t = nk[x];
               const uint32_t e = e0 + 2 * t;
               if (kseen > t || landed(e)) {
                 kseen = max(kseen, t + 1);
-                const int buf = WIDE ? x : t & 1;
+                const int buf = WIDE ? 2 * x + (t & 1) : t & 1;
                 tc::fence_after();
-                // (addresses of 14 bits in 16 bytes: constants on top do not carry)
-                const uint64_t qd = tc::desc_kmajor(qs + qb * S::kQBytes + x * 128 * 128 * (D / 64), 1024, tc::kLayoutSW128);
-                const uint64_t kd = tc::desc_kmajor(entry(e), 1024, tc::kLayoutSW128);
+                const uint32_t qd = (uint32_t)k0 | (qs4 + (qb * S::kQBytes + x * 128 * 128 * (D / 64)) / 16), kd = uniform((uint32_t)k0 | entry(e));
+                const uint32_t to = uniform(tm + S::kS + buf * S::kSStep);
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk)
-                  tc::mma_bf16(tmem + S::kS + buf * S::kSStep, qd + ((kk >> 2) * 128 * 128 + (kk & 3) * 32) / 16,
-                               kd + ((kk >> 2) * kKeys * 128 + (kk & 3) * 32) / 16, kIdS, kk > 0);
-                tc::mma_commit(&ctl.s_full[buf]);
+                  mma_ss(to, desc_of(qd + ((kk >> 2) * 128 * 128 + (kk & 3) * 32) / 16, (uint32_t)(k0 >> 32)),
+                         desc_of(kd + ((kk >> 2) * kKeys * 128 + (kk & 3) * 32) / 16, (uint32_t)(k0 >> 32)), kIdS, kk > 0, leader);
+                commit(&ctl.s_full[buf]);
                 ++nk[x];
                 if (tracks == 1 || nk[x ^ 1] >= nk[x]) {
-                  tc::mma_commit(&ctl.empty[e % kEntries]);
-                  if (nk[x] == nt) tc::mma_commit(&ctl.q_empty[qb]);
+                  commit(&ctl.empty[e % kEntries]);
+                  if (nk[x] == nt) commit(&ctl.q_empty[qb]);
                 }
                 any = true;
               }
@@ -866,17 +895,15 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             t0 = clock64();
             continue;
           }
-          __nanosleep(20);
-          if (clock64() - t0 > 4000000000LL || *(volatile int*)&ctl.err) {
+          if (__any_sync(0xffffffffu, clock64() - t0 > 4000000000LL || *(volatile int*)&ctl.err)) {
             atomicExch(&ctl.err, 1);
             break;
           }
         }
         e0 += 2 * nt;
       } while (w.next());
-      tc::mma_commit(&ctl.fin);
+      commit(&ctl.fin);
       if (!tc::mbar_wait(&ctl.fin, 0)) atomicExch(&ctl.err, 1);
-    }
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
@@ -888,7 +915,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       if (lane == 0) tc::mbar_arrive(b);
     };
     // queries of a segment's block of rows
-    auto load_q = [&](const Walk<kKeys>& w) {
+    auto load_q = [&](const Walk<kKeys, kTurn>& w) {
       const Seg& s = w.s;
       const int hk = s.hk, r0 = s.blk * S::kRows, rows = min(R - r0, S::kRows);
       const int qb = w.index % S::kQs;
@@ -954,7 +981,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       which = 1;
       return a.window > 0 && p >= f.lo && p - f.lo < 64 ? 1ull << (p - f.lo) : 0;
     };
-    Walk<kKeys> w(g, ctl.where, share);
+    Walk<kKeys, kTurn> w(g, ctl.where, share);
     uint32_t tile = 0;  // tiles behind
     auto placed = [&](uint32_t x) {
       wait(ctl, &ctl.placed[x & 3], (x >> 2) & 1);
@@ -1011,7 +1038,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             if (issued >= kEntries) wait(ctl, &ctl.empty[issued % kEntries], (issued / kEntries - 1) & 1);
             const uint32_t dst = ring + (issued % kEntries) * S::kEntry;
             const T* src = (const T*)(kv ? c.v : c.k) + ch * 8;
-            constexpr int kAtOnce = 8;
+            constexpr int kAtOnce = kKeys / kPass < 8 ? kKeys / kPass : 8;
 #pragma unroll 1
             for (int i0 = 0; i0 < kKeys / kPass; i0 += kAtOnce) {
               int64_t o[kAtOnce];  // read ahead of the copies, which the compiler keeps in their order
@@ -1080,7 +1107,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         if (__builtin_expect(check, 0)) spoils(from, fac, f);  // (a row's lanes are in one warp)
         unsigned char* dst = smem + S::kQs * S::kQBytes + (e % kEntries) * S::kEntry;
         // 8 codes from each half of the row: their chunks of the ring meet no bank twice
-        constexpr int kAtOnce = 4;
+        constexpr int kAtOnce = kEach < 4 ? kEach : 4;
         const unsigned char* own = from - pt * 16 + row0 * D + ch * 8;
 #pragma unroll 1
         for (int i0 = 0; i0 < kEach; i0 += kAtOnce) {
