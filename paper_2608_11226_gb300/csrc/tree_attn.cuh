@@ -61,7 +61,11 @@ struct Shape {
   // queries of two segments where there is room, so that the next one's are there in time
   static constexpr int kQs = WIDE || D == 256 ? 1 : 2;
   static constexpr int kEntries = WIDE ? (E8 && D == 128 ? 6 : 8) : D == 64 ? 6 : E8 ? 3 : 4;
-  static constexpr int kStages = !E8 ? 0 : WIDE ? 4 : 3;  // entries of codes on their way
+  static constexpr int kStages = !E8 ? 0 : WIDE || D == 64 ? 4 : 3;  // entries of codes on their way
+  // two producer warps for keys and two for values, where each kind has its own places (an odd number
+  // of them passes from one kind to the other, and a wait for the one would not see the other's turn)
+  static constexpr bool kSplit = kEntries % 2 == 0 && kStages % 2 == 0;
+  static constexpr int kBring = kSplit ? kProducers / 2 : kProducers;  // warps that bring an entry
   static constexpr int kTurn = WIDE ? 4 : 2;  // tiles that a segment's end is worth in the dealing (it takes 6-9 k clk)
   static constexpr int kQBytes = kRows * D * 2;
   static constexpr int kNeed = kQs * kQBytes + kEntries * kEntry + kStages * kEntry / 2 + 1024;
@@ -346,7 +350,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
   if (warp == 8) tc::tmem_alloc(&ctl.tmem, 512);
   if (tid == 0) {
     for (int i = 0; i < 8; ++i) {
-      tc::mbar_init(&ctl.full[i], E8 ? S::kProducers : 32 * S::kProducers);
+      tc::mbar_init(&ctl.full[i], E8 ? S::kBring : 32 * S::kBring);
       tc::mbar_init(&ctl.empty[i], 1);
     }
     constexpr int kPlacers = E8 ? 3 : 1;  // warps
@@ -358,11 +362,11 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       tc::mbar_init(&ctl.s_full[i], 1);
       tc::mbar_init(&ctl.p_full[i], WIDE ? 4 : 8);
       tc::mbar_init(&ctl.staged[i], 32);
-      tc::mbar_init(&ctl.unstaged[i], S::kProducers);
+      tc::mbar_init(&ctl.unstaged[i], S::kBring);
     }
     tc::mbar_init(&ctl.fin, 1);
     for (int i = 0; i < 2; ++i) {
-      tc::mbar_init(&ctl.q_full[i], E8 ? S::kProducers : 32 * S::kProducers);
+      tc::mbar_init(&ctl.q_full[i], E8 ? S::kBring : 32 * S::kBring);
       tc::mbar_init(&ctl.q_empty[i], 1);
       tc::mbar_init(&ctl.pv_done[i], 1);
     }
@@ -593,14 +597,15 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         } else if (!WIDE) {
           bar_sync(1 + (warp & 3), 64);
         }
+        // The end waits for the last output, so the one before it has to be seen first (scores say that all
+        // but two are done), and while the last one cannot be: a barrier two phases on looks like none
+        if (t > 0 && t == w.cnt - 1) wait(ctl, &ctl.pv_done[WIDE ? wg : 0], (pp - 1) & 1);
         tc::fence_before();
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&ctl.p_full[buf]);
         ++pp;
       }
       // -- the segment, or this CTA's part of it, ends
-      // (the last scores say that all products but two are done: no phase is skipped)
-      if (w.cnt > 1) wait(ctl, &ctl.pv_done[WIDE ? wg : 0], pp & 1);
       wait(ctl, &ctl.pv_done[WIDE ? wg : 0], (pp - 1) & 1);
       __syncwarp();
       tc::fence_after();
@@ -665,18 +670,30 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     } while (w.next());
   } else if (warp < 12) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
-    if (warp == 9) {
+    constexpr int kPlace = E8 ? 1 : 2;  // warps that place, every kPlace-th tile each
+    if (warp >= 9 && warp < 9 + kPlace) {
     // ================================================== places
-      // A lane finds the places of rows lane, lane + 32, ...; table entries are copied kAhead tiles ahead
+      // A lane finds the places of rows lane, lane + 32, ...; table entries are copied kAhead turns ahead
       constexpr int kMine = kKeys / 32, kAhead = 3;
-      Walk<kKeys, kTurn> nx(g, ctl.where, share), far = nx;
-      int nt = 0, tf = nx.ct;
-      bool more = true;
+      Walk<kKeys, kTurn> nx(g, ctl.where, share);
+      int nt = 0;
+      auto on = [&](Walk<kKeys, kTurn>& w, int& t, int n) {  // n tiles on; false past the end
+        bool there = true;
+        for (; n > 0 && there; --n)
+          if (++t == w.cnt) {
+            t = 0;
+            there = w.next();
+          }
+        return there;
+      };
+      bool more = on(nx, nt, warp - 9), here = more;
+      Walk<kKeys, kTurn> far = nx;
+      int tf = nt;
 #pragma unroll 1
-      for (int64_t at = -kAhead;; ++at) {
-        if (more) {  // table entries of tile at + kAhead
-          const int p0 = far.s.base + tf * kKeys;
-          int* to = ctl.page[(uint32_t)(at + kAhead) & 7];
+      for (int64_t at = warp - 9 - kAhead * kPlace; here; at += kPlace) {
+        if (more) {  // table entries of tile at + kAhead * kPlace
+          const int p0 = far.s.base + (far.ct + tf) * kKeys;
+          int* to = ctl.page[(uint32_t)(at + kAhead * kPlace) & 7];
 #pragma unroll 1
           for (int r = lane; r < kKeys; r += 32) {
             const int p = p0 + r;
@@ -687,10 +704,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             else
               to[r] = -1;
           }
-          if (++tf == far.ct + far.cnt) {
-            more = far.next();
-            tf = far.ct;
-          }
+          more = on(far, tf, kPlace);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
         if (at < 0) continue;
@@ -724,10 +738,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           tc::mbar_arrive(&ctl.info[x % kInfos]);
           tc::mbar_arrive(&ctl.placed[x & 3]);
         }
-        if (++nt == nx.cnt) {
-          nt = 0;
-          if (!nx.next()) break;
-        }
+        here = on(nx, nt, kPlace);
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
     }
@@ -908,14 +919,16 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
     // ================================================== producers
-    constexpr int kN = 32 * S::kProducers;
-    const int pt = tid - 384;
+    // (split, what an entry costs besides its copies is paid side by side)
+    constexpr int kN = 32 * S::kBring;
+    const int kind = S::kSplit ? (warp - 12) / S::kBring : 0, pt = tid - 384 - kind * kN;
     auto arrive = [&](uint64_t* b) {
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(b);
     };
-    // queries of a segment's block of rows
+    // queries of a segment's block of rows, by those who bring keys
     auto load_q = [&](const Walk<kKeys, kTurn>& w) {
+      if (kind != 0) return;
       const Seg& s = w.s;
       const int hk = s.hk, r0 = s.blk * S::kRows, rows = min(R - r0, S::kRows);
       const int qb = w.index % S::kQs;
@@ -991,18 +1004,10 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     if constexpr (!E8) {
       constexpr int kPass = kN / kChunks;  // rows of a pass
       const int row0 = pt / kChunks, ch = pt % kChunks;
-      uint32_t issued = 0;
-      // Values that are not finite, where rows attend to them differently, become zeros and a mark.  The entry
-      // is looked through after the next one has been sent for.
-      int waiting = -1;
-      const Info* of = nullptr;
-      auto spoils = [&](bool last) {
-        if (last)
-          asm volatile("cp.async.wait_group 0;" ::: "memory");
-        else
-          asm volatile("cp.async.wait_group 1;" ::: "memory");
-        const Info& f = *of;
-        const uint32_t at = S::kQs * S::kQBytes + (waiting % kEntries) * S::kEntry;
+      // Values that are not finite, where rows attend to them differently, become zeros and a mark
+      auto spoils = [&](uint32_t e, const Info& f) {
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        const uint32_t at = S::kQs * S::kQBytes + (e % kEntries) * S::kEntry;
         unsigned long long* bad = ctl.bad[f.flags >> 1];
 #pragma unroll 1
         for (int r = row0; r < kKeys; r += kPass) {
@@ -1024,8 +1029,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           }
         }
         tc::fence_async_smem();
-        tc::mbar_arrive(&ctl.full[waiting % kEntries]);
-        waiting = -1;
+        tc::mbar_arrive(&ctl.full[e % kEntries]);
       };
       do {
         for (int t = 0; t < w.cnt; ++t, ++tile) {
@@ -1033,38 +1037,33 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           placed(tile);
           const int64_t* offs = ctl.off[tile & 3];
           const Info& f = ctl.tile[tile % kInfos];
+          static_assert(S::kSplit, "16-bit entries have an even number of places");
+          const int kv = kind;
+          const uint32_t e = 2 * tile + kv;
+          if (e >= kEntries) wait(ctl, &ctl.empty[e % kEntries], (e / kEntries - 1) & 1);
+          const uint32_t dst = ring + (e % kEntries) * S::kEntry;
+          const T* src = (const T*)(kv ? c.v : c.k) + ch * 8;
+          constexpr int kAtOnce = 8;
 #pragma unroll 1
-          for (int kv = 0; kv < 2; ++kv) {
-            if (issued >= kEntries) wait(ctl, &ctl.empty[issued % kEntries], (issued / kEntries - 1) & 1);
-            const uint32_t dst = ring + (issued % kEntries) * S::kEntry;
-            const T* src = (const T*)(kv ? c.v : c.k) + ch * 8;
-            constexpr int kAtOnce = kKeys / kPass < 8 ? kKeys / kPass : 8;
-#pragma unroll 1
-            for (int i0 = 0; i0 < kKeys / kPass; i0 += kAtOnce) {
-              int64_t o[kAtOnce];  // read ahead of the copies, which the compiler keeps in their order
+          for (int i0 = 0; i0 < kKeys / kPass; i0 += kAtOnce) {
+            int64_t o[kAtOnce];  // read ahead of the copies, which the compiler keeps in their order
 #pragma unroll
-              for (int i = 0; i < kAtOnce; ++i) o[i] = offs[row0 + (i0 + i) * kPass];
+            for (int i = 0; i < kAtOnce; ++i) o[i] = offs[row0 + (i0 + i) * kPass];
 #pragma unroll
-              for (int i = 0; i < kAtOnce; ++i)
-                copy16(dst + chunk_at(row0 + (i0 + i) * kPass, ch, kKeys), src + (o[i] < 0 ? 0 : o[i]), o[i] >= 0);
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            if (__builtin_expect(waiting >= 0, 0)) spoils(false);
-            if (__builtin_expect(kv && (f.flags & 1), 0)) {
-              waiting = (int)issued;
-              of = &f;
-            } else {
-              // the thread arrives when its copies have landed
-              asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tc::smem_u32(&ctl.full[issued % kEntries])) : "memory");
-            }
-            ++issued;
+            for (int i = 0; i < kAtOnce; ++i)
+              copy16(dst + chunk_at(row0 + (i0 + i) * kPass, ch, kKeys), src + (o[i] < 0 ? 0 : o[i]), o[i] >= 0);
+          }
+          if (__builtin_expect(kv && (f.flags & 1), 0)) {
+            spoils(e, f);
+          } else {
+            // the thread arrives when its copies have landed
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tc::smem_u32(&ctl.full[e % kEntries])) : "memory");
           }
           arrive(&ctl.taken[tile & 3]);
           // where queries have one place, the first tile is under way before the last segment's are done with
           if (S::kQs == 1 && t == 0) load_q(w);
         }
       } while (w.next());
-      if (waiting >= 0) spoils(true);
       asm volatile("cp.async.wait_all;" ::: "memory");
     } else {
       // Codes are widened from their stage into the ring
@@ -1151,7 +1150,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           const Info& f = ctl.tile[tile % kInfos];
           uint16_t (*fac)[kKeys] = ctl.fac[tile & 3];
 #pragma unroll 1
-          for (int kv = 0; kv < 2; ++kv) put(2 * tile + kv, fac[kv], kv && (f.flags & 1), f);
+          for (int kv = kind; kv < (S::kSplit ? kind + 1 : 2); ++kv) put(2 * tile + kv, fac[kv], kv && (f.flags & 1), f);
           arrive(&ctl.taken[tile & 3]);
           if (S::kQs == 1 && t == 0) load_q(w);
         }
