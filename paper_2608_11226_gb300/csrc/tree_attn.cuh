@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     }
     tc::mbar_init(&ctl.fin, 1);
     for (int i = 0; i < 2; ++i) {
-      tc::mbar_init(&ctl.q_full[i], E8 ? S::kBring : 32 * S::kBring);
+      tc::mbar_init(&ctl.q_full[i], E8 ? S::kBring : 32);
       tc::mbar_init(&ctl.q_empty[i], 1);
       tc::mbar_init(&ctl.pv_done[i], 1);
     }
@@ -742,6 +742,25 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
     }
+    if constexpr (!E8) if (warp == 11) {
+      // ================================================ queries
+      const int ch = lane % kChunks;
+      Walk<kKeys, kTurn> w(g, ctl.where, share);
+      do {
+        const Seg& s = w.s;
+        const int r0 = s.blk * S::kRows, rows = min(R - r0, S::kRows), qb = w.index % S::kQs;
+        if (w.index >= S::kQs) wait(ctl, &ctl.q_empty[qb], (w.index / S::kQs - 1) & 1);
+        const T* q = (const T*)a.q + s.b * a.q_seq + (int64_t)s.hk * G * a.q_head + ch * 8;
+#pragma unroll 4
+        for (int r = lane / kChunks; r < rows; r += 32 / kChunks) {
+          const int node = g.group.of(r0 + r);
+          copy16(qs + qb * S::kQBytes + (r >> 7) * (128 * 128 * (D / 64)) + chunk_at(r & 127, ch, 128),
+                 q + node * a.q_node + (r0 + r - node * G) * a.q_head, true);
+        }
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tc::smem_u32(&ctl.q_full[qb])) : "memory");
+      } while (w.next());
+      asm volatile("cp.async.wait_all;" ::: "memory");
+    }
     if constexpr (E8) if (warp >= 10) {
       // ================================================ scales: of keys, of values
       // What brings a row's scale to the tile's largest; bytes are loaded a tile ahead.  Then the codes
@@ -926,7 +945,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(b);
     };
-    // queries of a segment's block of rows, by those who bring keys
+    // queries of a segment's block of rows (8 bits), by those who bring keys
     auto load_q = [&](const Walk<kKeys, kTurn>& w) {
       if (kind != 0) return;
       const Seg& s = w.s;
@@ -942,11 +961,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         return q + node * a.q_node + (r0 + r - node * G) * a.q_head + ch * 8;
       };
       auto place = [&](int r) { return qb * S::kQBytes + (r >> 7) * (128 * 128 * (D / 64)) + chunk_at(r & 127, ch, 128); };
-      if constexpr (!E8) {
-#pragma unroll 4
-        for (int r = pt / kChunks; r < rows; r += kStep) copy16(qs + place(r), row_of(r), true);
-        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tc::smem_u32(&ctl.q_full[qb])) : "memory");
-      } else {
+      {
         constexpr int kAtOnce = 4;
 #pragma unroll 1
         for (int r1 = 0; r1 < rows; r1 += kAtOnce * kStep) {
@@ -1009,8 +1024,11 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         asm volatile("cp.async.wait_all;" ::: "memory");
         const uint32_t at = S::kQs * S::kQBytes + (e % kEntries) * S::kEntry;
         unsigned long long* bad = ctl.bad[f.flags >> 1];
+        // (nodes' rows alone, where there is no window)
+        const int from = a.window > 0 ? 0 : max(f.n - f.p0, 0), to = a.window > 0 ? kKeys : min(kKeys, f.n + a.n_nodes - f.p0);
 #pragma unroll 1
-        for (int r = row0; r < kKeys; r += kPass) {
+        for (int r = row0 + (from - row0 + kPass - 1) / kPass * kPass; r < to; r += kPass) {
+          if (r < from) continue;
           int which;
           const uint64_t bit = apart(f, r, which);
           if (!bit || !((f.valid[r >> 5] >> (r & 31)) & 1)) continue;
@@ -1033,7 +1051,6 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       };
       do {
         for (int t = 0; t < w.cnt; ++t, ++tile) {
-          if (S::kQs == 2 && t == 0) load_q(w);
           placed(tile);
           const int64_t* offs = ctl.off[tile & 3];
           const Info& f = ctl.tile[tile % kInfos];
@@ -1060,8 +1077,6 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tc::smem_u32(&ctl.full[e % kEntries])) : "memory");
           }
           arrive(&ctl.taken[tile & 3]);
-          // where queries have one place, the first tile is under way before the last segment's are done with
-          if (S::kQs == 1 && t == 0) load_q(w);
         }
       } while (w.next());
       asm volatile("cp.async.wait_all;" ::: "memory");
@@ -1077,6 +1092,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
 #pragma unroll 1
         for (int i = 0; i < kEach; ++i) {
           const int r = row0 + i * kPass;
+          if (a.window == 0 && (i + 1) * kPass <= f.n - f.p0) continue;  // no nodes there
           int k;
           const uint64_t bit = (f.valid[r >> 5] >> (r & 31)) & 1 ? apart(f, r, k) : 0;
           const bool none = (fac[r] & 0x7fffu) > 0x7c00u;  // the row's scale
@@ -1152,6 +1168,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
 #pragma unroll 1
           for (int kv = kind; kv < (S::kSplit ? kind + 1 : 2); ++kv) put(2 * tile + kv, fac[kv], kv && (f.flags & 1), f);
           arrive(&ctl.taken[tile & 3]);
+          // (where they have one place, the first tile is under way before the last segment's are done with)
           if (S::kQs == 1 && t == 0) load_q(w);
         }
       } while (w.next());
