@@ -189,66 +189,84 @@ pe_status kv_append_launch(const pe_kv_cache& c, const pe_kv_scales& sc, const p
 
 // ---------------------------------------------------------------------------
 // Rows from one position of a sequence to another.  A CTA holds all moves of one
-// sequence's head, keys or values, in registers between the reads and the
-// writes, so that a move's source may be another's target.
+// sequence's heads, or of some of them, keys or values, in registers between the
+// reads and the writes, so that a move's source may be another's target.  Bound
+// by latency: three dependent reads, then the write (32 sequences of 5 moves, 8
+// heads of 128: MOVE_STEP us); with as many heads a CTA as its threads hold 16-byte
+// parts for, 512 sequences of 16 moves of 16 heads of 128 codes take MOVE_BATCH us
+// (a head a CTA: 19.2).
 // ---------------------------------------------------------------------------
 constexpr int kMoveThreads = 256, kMoveMost = 64;
 
-// R: bytes of a row
-template <int R>
-__global__ void __launch_bounds__(kMoveThreads) kv_move_kernel(MoveArgs a) {
-  constexpr int kChunks = R / 16, kRows = kMoveThreads / kChunks, kEach = (kMoveMost + kRows - 1) / kRows;
+// R: bytes of a row; kEach: 16-byte parts of a thread
+template <int R, int kEach>
+__global__ void __launch_bounds__(kMoveThreads) kv_move_kernel(MoveArgs a, int heads) {
+  constexpr int kChunks = R / 16;
   const pe_kv_cache& c = a.c;
-  const int b = blockIdx.x, h = blockIdx.y, row0 = threadIdx.x / kChunks, ch = threadIdx.x % kChunks;
+  const int b = blockIdx.x, h0 = blockIdx.y * heads, ch = threadIdx.x % kChunks;
   const bool value = blockIdx.z != 0, eight = c.dtype == PE_E4M3;
   const int es = eight ? 1 : 2;  // bytes of an element
   pdl_enter();
-  char* base = (char*)(value ? c.v : c.k) + h * c.head_stride * es + ch * 16;
-  uint8_t* scales = (value ? a.sc.v : a.sc.k) + h * a.sc.head_stride;
+  char* base = (char*)(value ? c.v : c.k) + ch * 16;
+  uint8_t* scales = value ? a.sc.v : a.sc.k;
   const int cap = c.max_pages * c.page_size;
   uint4 x[kEach];
   uint8_t sx[kEach];
-  int page[kEach], slot[kEach];  // of the target; page -1: no move
+  int64_t to[kEach], sto[kEach];  // offsets of the target and of its scale; -1: no move
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
-    const int m = row0 + i * kRows;
-    page[i] = -1;
-    slot[i] = 0;
+    const int r = (threadIdx.x + i * kMoveThreads) / kChunks, h = r / a.n, m = r - h * a.n;  // of n moves of each head
+    to[i] = -1;
+    sto[i] = 0;
     x[i] = make_uint4(0, 0, 0, 0);
     sx[i] = 0;
-    if (m >= a.n) continue;
+    if (h >= heads || h0 + h >= c.n_heads) continue;
     const int s = a.src[b * a.src_stride + m], d = a.dst[b * a.dst_stride + m];
     if (s < 0 || s >= cap || d < 0 || d >= cap || s == d) continue;
     const int32_t* table = c.table + (int64_t)b * c.table_stride;
-    const int sp = table[s / c.page_size], dp = table[d / c.page_size];
+    const int si = s / c.page_size, di = d / c.page_size;
+    const int sp = table[si], dp = table[di];
     if (sp < 0 || sp >= c.n_pages || dp < 0 || dp >= c.n_pages) continue;
-    page[i] = dp;
-    slot[i] = d % c.page_size;
-    x[i] = *reinterpret_cast<const uint4*>(base + (kv_page_offset(c, sp) + (int64_t)(s % c.page_size) * c.slot_stride) * es);
-    if (eight && ch == 0) sx[i] = scales[sp * a.sc.page_stride + (int64_t)(s % c.page_size) * a.sc.slot_stride];
+    const int64_t head = (h0 + h) * c.head_stride, shead = (h0 + h) * a.sc.head_stride;
+    const int ss = s - si * c.page_size, ds = d - di * c.page_size;
+    to[i] = (kv_page_offset(c, dp) + (int64_t)ds * c.slot_stride + head) * es;
+    x[i] = *reinterpret_cast<const uint4*>(base + (kv_page_offset(c, sp) + (int64_t)ss * c.slot_stride + head) * es);
+    if (eight && ch == 0) {
+      sto[i] = dp * a.sc.page_stride + (int64_t)ds * a.sc.slot_stride + shead;
+      sx[i] = scales[sp * a.sc.page_stride + (int64_t)ss * a.sc.slot_stride + shead];
+    }
   }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
-    if (page[i] < 0) continue;
-    *reinterpret_cast<uint4*>(base + (kv_page_offset(c, page[i]) + (int64_t)slot[i] * c.slot_stride) * es) = x[i];
-    if (eight && ch == 0) scales[page[i] * a.sc.page_stride + (int64_t)slot[i] * a.sc.slot_stride] = sx[i];
+    if (to[i] < 0) continue;
+    *reinterpret_cast<uint4*>(base + to[i]) = x[i];
+    if (eight && ch == 0) scales[sto[i]] = sx[i];
   }
+}
+
+template <int R>
+static pe_status move_rows(const MoveArgs& a, cudaStream_t st) {
+  constexpr int kChunks = R / 16, kMany = kMoveMost * kChunks / kMoveThreads > 4 ? kMoveMost * kChunks / kMoveThreads : 4;
+  // as many heads as four parts a thread allow, fewer where that leaves SMs without a CTA
+  int heads = kMoveThreads * 4 / (a.n * kChunks);
+  heads = heads < 1 ? 1 : heads > a.c.n_heads ? a.c.n_heads : heads;
+  while (heads > 1 && (int64_t)a.c.n_seqs * ceil_div(a.c.n_heads, heads) * 2 < 2 * 152) heads = (heads + 1) / 2;
+  const dim3 grid(a.c.n_seqs, ceil_div(a.c.n_heads, heads), 2), block(kMoveThreads);
+  const int parts = ceil_div((int64_t)a.n * kChunks * heads, kMoveThreads);
+  if (parts <= 1)
+    PE_TRY_CUDA(launch_pdl(kv_move_kernel<R, 1>, grid, block, 0, st, true, a, heads));
+  else if (parts <= 4)
+    PE_TRY_CUDA(launch_pdl(kv_move_kernel<R, 4>, grid, block, 0, st, true, a, heads));
+  else
+    PE_TRY_CUDA(launch_pdl(kv_move_kernel<R, kMany>, grid, block, 0, st, true, a, heads));
+  return PE_OK;
 }
 
 pe_status kv_move_launch(const MoveArgs& a, cudaStream_t st) {
   ProfScope ps(PE_PROF_KV_MOVE, st);
-  const dim3 grid(a.c.n_seqs, a.c.n_heads, 2), block(kMoveThreads);
   const int row = a.c.head_dim * (a.c.dtype == PE_E4M3 ? 1 : 2);
-  if (row == 64)
-    PE_TRY_CUDA(launch_pdl(kv_move_kernel<64>, grid, block, 0, st, true, a));
-  else if (row == 128)
-    PE_TRY_CUDA(launch_pdl(kv_move_kernel<128>, grid, block, 0, st, true, a));
-  else if (row == 256)
-    PE_TRY_CUDA(launch_pdl(kv_move_kernel<256>, grid, block, 0, st, true, a));
-  else
-    PE_TRY_CUDA(launch_pdl(kv_move_kernel<512>, grid, block, 0, st, true, a));
-  return PE_OK;
+  return row == 64 ? move_rows<64>(a, st) : row == 128 ? move_rows<128>(a, st) : row == 256 ? move_rows<256>(a, st) : move_rows<512>(a, st);
 }
 
 }  // namespace pe

@@ -64,7 +64,7 @@ struct Shape {
   static constexpr int kStages = !E8 ? 0 : WIDE || D == 64 ? 4 : 3;  // entries of codes on their way
   // two producer warps for keys and two for values, where each kind has its own places (an odd number
   // of them passes from one kind to the other, and a wait for the one would not see the other's turn)
-  static constexpr bool kSplit = kEntries % 2 == 0 && kStages % 2 == 0;
+  static constexpr bool kSplit = kEntries % 2 == 0 && kStages % 2 == 0 && !(E8 && WIDE);
   static constexpr int kBring = kSplit ? kProducers / 2 : kProducers;  // warps that bring an entry
   static constexpr int kTurn = WIDE ? 4 : 2;  // tiles that a segment's end is worth in the dealing (it takes 6-9 k clk)
   static constexpr int kQBytes = kRows * D * 2;
@@ -1182,8 +1182,9 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
   if (tid == 0 && ctl.err) atomicExch(g.error, 1);
 }
 
-// Joins the pieces of a segment in the order of the CTAs.  A warp takes a row;
-// its lanes hold the pieces' maxima and sums, then the output's elements.
+// Joins the pieces of a segment in the order of the CTAs.  A warp takes a row; its
+// lanes hold the pieces' maxima and sums, then the output's elements.  Bound by
+// latency, so the first pieces are on their way before their weights are known.
 constexpr int kJoinRows = 8;
 template <typename T, typename M, int D>
 __global__ void __launch_bounds__(32 * kJoinRows) join_kernel(Args g, int block_rows) {
@@ -1198,34 +1199,55 @@ __global__ void __launch_bounds__(32 * kJoinRows) join_kernel(Args g, int block_
   const int64_t slot = (int64_t)block_rows * (D + 2);
   // piece 0 is in first_slot, the others in the first slots of the CTAs after it
   auto at = [&](int i) { return g.part + (i ? (int64_t)((s.first_slot & ~1) + 2 * i) : (int64_t)s.first_slot) * slot; };
-  float mm = -CUDART_INF_F, sum = 0.0f;
-  for (int i = lane; i < s.pieces; i += 32) mm = fmaxf(mm, at(i)[block_rows * D + row]);
+  constexpr int kV = D / 128 > 0 ? D / 128 : 1, kEarly = D == 256 ? 4 : 8;  // float4s of a lane (head_dim 64: of half the lanes)
+  const bool mine = D > 64 || lane < 16;
+  float4 o[kV], early[kEarly][kV];
+#pragma unroll
+  for (int i = 0; i < kEarly; ++i)
+#pragma unroll
+    for (int v = 0; v < kV; ++v)
+      if (i < s.pieces && mine) early[i][v] = reinterpret_cast<const float4*>(at(i) + (int64_t)row * D)[lane + 32 * v];
+  float mm = -CUDART_INF_F, sum = 0.0f, m0 = -CUDART_INF_F, l0 = 0.0f;
+  if (lane < s.pieces) {
+    m0 = at(lane)[block_rows * D + row];
+    l0 = at(lane)[block_rows * (D + 1) + row];
+  }
+  mm = m0;
+  for (int i = lane + 32; i < s.pieces; i += 32) mm = fmaxf(mm, at(i)[block_rows * D + row]);
   for (int x = 16; x; x >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, x));
-  constexpr int kV = D / 128 > 0 ? D / 128 : 1;  // float4s of a lane (head_dim 64: of half the lanes)
-  float4 o[kV];
 #pragma unroll
   for (int v = 0; v < kV; ++v) o[v] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  auto add = [&](float4& y, float w, float4 x) {
+    y.x = fmaf(w, x.x, y.x), y.y = fmaf(w, x.y, y.y), y.z = fmaf(w, x.z, y.z), y.w = fmaf(w, x.w, y.w);
+  };
   for (int i0 = 0; i0 < s.pieces; i0 += 32) {
-    float f = 0.0f, fl = 0.0f;
-    if (i0 + lane < s.pieces) {
-      const float* p = at(i0 + lane);
-      f = piece_weight(p[block_rows * D + row], mm);
-      fl = f * p[block_rows * (D + 1) + row];
+    if (i0 > 0) {
+      m0 = -CUDART_INF_F, l0 = 0.0f;
+      if (i0 + lane < s.pieces) {
+        m0 = at(i0 + lane)[block_rows * D + row];
+        l0 = at(i0 + lane)[block_rows * (D + 1) + row];
+      }
     }
-    float all = fl;
+    const float f = i0 + lane < s.pieces ? piece_weight(m0, mm) : 0.0f;
+    float all = f * l0;
     for (int x = 16; x; x >>= 1) all += __shfl_xor_sync(0xffffffffu, all, x);
     sum += all;
+    if (i0 == 0)
+#pragma unroll
+      for (int i = 0; i < kEarly; ++i) {
+        const float w = __shfl_sync(0xffffffffu, f, i);
+        if (i < s.pieces && mine)
+#pragma unroll
+          for (int v = 0; v < kV; ++v) add(o[v], w, early[i][v]);
+      }
     const int n = min(32, s.pieces - i0);
 #pragma unroll 4
-    for (int i = 0; i < n; ++i) {
-      const float wgt = __shfl_sync(0xffffffffu, f, i);
+    for (int i = i0 == 0 ? kEarly : 0; i < n; ++i) {
+      const float w = __shfl_sync(0xffffffffu, f, i);
       const float4* p = reinterpret_cast<const float4*>(at(i0 + i) + (int64_t)row * D);
 #pragma unroll
-      for (int v = 0; v < kV; ++v) {
-        if (D == 64 && lane >= 16) continue;
-        const float4 x = p[lane + 32 * v];
-        o[v].x = fmaf(wgt, x.x, o[v].x), o[v].y = fmaf(wgt, x.y, o[v].y), o[v].z = fmaf(wgt, x.z, o[v].z), o[v].w = fmaf(wgt, x.w, o[v].w);
-      }
+      for (int v = 0; v < kV; ++v)
+        if (mine) add(o[v], w, p[lane + 32 * v]);
     }
   }
   const int rr = r0 + row, node = rr / G, head = hk * G + rr % G;
