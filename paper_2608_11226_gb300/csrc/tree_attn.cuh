@@ -17,8 +17,10 @@
 // fp16), one thread issues the products, two warpgroups take the softmax: a
 // thread reads its row of S from TMEM and puts the weights P back as the second
 // product's operand.
-//   Wide (more than 128 rows in a block): each warpgroup has 128 rows of its own;
-//     tiles of 64 positions, so that S has two buffers here as well, and P replaces S.
+//   Wide (more than 128 rows in a block): each warpgroup has 128 rows of its own,
+//     whose products run while the other works on its weights; P replaces S.  (Tiles of
+//     64 positions, with two buffers of S, were slower: what a tile costs besides its
+//     products came twice as often.)
 //   Narrow: both warpgroups share one tile of 128 rows, half of the tile's columns
 //     each (they exchange the maxima), and S and P have two buffers.
 //
@@ -52,7 +54,8 @@ struct SegMeta {
 template <int D, bool E8, bool WIDE>
 struct Shape {
   static_assert(!(WIDE && D == 256), "two outputs of 256 columns leave no room for scores");
-  static constexpr int kKeys = D == 256 || WIDE ? 64 : 128;
+  static constexpr int kKeys = D == 256 ? 64 : 128;
+  static constexpr int kBufs = WIDE ? 1 : 2;  // of scores, for each track of rows
   static constexpr int kRows = WIDE ? 256 : 128;  // of a block
   static constexpr int kShared = WIDE ? 1 : 128;  // rows that two threads share
   static constexpr int kProducers = 4;            // warps
@@ -60,13 +63,13 @@ struct Shape {
   static constexpr int kEntry = kKeys * D * 2;
   // queries of two segments where there is room, so that the next one's are there in time
   static constexpr int kQs = WIDE || D == 256 ? 1 : 2;
-  static constexpr int kEntries = WIDE ? (E8 && D == 128 ? 6 : 8) : D == 64 ? 6 : E8 ? 3 : 4;
-  static constexpr int kStages = !E8 ? 0 : WIDE || D == 64 ? 4 : 3;  // entries of codes on their way
+  static constexpr int kEntries = D == 64 ? (WIDE ? 8 : 6) : E8 ? 3 : 4;
+  static constexpr int kStages = !E8 ? 0 : D == 64 ? 4 : 3;  // entries of codes on their way
   // two producer warps for keys and two for values, where each kind has its own places (an odd number
   // of them passes from one kind to the other, and a wait for the one would not see the other's turn)
   static constexpr bool kSplit = kEntries % 2 == 0 && kStages % 2 == 0 && !(E8 && WIDE);
   static constexpr int kBring = kSplit ? kProducers / 2 : kProducers;  // warps that bring an entry
-  static constexpr int kTurn = WIDE ? 4 : 2;  // tiles that a segment's end is worth in the dealing (it takes 6-9 k clk)
+  static constexpr int kTurn = 2;  // tiles that a segment's end is worth in the dealing (it takes 6-9 k clk)
   static constexpr int kQBytes = kRows * D * 2;
   static constexpr int kNeed = kQs * kQBytes + kEntries * kEntry + kStages * kEntry / 2 + 1024;
   static constexpr int kSmem = kNeed > kPdlTmemSmem ? kNeed : kPdlTmemSmem + 1024;
@@ -486,7 +489,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         continue;
       }
       for (int t = 0; t < w.cnt; ++t, ++ip) {
-        const int b2 = t & 1, buf = WIDE ? 2 * wg + b2 : b2;  // of scores and weights
+        const int b2 = t % S::kBufs, buf = WIDE ? wg : b2;  // of scores and weights
         wait(ctl, &ctl.info[ip % kInfos], (ip / kInfos) & 1);
         const Info& f = ctl.tile[ip % kInfos];
         wait(ctl, &ctl.s_full[buf], sp[b2] & 1);
@@ -877,7 +880,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             if (x >= tracks) break;
             // a track's next scores right behind its outputs: what waits for them is its softmax
             if (np[x] < nk[x]) {
-              const int t = np[x], b2 = t & 1, buf = WIDE ? 2 * x + b2 : b2;
+              const int t = np[x], b2 = t % S::kBufs, buf = WIDE ? x : b2;
               const uint32_t e = e0 + 2 * t + 1, phase = b2 ? ps[2 * x + 1] : ps[2 * x];
               if (__all_sync(0xffffffffu, mbar_test(&ctl.p_full[buf], phase & 1)) && (vseen > t || landed(e))) {
                 vseen = max(vseen, t + 1);
@@ -897,13 +900,13 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
                 any = true;
               }
             }
-            // (two tiles ahead of the outputs)
-            if (nk[x] < nt && nk[x] < np[x] + 2) {
+            // (kBufs tiles ahead of the outputs)
+            if (nk[x] < nt && nk[x] < np[x] + S::kBufs) {
               const int t = nk[x];
               const uint32_t e = e0 + 2 * t;
               if (kseen > t || landed(e)) {
                 kseen = max(kseen, t + 1);
-                const int buf = WIDE ? 2 * x + (t & 1) : t & 1;
+                const int buf = WIDE ? x : t & 1;
                 tc::fence_after();
                 const uint32_t qd = (uint32_t)k0 | (qs4 + (qb * S::kQBytes + x * 128 * 128 * (D / 64)) / 16), kd = uniform((uint32_t)k0 | entry(e));
                 const uint32_t to = uniform(tm + S::kS + buf * S::kSStep);
