@@ -861,76 +861,99 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       auto commit = [&](uint64_t* b) {
         if (leader) tc::mma_commit(b);
       };
-      uint32_t ps[4] = {0, 0, 0, 0};  // phases of the weights
-      uint32_t e0 = 0;                // entry of the segment's first keys
+      // output of tile t of track x: the weights are there, and the values
+      auto outputs = [&](int x, int buf, uint32_t e, bool first) {
+        tc::fence_after();
+        const uint32_t vd = uniform((uint32_t)v0 | entry(e)), out = tm + S::kO + x * S::kOStep, p = uniform(tm + S::kP + buf * S::kPStep);
+        const uint32_t more = uniform(!first);
+#pragma unroll
+        for (int kk = 0; kk < kKeys / 16; ++kk)
+          mma_ts(out, p + 8 * kk, desc_of(vd + kk * 128, (uint32_t)(v0 >> 32)), kIdO, kk > 0 ? 1u : more, leader);
+        commit(&ctl.pv_done[x]);
+      };
+      auto scores = [&](int x, int buf, int qb, uint32_t e) {
+        tc::fence_after();
+        const uint32_t qd = (uint32_t)k0 | (qs4 + (qb * S::kQBytes + x * 128 * 128 * (D / 64)) / 16), kd = uniform((uint32_t)k0 | entry(e));
+        const uint32_t to = uniform(tm + S::kS + buf * S::kSStep);
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)
+          mma_ss(to, desc_of(qd + ((kk >> 2) * 128 * 128 + (kk & 3) * 32) / 16, (uint32_t)(k0 >> 32)),
+                 desc_of(kd + ((kk >> 2) * kKeys * 128 + (kk & 3) * 32) / 16, (uint32_t)(k0 >> 32)), kIdS, kk > 0, leader);
+        commit(&ctl.s_full[buf]);
+      };
+      uint32_t ps[2] = {0, 0};  // phases of the weights
+      uint32_t e0 = 0;          // entry of the segment's first keys
       Walk<kKeys, kTurn> w(g, ctl.where, share);
       do {
         const int rows = min(R - w.s.blk * S::kRows, S::kRows), nt = (int)uniform(w.cnt);
-        const int tracks = WIDE && uniform(rows > 128) ? 2 : 1;  // of rows with products of their own
         const int qb = S::kQs == 1 ? 0 : (int)uniform(w.index & 1);
         wait(ctl, &ctl.q_full[qb], (w.index / S::kQs) & 1);
         __syncwarp();
         if (!E8) tc::fence_async_smem();
-        int nk[2] = {0, 0}, np[2] = {0, 0}, kseen = 0, vseen = 0;  // tiles whose scores, outputs are under way; that have landed
-        long long t0 = clock64();
-        while (np[0] < nt || (tracks == 2 && np[1] < nt)) {
-          bool any = false;
+        if constexpr (WIDE) {
+          // The tracks take turns: a track's next scores go right behind its outputs, for its softmax is what
+          // waits for them.  (Waits in this order wake faster than a look at everything in turn: 400-800 clk.)
+          const int tracks = uniform(rows > 128) ? 2 : 1;
+          auto await = [&](uint32_t e) {
+            wait(ctl, &ctl.full[e % kEntries], (e / kEntries) & 1);
+            __syncwarp();
+            if (!E8) tc::fence_async_smem();
+          };
+          await(e0);
+          for (int x = 0; x < tracks; ++x) scores(x, x, qb, e0);
+          commit(&ctl.empty[e0 % kEntries]);
+          if (nt == 1) commit(&ctl.q_empty[qb]);
+#pragma unroll 1
+          for (int t = 0; t < nt; ++t) {
+            const uint32_t ve = e0 + 2 * t + 1, ke = ve + 1;
+            await(ve);
 #pragma unroll
-          for (int x = 0; x < (WIDE ? 2 : 1); ++x) {
-            if (x >= tracks) break;
-            // a track's next scores right behind its outputs: what waits for them is its softmax
-            if (np[x] < nk[x]) {
-              const int t = np[x], b2 = t % S::kBufs, buf = WIDE ? x : b2;
-              const uint32_t e = e0 + 2 * t + 1, phase = b2 ? ps[2 * x + 1] : ps[2 * x];
-              if (__all_sync(0xffffffffu, mbar_test(&ctl.p_full[buf], phase & 1)) && (vseen > t || landed(e))) {
-                vseen = max(vseen, t + 1);
-                if (b2)
-                  ++ps[2 * x + 1];
-                else
-                  ++ps[2 * x];
-                tc::fence_after();
-                const uint32_t vd = uniform((uint32_t)v0 | entry(e)), out = tm + S::kO + x * S::kOStep, p = uniform(tm + S::kP + buf * S::kPStep);
-                const uint32_t more = uniform(t != 0);
-#pragma unroll
-                for (int kk = 0; kk < kKeys / 16; ++kk)
-                  mma_ts(out, p + 8 * kk, desc_of(vd + kk * 128, (uint32_t)(v0 >> 32)), kIdO, kk > 0 ? 1u : more, leader);
-                commit(&ctl.pv_done[x]);
-                ++np[x];
-                if (tracks == 1 || np[x ^ 1] >= np[x]) commit(&ctl.empty[e % kEntries]);
-                any = true;
-              }
-            }
-            // (kBufs tiles ahead of the outputs)
-            if (nk[x] < nt && nk[x] < np[x] + S::kBufs) {
-              const int t = nk[x];
-              const uint32_t e = e0 + 2 * t;
-              if (kseen > t || landed(e)) {
-                kseen = max(kseen, t + 1);
-                const int buf = WIDE ? x : t & 1;
-                tc::fence_after();
-                const uint32_t qd = (uint32_t)k0 | (qs4 + (qb * S::kQBytes + x * 128 * 128 * (D / 64)) / 16), kd = uniform((uint32_t)k0 | entry(e));
-                const uint32_t to = uniform(tm + S::kS + buf * S::kSStep);
-#pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk)
-                  mma_ss(to, desc_of(qd + ((kk >> 2) * 128 * 128 + (kk & 3) * 32) / 16, (uint32_t)(k0 >> 32)),
-                         desc_of(kd + ((kk >> 2) * kKeys * 128 + (kk & 3) * 32) / 16, (uint32_t)(k0 >> 32)), kIdS, kk > 0, leader);
-                commit(&ctl.s_full[buf]);
-                ++nk[x];
-                if (tracks == 1 || nk[x ^ 1] >= nk[x]) {
-                  commit(&ctl.empty[e % kEntries]);
-                  if (nk[x] == nt) commit(&ctl.q_empty[qb]);
-                }
-                any = true;
+            for (int x = 0; x < 2; ++x) {
+              if (x >= tracks) break;
+              wait(ctl, &ctl.p_full[x], ps[x] & 1);
+              __syncwarp();
+              ++ps[x];
+              outputs(x, x, ve, t == 0);
+              if (x == tracks - 1) commit(&ctl.empty[ve % kEntries]);
+              if (t + 1 == nt) continue;
+              if (x == 0) await(ke);
+              scores(x, x, qb, ke);
+              if (x == tracks - 1) {
+                commit(&ctl.empty[ke % kEntries]);
+                if (t + 2 == nt) commit(&ctl.q_empty[qb]);
               }
             }
           }
-          if (any) {
-            t0 = clock64();
-            continue;
-          }
-          if (__any_sync(0xffffffffu, clock64() - t0 > 4000000000LL || *(volatile int*)&ctl.err)) {
-            atomicExch(&ctl.err, 1);
-            break;
+        } else {
+          int nk = 0, np = 0;  // tiles whose scores, outputs are under way: by what has arrived, scores two tiles ahead
+          long long t0 = clock64();
+          while (np < nt) {
+            bool any = false;
+            if (np < nk && __all_sync(0xffffffffu, mbar_test(&ctl.p_full[np & 1], ((np & 1) ? ps[1] : ps[0]) & 1)) &&
+                landed(e0 + 2 * np + 1)) {
+              if (np & 1)
+                ++ps[1];
+              else
+                ++ps[0];
+              const uint32_t e = e0 + 2 * np + 1;
+              outputs(0, np & 1, e, np == 0);
+              commit(&ctl.empty[e % kEntries]);
+              ++np;
+              any = true;
+            }
+            if (nk < nt && nk < np + 2 && landed(e0 + 2 * nk)) {
+              const uint32_t e = e0 + 2 * nk;
+              scores(0, nk & 1, qb, e);
+              commit(&ctl.empty[e % kEntries]);
+              if (++nk == nt) commit(&ctl.q_empty[qb]);
+              any = true;
+            }
+            if (any) {
+              t0 = clock64();
+            } else if (__any_sync(0xffffffffu, clock64() - t0 > 4000000000LL || *(volatile int*)&ctl.err)) {
+              atomicExch(&ctl.err, 1);
+              break;
+            }
           }
         }
         e0 += 2 * nt;
