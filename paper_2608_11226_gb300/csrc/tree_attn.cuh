@@ -97,7 +97,7 @@ struct Control {
   uint16_t fac[4][2][S::kKeys];  // 2^(e - E) in fp16
   int64_t sum[16];
   float mx[2][2][S::kShared], l[2][S::kShared], qf[4][S::kRows];
-  int where[4];
+  int where[5];  // sequence, key head and block, tile, length; what the share has of a segment's end ahead of that
   uint32_t tmem;
   int err;
 };
@@ -140,14 +140,18 @@ __device__ __forceinline__ void seg_range(const TreeArgs& a, int len, Seg& s) {
 
 // The line of `total` tiles dealt out to `workers` CTAs: the first `more` get one
 // more than the others.
+__device__ __forceinline__ int64_t quotient(int64_t a, int b) {  // of numbers that mostly have 32 bits
+  return a >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
 struct Deal {
   int64_t each;
   int more;
-  __device__ __forceinline__ Deal(int64_t total, int workers) : each(total / workers), more((int)(total % workers)) {}
+  __device__ __forceinline__ Deal(int64_t total, int workers) : each(quotient(total, workers)), more((int)(total - each * workers)) {}
   __device__ __forceinline__ int64_t start(int w) const { return w * each + min(w, more); }
   __device__ __forceinline__ int worker(int64_t tile) const {
     const int64_t cut = more * (each + 1);
-    return tile < cut ? (int)(tile / (each + 1)) : more + (int)((tile - cut) / each);
+    return each >> 30 ? (tile < cut ? (int)(tile / (each + 1)) : more + (int)((tile - cut) / each))
+                      : (tile < cut ? (int)quotient(tile, (int)each + 1) : more + (int)quotient(tile - cut, (int)each));
   }
 };
 
@@ -417,42 +421,34 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       if (start < at + (int64_t)(s0.nt + kTurn) * g.groups) break;
       at += (int64_t)(s0.nt + kTurn) * g.groups;
     }
-    ctl.where[0] = b;
-    ctl.where[1] = (int)((start - at) / (s0.nt + kTurn));
-    ctl.where[2] = (int)((start - at) % (s0.nt + kTurn));
-    ctl.where[3] = len;
-  }
-  __syncthreads();
-  const uint32_t tmem = ctl.tmem;
-  int skip = 0;  // what the share has of a segment's end
-  if (share > 0) {
-    Walk<kKeys, kTurn> w(g, ctl.where, share);
-    if (w.ct >= w.s.nt) {
+    int grp = (int)quotient(start - at, s0.nt + kTurn), skip = 0;
+    int ct = (int)(start - at - (int64_t)grp * (s0.nt + kTurn));
+    if (ct >= s0.nt) {
       // the share starts within a segment's end: with the next segment, if it has one
-      skip = w.s.nt + kTurn - w.ct;
-      share -= skip;
-      __syncthreads();
-      if (tid == 0 && share > 0) {
-        w.advance();
-        ctl.where[0] = w.s.b, ctl.where[1] = w.s.hk * g.blocks + w.s.blk, ctl.where[2] = 0, ctl.where[3] = a.lens[w.s.b];
+      skip = s0.nt + kTurn - ct;
+      ct = 0;
+      if (++grp == g.groups) {
+        grp = 0;
+        if (++b < B) len = a.lens[b];
       }
-      __syncthreads();
     }
-  }
-  if (tid == 0) {
-    // the boundary at this CTA's start joins the segment if it is the first inside it
+    ctl.where[0] = b, ctl.where[1] = grp, ctl.where[2] = ct, ctl.where[3] = len, ctl.where[4] = skip;
     SegMeta m{0, 0, 0, 0};
-    if (share > 0) {
-      Walk<kKeys, kTurn> w(g, ctl.where, share);
-      const int64_t g0 = start + skip - w.ct, prev = blockIdx.x ? deal.start((int)blockIdx.x - 1) : 0;
-      m.seq = w.s.b, m.group = w.s.hk * g.blocks + w.s.blk;
-      if (w.ct > 0 && prev <= g0) {
-        m.pieces = deal.worker(g0 + w.s.nt - 1) - blockIdx.x + 2;
+    if (share > skip && ct > 0) {
+      // the boundary at this CTA's start joins the segment if it is the first inside it
+      const int64_t g0 = start - ct, prev = deal.start((int)blockIdx.x - 1);
+      if (prev <= g0) {
+        m.seq = b, m.group = grp;
+        m.pieces = deal.worker(g0 + s0.nt - 1) - blockIdx.x + 2;
         m.first_slot = 2 * (blockIdx.x - 1) + (prev < g0 - kTurn ? 1 : 0);  // (not its first segment)
       }
     }
-    g.meta[blockIdx.x] = m;
+    if (share > 0) g.meta[blockIdx.x] = m;
   }
+  if (tid == 0 && share <= 0) g.meta[blockIdx.x] = SegMeta{0, 0, 0, 0};
+  __syncthreads();
+  const uint32_t tmem = ctl.tmem;
+  share -= share > 0 ? ctl.where[4] : 0;
 
   if (share <= 0) {
     // nothing to do
