@@ -154,17 +154,21 @@ struct Segment {
   int b, h, hk;     // sequence, head group, key head
   int nt;           // tiles
   int base, lo, n;  // position of the first (a multiple of the unit), attended range [lo, n)
+  int ctx;          // of drafted nodes: where they start
   int ahead;        // length of the next sequence, on its way
 };
 
 // nt counts tiles of `tile` positions; base is a multiple of `align`
+template <bool TREE>
 __device__ __forceinline__ void seq_range(const DecodeArgs& a, int len, int align, int tile, Segment& s) {
   const int cap = a.c.max_pages * a.c.page_size;
   s.n = min(max(len, 0), cap);
-  s.lo = a.window > 0 ? max(0, s.n - a.window) : 0;
+  s.lo = a.window > 0 ? max(0, s.n + (TREE ? 1 : 0) - a.window) : 0;
+  if (TREE) s.ctx = s.n, s.n = min(cap, s.n + a.n_nodes);
   s.base = s.lo & ~(align - 1);
   s.nt = max(1, (s.n - s.base + tile - 1) / tile);  // an empty sequence has one empty tile
 }
+template <bool TREE>
 __device__ __forceinline__ void next_segment(const DecodeArgs& a, int groups, int per_head, int align, int tile, Segment& s) {
   if (++s.h < groups) {
     s.hk = s.h / per_head;
@@ -172,7 +176,7 @@ __device__ __forceinline__ void next_segment(const DecodeArgs& a, int groups, in
   }
   s.h = s.hk = 0;
   ++s.b;
-  seq_range(a, s.ahead, align, tile, s);
+  seq_range<TREE>(a, s.ahead, align, tile, s);
   s.ahead = a.lens[min(s.b + 1, a.c.n_seqs - 1)];
 }
 
@@ -189,18 +193,19 @@ template <typename T> __device__ __forceinline__ float log_sum(float mm, float s
 // leaves it in a warp, scaled by the lane's two heads' factors: transposed in
 // registers, so that a lane writes two neighbouring elements of one head.
 // Over codes the rows of a tile are the elements 0, 2, ... 14, 1, 3, ... 15.
+// `out` is the row of head lane / 4.
 template <typename T, bool E8>
-__device__ __forceinline__ void store_tile(T* out, int64_t head_stride, int heads, int kk, float4 o, float f0, float f1) {
+__device__ __forceinline__ void store_tile(T* out, int heads, int kk, float4 o, float f0, float f1) {
   const int lane = threadIdx.x & 31;
   // a factor of 0 stands for a sum of 0, nothing attended to
   const uint32_t lo = transpose8(pack2<T>(f0 == 0.0f ? 0.0f : o.x * f0, f1 == 0.0f ? 0.0f : o.y * f1));
   const uint32_t hi = transpose8(pack2<T>(f0 == 0.0f ? 0.0f : o.z * f0, f1 == 0.0f ? 0.0f : o.w * f1));
   if (lane / 4 < heads) {
     if constexpr (E8) {
-      *reinterpret_cast<uint2*>(out + (lane / 4) * head_stride + kk * 16 + 4 * (lane & 3)) =
+      *reinterpret_cast<uint2*>(out + kk * 16 + 4 * (lane & 3)) =
           make_uint2(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632));
     } else {
-      uint32_t* p = reinterpret_cast<uint32_t*>(out + (lane / 4) * head_stride + kk * 16 + 2 * (lane & 3));
+      uint32_t* p = reinterpret_cast<uint32_t*>(out + kk * 16 + 2 * (lane & 3));
       p[0] = lo;
       p[4] = hi;
     }
@@ -268,26 +273,47 @@ struct Deal {
   }
 };
 
-// the result of a tile: eight heads from `head` on, of which `heads` exist
-template <typename T, bool E8>
-__device__ __forceinline__ void finish(const DecodeArgs& a, int seq, int64_t head, int heads, int kk, const Joined& j) {
+// Rows of a key head: its query heads, for drafted nodes (TREE) those of every
+// node, one node after the other.
+template <bool TREE> __device__ __forceinline__ int rows_of(const DecodeArgs& a) {
+  return a.n_q_heads / a.c.n_heads * (TREE ? a.n_nodes : 1);
+}
+// offset of row r within a sequence's queries or output
+template <bool TREE>
+__device__ __forceinline__ int64_t row_at(const DecodeArgs& a, int hk, int r, int64_t node_stride, int64_t head_stride) {
+  const int g = a.n_q_heads / a.c.n_heads, node = TREE ? r / g : 0;
+  return (TREE ? node * node_stride : 0) + ((int64_t)hk * g + r - node * g) * head_stride;
+}
+template <bool TREE> __device__ __forceinline__ int64_t lse_at(const DecodeArgs& a, int seq, int hk, int r) {
+  const int g = a.n_q_heads / a.c.n_heads, node = TREE ? r / g : 0;
+  return ((int64_t)seq * (TREE ? a.n_nodes : 1) + node) * a.n_q_heads + (int64_t)hk * g + r - node * g;
+}
+// mask of a row's node; 0 where there is none
+__device__ __forceinline__ uint64_t node_bits(const DecodeArgs& a, int seq, int r) {
+  const int node = r / (a.n_q_heads / a.c.n_heads);
+  return node < a.n_nodes ? a.mask[seq * a.mask_stride + node] & (0xffffffffffffffffull >> (64 - a.n_nodes)) : 0;
+}
+
+// the result of a tile: eight rows from `r` on, of which `rows` exist
+template <typename T, bool E8, bool TREE>
+__device__ __forceinline__ void finish(const DecodeArgs& a, int seq, int hk, int r, int rows, int kk, const Joined& j) {
   const int lane = threadIdx.x & 31;
   if (kk == 0 && lane < 4 && a.lse) {
-    float* lse = a.lse + (int64_t)seq * a.n_q_heads + head + 2 * lane;
-    if (2 * lane < heads) lse[0] = log_sum<Product<T, E8>>(j.m.x, j.l.x);
-    if (2 * lane + 1 < heads) lse[1] = log_sum<Product<T, E8>>(j.m.y, j.l.y);
+    if (2 * lane < rows) a.lse[lse_at<TREE>(a, seq, hk, r + 2 * lane)] = log_sum<Product<T, E8>>(j.m.x, j.l.x);
+    if (2 * lane + 1 < rows) a.lse[lse_at<TREE>(a, seq, hk, r + 2 * lane + 1)] = log_sum<Product<T, E8>>(j.m.y, j.l.y);
   }
-  store_tile<T, E8>((T*)a.out + seq * a.o_seq + head * a.o_head, a.o_head, heads, kk, j.x,
-                j.l.x == 0.0f ? 0.0f : 1.0f / j.l.x, j.l.y == 0.0f ? 0.0f : 1.0f / j.l.y);
+  store_tile<T, E8>((T*)a.out + seq * a.o_seq + row_at<TREE>(a, hk, r + lane / 4, a.o_node, a.o_head), rows, kk, j.x,
+                    j.l.x == 0.0f ? 0.0f : 1.0f / j.l.x, j.l.y == 0.0f ? 0.0f : 1.0f / j.l.y);
 }
 
 // CL: one cluster for each segment, whose teams share its units and join in
 // shared memory; otherwise the line of all tiles, dealt out to the CTAs, at
 // least `least` to each.  by_seg: the joining kernel goes by segments and not
-// by CTAs.
-template <typename T, bool E8, int D, int NT, int HT, bool CL>
+// by CTAs.  TREE: drafted nodes (one warp a team).
+template <typename T, bool E8, int D, int NT, int HT, bool CL, bool TREE>
 __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeShape<E8, D, NT, HT>::kBlocks)
     decode_attn_kernel(DecodeArgs a, int groups, int per_head, int page_shift, int ranks, int least, bool by_seg, float* part, SegMeta* meta) {
+  static_assert(!TREE || HT == 1, "a unit is its warp's own");
   using S = DecodeShape<E8, D, NT, HT>;
   using W = Product<T, E8>;
   using M = Mma<W>;
@@ -317,7 +343,7 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
     const int seg = blockIdx.x / ranks, worker = blockIdx.x % ranks * kTeams + team;
     cs.b = seg / groups;
     cs.h = seg % groups;
-    seq_range(a, a.lens[cs.b], kUnit, kTile, cs);
+    seq_range<TREE>(a, a.lens[cs.b], kUnit, kTile, cs);
     start = (int64_t)cs.nt * worker / (ranks * kTeams);
     end = (int64_t)cs.nt * (worker + 1) / (ranks * kTeams);
     first = (int)start;
@@ -330,7 +356,7 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
     Segment s;
     for (int b = tid * chunk; b < min(B, (tid + 1) * chunk); ++b) {
       len = a.lens[b];
-      seq_range(a, len, kUnit, kTile, s);
+      seq_range<TREE>(a, len, kUnit, kTile, s);
       sum += s.nt;
     }
     int64_t incl = sum;
@@ -364,7 +390,7 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
       if (chunk > 1)
         for (;; ++b) {
           len = a.lens[b];
-          seq_range(a, len, kUnit, kTile, s);
+          seq_range<TREE>(a, len, kUnit, kTile, s);
           if (start < at + (int64_t)s.nt * groups) break;
           at += (int64_t)s.nt * groups;
         }
@@ -379,7 +405,7 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
     cs.b = s_where[0];
     cs.h = s_where[1];
     first = s_where[2];
-    seq_range(a, s_where[3], kUnit, kTile, cs);
+    seq_range<TREE>(a, s_where[3], kUnit, kTile, cs);
     if (!by_seg && tid == 0) {
       // the boundary at this CTA's start joins the segment if it is the first inside it
       const int64_t g0 = start - first, prev = deal.start((int)blockIdx.x - 1);
@@ -491,7 +517,7 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
       --lleft;
       if (++lt == ls.nt) {
         lt = 0;
-        if (!CL && lleft > 0) next_segment(a, groups, per_head, kUnit, kTile, ls);
+        if (!CL && lleft > 0) next_segment<TREE>(a, groups, per_head, kUnit, kTile, ls);
       }
       if (lleft > 0) aim();
     }
@@ -521,22 +547,23 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
       asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(32 * HT) : "memory");
   };
   const float qscale = a.scale * 1.4426950408889634f;  // scores in powers of two
-  const int group = a.n_q_heads / c.n_heads;            // query heads of a key head
+  const int group = rows_of<TREE>(a);                   // query heads of a key head
   uint32_t qf[D / 16][NT][2];
   float o[D / 16][NT][4], m[NT][2], l[NT][2];
   float qc[E8 ? NT : 1][2];  // of the lane's heads: scale over the query's power of two
   auto load_q = [&]() {
-    const T* q = (const T*)a.q + cs.b * a.q_seq + (int64_t)cs.hk * group * a.q_head;
+    const T* q = (const T*)a.q + cs.b * a.q_seq;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int h = (cs.h - cs.hk * per_head) * S::kHeads + hw * 8 * NT + nt * 8 + lane / 4;
+      const T* row = q + row_at<TREE>(a, cs.hk, h < group ? h : 0, a.q_node, a.q_head);
       if constexpr (E8) {
         // the elements that a lane's four codes meet, in fp16 with the row's largest in [2^14, 2^15)
         uint2 w[D / 16];
         uint32_t most = 0;
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
-          w[kk] = h < group ? *reinterpret_cast<const uint2*>(q + h * a.q_head + kk * 16 + 4 * (lane & 3)) : make_uint2(0, 0);
+          w[kk] = h < group ? *reinterpret_cast<const uint2*>(row + kk * 16 + 4 * (lane & 3)) : make_uint2(0, 0);
           const float2 x = unpack2<T>(w[kk].x), y = unpack2<T>(w[kk].y);
           most = max(max(most, max(__float_as_uint(x.x) & 0x7fffffffu, __float_as_uint(x.y) & 0x7fffffffu)),
                      max(__float_as_uint(y.x) & 0x7fffffffu, __float_as_uint(y.y) & 0x7fffffffu));
@@ -557,7 +584,7 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
       } else {
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
-          const uint32_t* p = reinterpret_cast<const uint32_t*>(q + h * a.q_head + kk * 16 + 2 * (lane & 3));
+          const uint32_t* p = reinterpret_cast<const uint32_t*>(row + kk * 16 + 2 * (lane & 3));
           qf[kk][nt][0] = h < group ? p[0] : 0u;
           qf[kk][nt][1] = h < group ? p[4] : 0u;
         }
@@ -575,11 +602,12 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
       l[nt][0] = l[nt][1] = 0.0f;
     }
   };
-  auto sum_lanes = [&]() {  // l over the lanes that hold a head's positions
+  auto sum_lanes = [&](int seq) {  // l over the lanes that hold a head's positions
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
+        if (TREE && node_bits(a, seq, nt * 8 + 2 * (lane & 3) + i) == 0) m[nt][i] = -CUDART_INF_F, l[nt][i] = 0.0f;  // padding
         l[nt][i] += __shfl_xor_sync(0xffffffffu, l[nt][i], 4);
         l[nt][i] += __shfl_xor_sync(0xffffffffu, l[nt][i], 8);
         l[nt][i] += __shfl_xor_sync(0xffffffffu, l[nt][i], 16);
@@ -596,6 +624,72 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
         *reinterpret_cast<float2*>(p + 8 * NT * (D + 1) + nt * 8 + 2 * lane) = make_float2(l[nt][0], l[nt][1]);
       }
     }
+  };
+  // A unit that rows attend to differently (drafted nodes, the head of a window): scores that a row leaves out,
+  // and values that are not finite, which become zero and make the elements of those who attend NaN.
+  auto by_row = [&](int p0, uint32_t unit, float (&s)[kUnit / 16][NT][4]) {
+    uint64_t bits[NT][2];
+    int row_lo[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        bits[nt][i] = node_bits(a, cs.b, nt * 8 + 2 * (lane & 3) + i);
+        row_lo[nt][i] = a.window > 0 ? max(0, cs.ctx + __popcll(bits[nt][i]) - a.window) : 0;
+      }
+    auto attends = [&](int nt, int i, int p) {
+      return p < cs.ctx ? bits[nt][i] != 0 && p >= row_lo[nt][i] : p - cs.ctx < 64 && ((bits[nt][i] >> (p - cs.ctx)) & 1);
+    };
+#pragma unroll
+    for (int u = 0; u < kUnit / 16; ++u)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!attends(nt, i & 1, p0 + 16 * u + lane / 4 + 8 * (i / 2))) s[u][nt][i] = -CUDART_INF_F;
+    unsigned char* values = smem + (unit - (uint32_t)__cvta_generic_to_shared(smem)) + kUnit * kRow;
+    auto none = [](uint32_t w, int i) {  // element i of a word
+      return E8 ? ((w >> (8 * i)) & 0x7f) == 0x7f : ((w >> (16 * i)) & (std::is_same<T, __nv_bfloat16>::value ? 0x7f80u : 0x7c00u)) ==
+                                                        (std::is_same<T, __nv_bfloat16>::value ? 0x7f80u : 0x7c00u);
+    };
+    constexpr int kIn = E8 ? 4 : 2;  // elements of a word
+    uint32_t rows = 0;
+#pragma unroll 1
+    for (int x = lane; x < kUnit * kRow / 4; x += 32) {
+      const uint32_t w = reinterpret_cast<const uint32_t*>(values)[x];
+#pragma unroll
+      for (int i = 0; i < kIn; ++i)
+        if (none(w, i)) rows |= 1u << (x / (kRow / 4));
+    }
+    rows = __reduce_or_sync(0xffffffffu, rows);
+    if (__builtin_expect(rows == 0, 1)) return;
+#pragma unroll 1
+    for (int r = 0; r < kUnit; ++r) {
+      if (!((rows >> r) & 1)) continue;
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int e = kk * 16 + (E8 ? 2 * (lane / 4) + half : lane / 4 + 8 * half), byte = e * (int)sizeof(E);
+          const unsigned char* at = values + r * kRow + (swizzle(r, byte >> 4) << 4) + (byte & 15);
+          if (!none(E8 ? *at : *reinterpret_cast<const uint16_t*>(at), 0)) continue;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              if (attends(nt, i, p0 + r)) o[kk][nt][2 * half + i] = CUDART_NAN_F;
+        }
+    }
+    __syncwarp();
+#pragma unroll 1
+    for (int x = lane; x < kUnit * kRow / 4; x += 32) {
+      uint32_t w = reinterpret_cast<const uint32_t*>(values)[x];
+#pragma unroll
+      for (int i = 0; i < kIn; ++i)
+        if (none(w, i)) w &= ~((E8 ? 0xffu : 0xffffu) << ((E8 ? 8 : 16) * i));
+      reinterpret_cast<uint32_t*>(values)[x] = w;
+    }
+    __syncwarp();
   };
   load_q();
   reset();
@@ -670,6 +764,10 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
             if (!r1) s[u][nt][2] = s[u][nt][3] = -CUDART_INF_F;
           }
         }
+      }
+      if constexpr (TREE) {
+        const int p0 = cs.base + ct * kTile + at0;
+        if (p0 + kUnit > cs.ctx || (a.window > 0 && p0 < cs.lo + 64)) by_row(p0, unit, s);
       }
       // the reference of the exponentials follows the maximum only when it is
       // passed by 8 (a factor of 256): few units rescale
@@ -764,20 +862,19 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
     const bool whole = ct == done.nt && from_first, had_first = from_first;
     const int64_t g0 = end - left + 1 - ct;  // the segment's first tile in the line
     if (left > 1) {  // the next segment's queries come while this one is written
-      next_segment(a, groups, per_head, kUnit, kTile, cs);
+      next_segment<TREE>(a, groups, per_head, kUnit, kTile, cs);
       ct = 0;
       from_first = true;
       load_q();
     }
-    sum_lanes();
+    sum_lanes(done.b);
     const int h0 = (done.h - done.hk * per_head) * S::kHeads;  // the segment's first head within its key head
-    const int64_t head = (int64_t)done.hk * group + h0;
     // a CTA has two slots: its first segment's, and that of a segment it starts and does not end
     float* to = part + (2 * (int64_t)blockIdx.x + (g0 > start ? 1 : 0)) * HT * S::kPiece;
     auto put = [&](int w, int t, const Joined& j) {  // tile t of the team's warp w
       const int nt = t / (D / 16), kk = t % (D / 16), h = w * 8 * NT + nt * 8;
       if (whole) {
-        finish<T, E8>(a, done.b, head + h, group - h0 - h, kk, j);
+        finish<T, E8, TREE>(a, done.b, done.hk, h0 + h, group - h0 - h, kk, j);
       } else {
         float* p = to + w * S::kPiece;
         *reinterpret_cast<float4*>(p + t * 128 + lane * 4) = j.x;
@@ -850,7 +947,7 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
     team_sync();  // the team's last unit has been read
     constexpr int kTeamFloats = kStages * S::kUnitBytes / 4;
     float* own = reinterpret_cast<float*>(smem);
-    sum_lanes();
+    sum_lanes(cs.b);
     store_piece(own + team * kTeamFloats + hw * S::kPiece);
     const int pieces = ranks * kTeams;
     float* wm = reinterpret_cast<float*>(smem + S::kRing);  // [piece][head]: maxima, then weights
@@ -872,7 +969,6 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
     }
     __syncthreads();
     const int h0 = (cs.h - cs.hk * per_head) * S::kHeads;
-    const int64_t head = (int64_t)cs.hk * group + h0;
     if (tid < S::kHeads) {
       float mm = -CUDART_INF_F, sum = 0.0f;
       for (int p = 0; p < pieces; ++p) mm = fmaxf(mm, wm[p * S::kHeads + tid]);
@@ -880,7 +976,7 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
       const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
       for (int p = 0; p < pieces; ++p) wm[p * S::kHeads + tid] = piece_weight(wm[p * S::kHeads + tid], mm) * inv;
       wl[tid] = sum == 0.0f ? 0.0f : 1.0f;  // 0: nothing attended to, whatever the values are (0 times inf is no 0)
-      if (a.lse && blockIdx.x % ranks == 0 && h0 + tid < group) a.lse[(int64_t)cs.b * a.n_q_heads + head + tid] = log_sum<W>(mm, sum);
+      if (a.lse && blockIdx.x % ranks == 0 && h0 + tid < group) a.lse[lse_at<TREE>(a, cs.b, cs.hk, h0 + tid)] = log_sum<W>(mm, sum);
     }
     __syncthreads();
     // a warp joins tiles of 16 elements x 8 heads
@@ -899,7 +995,8 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
         x.w = fmaf(f.y, v.w, x.w);
       }
       const float2 any = *reinterpret_cast<const float2*>(wl + h + 2 * (lane & 3));
-      store_tile<T, E8>((T*)a.out + cs.b * a.o_seq + (head + h) * a.o_head, a.o_head, group - h0 - h, in % (D / 16), x, any.x, any.y);
+      store_tile<T, E8>((T*)a.out + cs.b * a.o_seq + row_at<TREE>(a, cs.hk, h0 + h + lane / 4, a.o_node, a.o_head), group - h0 - h,
+                        in % (D / 16), x, any.x, any.y);
     }
     if (ranks > 1) cl.sync();  // the others have read this rank's pieces
   }
@@ -909,14 +1006,14 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
 // `tiles` of their D / 16 tiles; the warps of a tile share its pieces, each
 // with a running maximum, and join in shared memory.
 constexpr int kJoinWarps = 8;
-template <typename T, bool E8, int D>
+template <typename T, bool E8, int D, bool TREE>
 __global__ void __launch_bounds__(32 * kJoinWarps)
     decode_join_kernel(DecodeArgs a, int per_head, int seg_heads, int warp_heads, int tiles, const float* part, const SegMeta* meta) {
   __shared__ float4 s_x[kJoinWarps][32];
   __shared__ float2 s_m[kJoinWarps][4], s_l[kJoinWarps][4];
   cudaGridDependencySynchronize();
   cudaTriggerProgrammaticLaunchCompletion();
-  const int group = a.n_q_heads / a.c.n_heads;
+  const int group = rows_of<TREE>(a);
   const SegMeta s = meta[blockIdx.x];
   const int h = blockIdx.y * 8, h0 = (s.head_group % per_head) * seg_heads;  // heads within the segment, and within the key head
   if (s.pieces == 0 || h0 + h >= group) return;
@@ -943,8 +1040,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
     j.rescale(top);
     for (int w = 1; w < share; ++w) j.add(s_m[warp + w][lane & 3], s_l[warp + w][lane & 3], s_x[warp + w][lane]);
   }
-  const int64_t head = (int64_t)(s.head_group / per_head) * group + h0 + h;
-  finish<T, E8>(a, s.seq, head, group - h0 - h, tile, j);
+  finish<T, E8, TREE>(a, s.seq, s.head_group / per_head, h0 + h, group - h0 - h, tile, j);
 }
 
 constexpr int64_t kMetaBytes = (kDecodeCtas * (int64_t)sizeof(SegMeta) + 255) / 256 * 256;
@@ -977,7 +1073,7 @@ inline int64_t decode_ws_bytes(const pe_kv_cache& c, int n_q_heads) {
 // of 64 16.8 against 13.5, 1 of 16,384 29.8 against 20.4.
 inline int cluster_ranks(const DecodeArgs& a, int64_t segments, int tile) {
   int64_t most = (int64_t)a.c.max_pages * a.c.page_size;
-  if (a.window > 0 && (int64_t)a.window + 32 < most) most = (int64_t)a.window + 32;
+  if (a.window > 0 && (int64_t)a.window + a.n_nodes + 32 < most) most = (int64_t)a.window + a.n_nodes + 32;
   const int64_t tiles = (most + tile - 1) / tile;
   if (tiles * segments > 2048 || tiles > 64 || segments > 4 * 152) return 0;
   // A larger cluster starts and joins later.  One sequence, 8 key heads, in 2, 4
@@ -989,10 +1085,10 @@ inline int cluster_ranks(const DecodeArgs& a, int64_t segments, int tile) {
   return r;
 }
 
-template <typename T, bool E8, int D, int NT, int HT>
+template <typename T, bool E8, int D, int NT, int HT, bool TREE = false>
 static pe_status go(const DecodeArgs& a, void* ws, cudaStream_t st) {
   using S = DecodeShape<E8, D, NT, HT>;
-  const int group = a.n_q_heads / a.c.n_heads;
+  const int group = a.n_q_heads / a.c.n_heads * (TREE ? a.n_nodes : 1);
   const int per_head = (group + S::kHeads - 1) / S::kHeads, groups = a.c.n_heads * per_head;
   const int64_t segments = (int64_t)a.c.n_seqs * groups;
   int shift = -1;  // of a page size that is a power of two
@@ -1000,7 +1096,7 @@ static pe_status go(const DecodeArgs& a, void* ws, cudaStream_t st) {
     while (a.c.page_size >> (shift + 1)) ++shift;
   const int ranks = cluster_ranks(a, segments, S::kTeams * S::kUnit);
   if (ranks) {
-    auto kern = decode_attn_kernel<T, E8, D, NT, HT, true>;
+    auto kern = decode_attn_kernel<T, E8, D, NT, HT, true, TREE>;
     PE_TRY_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
     cudaLaunchAttribute at[2] = {};
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1018,7 +1114,7 @@ static pe_status go(const DecodeArgs& a, void* ws, cudaStream_t st) {
     PE_TRY_CUDA(cudaLaunchKernelEx(&lc, kern, a, groups, per_head, shift, ranks, 0, false, (float*)nullptr, (SegMeta*)nullptr));
     return PE_OK;
   }
-  auto kern = decode_attn_kernel<T, E8, D, NT, HT, false>;
+  auto kern = decode_attn_kernel<T, E8, D, NT, HT, false, TREE>;
   PE_TRY_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
   SegMeta* meta = reinterpret_cast<SegMeta*>(ws);
   float* part = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + kMetaBytes);
@@ -1030,7 +1126,7 @@ static pe_status go(const DecodeArgs& a, void* ws, cudaStream_t st) {
   // few segments have many pieces each: their tiles go to CTAs of their own
   const int heads = group < S::kHeads ? group : S::kHeads;
   const int tiles = segments <= 152 ? 1 : D == 64 ? 4 : 8;
-  PE_TRY_CUDA(launch_pdl(decode_join_kernel<T, E8, D>, dim3((unsigned)(by_seg ? segments : S::kCtas), (heads + 7) / 8, D / 16 / tiles),
+  PE_TRY_CUDA(launch_pdl(decode_join_kernel<T, E8, D, TREE>, dim3((unsigned)(by_seg ? segments : S::kCtas), (heads + 7) / 8, D / 16 / tiles),
                          dim3(32 * kJoinWarps), 0, st, true, a, per_head, (int)S::kHeads, 8 * NT, tiles, (const float*)part, (const SegMeta*)meta));
   return PE_OK;
 }

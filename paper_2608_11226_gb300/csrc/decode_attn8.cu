@@ -10,7 +10,8 @@ static pe_status go_heads(const DecodeArgs& a, void* ws, cudaStream_t st) {
   const int n = seg_heads(D, a.n_q_heads / a.c.n_heads);
   if (n == 8) return go<T, true, D, 1, 1>(a, ws, st);
   if (n == 16) return go<T, true, D, D == 256 ? 1 : 2, D == 256 ? 2 : 1>(a, ws, st);
-  return go<T, true, D, D == 256 ? 1 : 3, D == 256 ? 3 : 1>(a, ws, st);  // 24: more go to tree_attn8_launch
+  if constexpr (D < 256) return go<T, true, D, 3, 1>(a, ws, st);  // 24
+  return fail(PE_EINVAL, "too many heads");  // they go to tree_attn_launch
 }
 
 template <typename T>

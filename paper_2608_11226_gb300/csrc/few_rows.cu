@@ -1,0 +1,32 @@
+// Attention of drafted tokens with few rows a key head on the one-token kernel
+// (decode_attn.cuh): workspace, dispatch, 16-bit caches.
+#include "few_rows.cuh"
+
+namespace pe {
+
+pe_status few_rows8_launch(const DecodeArgs& a, int dtype, void* ws, cudaStream_t st);
+
+// Which kernel takes a tree: this one up to as many rows as one warp holds, the one
+// of tiles (tree_attn.cuh) beyond.  Measured with 8 key heads, 8 sequences of
+// 32,640 positions, this against that: 8 bits, head_dim 128, 8 rows 93 against 208
+// us, 16 rows 110, 24 rows 188 (2 sequences of 512: 11.4, 14.4, 17.2 against 16.1);
+// head_dim 64, 24 rows 98 against 166; head_dim 256, 8 rows 172 against 377.
+// 16 bits, head_dim 128, 8 rows 165 against 169, 16 rows 171 against 169 (64
+// sequences of 2,048: 95 against 102), 24 rows 175 against 170 (107 against 102);
+// head_dim 64, 24 rows 96 against 130; head_dim 256, 8 rows 310 against 319.
+bool few_rows(const pe_kv_cache& c, int n_nodes, int n_q_heads) {
+  const int rows = n_nodes * (n_q_heads / c.n_heads);
+  return rows <= (c.head_dim == 256 ? 8 : c.head_dim == 64 || c.dtype == PE_E4M3 ? 24 : 16);
+}
+
+int64_t few_rows_ws_bytes(const pe_kv_cache& c, int n_nodes, int n_q_heads) { return decode_ws_bytes(c, n_nodes * n_q_heads); }
+
+pe_status few_rows_launch(const TreeArgs& a, void* ws, cudaStream_t st) {
+  ProfScope ps(PE_PROF_TREE_ATTN, st);
+  const DecodeArgs d{a.c, a.sc, a.q, a.out, a.lse, a.lens, a.q_seq, a.q_head, a.o_seq, a.o_head, a.scale, a.n_q_heads, a.window,
+                     a.n_nodes, a.mask, a.q_node, a.o_node, a.mask_stride};
+  if (a.c.dtype == PE_E4M3) return few_rows8_launch(d, a.dtype, ws, st);
+  return a.dtype == PE_BF16 ? few_dim<__nv_bfloat16, false>(d, ws, st) : few_dim<__half, false>(d, ws, st);
+}
+
+}  // namespace pe

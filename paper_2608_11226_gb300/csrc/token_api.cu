@@ -110,10 +110,14 @@ static bool bad_group(const pe_kv_cache* c, int32_t n_q_heads) {
   return n_q_heads < 1 || n_q_heads > 65536 || n_q_heads % c->n_heads != 0;
 }
 
+static int64_t tree_ws_bytes(const pe_kv_cache& c, int n_nodes, int n_q_heads) {
+  return few_rows(c, n_nodes, n_q_heads) ? few_rows_ws_bytes(c, n_nodes, n_q_heads) : tree_attn_ws_bytes(c, n_nodes, n_q_heads);
+}
+
 int64_t pe_tree_attn_workspace_bytes(const pe_kv_cache* cache, int32_t n_nodes, int32_t n_q_heads) {
   if (check_cache(cache, true) != PE_OK) return -1;
   if (bad_group(cache, n_q_heads) || n_nodes < 0 || n_nodes > 64) return -1;
-  return n_nodes == 0 ? 0 : tree_attn_ws_bytes(*cache, n_nodes, n_q_heads);
+  return n_nodes == 0 ? 0 : tree_ws_bytes(*cache, n_nodes, n_q_heads);
 }
 
 static pe_status check_workspace(const void* workspace, int64_t bytes, int64_t need) {
@@ -141,16 +145,23 @@ pe_status pe_tree_attn(const pe_kv_cache* cache, const pe_kv_scales* scales, con
     return fail(PE_EINVAL, "q and out strides must be multiples of 8 elements");
   if (off(t->q, 16) || off(t->out, 16)) return fail(PE_EINVAL, "q and out must be 16-byte aligned");
   if (off(t->mask, 8)) return fail(PE_EINVAL, "mask must be 8-byte aligned");
-  s = check_workspace(workspace, workspace_bytes, tree_attn_ws_bytes(*cache, t->n_nodes, t->n_q_heads));
+  s = check_workspace(workspace, workspace_bytes, tree_ws_bytes(*cache, t->n_nodes, t->n_q_heads));
   if (s != PE_OK) return s;
   TreeArgs a{*cache, scales ? *scales : pe_kv_scales{}, t->q, t->out, t->lse, t->lens, t->mask, t->q_seq_stride, t->q_node_stride,
              t->q_head_stride, t->out_seq_stride, t->out_node_stride, t->out_head_stride, t->mask_stride, scale, t->n_nodes,
              t->n_q_heads, window, t->dtype};
-  return tree_attn_launch(a, workspace, reinterpret_cast<cudaStream_t>(stream));
+  const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  return few_rows(*cache, t->n_nodes, t->n_q_heads) ? few_rows_launch(a, workspace, st) : tree_attn_launch(a, workspace, st);
 }
 
-// whether one token's heads of a key head are enough for tiles of 128 rows
-static bool many_heads(const pe_kv_cache& c, int n_q_heads) { return n_q_heads / c.n_heads > 24; }
+// Whether one token's heads of a key head are enough for tiles of 128 rows.  Measured
+// over 8 bits, 8 key heads, 8 sequences of 32,640 positions, the one-token kernel
+// against tiles: head_dim 128, 16 heads 107 against 208 us, 24 heads 153 against 207,
+// 32 heads 281 against 206, 64 heads 400 against 211; head_dim 64, 24 heads 91 against
+// 164, 32 heads 164 against 163, 64 heads 236 against 168; head_dim 256, 16 heads 207
+// against 375, 24 heads 446 against 370.  (Short sequences are latency: 2 of 512,
+// 32 heads of 128, 12.3 against 15.2.)
+static bool many_heads(const pe_kv_cache& c, int n_q_heads) { return n_q_heads / c.n_heads > (c.head_dim == 256 ? 16 : 24); }
 
 static int64_t decode8_ws_bytes(const pe_kv_cache& c, int n_q_heads) {
   return many_heads(c, n_q_heads) ? tree_attn_ws_bytes(c, 1, n_q_heads) : decode_attn8_ws_bytes(c, n_q_heads);

@@ -56,6 +56,10 @@ struct DecodeArgs {
   int64_t q_seq, q_head, o_seq, o_head;
   float scale;
   int32_t n_q_heads, window;
+  // of drafted nodes (few rows a key head); n_nodes 0: one token
+  int32_t n_nodes;
+  const uint64_t* mask;
+  int64_t q_node, o_node, mask_stride;
 };
 
 // scale of a row of an 8-bit cache (pe.h: pe_kv_scales)
@@ -111,6 +115,9 @@ pe_status kv_append_launch(const pe_kv_cache& c, const pe_kv_scales& sc, const p
 pe_status kv_move_launch(const MoveArgs& a, cudaStream_t st);
 int64_t tree_attn_ws_bytes(const pe_kv_cache& c, int n_nodes, int n_q_heads);
 pe_status tree_attn_launch(const TreeArgs& a, void* ws, cudaStream_t st);
+bool few_rows(const pe_kv_cache& c, int n_nodes, int n_q_heads);
+int64_t few_rows_ws_bytes(const pe_kv_cache& c, int n_nodes, int n_q_heads);
+pe_status few_rows_launch(const TreeArgs& a, void* ws, cudaStream_t st);
 int64_t decode_attn_ws_bytes(const pe_kv_cache& c, int n_q_heads);
 pe_status decode_attn_launch(const DecodeArgs& a, void* ws, cudaStream_t st);
 int64_t decode_attn8_ws_bytes(const pe_kv_cache& c, int n_q_heads);

@@ -664,3 +664,156 @@ def test_a_drafted_step(eight, graph):
     last = torch.empty_like(y)
     pe.decode_attn(Q.cache, y, after, last)
     assert torch.equal(end, last)
+
+
+# ---------------------------------------------------------------------------
+# drafted nodes with few rows a key head, and calls that share what they use
+# ---------------------------------------------------------------------------
+FEW = [
+    # dtype, eight, lens, N, max_pages, page, Hq, Hkv, D, layout
+    (BF16, True, [900, 0, 31, 257], 4, 30, 32, 8, 2, 128, "slot"),
+    (F16, True, [64, 63, 65, 5], 5, 6, 13, 8, 2, 128, "head"),
+    (BF16, True, [3000], 24, 64, 48, 3, 3, 64, "slot"),
+    (BF16, True, [500, 40], 23, 40, 16, 1, 1, 128, "head"),
+    (F16, True, [77, 1400], 2, 60, 24, 24, 2, 64, "slot"),
+    (BF16, True, [600, 3], 8, 40, 16, 2, 2, 256, "slot"),
+    (F16, True, [129], 1, 20, 8, 16, 1, 128, "head"),
+    (BF16, False, [900, 0, 31, 257], 4, 30, 32, 8, 2, 128, "slot"),
+    (F16, False, [64, 63, 65, 5], 5, 6, 13, 6, 2, 128, "head"),
+    (BF16, False, [3000], 16, 64, 48, 3, 3, 64, "slot"),
+    (F16, False, [500, 40], 7, 40, 16, 4, 2, 64, "head"),
+    (BF16, False, [600, 3], 8, 40, 16, 2, 2, 256, "slot"),
+    (F16, False, [150, 9], 2, 20, 24, 4, 1, 256, "head"),
+    (F16, True, [20, 8, -3], 20, 3, 8, 2, 2, 128, "slot"),  # nodes beyond the table
+]
+
+
+@pytest.mark.parametrize("dtype,eight,lens,N,max_pages,page,Hq,Hkv,D,layout", FEW)
+@pytest.mark.parametrize("window", [0, 64, 200])
+def test_few_rows(dtype, eight, lens, N, max_pages, page, Hq, Hkv, D, layout, window):
+    test_tree(dtype, eight, lens, N, max_pages, page, Hq, Hkv, D, layout, window)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("Hq,N,D,n", [(2, 8, 64, 500), (4, 4, 128, 90), (4, 12, 128, 5000), (2, 7, 256, 300), (24, 1, 64, 40)])
+@pytest.mark.parametrize("window", [0, 70])
+def test_few_rows_and_values_that_are_no_numbers(eight, Hq, N, D, n, window):
+    """A NaN in a node's values, and at the window's start: NaN in that element of the rows that attend to it, nowhere else."""
+    page = 16
+    P = Pool(2, -(-(n + N) // page), page, 2, D, BF16, eight, "slot", 5)
+    masks = tree_masks(2, N, 9)
+    q = torch.randn((2, N, Hq, D), generator=gen(1), device="cuda").to(BF16)
+    lens = [n, n - 3]
+    ro, rl, to, tl = attend(P, q, lens, D ** -0.5, window, masks)
+    nan = torch.zeros(q.shape, dtype=torch.bool, device="cuda")
+    G = Hq // 2
+
+    def spoil(b, p, h, e):
+        at = (int(P.table[b, p // page]), p % page, h, e)
+        if eight:
+            P.v.view(torch.uint8)[at] = 0xFF
+        else:
+            P.v[at] = NAN
+        for i, m in enumerate(masks[b]):
+            lo = max(0, lens[b] + bin(m).count("1") - window) if window else 0
+            if (lo <= p < lens[b]) if p < lens[b] else (m >> (p - lens[b]) & 1):
+                nan[b, i, h * G:(h + 1) * G, e] = True
+
+    spoil(0, lens[0] + N // 2, 1, 0)
+    spoil(0, lens[0], 0, D - 1)
+    spoil(1, lens[1] + N - 1, 0, 21)
+    spoil(1, max(0, lens[1] + 2 - window), 1, D // 2 + 8)
+    spoil(1, lens[1] - 1, 1, 7)
+    out, lse = torch.empty_like(q), torch.empty((2, N, Hq), device="cuda")
+    pe.tree_attn(P.cache, q, torch.tensor(lens, dtype=torch.int32, device="cuda"), tensor_of(masks), out, window=window, lse=lse)
+    close(out, torch.where(nan, NAN, ro), to)
+    close(lse, rl, tl)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("B,longest", [(90, 300), (3, 9000), (700, 2), (1, 20000)])
+@pytest.mark.parametrize("Hq,N,D", [(4, 8, 64), (12, 5, 128), (4, 6, 256)])
+def test_few_rows_of_many_segments(eight, Hq, N, D, B, longest):
+    test_many_segments(eight, D, Hq, N, B, longest)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("Hq,N,D", [(20, 14, 128), (20, 14, 64), (32, 64, 128)])
+def test_blocks_that_are_nearly_empty(eight, Hq, N, D):
+    """Rows just beyond a block, with as many tiles in it as in the full one: a part of the CTA has nothing to do for long."""
+    H, page, lens = 1, 64, [16000, 9000, 16001, 30, 12000, 7000]
+    P = Pool(len(lens), -(-(max(lens) + N) // page), page, H, D, BF16, eight, "slot", 3)
+    masks = tree_masks(1, N, 7) * len(lens)
+    q = torch.randn((len(lens), N, Hq, D), generator=gen(4), device="cuda").to(BF16)
+    out = torch.full_like(q, NAN)
+    pe.tree_attn(P.cache, q, torch.tensor(lens, dtype=torch.int32, device="cuda"), tensor_of(masks), out)
+    pe.device_check()
+    whole = P.table
+    for b in (0, 2, 3):
+        P.table = whole[b:b + 1]
+        ro, _, to, _ = attend(P, q[b:b + 1, :1], [lens[b]], D ** -0.5, 0, [[1]])  # node 0 attends to itself alone
+        close(out[b, 0], ro[0, 0], to[0, 0])
+    assert torch.isfinite(out.float()).all()
+    # a node by itself, in a call of its own with the other nodes' rows left out
+    alone = torch.full_like(q, NAN)
+    only = [[m if i in (N // 2, N - 1) else 0 for i, m in enumerate(row)] for row in masks]
+    P.table = whole
+    pe.tree_attn(P.cache, q, torch.tensor(lens, dtype=torch.int32, device="cuda"), tensor_of(only), alone)
+    for i in (N // 2, N - 1):
+        assert torch.equal(alone[:, i], out[:, i])
+    assert not alone[:, 0].any()
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_calls_at_once_and_in_place(eight):
+    """Two streams with workspaces of their own; two captured calls that share one; the output in the queries' place."""
+    D, H, page, N, lens = 128, 4, 64, 9, [3000, 1700, 40, 2500]
+    P = Pool(4, 48, page, H, D, BF16, eight, "slot", 3)
+    t = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    calls = []
+    for Hq, n in ((16, N), (8, 2), (16, 40), (32, 64)):
+        masks = tensor_of(tree_masks(4, n, 5))
+        q = torch.randn((4, n, Hq, D), generator=gen(Hq), device="cuda").to(BF16)
+        ref = torch.empty_like(q)
+        pe.tree_attn(P.cache, q, t, masks, ref)
+        calls.append((q, masks, ref))
+    token = torch.randn((4, 128, D), generator=gen(1), device="cuda").to(BF16)  # 32 heads a key head
+    one = torch.empty_like(token)
+    pe.decode_attn(P.cache, token, t, one)
+    torch.cuda.synchronize()
+
+    streams = [torch.cuda.Stream() for _ in range(5)]
+    spaces = [torch.empty(pe.tree_attn_workspace_bytes(P.cache, q.shape[1], q.shape[2]), dtype=torch.uint8, device="cuda") for q, _, _ in calls]
+    outs = [torch.full_like(q, NAN) for q, _, _ in calls]
+    got = torch.full_like(token, NAN)
+    space = torch.empty(pe.decode_attn_workspace_bytes(P.cache, 128), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, (q, masks, _), o, w in zip(streams, calls, outs, spaces):
+            pe.tree_attn(P.cache, q, t, masks, o, workspace=w, stream=s)
+        pe.decode_attn(P.cache, token, t, got, workspace=space, stream=streams[4])
+    torch.cuda.synchronize()
+    for (_, _, ref), o in zip(calls, outs):
+        assert torch.equal(o, ref)
+    assert torch.equal(got, one)
+
+    shared = torch.empty(max(w.numel() for w in spaces), dtype=torch.uint8, device="cuda")
+    graphs = []
+    for (q, masks, _), o in zip(calls, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            pe.tree_attn(P.cache, q, t, masks, o, workspace=shared)
+        graphs.append(g)
+    for o in outs:
+        o.fill_(NAN)
+    shared.fill_(255)
+    for _ in range(2):
+        for g in graphs:
+            g.replay()
+    torch.cuda.synchronize()
+    for (_, _, ref), o in zip(calls, outs):
+        assert torch.equal(o, ref)
+    for q, masks, ref in calls:
+        pe.tree_attn(P.cache, q, t, masks, q)
+        assert torch.equal(q, ref)
+    pe.device_check()
