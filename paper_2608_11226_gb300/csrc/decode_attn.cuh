@@ -273,20 +273,20 @@ struct Deal {
   }
 };
 
-// Rows of a key head: its query heads, for drafted nodes (TREE) those of every
+// Rows of a key head: its g query heads, for drafted nodes (TREE) those of every
 // node, one node after the other.
-template <bool TREE> __device__ __forceinline__ int rows_of(const DecodeArgs& a) {
-  return a.n_q_heads / a.c.n_heads * (TREE ? a.n_nodes : 1);
-}
+template <bool TREE> __device__ __forceinline__ int rows_of(const DecodeArgs& a, int g) { return g * (TREE ? a.n_nodes : 1); }
 // offset of row r within a sequence's queries or output
 template <bool TREE>
-__device__ __forceinline__ int64_t row_at(const DecodeArgs& a, int hk, int r, int64_t node_stride, int64_t head_stride) {
-  const int g = a.n_q_heads / a.c.n_heads, node = TREE ? r / g : 0;
-  return (TREE ? node * node_stride : 0) + ((int64_t)hk * g + r - node * g) * head_stride;
+__device__ __forceinline__ int64_t row_at(int g, int hk, int r, int64_t node_stride, int64_t head_stride) {
+  if (!TREE) return ((int64_t)hk * g + r) * head_stride;
+  const int node = r / g;
+  return node * node_stride + ((int64_t)hk * g + r - node * g) * head_stride;
 }
-template <bool TREE> __device__ __forceinline__ int64_t lse_at(const DecodeArgs& a, int seq, int hk, int r) {
-  const int g = a.n_q_heads / a.c.n_heads, node = TREE ? r / g : 0;
-  return ((int64_t)seq * (TREE ? a.n_nodes : 1) + node) * a.n_q_heads + (int64_t)hk * g + r - node * g;
+template <bool TREE> __device__ __forceinline__ int64_t lse_at(const DecodeArgs& a, int seq, int g, int hk, int r) {
+  if (!TREE) return (int64_t)seq * a.n_q_heads + (int64_t)hk * g + r;
+  const int node = r / g;
+  return ((int64_t)seq * a.n_nodes + node) * a.n_q_heads + (int64_t)hk * g + r - node * g;
 }
 // mask of a row's node; 0 where there is none
 __device__ __forceinline__ uint64_t node_bits(const DecodeArgs& a, int seq, int r) {
@@ -296,13 +296,13 @@ __device__ __forceinline__ uint64_t node_bits(const DecodeArgs& a, int seq, int 
 
 // the result of a tile: eight rows from `r` on, of which `rows` exist
 template <typename T, bool E8, bool TREE>
-__device__ __forceinline__ void finish(const DecodeArgs& a, int seq, int hk, int r, int rows, int kk, const Joined& j) {
+__device__ __forceinline__ void finish(const DecodeArgs& a, int seq, int g, int hk, int r, int rows, int kk, const Joined& j) {
   const int lane = threadIdx.x & 31;
   if (kk == 0 && lane < 4 && a.lse) {
-    if (2 * lane < rows) a.lse[lse_at<TREE>(a, seq, hk, r + 2 * lane)] = log_sum<Product<T, E8>>(j.m.x, j.l.x);
-    if (2 * lane + 1 < rows) a.lse[lse_at<TREE>(a, seq, hk, r + 2 * lane + 1)] = log_sum<Product<T, E8>>(j.m.y, j.l.y);
+    if (2 * lane < rows) a.lse[lse_at<TREE>(a, seq, g, hk, r + 2 * lane)] = log_sum<Product<T, E8>>(j.m.x, j.l.x);
+    if (2 * lane + 1 < rows) a.lse[lse_at<TREE>(a, seq, g, hk, r + 2 * lane + 1)] = log_sum<Product<T, E8>>(j.m.y, j.l.y);
   }
-  store_tile<T, E8>((T*)a.out + seq * a.o_seq + row_at<TREE>(a, hk, r + lane / 4, a.o_node, a.o_head), rows, kk, j.x,
+  store_tile<T, E8>((T*)a.out + seq * a.o_seq + row_at<TREE>(g, hk, r + lane / 4, a.o_node, a.o_head), rows, kk, j.x,
                     j.l.x == 0.0f ? 0.0f : 1.0f / j.l.x, j.l.y == 0.0f ? 0.0f : 1.0f / j.l.y);
 }
 
@@ -547,7 +547,7 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
       asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(32 * HT) : "memory");
   };
   const float qscale = a.scale * 1.4426950408889634f;  // scores in powers of two
-  const int group = rows_of<TREE>(a);                   // query heads of a key head
+  const int g = a.n_q_heads / c.n_heads, group = rows_of<TREE>(a, g);  // query heads, rows of a key head
   uint32_t qf[D / 16][NT][2];
   float o[D / 16][NT][4], m[NT][2], l[NT][2];
   float qc[E8 ? NT : 1][2];  // of the lane's heads: scale over the query's power of two
@@ -556,7 +556,7 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int h = (cs.h - cs.hk * per_head) * S::kHeads + hw * 8 * NT + nt * 8 + lane / 4;
-      const T* row = q + row_at<TREE>(a, cs.hk, h < group ? h : 0, a.q_node, a.q_head);
+      const T* row = q + row_at<TREE>(g, cs.hk, h < group ? h : 0, a.q_node, a.q_head);
       if constexpr (E8) {
         // the elements that a lane's four codes meet, in fp16 with the row's largest in [2^14, 2^15)
         uint2 w[D / 16];
@@ -874,7 +874,7 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
     auto put = [&](int w, int t, const Joined& j) {  // tile t of the team's warp w
       const int nt = t / (D / 16), kk = t % (D / 16), h = w * 8 * NT + nt * 8;
       if (whole) {
-        finish<T, E8, TREE>(a, done.b, done.hk, h0 + h, group - h0 - h, kk, j);
+        finish<T, E8, TREE>(a, done.b, g, done.hk, h0 + h, group - h0 - h, kk, j);
       } else {
         float* p = to + w * S::kPiece;
         *reinterpret_cast<float4*>(p + t * 128 + lane * 4) = j.x;
@@ -976,7 +976,7 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
       const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
       for (int p = 0; p < pieces; ++p) wm[p * S::kHeads + tid] = piece_weight(wm[p * S::kHeads + tid], mm) * inv;
       wl[tid] = sum == 0.0f ? 0.0f : 1.0f;  // 0: nothing attended to, whatever the values are (0 times inf is no 0)
-      if (a.lse && blockIdx.x % ranks == 0 && h0 + tid < group) a.lse[lse_at<TREE>(a, cs.b, cs.hk, h0 + tid)] = log_sum<W>(mm, sum);
+      if (a.lse && blockIdx.x % ranks == 0 && h0 + tid < group) a.lse[lse_at<TREE>(a, cs.b, g, cs.hk, h0 + tid)] = log_sum<W>(mm, sum);
     }
     __syncthreads();
     // a warp joins tiles of 16 elements x 8 heads
@@ -995,7 +995,7 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
         x.w = fmaf(f.y, v.w, x.w);
       }
       const float2 any = *reinterpret_cast<const float2*>(wl + h + 2 * (lane & 3));
-      store_tile<T, E8>((T*)a.out + cs.b * a.o_seq + row_at<TREE>(a, cs.hk, h0 + h + lane / 4, a.o_node, a.o_head), group - h0 - h,
+      store_tile<T, E8>((T*)a.out + cs.b * a.o_seq + row_at<TREE>(g, cs.hk, h0 + h + lane / 4, a.o_node, a.o_head), group - h0 - h,
                         in % (D / 16), x, any.x, any.y);
     }
     if (ranks > 1) cl.sync();  // the others have read this rank's pieces
@@ -1013,7 +1013,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
   __shared__ float2 s_m[kJoinWarps][4], s_l[kJoinWarps][4];
   cudaGridDependencySynchronize();
   cudaTriggerProgrammaticLaunchCompletion();
-  const int group = rows_of<TREE>(a);
+  const int g = a.n_q_heads / a.c.n_heads, group = rows_of<TREE>(a, g);
   const SegMeta s = meta[blockIdx.x];
   const int h = blockIdx.y * 8, h0 = (s.head_group % per_head) * seg_heads;  // heads within the segment, and within the key head
   if (s.pieces == 0 || h0 + h >= group) return;
@@ -1040,7 +1040,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
     j.rescale(top);
     for (int w = 1; w < share; ++w) j.add(s_m[warp + w][lane & 3], s_l[warp + w][lane & 3], s_x[warp + w][lane]);
   }
-  finish<T, E8, TREE>(a, s.seq, s.head_group / per_head, h0 + h, group - h0 - h, tile, j);
+  finish<T, E8, TREE>(a, s.seq, g, s.head_group / per_head, h0 + h, group - h0 - h, tile, j);
 }
 
 constexpr int64_t kMetaBytes = (kDecodeCtas * (int64_t)sizeof(SegMeta) + 255) / 256 * 256;
