@@ -538,8 +538,8 @@ pe_status pe_kv_append_at(const pe_kv_cache* cache, const pe_kv_scales* scales, 
                           const int32_t* slots, int32_t dtype, void* stream);
 
 /* pe_decode_attn over an 8-bit cache; q and out are of `dtype` (PE_BF16 or
- * PE_F16).  A position whose key or value scale is 255 makes the heads that
- * attend to it NaN. */
+ * PE_F16).  A position whose key or value scale is 255 makes the output of the
+ * heads that attend to it NaN (a key's the log sum too; a value's may). */
 int64_t pe_decode_attn8_workspace_bytes(const pe_kv_cache* cache, int32_t n_q_heads);
 pe_status pe_decode_attn8(const pe_kv_cache* cache, const pe_kv_scales* scales, int32_t dtype, const void* q,
                           int64_t q_seq_stride, int64_t q_head_stride, int32_t n_q_heads, const int32_t* lens,
@@ -571,8 +571,9 @@ typedef struct pe_tree_queries {
  * no part.  Formulas, head groups, scale and what is made of empty rows and of
  * slots that are not attended to as in pe_decode_attn, for each node by
  * itself: a row that does not attend to a node does not see what that holds.
- * Weights enter the sum of values rounded to 16 bits (bf16 cache: bf16, others:
- * fp16, where one below 2^-30 of the largest may count as 0).
+ * Weights enter the sum of values with 16 bits at least (bf16 cache: bf16, others:
+ * fp16, where one below 2^-30 of the largest may count as 0).  An attended value
+ * that is not finite makes its element NaN, a scale of 255 the node's output.
  *  strides in elements, multiples of 8, 16-byte aligned; window 0 or >= 64.
  *  workspace: >= pe_tree_attn_workspace_bytes(...) bytes of device memory,
  *  256-byte aligned; its contents need not be kept between calls.

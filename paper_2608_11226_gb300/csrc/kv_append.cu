@@ -8,6 +8,11 @@
 // chunks of kAhead heads are in flight at a time: three, with five CTAs on an
 // SM (32,768 tokens of 64 + 16 heads of 128: 201 us, the copy rate; four with four
 // CTAs took 1% longer, two with eight 3%).
+//
+// Into an 8-bit cache a row's lanes find its largest element with shuffles and
+// take the scale from that one's exponent and mantissa: no division, and every
+// quotient is exact until it becomes a code (31,000 tokens of 64 + 16 heads of
+// 128: 199 us, 96% of the copy rate; 32 tokens 5 us).
 #include "tokens.cuh"
 
 namespace pe {
@@ -192,8 +197,8 @@ pe_status kv_append_launch(const pe_kv_cache& c, const pe_kv_scales& sc, const p
 // sequence's heads, or of some of them, keys or values, in registers between the
 // reads and the writes, so that a move's source may be another's target.  Bound
 // by latency: three dependent reads, then the write (32 sequences of 5 moves, 8
-// heads of 128: MOVE_STEP us); with as many heads a CTA as its threads hold 16-byte
-// parts for, 512 sequences of 16 moves of 16 heads of 128 codes take MOVE_BATCH us
+// heads of 128: 5.7 us); with as many heads a CTA as its threads hold 16-byte
+// parts for, 512 sequences of 16 moves of 16 heads of 128 codes take 15.0 us
 // (a head a CTA: 19.2).
 // ---------------------------------------------------------------------------
 constexpr int kMoveThreads = 256, kMoveMost = 64;

@@ -4,31 +4,57 @@
 // A sequence's new tokens and the query heads of a key head are the rows of one
 // matrix, so keys and values are read once for all of them: S = Q K^T and
 // O += P V are products of 128 rows with tiles of kKeys positions.  Up to 128
-// rows the cache's bytes bound it (bf16, head_dim 128: 512 clk of products against
-// 2,790 of HBM for 128 positions), beyond 256 the products do.
+// rows the cache's bytes bound it (bf16, head_dim 128: 1,024 clk of products against
+// 2,790 of HBM for 128 positions), beyond 256 the products and the exponentials do.
 //
 // One CTA on an SM.  Tiles of all (sequence, key head, block of rows) segments
 // form one line that is dealt out evenly to the CTAs; a segment that crosses CTAs
 // leaves pieces (unnormalised output, maxima, sums) that a second kernel joins in
-// the order of the CTAs.
+// the order of the CTAs.  A segment's end (the last output waited for, 128 rows
+// stored) takes 6-9 k clk, in which little else goes on: in the dealing it counts
+// as kTurn tiles (64 x up to 8,192 positions: 208 us for 250 without).
 //
-// Roles: producer warps bring keys and values into a ring of swizzled entries
-// (cp.async from whatever pages; 8-bit codes go through registers and become
-// fp16), one thread issues the products, two warpgroups take the softmax: a
-// thread reads its row of S from TMEM and puts the weights P back as the second
-// product's operand.
+// Roles of the 16 warps; what one waits for never holds up another's work:
+//   0-7    softmax: a thread reads its row of S from TMEM and puts the weights P
+//          back as the second product's operand
+//   8      issues the products
+//   9, 10  places: page of each position, offsets, masks, some tiles ahead (table
+//          entries are on their way three turns before; 8 bits: one warp)
+//   11     queries (16 bits)
+//   10, 11 scales of keys and of values, and copies of the codes to stages (8 bits)
+//   12-15  bring entries into the ring that the products read: 16 bits by cp.async
+//          from whatever pages, two warps keys and two values; 8 bits from the
+//          stages through registers, where codes become fp16
+// A role's code is kept short: together they pass the instruction cache, which was
+// what cost most (whole tiles without masks, loops not unrolled: 549 to 510 us for 512
+// rows over 8 bits).  Bulk copies by the TMA in place of cp.async, a row a copy,
+// gave nothing for 16 bits.
 //   Wide (more than 128 rows in a block): each warpgroup has 128 rows of its own,
 //     whose products run while the other works on its weights; P replaces S.  (Tiles of
-//     64 positions, with two buffers of S, were slower: what a tile costs besides its
-//     products came twice as often.)
+//     64 positions, with two buffers of S, were as fast at best: what a tile costs
+//     besides its products came twice as often.)
 //   Narrow: both warpgroups share one tile of 128 rows, half of the tile's columns
 //     each (they exchange the maxima), and S and P have two buffers.
+//
+// Measured, 8 sequences of 32,640 positions, 8 key heads: 16 bits, head_dim 128, 128
+// rows a key head 185 us (5.8 TB/s, 86% of the copy rate), 256 rows 248; head_dim 256, 128
+// rows 345 (92%).  8 bits, head_dim 128, 128 rows 242 us, 256 rows 408: there the
+// warps that widen codes and the softmax set the pace (issue active 33%, a quarter
+// of the stalls for instructions).
 //
 // An 8-bit row is its codes times 2^e.  Within a tile the codes become fp16 as
 // code * 2^(e - E), E the tile's largest exponent (exact down to e - E = -15; the
 // rest is below 2^-24 of the largest scale), and 2^E goes into the exponentials'
-// argument.  Queries become fp16 with a power of two of their own, which is exact
-// for all that fp32 would keep.
+// argument.  Queries become fp16 with a power of two of their own: exact for fp16,
+// for bf16 down to 2^-31 of the row's largest (the rest is off by 2^-39 of that at most).
+//
+// P is one 16-bit number (bf16, or fp16 over fp16 and 8 bits), rounded once: its
+// error, 2^-8 (bf16) or 2^-11 of a weight at most and as often up as down, is of the size of the
+// result's own rounding (2.0e-3 in the relative 2-norm for bf16, against 1.6e-3 with
+// fp32 weights; 2.8e-4 against 2.1e-4 for fp16).  A second product for what is left,
+// as one token's kernel makes, would cost half as much again of the tensor core's
+// time and another 64 columns of TMEM that head_dim 256 and wide blocks do not have.
+// Sums of weights are of the fp32 weights.
 //
 // Weights are relative to a running maximum that follows only when it is passed
 // by 8 (a factor of 256), so the output is seldom rescaled.
@@ -1287,6 +1313,10 @@ __global__ void __launch_bounds__(32 * kJoinRows) join_kernel(Args g, int block_
 
 constexpr int64_t kMetaBytes = (kCtas * (int64_t)sizeof(SegMeta) + 255) / 256 * 256;
 
+// Blocks of 256 rows where one of 128 does not hold them all: keys and values are
+// brought once for both (256 rows over 16 bits: 248 us; 128 rows alone are 185, and two
+// such blocks would be two passes over the cache).  With up to 128 rows a wide block's
+// second warpgroup would have nothing to do.
 static inline bool wide(int D, int rows) { return D < 256 && rows > 128; }
 
 template <typename T, bool E8, int D, bool WIDE>
