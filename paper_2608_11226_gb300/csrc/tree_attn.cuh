@@ -27,8 +27,12 @@
 //          stages through registers, where codes become fp16
 // A role's code is kept short: together they pass the instruction cache, which was
 // what cost most (whole tiles without masks, loops not unrolled: 549 to 510 us for 512
-// rows over 8 bits).  Bulk copies by the TMA in place of cp.async, a row a copy,
-// gave nothing for 16 bits.
+// rows over 8 bits).  Tensor copies of a page's rows in place of cp.async gave nothing
+// for 16 bits; a bulk copy for each row of 8 bits took 36 clk each (524 us for 208 with 32
+// rows and 32,640 positions).  There a tile takes 3.4 k clk: a scale warp's loop, 1.6 k of
+// it copies at the rate of cp.async (22 clk an instruction of a warp), and next to it
+// 2.9 k of widening.  Eight widening warps up to 64 rows, whose softmax needs four, were
+// slower (235), and so were more copies at once.
 //   Wide (more than 128 rows in a block): each warpgroup has 128 rows of its own,
 //     whose products run while the other works on its weights; P replaces S.  (Tiles of
 //     64 positions, with two buffers of S, were as fast at best: what a tile costs
