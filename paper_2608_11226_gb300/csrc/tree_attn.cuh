@@ -41,8 +41,8 @@
 //     each (they exchange the maxima), and S and P have two buffers.
 //
 // Measured, 8 sequences of 32,640 positions, 8 key heads: 16 bits, head_dim 128, 128
-// rows a key head 185 us (5.8 TB/s, 86% of the copy rate), 256 rows 248; head_dim 256, 128
-// rows 345 (92%).  8 bits, head_dim 128, 128 rows 242 us, 256 rows 408: there the
+// rows a key head 184 us (5.8 TB/s, 86% of the copy rate), 256 rows 242; head_dim 256, 128
+// rows 344 (92%).  8 bits, head_dim 128, 128 rows 239 us, 256 rows 356: there the
 // warps that widen codes and the softmax set the pace (issue active 33%, a quarter
 // of the stalls for instructions).
 //
@@ -516,6 +516,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       }
       for (int t = 0; t < w.cnt; ++t, ++ip) {
         const int b2 = t % S::kBufs, buf = WIDE ? wg : b2;  // of scores and weights
+        // (passed too early by a warpgroup that left 16 tiles out: then the scores' barrier is what holds it)
         wait(ctl, &ctl.info[ip % kInfos], (ip / kInfos) & 1);
         const Info& f = ctl.tile[ip % kInfos];
         wait(ctl, &ctl.s_full[buf], sp[b2] & 1);
@@ -1318,7 +1319,7 @@ __global__ void __launch_bounds__(32 * kJoinRows) join_kernel(Args g, int block_
 constexpr int64_t kMetaBytes = (kCtas * (int64_t)sizeof(SegMeta) + 255) / 256 * 256;
 
 // Blocks of 256 rows where one of 128 does not hold them all: keys and values are
-// brought once for both (256 rows over 16 bits: 248 us; 128 rows alone are 185, and two
+// brought once for both (256 rows over 16 bits: 242 us; 128 rows alone are 184, and two
 // such blocks would be two passes over the cache).  With up to 128 rows a wide block's
 // second warpgroup would have nothing to do.
 static inline bool wide(int D, int rows) { return D < 256 && rows > 128; }
