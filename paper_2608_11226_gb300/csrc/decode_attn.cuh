@@ -316,11 +316,10 @@ __device__ __forceinline__ void finish(const DecodeArgs& a, int seq, int g, int 
 // CL: one cluster for each segment, whose teams share its units and join in
 // shared memory; otherwise the line of all tiles, dealt out to the CTAs, at
 // least `least` to each.  by_seg: the joining kernel goes by segments and not
-// by CTAs.  TREE: drafted nodes (one warp a team).
+// by CTAs.  TREE: drafted nodes.
 template <typename T, bool E8, int D, int NT, int HT, bool CL, bool TREE>
 __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeShape<E8, D, NT, HT>::kBlocks)
     decode_attn_kernel(DecodeArgs a, int groups, int per_head, int page_shift, int ranks, int least, bool by_seg, float* part, SegMeta* meta) {
-  static_assert(!TREE || HT == 1, "a unit is its warp's own");
   using S = DecodeShape<E8, D, NT, HT>;
   using W = Product<T, E8>;
   using M = Mma<W>;
@@ -614,7 +613,7 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        if (TREE && node_bits(a, seq, nt * 8 + 2 * (lane & 3) + i) == 0) m[nt][i] = -CUDART_INF_F, l[nt][i] = 0.0f;  // padding
+        if (TREE && node_bits(a, seq, hw * 8 * NT + nt * 8 + 2 * (lane & 3) + i) == 0) m[nt][i] = -CUDART_INF_F, l[nt][i] = 0.0f;  // padding
         l[nt][i] += __shfl_xor_sync(0xffffffffu, l[nt][i], 4);
         l[nt][i] += __shfl_xor_sync(0xffffffffu, l[nt][i], 8);
         l[nt][i] += __shfl_xor_sync(0xffffffffu, l[nt][i], 16);
@@ -641,7 +640,7 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        bits[nt][i] = node_bits(a, cs.b, nt * 8 + 2 * (lane & 3) + i);
+        bits[nt][i] = node_bits(a, cs.b, hw * 8 * NT + nt * 8 + 2 * (lane & 3) + i);
         row_lo[nt][i] = a.window > 0 ? max(0, cs.ctx + __popcll(bits[nt][i]) - a.window) : 0;
       }
     auto attends = [&](int nt, int i, int p) {
@@ -687,16 +686,16 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
               if (attends(nt, i, p0 + r)) o[kk][nt][2 * half + i] = CUDART_NAN_F;
         }
     }
-    __syncwarp();
+    team_sync();  // the team's warps have all looked
 #pragma unroll 1
-    for (int x = lane; x < kUnit * kRow / 4; x += 32) {
+    for (int x = lane; x < kUnit * kRow / 4; x += 32) {  // (each of them: the same words)
       uint32_t w = reinterpret_cast<const uint32_t*>(values)[x];
 #pragma unroll
       for (int i = 0; i < kIn; ++i)
         if (none(w, i)) w &= ~((E8 ? 0xffu : 0xffffu) << ((E8 ? 8 : 16) * i));
       reinterpret_cast<uint32_t*>(values)[x] = w;
     }
-    __syncwarp();
+    team_sync();
   };
   load_q();
   reset();

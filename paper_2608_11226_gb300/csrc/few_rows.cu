@@ -6,17 +6,19 @@ namespace pe {
 
 pe_status few_rows8_launch(const DecodeArgs& a, int dtype, void* ws, cudaStream_t st);
 
-// Which kernel takes a tree: this one up to as many rows as one warp holds, the one
-// of tiles (tree_attn.cuh) beyond.  Measured with 8 key heads, 8 sequences of
+// Which kernel takes a tree: this one up to as many rows as one warp holds (over 8 bits
+// of head_dim 256 two), the one of tiles (tree_attn.cuh) beyond.  Measured with 8 key heads, 8 sequences of
 // 32,640 positions, this against that: 8 bits, head_dim 128, 8 rows 93 against 208
 // us, 16 rows 110, 24 rows 188 (2 sequences of 512: 11.4, 14.4, 17.2 against 16.1);
-// head_dim 64, 24 rows 98 against 166; head_dim 256, 8 rows 172 against 377.
+// head_dim 64, 24 rows 98 against 166; head_dim 256, 8 rows 172 against 377, 16 rows
+// 209 against 370.
 // 16 bits, head_dim 128, 8 rows 165 against 169, 16 rows 171 against 169 (64
 // sequences of 2,048: 95 against 102), 24 rows 175 against 170 (107 against 102);
 // head_dim 64, 24 rows 96 against 130; head_dim 256, 8 rows 310 against 319.
 bool few_rows(const pe_kv_cache& c, int n_nodes, int n_q_heads) {
   const int rows = n_nodes * (n_q_heads / c.n_heads);
-  return rows <= (c.head_dim == 256 ? 8 : c.head_dim == 64 || c.dtype == PE_E4M3 ? 24 : 16);
+  const bool eight = c.dtype == PE_E4M3;
+  return rows <= (c.head_dim == 256 ? (eight ? 16 : 8) : c.head_dim == 64 || eight ? 24 : 16);
 }
 
 int64_t few_rows_ws_bytes(const pe_kv_cache& c, int n_nodes, int n_q_heads) { return decode_ws_bytes(c, n_nodes * n_q_heads); }

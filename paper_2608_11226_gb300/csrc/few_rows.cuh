@@ -9,9 +9,13 @@ template <typename T, bool E8, int D>
 static pe_status few_go(const DecodeArgs& a, void* ws, cudaStream_t st) {
   const int n = seg_heads(D, a.n_nodes * (a.n_q_heads / a.c.n_heads));
   if (n == 8) return go<T, E8, D, 1, 1, true>(a, ws, st);
-  if constexpr (D < 256) {
+  if constexpr (D == 256) {
+    if constexpr (E8)
+      if (n == 16) return go<T, E8, D, 1, 2, true>(a, ws, st);
+  } else {
     if (n == 16) return go<T, E8, D, 2, 1, true>(a, ws, st);
-    if constexpr (E8 || D == 64) return go<T, E8, D, 3, 1, true>(a, ws, st);
+    if constexpr (E8 || D == 64)
+      if (n == 24) return go<T, E8, D, 3, 1, true>(a, ws, st);
   }
   return fail(PE_EINVAL, "too many rows");  // few_rows() is false for them
 }

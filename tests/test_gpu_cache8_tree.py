@@ -685,6 +685,8 @@ FEW = [
     (BF16, False, [600, 3], 8, 40, 16, 2, 2, 256, "slot"),
     (F16, False, [150, 9], 2, 20, 24, 4, 1, 256, "head"),
     (F16, True, [20, 8, -3], 20, 3, 8, 2, 2, 128, "slot"),  # nodes beyond the table
+    (BF16, True, [600, 3, 0, 90], 5, 40, 16, 6, 2, 256, "slot"),
+    (F16, True, [1000], 16, 90, 13, 1, 1, 256, "head"),
 ]
 
 
@@ -695,7 +697,7 @@ def test_few_rows(dtype, eight, lens, N, max_pages, page, Hq, Hkv, D, layout, wi
 
 
 @pytest.mark.parametrize("eight", [False, True])
-@pytest.mark.parametrize("Hq,N,D,n", [(2, 8, 64, 500), (4, 4, 128, 90), (4, 12, 128, 5000), (2, 7, 256, 300), (24, 1, 64, 40)])
+@pytest.mark.parametrize("Hq,N,D,n", [(2, 8, 64, 500), (4, 4, 128, 90), (4, 12, 128, 5000), (2, 7, 256, 300), (4, 7, 256, 300), (24, 1, 64, 40)])
 @pytest.mark.parametrize("window", [0, 70])
 def test_few_rows_and_values_that_are_no_numbers(eight, Hq, N, D, n, window):
     """A NaN in a node's values, and at the window's start: NaN in that element of the rows that attend to it, nowhere else."""
@@ -732,7 +734,7 @@ def test_few_rows_and_values_that_are_no_numbers(eight, Hq, N, D, n, window):
 
 @pytest.mark.parametrize("eight", [False, True])
 @pytest.mark.parametrize("B,longest", [(90, 300), (3, 9000), (700, 2), (1, 20000)])
-@pytest.mark.parametrize("Hq,N,D", [(4, 8, 64), (12, 5, 128), (4, 6, 256)])
+@pytest.mark.parametrize("Hq,N,D", [(4, 8, 64), (12, 5, 128), (4, 6, 256), (8, 6, 256)])
 def test_few_rows_of_many_segments(eight, Hq, N, D, B, longest):
     test_many_segments(eight, D, Hq, N, B, longest)
 
