@@ -31,8 +31,9 @@
 // for 16 bits; a bulk copy for each row of 8 bits took 36 clk each (524 us for 208 with 32
 // rows and 32,640 positions).  There a tile takes 3.4 k clk: a scale warp's loop, 1.6 k of
 // it copies at the rate of cp.async (22 clk an instruction of a warp), and next to it
-// 2.9 k of widening.  Eight widening warps up to 64 rows, whose softmax needs four, were
-// slower (235), and so were more copies at once.
+// 2.9 k of widening.  Up to 64 rows the softmax needs four warps; the others as widening
+// warps (235 us) or copying apart from the scales (229) made it slower, and so did more
+// copies at once: what they share is the path to shared memory.
 //   Wide (more than 128 rows in a block): each warpgroup has 128 rows of its own,
 //     whose products run while the other works on its weights; P replaces S.  (Tiles of
 //     64 positions, with two buffers of S, were as fast at best: what a tile costs
