@@ -443,7 +443,8 @@ pe_status pe_fleet_windows_noalloc(const float* traces, int32_t G, int32_t L,
  *  table: [n_seqs] rows of max_pages int32, table_stride >= max_pages apart,
  *  device;
  *  head_dim in {64, 128, 256}; page_size in [1, 65536];
- *  max_pages * page_size <= 2^30; dtype PE_BF16 or PE_F16. */
+ *  max_pages * page_size <= 2^30; dtype PE_BF16 or PE_F16 (with pe_kv_scales
+ *  also PE_E4M3). */
 typedef struct pe_kv_cache {
   void* k;
   void* v;
@@ -532,6 +533,8 @@ typedef struct pe_kv_scales {
  *   e = the least integer >= -64 with a <= 448 * 2^e,  scale byte e + 127,
  *   codes x_d / 2^e rounded to nearest even (nothing saturates);
  * a row with an element that is not finite gets scale 255 and codes 0.
+ * Two tokens at one slot of one sequence leave a mix of both, codes of one and
+ * scale of the other included.
  *  dtype: of q, k and v (PE_BF16 or PE_F16; the cache's if that has 16 bits).
  * Errors: PE_EINVAL, PE_ECUDA. */
 pe_status pe_kv_append_at(const pe_kv_cache* cache, const pe_kv_scales* scales, const pe_kv_tokens* tokens,
@@ -573,11 +576,14 @@ typedef struct pe_tree_queries {
  * itself: a row that does not attend to a node does not see what that holds.
  * Weights enter the sum of values with 16 bits at least (bf16 cache: bf16, others:
  * fp16, where one below 2^-30 of the largest may count as 0).  An attended value
- * that is not finite makes its element NaN, a scale of 255 the node's output.
+ * that is not finite leaves its element not finite (an infinite one may become
+ * NaN); a scale of 255 makes the node's output NaN.
  *  strides in elements, multiples of 8, 16-byte aligned; window 0 or >= 64.
  *  workspace: >= pe_tree_attn_workspace_bytes(...) bytes of device memory,
- *  256-byte aligned; its contents need not be kept between calls.
- * Errors: PE_EINVAL, PE_ECUDA. */
+ *  256-byte aligned; its contents need not be kept between calls, and calls that
+ *  may run at once need one each.
+ * Errors: PE_EINVAL (also where a CTA's positions could pass 2^31), PE_ECUDA; a
+ * wait on the device that gave up is reported by pe_device_check. */
 int64_t pe_tree_attn_workspace_bytes(const pe_kv_cache* cache, int32_t n_nodes, int32_t n_q_heads);
 pe_status pe_tree_attn(const pe_kv_cache* cache, const pe_kv_scales* scales, const pe_tree_queries* tree, float scale,
                        int32_t window, void* workspace, int64_t workspace_bytes, void* stream);
