@@ -47,10 +47,11 @@
 // warps that widen codes and the softmax set the pace (issue active 33%, a quarter
 // of the stalls for instructions).
 //
-// An 8-bit row is its codes times 2^e.  Within a tile the codes become fp16 as
-// code * 2^(e - E), E the tile's largest exponent (exact down to e - E = -15; the
-// rest is below 2^-24 of the largest scale), and 2^E goes into the exponentials'
-// argument.  Queries become fp16 with a power of two of their own: exact for fp16,
+// An 8-bit row is its codes times 2^e.  The products are of the codes themselves, exact in
+// fp16; a key's scale multiplies its column of scores and a value's exponent is added to it,
+// so that the running maximum is that of weight times scale, and the sum of the weights takes
+// the value's scale out again.  A row's scale so counts for that row alone, and for those who
+// attend to it.  Queries become fp16 with a power of two of their own: exact for fp16,
 // for bf16 down to 2^-31 of the row's largest (the rest is off by 2^-39 of that at most).
 //
 // P is one 16-bit number (bf16, or fp16 over fp16 and 8 bits), rounded once: its
@@ -96,6 +97,7 @@ struct Shape {
   static constexpr int kQs = WIDE || D == 256 ? 1 : 2;
   static constexpr int kEntries = D == 64 ? (WIDE ? 8 : 6) : E8 ? 3 : 4;
   static constexpr int kStages = !E8 ? 0 : D == 64 ? 4 : 3;  // entries of codes on their way
+  static constexpr int kScales = E8 ? 3 : 0;                 // tiles whose scales are kept: the softmax's two, and the next
   // two producer warps for keys and two for values, where each kind has its own places (an odd number
   // of them passes from one kind to the other, and a wait for the one would not see the other's turn)
   static constexpr bool kSplit = kEntries % 2 == 0 && kStages % 2 == 0 && !(E8 && WIDE);
@@ -109,25 +111,24 @@ struct Shape {
   static constexpr int kO = 0, kOStep = 128, kS = 256, kSStep = kKeys;
   static constexpr int kP = WIDE ? 256 : D == 256 ? 384 : 128, kPStep = WIDE ? kKeys : kKeys / 2;
   static_assert(kSmem > kPdlTmemSmem, "no second kernel with tensor memory beside it");
-  static_assert(kSmem + 14000 <= 232448, "shared memory of an SM");
 };
 
 struct Info {  // a tile
   uint32_t valid[4];  // its positions that exist: in the sequence's range, on present pages
   int p0, n, lo, flags;  // first position; the sequence's length and lowest position; 1: rows attend to it differently (segment from bit 1 on)
-  float ek, ev;       // exponents of an 8-bit tile's factors
 };
 
 template <class S>
 struct Control {
-  uint64_t full[8], empty[8], info[kInfos], paged[8], placed[4], taken[4], staged[4], unstaged[4], q_full[2], q_empty[2], s_full[4], p_full[4], pv_done[2], fin;
+  uint64_t full[8], empty[8], info[kInfos], paged[8], placed[4], taken[4], staged[4], unstaged[4], q_full[2], q_empty[2], s_full[4], p_full[4], pv_done[2], used[3], fin;
   Info tile[kInfos];
   unsigned long long bad[16][2];  // per segment: nodes, and positions from lo on, with values that are not finite
   int64_t off[4][S::kKeys];      // element offsets of a tile's rows, -1: none
   int page[8][S::kKeys];         // pages of a tile's rows, -1: none
-  uint16_t fac[4][2][S::kKeys];  // 2^(e - E) in fp16
+  // of each position of an 8-bit tile: key scale, exponent of the value scale, and 2 to minus that
+  float4 scale[S::kScales ? S::kScales : 1][3][S::kScales ? S::kKeys / 4 : 1];
   int64_t sum[16];
-  float mx[2][2][S::kShared], l[2][S::kShared], qf[4][S::kRows];
+  float mx[2][2][S::kShared], qf[3][S::kRows];  // maxima (a segment's sums at its end); what is left of a query's scale
   int where[5];  // sequence, key head and block, tile, length; what the share has of a segment's end ahead of that
   uint32_t tmem;
   int err;
@@ -360,7 +361,6 @@ __device__ __forceinline__ uint32_t spoilt_columns(const TreeArgs& a, int b, int
     const int p = k < 64 ? n + k : lo + k - 64;
     const int page = c.table[(int64_t)b * c.table_stride + p / c.page_size], sl = p % c.page_size;
     const int64_t at = kv_page_offset(c, page) + (int64_t)sl * c.slot_stride + hk * c.head_stride + d;
-    if (E8 && a.sc.v[page * a.sc.page_stride + (int64_t)sl * a.sc.slot_stride + hk * a.sc.head_stride] == 255) return 0xffffffffu;
 #pragma unroll 1
     for (int j = 0; j < 16; ++j)
       if (E8 ? (((const uint8_t*)c.v)[at + j] & 0x7f) == 0x7f : not_finite<T>(((const uint16_t*)c.v)[at + j], 0)) nan |= 1u << j;
@@ -391,11 +391,11 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       tc::mbar_init(&ctl.full[i], E8 ? S::kBring : 32 * S::kBring);
       tc::mbar_init(&ctl.empty[i], 1);
     }
-    constexpr int kPlacers = E8 ? 3 : 1;  // warps
-    for (int i = 0; i < kInfos; ++i) tc::mbar_init(&ctl.info[i], kPlacers);
+    for (int i = 0; i < kInfos; ++i) tc::mbar_init(&ctl.info[i], E8 ? 3 : 1);  // warps: places, scales of keys, of values
+    for (int i = 0; i < 3; ++i) tc::mbar_init(&ctl.used[i], 8);
     for (int i = 0; i < 8; ++i) tc::mbar_init(&ctl.paged[i], 1);
     for (int i = 0; i < 4; ++i) {
-      tc::mbar_init(&ctl.placed[i], kPlacers);
+      tc::mbar_init(&ctl.placed[i], 1);
       tc::mbar_init(&ctl.taken[i], E8 ? S::kProducers + 2 : S::kProducers);
       tc::mbar_init(&ctl.s_full[i], 1);
       tc::mbar_init(&ctl.p_full[i], WIDE ? 4 : 8);
@@ -511,8 +511,18 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       const bool warp_live = __any_sync(0xffffffffu, exists);
       const bool both = !WIDE || rows > 128;  // the second warpgroup has work
       float m = -CUDART_INF_F, l = 0.0f, qf = 1.0f;
+      auto use = [&](uint32_t tile) {  // the warp has read the tile's scales
+        __syncwarp();
+        if (E8 && lane == 0) tc::mbar_arrive(&ctl.used[tile % 3]);
+      };
       if (WIDE && wg == 1 && !both) {
-        ip += w.cnt;
+        if constexpr (E8)
+          for (int t = 0; t < w.cnt; ++t, ++ip) {
+            wait(ctl, &ctl.info[ip % kInfos], (ip / kInfos) & 1);
+            use(ip);
+          }
+        else
+          ip += w.cnt;
         continue;
       }
       for (int t = 0; t < w.cnt; ++t, ++ip) {
@@ -524,10 +534,11 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         ++sp[b2];
         __syncwarp();
         tc::fence_after();
-        if (E8 && t == 0) qf = ctl.qf[w.index & 3][(WIDE ? wg * 128 : 0) + row];
-        const float ev = E8 ? f.ev : 0.0f;
-        // (a scale of 0 as the least there is: what is masked stays -inf)
-        const float cf = fmaxf(E8 ? qlog * qf * exp2f(f.ek) : qlog, 1e-37f);
+        if (E8 && t == 0) qf = qlog * ctl.qf[w.index % 3][(WIDE ? wg * 128 : 0) + row];
+        // (16 bits: a scale of 0 as the least there is, what is masked stays -inf)
+        const float cf = E8 ? qf : fmaxf(qlog, 1e-37f);
+        const float2 cf2 = make_float2(cf, cf);
+        const float4* scale = &ctl.scale[E8 ? ip % 3 : 0][0][E8 && !WIDE ? wg * (S::kCols / 4) : 0];
         if (warp_live) {
           const uint32_t sc = lanes + S::kS + buf * S::kSStep + (WIDE ? 0 : wg * S::kCols);
           const uint32_t pc = lanes + S::kP + buf * S::kPStep + (WIDE ? 0 : wg * S::kCols / 2);
@@ -553,6 +564,17 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             for (int h = 0; h < kHalves; ++h) ld32(sc + 64 * turn + 32 * h, v[h]);
 #pragma unroll
             for (int h = 0; h < kHalves; ++h) ld_wait(v[h]);
+            if constexpr (E8) {  // in powers of two, the value's exponent in it
+#pragma unroll
+              for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+                for (int j = 0; j < 32; j += 4) {
+                  const float4 k = scale[16 * turn + 8 * h + j / 4], e = scale[kKeys / 4 + 16 * turn + 8 * h + j / 4];
+                  const float2 a = __ffma2_rn(__fmul2_rn(make_float2(v[h][j], v[h][j + 1]), make_float2(k.x, k.y)), cf2, make_float2(e.x, e.y));
+                  const float2 b = __ffma2_rn(__fmul2_rn(make_float2(v[h][j + 2], v[h][j + 3]), make_float2(k.z, k.w)), cf2, make_float2(e.z, e.w));
+                  v[h][j] = a.x, v[h][j + 1] = a.y, v[h][j + 2] = b.x, v[h][j + 3] = b.y;
+                }
+            }
             if (__builtin_expect(!whole, 0)) {
 #pragma unroll
               for (int h = 0; h < kHalves; ++h) {
@@ -581,7 +603,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             bar_sync(1 + (warp & 3), 64);
             top = fmaxf(top, ctl.mx[ip & 1][wg ^ 1][row]);
           }
-          top = top == -CUDART_INF_F ? top : fmaf(top, cf, ev);
+          if (!E8) top = top == -CUDART_INF_F ? top : top * cf;
           const bool over = top > m + 8.0f;
           if (__builtin_expect(__any_sync(0xffffffffu, over), 0)) {
             const float x = over ? top : m;
@@ -604,8 +626,8 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
               }
             }
           }
-          const float off = ev + Weights<M>::kBias - (m == -CUDART_INF_F ? 0.0f : m);
-          const float2 cf2 = make_float2(cf, cf), off2 = make_float2(off, off);
+          const float off = Weights<M>::kBias - (m == -CUDART_INF_F ? 0.0f : m);
+          const float2 off2 = make_float2(off, off);
           float2 part = make_float2(0.0f, 0.0f);
 #pragma unroll 1
           for (int turn = 0; turn < kTurns; ++turn) {
@@ -614,20 +636,26 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             for (int h = 0; h < kHalves; ++h) {
               uint32_t pk[16];
 #pragma unroll
-              for (int j = 0; j < 32; j += 2) {
-                const float2 e = __ffma2_rn(make_float2(v[h][j], v[h][j + 1]), cf2, off2);
-                const float2 p = make_float2(exp2_fast(e.x), exp2_fast(e.y));
-                part = __fadd2_rn(part, p);
-                pk[j / 2] = pack2<M>(p.x, p.y);
+              for (int j = 0; j < 32; j += 4) {
+                float2 e[2] = {make_float2(v[h][j], v[h][j + 1]), make_float2(v[h][j + 2], v[h][j + 3])};
+                const float4 back = E8 ? scale[2 * (kKeys / 4) + 16 * turn + 8 * h + j / 4] : make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                  e[i] = E8 ? __fadd2_rn(e[i], off2) : __ffma2_rn(e[i], cf2, off2);
+                  const float2 p = make_float2(exp2_fast(e[i].x), exp2_fast(e[i].y));
+                  part = E8 ? __ffma2_rn(p, i ? make_float2(back.z, back.w) : make_float2(back.x, back.y), part) : __fadd2_rn(part, p);
+                  pk[j / 2 + i] = pack2<M>(p.x, p.y);
+                }
               }
               st16(pc + 32 * turn + 16 * h, pk);
             }
           }
-          l = E8 ? fmaf(part.x + part.y, exp2f(-ev), l) : l + (part.x + part.y);
+          l += part.x + part.y;
           st_wait();
         } else if (!WIDE) {
           bar_sync(1 + (warp & 3), 64);
         }
+        if (E8) use(ip);
         // The end waits for the last output, so the one before it has to be seen first (scores say that all
         // but two are done), and while the last one cannot be: a barrier two phases on looks like none
         if (t > 0 && t == w.cnt - 1) wait(ctl, &ctl.pv_done[WIDE ? wg : 0], (pp - 1) & 1);
@@ -642,9 +670,11 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       tc::fence_after();
       if (!live) m = -CUDART_INF_F, l = 0.0f;
       if (!WIDE) {
-        ctl.l[wg][row] = l;
+        // (in place of the last tile's maxima: all have read those, or its output would not be there)
+        float (&sums)[2][S::kShared] = ctl.mx[(ip - 1) & 1];
+        sums[wg][row] = l;
         bar_sync(1 + (warp & 3), 64);
-        l += ctl.l[wg ^ 1][row];
+        l += sums[wg ^ 1][row];
       }
       if (warp_live) {
         const bool whole = w.ct == 0 && w.cnt == s.nt;
@@ -794,8 +824,8 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     }
     if constexpr (E8) if (warp >= 10) {
       // ================================================ scales: of keys, of values
-      // What brings a row's scale to the tile's largest; bytes are loaded a tile ahead.  Then the codes
-      // themselves, to a stage: copies wait their turn here, apart from the warps that widen them.
+      // The codes go to a stage: copies wait their turn here, apart from the warps that widen them.  Then the
+      // scales, as the softmax takes them; their bytes are loaded a tile ahead.
       constexpr int kMine = kKeys / 32;
       const int which = warp - 10;
       const uint8_t* base = which ? a.sc.v : a.sc.k;
@@ -822,53 +852,44 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       load(b, 0);
 #pragma unroll 1
       for (uint32_t x = 0;; ++x) {
-        {
-          // bytes in [63, 247]; 255 takes no part in the largest
-          auto fit = [](int b) { return b < 0 || b == 255 ? -1 : min(max(b, 63), 247); };
-          int big = -1;
-#pragma unroll
-          for (int j = 0; j < kMine; ++j) big = max(big, fit(b[j]));
-          big = __reduce_max_sync(0xffffffffu, big);
-          if (big < 0) big = 127;
-          if (x >= 4) wait(ctl, &ctl.taken[x & 3], ((x >> 2) - 1) & 1);
-          __syncwarp();
-#pragma unroll
-          for (int j = 0; j < kMine; ++j) {
-            const int d = fit(b[j]) - big;  // at most 0; a factor below 2^-24 is 0
-            const float z = b[j] < 0 ? 0.0f : b[j] == 255 ? CUDART_NAN_F : __int_as_float(max(127 + d, 0) << 23);
-            ctl.fac[x & 3][which][lane + 32 * j] = __half_as_ushort(__float2half_rn(z));
-          }
-          Info& f = ctl.tile[x % kInfos];
-          if (lane == 0) (which ? f.ev : f.ek) = (float)(big - 127);
-          __syncwarp();
-          if (lane == 0) {
-            tc::mbar_arrive(&ctl.info[x % kInfos]);
-            tc::mbar_arrive(&ctl.placed[x & 3]);
-          }
-          const bool last = !more;
-          load(next, x + 1);
-          const uint32_t e = 2 * x + which, st = e % S::kStages;
-          if (e >= S::kStages) wait(ctl, &ctl.unstaged[st], (e / S::kStages - 1) & 1);
-          __syncwarp();
-          constexpr int kCh = D / 16, kPass = 32 / kCh, kAtOnce = 4;
-          const int64_t* offs = ctl.off[x & 3] + lane / kCh;
-          const uint8_t* codes = (const uint8_t*)(which ? c.v : c.k) + lane % kCh * 16;
-          const uint32_t dst = ring + kEntries * S::kEntry + st * (S::kEntry / 2) + lane * 16;
+        const bool last = !more;
+        load(next, x + 1);
+        const uint32_t e = 2 * x + which, st = e % S::kStages;
+        if (e >= S::kStages) wait(ctl, &ctl.unstaged[st], (e / S::kStages - 1) & 1);
+        __syncwarp();
+        constexpr int kCh = D / 16, kPass = 32 / kCh, kAtOnce = 4;
+        const int64_t* offs = ctl.off[x & 3] + lane / kCh;
+        const uint8_t* codes = (const uint8_t*)(which ? c.v : c.k) + lane % kCh * 16;
+        const uint32_t dst = ring + kEntries * S::kEntry + st * (S::kEntry / 2) + lane * 16;
 #pragma unroll 1
-          for (int i0 = 0; i0 < kKeys / kPass; i0 += kAtOnce) {
-            int64_t o[kAtOnce];  // read ahead of the copies, which the compiler keeps in their order
+        for (int i0 = 0; i0 < kKeys / kPass; i0 += kAtOnce) {
+          int64_t o[kAtOnce];  // read ahead of the copies, which the compiler keeps in their order
 #pragma unroll
-            for (int y = 0; y < kAtOnce; ++y) o[y] = offs[(i0 + y) * kPass];
+          for (int y = 0; y < kAtOnce; ++y) o[y] = offs[(i0 + y) * kPass];
 #pragma unroll
-            for (int y = 0; y < kAtOnce; ++y) copy16(dst + (i0 + y) * 512, codes + (o[y] < 0 ? 0 : o[y]), o[y] >= 0);
-          }
-          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tc::smem_u32(&ctl.staged[st])) : "memory");
-          __syncwarp();
-          if (lane == 0) tc::mbar_arrive(&ctl.taken[x & 3]);
-#pragma unroll
-          for (int j = 0; j < kMine; ++j) b[j] = next[j];
-          if (last) break;
+          for (int y = 0; y < kAtOnce; ++y) copy16(dst + (i0 + y) * 512, codes + (o[y] < 0 ? 0 : o[y]), o[y] >= 0);
         }
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tc::smem_u32(&ctl.staged[st])) : "memory");
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&ctl.taken[x & 3]);
+        if (x >= 3) wait(ctl, &ctl.used[x % 3], (x / 3 - 1) & 1);
+        __syncwarp();
+        float* to = reinterpret_cast<float*>(ctl.scale[x % 3][which]);
+#pragma unroll
+        for (int j = 0; j < kMine; ++j) {
+          const int r = lane + 32 * j, byte = b[j], ve = min(max(byte, 63), 247);  // (what is not there is masked: any number will do)
+          if (which == 0) {
+            to[r] = byte < 0 ? 0.0f : scale_of(byte);
+          } else {
+            to[r] = byte < 0 ? 0.0f : byte == 255 ? CUDART_NAN_F : (float)(ve - 127);
+            to[kKeys + r] = __int_as_float((254 - ve) << 23);
+          }
+        }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&ctl.info[x % kInfos]);
+#pragma unroll
+        for (int j = 0; j < kMine; ++j) b[j] = next[j];
+        if (last) break;
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
     }
@@ -1046,7 +1067,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[i] = pack2<__half>(f[i].x * fac, f[i].y * fac);
             if (r < rows) {
-              if (ch == 0) ctl.qf[w.index & 3][r] = __uint_as_float((uint32_t)(254 - up) << 23);
+              if (ch == 0) ctl.qf[w.index % 3][r] = __uint_as_float((uint32_t)(254 - up) << 23);
               *reinterpret_cast<uint4*>(smem + place(r)) = x[u];
             }
           }
@@ -1140,8 +1161,9 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       constexpr int kStages = S::kStages;
       const int row0 = pt / kCh, ch = pt % kCh;
       unsigned char* stages = smem + S::kQs * S::kQBytes + kEntries * S::kEntry + pt * 16;
-      // a value that is no number, where rows attend to it differently, becomes zero and a mark
-      auto spoils = [&](unsigned char* from, uint16_t* fac, const Info& f) {
+      // a value that is no number, where rows attend to it differently, becomes zero and a mark (a scale that is
+      // none is in the column of scores, masked like those)
+      auto spoils = [&](unsigned char* from, const Info& f) {
         unsigned long long* bad = ctl.bad[f.flags >> 1];
 #pragma unroll 1
         for (int i = 0; i < kEach; ++i) {
@@ -1149,13 +1171,10 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           if (a.window == 0 && (i + 1) * kPass <= f.n - f.p0) continue;  // no nodes there
           int k;
           const uint64_t bit = (f.valid[r >> 5] >> (r & 31)) & 1 ? apart(f, r, k) : 0;
-          const bool none = (fac[r] & 0x7fffu) > 0x7c00u;  // the row's scale
-          __syncwarp();  // a row's lanes are in one warp
-          if (bit && none && ch == 0) fac[r] = 0;
           if (!bit) continue;
           uint4 z = *reinterpret_cast<const uint4*>(from + i * kN * 16);
           uint32_t* y = reinterpret_cast<uint32_t*>(&z);
-          bool any = none;
+          bool any = false;
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -1168,39 +1187,33 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         }
         __syncwarp();
       };
-      auto put = [&](uint32_t e, uint16_t* fac, bool check, const Info& f) {
+      auto put = [&](uint32_t e, bool check, const Info& f) {
         wait(ctl, &ctl.staged[e % kStages], (e / kStages) & 1);
         if (e >= kEntries) wait(ctl, &ctl.empty[e % kEntries], (e / kEntries - 1) & 1);
         __syncwarp();
         unsigned char* from = stages + (e % kStages) * (S::kEntry / 2);
-        if (__builtin_expect(check, 0)) spoils(from, fac, f);  // (a row's lanes are in one warp)
+        if (__builtin_expect(check, 0)) spoils(from, f);  // (a row's lanes are in one warp)
         unsigned char* dst = smem + S::kQs * S::kQBytes + (e % kEntries) * S::kEntry;
         // 8 codes from each half of the row: their chunks of the ring meet no bank twice
         constexpr int kAtOnce = kEach < 4 ? kEach : 4;
         const unsigned char* own = from - pt * 16 + row0 * D + ch * 8;
 #pragma unroll 1
         for (int i0 = 0; i0 < kEach; i0 += kAtOnce) {
-          uint32_t fr[kAtOnce];
           uint2 z[kAtOnce][2];
 #pragma unroll
           for (int i = 0; i < kAtOnce; ++i) {
-            fr[i] = fac[row0 + (i0 + i) * kPass] * 0x10001u;
             z[i][0] = *reinterpret_cast<const uint2*>(own + (i0 + i) * kPass * D);
             z[i][1] = *reinterpret_cast<const uint2*>(own + (i0 + i) * kPass * D + D / 2);
           }
 #pragma unroll
           for (int i = 0; i < kAtOnce; ++i) {
-            const __half2 ff = *reinterpret_cast<const __half2*>(&fr[i]);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               uint32_t y[4];
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
                 const uint32_t w = j < 2 ? z[i][h].x : z[i][h].y;
-                uint32_t v;
-                asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(v) : "h"((uint16_t)(w >> (16 * (j & 1)))));
-                const __half2 p = __hmul2(*reinterpret_cast<const __half2*>(&v), ff);
-                y[j] = *reinterpret_cast<const uint32_t*>(&p);
+                asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[j]) : "h"((uint16_t)(w >> (16 * (j & 1)))));
               }
               *reinterpret_cast<uint4*>(dst + chunk_at(row0 + (i0 + i) * kPass, ch + h * kCh, kKeys)) = make_uint4(y[0], y[1], y[2], y[3]);
             }
@@ -1218,9 +1231,8 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           if (S::kQs == 2 && t == 0) load_q(w);
           placed(tile);
           const Info& f = ctl.tile[tile % kInfos];
-          uint16_t (*fac)[kKeys] = ctl.fac[tile & 3];
 #pragma unroll 1
-          for (int kv = kind; kv < (S::kSplit ? kind + 1 : 2); ++kv) put(2 * tile + kv, fac[kv], kv && (f.flags & 1), f);
+          for (int kv = kind; kv < (S::kSplit ? kind + 1 : 2); ++kv) put(2 * tile + kv, kv && (f.flags & 1), f);
           arrive(&ctl.taken[tile & 3]);
           // (where they have one place, the first tile is under way before the last segment's are done with)
           if (S::kQs == 1 && t == 0) load_q(w);
