@@ -279,11 +279,15 @@ pe_status pe_rollout_replay(pe_env* env, const uint8_t* actions, int32_t horizon
  *          arrives -> the wait runs out -> PE_ETIMEOUT;
  *  mode 1: the same barrier with both CTAs arriving -> PE_OK;
  *  mode 2: an mbarrier wait (as in the tensor-core kernels) that nothing
- *          completes -> PE_ETIMEOUT.
- *  workspace: >= 16 bytes of device memory.  The call waits for the result.
- * Errors: PE_EINVAL (mode outside [0, 2], limit_cycles outside [1e3, 8e9],
- * null workspace), PE_ETIMEOUT (a wait gave up, as modes 0 and 2 intend),
- * PE_ECUDA. */
+ *          completes -> PE_ETIMEOUT;
+ *  mode 3, 4: pe_tree_attn's kernel over a cache in 16, in 8 bits, whose
+ *          tiles are never placed: its roles give up, run through their
+ *          share and end -> PE_ETIMEOUT.
+ *  workspace: >= 16 bytes of device memory; modes 3 and 4: >= 2^26 bytes,
+ *  256-byte aligned.  The call waits for the result.
+ * Errors: PE_EINVAL (mode outside [0, 4], limit_cycles outside [1e3, 8e9],
+ * null or misaligned workspace), PE_ETIMEOUT (a wait gave up, as modes 0, 2,
+ * 3 and 4 intend), PE_ECUDA. */
 pe_status pe_wait_selftest(int32_t mode, int64_t limit_cycles, void* workspace, void* stream);
 
 /* Dual ascent on the Lagrange multiplier of the Eq. 6 reward (Eq. 7,

@@ -114,7 +114,13 @@ pe_status kv_append_launch(const pe_kv_cache& c, const pe_kv_scales& sc, const p
                            cudaStream_t st);
 pe_status kv_move_launch(const MoveArgs& a, cudaStream_t st);
 int64_t tree_attn_ws_bytes(const pe_kv_cache& c, int n_nodes, int n_q_heads);
-pe_status tree_attn_launch(const TreeArgs& a, void* ws, cudaStream_t st);
+// how long the waits of the kernel of tiles wait; `hold`: for what never comes (self-test)
+struct Patience {
+  long long clocks = 4000000000LL;
+  bool hold = false;
+};
+pe_status tree_attn_launch(const TreeArgs& a, void* ws, cudaStream_t st, const Patience& patience = Patience());
+pe_status tree_attn_selftest(bool eight, long long limit, void* ws, cudaStream_t st);
 bool few_rows(const pe_kv_cache& c, int n_nodes, int n_q_heads);
 int64_t few_rows_ws_bytes(const pe_kv_cache& c, int n_nodes, int n_q_heads);
 pe_status few_rows_launch(const TreeArgs& a, void* ws, cudaStream_t st);

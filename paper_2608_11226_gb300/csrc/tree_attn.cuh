@@ -129,6 +129,7 @@ struct Control {
   float4 scale[S::kScales ? S::kScales : 1][3][S::kScales ? S::kKeys / 4 : 1];
   int64_t sum[16];
   float mx[2][2][S::kShared], qf[3][S::kRows];  // maxima (a segment's sums at its end); what is left of a query's scale
+  long long patience;  // of a wait, in clocks
   int where[5];  // sequence, key head and block, tile, length; what the share has of a segment's end ahead of that
   uint32_t tmem;
   int err;
@@ -154,6 +155,8 @@ struct Args {
   float* part;
   SegMeta* meta;
   int32_t* error;
+  long long patience;  // clocks after which a wait gives up
+  bool hold;           // self-test: no tile is placed, every wait for one runs out
 };
 
 struct Seg {
@@ -306,12 +309,15 @@ __device__ __forceinline__ bool mbar_test(uint64_t* b, uint32_t parity) {  // wi
   return ok != 0;
 }
 
-// a bounded wait; once one has given up, the others do not wait either
-__device__ __forceinline__ void wait_long(int* err, uint64_t* b, uint32_t parity) {
+// A bounded wait; once one has given up, the others do not wait either.  The roles then run through what is
+// left of their share without waiting (the warps of a named barrier stay in step), over whatever shared memory
+// holds: what addresses come from is either as it was set at the start, nothing there, or of some tile of the
+// share, and page numbers are held against n_pages where they are used.  The results are not; the flag says so.
+__device__ __forceinline__ void wait_long(int* err, long long patience, uint64_t* b, uint32_t parity) {
   const long long t0 = clock64();
   while (!tc::mbar_try_wait(b, parity)) {
     if (*(volatile int*)err) return;
-    if (clock64() - t0 > 4000000000LL) {
+    if (clock64() - t0 > patience) {
       atomicExch(err, 1);
       return;
     }
@@ -319,7 +325,7 @@ __device__ __forceinline__ void wait_long(int* err, uint64_t* b, uint32_t parity
 }
 template <class C>
 __device__ __forceinline__ void wait(C& c, uint64_t* b, uint32_t parity) {
-  if (__builtin_expect(!tc::mbar_try_wait(b, parity), 0)) wait_long(&c.err, b, parity);
+  if (__builtin_expect(!tc::mbar_try_wait(b, parity), 0)) wait_long(&c.err, c.patience, b, parity);
 }
 
 // the weight of a piece with maximum m where the largest is mm; a piece that
@@ -359,7 +365,9 @@ __device__ __forceinline__ uint32_t spoilt_columns(const TreeArgs& a, int b, int
   for (int k = 0; k < 128; ++k) {
     if (!((k < 64 ? nodes >> k : ahead >> (k - 64)) & 1)) continue;
     const int p = k < 64 ? n + k : lo + k - 64;
+    if (p >= c.max_pages * c.page_size) continue;
     const int page = c.table[(int64_t)b * c.table_stride + p / c.page_size], sl = p % c.page_size;
+    if (page < 0 || page >= c.n_pages) continue;  // (marks after a wait that gave up may be another segment's)
     const int64_t at = kv_page_offset(c, page) + (int64_t)sl * c.slot_stride + hk * c.head_stride + d;
 #pragma unroll 1
     for (int j = 0; j < 16; ++j)
@@ -409,8 +417,13 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       tc::mbar_init(&ctl.pv_done[i], 1);
     }
     ctl.err = 0;
+    ctl.patience = g.patience;
     tc::fence_mbar_init();
   }
+  // nothing is there: what a role finds whose wait for a tile gave up
+  for (int i = tid; i < 4 * kKeys; i += S::kThreads) (&ctl.off[0][0])[i] = -1;
+  for (int i = tid; i < 8 * kKeys; i += S::kThreads) (&ctl.page[0][0])[i] = -1;
+  if (tid < kInfos) ctl.tile[tid] = Info{}, ctl.bad[tid][0] = ctl.bad[tid][1] = 0;
   cudaGridDependencySynchronize();
   cudaTriggerProgrammaticLaunchCompletion();
 
@@ -732,7 +745,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
   } else if (warp < 12) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
     constexpr int kPlace = E8 ? 1 : 2;  // warps that place, every kPlace-th tile each
-    if (warp >= 9 && warp < 9 + kPlace) {
+    if (warp >= 9 && warp < 9 + kPlace && !g.hold) {
     // ================================================== places
       // A lane finds the places of rows lane, lane + 32, ...; table entries are copied kAhead turns ahead
       constexpr int kMine = kKeys / 32, kAhead = 3;
@@ -842,7 +855,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
 #pragma unroll
         for (int j = 0; j < kMine; ++j) {
           const int r = lane + 32 * j, p = p0 + r, page = pages[r];
-          to[j] = page < 0 ? -1 : head[page * a.sc.page_stride + (int64_t)(p - g.page.of(p) * c.page_size) * a.sc.slot_stride];
+          to[j] = page < 0 || page >= c.n_pages ? -1 : head[page * a.sc.page_stride + (int64_t)(p - g.page.of(p) * c.page_size) * a.sc.slot_stride];
         }
         if (++tf == far.ct + far.cnt) {
           more = far.next();
@@ -999,7 +1012,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             }
             if (any) {
               t0 = clock64();
-            } else if (__any_sync(0xffffffffu, clock64() - t0 > 4000000000LL || *(volatile int*)&ctl.err)) {
+            } else if (__any_sync(0xffffffffu, clock64() - t0 > ctl.patience || *(volatile int*)&ctl.err)) {
               atomicExch(&ctl.err, 1);
               break;
             }
@@ -1338,7 +1351,7 @@ constexpr int64_t kMetaBytes = (kCtas * (int64_t)sizeof(SegMeta) + 255) / 256 * 
 static inline bool wide(int D, int rows) { return D < 256 && rows > 128; }
 
 template <typename T, bool E8, int D, bool WIDE>
-static pe_status go(const TreeArgs& a, void* ws, int32_t* error, cudaStream_t st) {
+static pe_status go(const TreeArgs& a, void* ws, int32_t* error, const Patience& patience, cudaStream_t st) {
   using S = Shape<D, E8, WIDE>;
   using M = typename std::conditional<E8, __half, T>::type;
   const int rows = a.n_nodes * (a.n_q_heads / a.c.n_heads);
@@ -1351,6 +1364,8 @@ static pe_status go(const TreeArgs& a, void* ws, int32_t* error, cudaStream_t st
   g.meta = reinterpret_cast<SegMeta*>(ws);
   g.part = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + kMetaBytes);
   g.error = error;
+  g.patience = patience.clocks;
+  g.hold = patience.hold;
   // a CTA's tiles are counted in 31 bits
   if ((double)a.c.n_seqs * g.groups * ((double)a.c.max_pages * a.c.page_size / S::kKeys + 2) / kCtas >= 2147483000.0)
     return fail(PE_EINVAL, "n_seqs * n_heads * max_pages * page_size too large");
@@ -1363,11 +1378,11 @@ static pe_status go(const TreeArgs& a, void* ws, int32_t* error, cudaStream_t st
 }
 
 template <typename T, bool E8>
-static pe_status go_dim(const TreeArgs& a, void* ws, int32_t* error, cudaStream_t st) {
+static pe_status go_dim(const TreeArgs& a, void* ws, int32_t* error, const Patience& p, cudaStream_t st) {
   const int rows = a.n_nodes * (a.n_q_heads / a.c.n_heads);
-  if (a.c.head_dim == 64) return wide(64, rows) ? go<T, E8, 64, true>(a, ws, error, st) : go<T, E8, 64, false>(a, ws, error, st);
-  if (a.c.head_dim == 128) return wide(128, rows) ? go<T, E8, 128, true>(a, ws, error, st) : go<T, E8, 128, false>(a, ws, error, st);
-  return go<T, E8, 256, false>(a, ws, error, st);
+  if (a.c.head_dim == 64) return wide(64, rows) ? go<T, E8, 64, true>(a, ws, error, p, st) : go<T, E8, 64, false>(a, ws, error, p, st);
+  if (a.c.head_dim == 128) return wide(128, rows) ? go<T, E8, 128, true>(a, ws, error, p, st) : go<T, E8, 128, false>(a, ws, error, p, st);
+  return go<T, E8, 256, false>(a, ws, error, p, st);
 }
 
 // the flag that a wait of this translation unit's kernels sets when it gives up

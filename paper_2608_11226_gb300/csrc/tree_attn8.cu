@@ -9,11 +9,11 @@ pe_status read_flag(const void* symbol, bool* set);
 
 pe_status tree_attn8_check(bool* gave_up) { return read_flag(&g_gave_up8, gave_up); }
 
-pe_status tree_attn8_launch(const TreeArgs& a, void* ws, cudaStream_t st) {
+pe_status tree_attn8_launch(const TreeArgs& a, void* ws, const Patience& patience, cudaStream_t st) {
   int32_t* error;
   const pe_status s = tree::flag_address(&g_gave_up8, &error);
   if (s != PE_OK) return s;
-  return a.dtype == PE_BF16 ? tree::go_dim<__nv_bfloat16, true>(a, ws, error, st) : tree::go_dim<__half, true>(a, ws, error, st);
+  return a.dtype == PE_BF16 ? tree::go_dim<__nv_bfloat16, true>(a, ws, error, patience, st) : tree::go_dim<__half, true>(a, ws, error, patience, st);
 }
 
 }  // namespace pe

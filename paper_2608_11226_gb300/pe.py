@@ -349,6 +349,8 @@ def rollout_replay(env: Env, actions: torch.Tensor, T: int, iteration: int, buf:
 def wait_selftest(mode: int, limit_cycles: int, workspace: torch.Tensor, stream=None):
     """Run one of the library's bounded waits with a short budget (see pe.h);
     raises PEError with PE_ETIMEOUT when the wait gives up."""
+    if workspace.numel() * workspace.element_size() < (1 << 26 if mode in (3, 4) else 16):
+        raise ValueError("workspace too small")
     _check(lib().pe_wait_selftest(mode, int(limit_cycles), _ptr(workspace), _stream(stream)))
 
 
