@@ -1124,7 +1124,11 @@ pe_status rollout_bf16(const EnvDev& env, const pe_net& net, const float* params
               net.obs_dim, net.hidden, net.n_actions, env.C, env.obs_kind);
 }
 
-pe_status tree_attn_check(bool* gave_up);  // tree_attn.cu
+// where kernels of other translation units report the same
+pe_status tc_error_flag(int32_t** p) {
+  PE_TRY_CUDA(cudaGetSymbolAddress(reinterpret_cast<void**>(p), g_tc_error));
+  return PE_OK;
+}
 
 pe_status device_check(cudaStream_t st) {
   PE_TRY_CUDA(cudaStreamSynchronize(st));
@@ -1133,11 +1137,8 @@ pe_status device_check(cudaStream_t st) {
   if (flag) {
     const int32_t zero = 0;
     PE_TRY_CUDA(cudaMemcpyToSymbol(g_tc_error, &zero, sizeof(zero)));
+    return fail(PE_ETIMEOUT, "a bounded tensor-core wait timed out in an earlier launch");
   }
-  bool attention = false;
-  const pe_status s = tree_attn_check(&attention);
-  if (s != PE_OK) return s;
-  if (flag || attention) return fail(PE_ETIMEOUT, "a bounded tensor-core wait timed out in an earlier launch");
   return PE_OK;
 }
 

@@ -3,27 +3,9 @@
 
 namespace pe {
 
-static __device__ int32_t g_gave_up = 0;
-
-pe_status tree_attn8_launch(const TreeArgs& a, void* ws, const Patience& patience, cudaStream_t st);
-pe_status tree_attn8_check(bool* gave_up);
-
-// reads and clears a flag; the caller has waited for the launches
-pe_status read_flag(const void* symbol, bool* set) {
-  int32_t v = 0;
-  PE_TRY_CUDA(cudaMemcpyFromSymbol(&v, symbol, sizeof(v)));
-  if (v) {
-    *set = true;
-    v = 0;
-    PE_TRY_CUDA(cudaMemcpyToSymbol(symbol, &v, sizeof(v)));
-  }
-  return PE_OK;
-}
-
-pe_status tree_attn_check(bool* gave_up) {
-  const pe_status s = read_flag(&g_gave_up, gave_up);
-  return s != PE_OK ? s : tree_attn8_check(gave_up);
-}
+pe_status tree_attn8_launch(const TreeArgs& a, void* ws, int32_t* error, const Patience& patience, cudaStream_t st);
+pe_status tc_error_flag(int32_t** p);        // mlp_bf16.cu
+pe_status device_check(cudaStream_t st);
 
 int64_t tree_attn_ws_bytes(const pe_kv_cache& c, int n_nodes, int n_q_heads) {
   const int rows = tree::wide(c.head_dim, n_nodes * (n_q_heads / c.n_heads)) ? 256 : 128;
@@ -32,10 +14,10 @@ int64_t tree_attn_ws_bytes(const pe_kv_cache& c, int n_nodes, int n_q_heads) {
 
 pe_status tree_attn_launch(const TreeArgs& a, void* ws, cudaStream_t st, const Patience& patience) {
   ProfScope ps(a.mask ? PE_PROF_TREE_ATTN : PE_PROF_DECODE_ATTN, st);
-  if (a.c.dtype == PE_E4M3) return tree_attn8_launch(a, ws, patience, st);
-  int32_t* error;
-  const pe_status s = tree::flag_address(&g_gave_up, &error);
+  int32_t* error;  // set when a wait gives up
+  const pe_status s = tc_error_flag(&error);
   if (s != PE_OK) return s;
+  if (a.c.dtype == PE_E4M3) return tree_attn8_launch(a, ws, error, patience, st);
   return a.dtype == PE_BF16 ? tree::go_dim<__nv_bfloat16, false>(a, ws, error, patience, st) : tree::go_dim<__half, false>(a, ws, error, patience, st);
 }
 
@@ -75,11 +57,9 @@ pe_status tree_attn_selftest(bool eight, long long limit, void* ws, cudaStream_t
     p.clocks = limit, p.hold = true;
     const pe_status s = tree_attn_launch(a, at, st, p);
     if (s != PE_OK) return s;
-    PE_TRY_CUDA(cudaStreamSynchronize(st));
-    bool now = false;
-    const pe_status r = tree_attn_check(&now);
-    if (r != PE_OK) return r;
-    gave_up |= now;
+    const pe_status r = device_check(st);
+    if (r != PE_OK && r != PE_ETIMEOUT) return r;
+    gave_up |= r == PE_ETIMEOUT;
   }
   return gave_up ? fail(PE_ETIMEOUT, "bounded waits of the attention kernel gave up (self-test)") : PE_OK;
 }
