@@ -578,8 +578,10 @@ typedef struct pe_tree_queries {
  * no part.  Formulas, head groups, scale and what is made of empty rows and of
  * slots that are not attended to as in pe_decode_attn, for each node by
  * itself: a row that does not attend to a node does not see what that holds.
- * Weights enter the sum of values with 16 bits at least (bf16 cache: bf16, others:
- * fp16, where one below 2^-30 of the largest may count as 0).  An attended value
+ * Weights enter the sum of values as two numbers of 16 bits (bf16 cache: bf16, others:
+ * fp16, where one below 2^-30 of the largest may count as 0), with bf16 queries over
+ * an 8-bit cache and more than 24 rows (16 of head_dim 256) of nodes and heads a key head
+ * as one fp16 number.  An attended value
  * that is not finite leaves its element not finite (an infinite one may become
  * NaN); a scale of 255 makes the node's output NaN.
  *  strides in elements, multiples of 8, 16-byte aligned; window 0 or >= 64.

@@ -39,7 +39,7 @@
 //     64 positions, with two buffers of S, were as fast at best: what a tile costs
 //     besides its products came twice as often.)
 //   Narrow: both warpgroups share one tile of 128 rows, half of the tile's columns
-//     each (they exchange the maxima), and S and P have two buffers.
+//     each (they exchange the maxima), and S, which P replaces, has two buffers.
 //
 // Measured, 8 sequences of 32,640 positions, 8 key heads: 16 bits, head_dim 128, 128
 // rows a key head 184 us (5.8 TB/s, 86% of the copy rate), 256 rows 242; head_dim 256, 128
@@ -54,12 +54,14 @@
 // attend to it.  Queries become fp16 with a power of two of their own: exact for fp16,
 // for bf16 down to 2^-31 of the row's largest (the rest is off by 2^-39 of that at most).
 //
-// P is one 16-bit number (bf16, or fp16 over fp16 and 8 bits), rounded once: its
-// error, 2^-8 (bf16) or 2^-11 of a weight at most and as often up as down, is of the size of the
-// result's own rounding (2.0e-3 in the relative 2-norm for bf16, against 1.6e-3 with
-// fp32 weights; 2.8e-4 against 2.1e-4 for fp16).  A second product for what is left,
-// as one token's kernel makes, would cost half as much again of the tensor core's
-// time and another 64 columns of TMEM that head_dim 256 and wide blocks do not have.
+// P enters the second product as a sum of two 16-bit numbers, hi + lo (bf16, or fp16 over
+// fp16 and 8 bits), which leave 2^-18 (fp16: 2^-24) of a weight, as on the one-token kernel: the
+// result is as exact as its own rounding for any number of rows.  (One number alone: 2.0e-3
+// in the relative 2-norm for 1.6e-3 in bf16, 2.8e-4 for 2.1e-4 in fp16.)  Both parts lie where the
+// scores of their keys were.  The second product and the splitting cost 2% with 128 rows
+// of head_dim 128 (16 bits, 8 sequences of 32,640 positions), 18% of head_dim 64, 22% with 256 rows.
+// With bf16 queries over 8 bits P is one fp16 number: off by 2^-12 at most, an eighth
+// of what the result's rounding may be off by (a low part would cost 13-22% there).
 // Sums of weights are of the fp32 weights.
 //
 // Weights are relative to a running maximum that follows only when it is passed
@@ -109,7 +111,8 @@ struct Shape {
   static constexpr int kCols = WIDE ? kKeys : kKeys / 2;  // columns of a thread
   // TMEM columns
   static constexpr int kO = 0, kOStep = 128, kS = 256, kSStep = kKeys;
-  static constexpr int kP = WIDE ? 256 : D == 256 ? 384 : 128, kPStep = WIDE ? kKeys : kKeys / 2;
+  // weights take the place of their scores: of kGroup keys a thread at a time, the high parts, then the low ones
+  static constexpr int kGroup = kCols >= 64 ? 64 : 32;
   static_assert(kSmem > kPdlTmemSmem, "no second kernel with tensor memory beside it");
 };
 
@@ -346,6 +349,13 @@ template <typename M> __device__ __forceinline__ float log_sum(float m, float l)
   return l == 0.0f ? -CUDART_INF_F : (m == -CUDART_INF_F ? 0.0f : m - Weights<M>::kBias) * 0.69314718f + logf(l);
 }
 
+// the first 16-bit part of two weights, packed, and what it leaves of them
+template <typename M> __device__ __forceinline__ float2 high_part(float2 p, uint32_t& high) {
+  high = pack2<M>(p.x, p.y);
+  const float2 h = unpack2<M>(high);
+  return make_float2(p.x - h.x, p.y - h.y);
+}
+
 template <typename M> __device__ __forceinline__ bool not_finite(uint32_t w, int half) {
   const uint32_t e = std::is_same<M, __nv_bfloat16>::value ? 0x7f80u : 0x7c00u;
   return ((w >> (16 * half)) & e) == e;
@@ -383,6 +393,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
   using S = Shape<D, E8, WIDE>;
   using M = typename std::conditional<E8, __half, T>::type;  // type of the products
   constexpr int kKeys = S::kKeys, kChunks = D / 8, kEntries = S::kEntries, kTurn = S::kTurn;
+  constexpr bool kLow = !std::is_same<M, __half>::value || std::is_same<T, __half>::value;  // weights have a low part
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(16) Control<S> ctl;
   static_assert(S::kSmem + sizeof(Control<S>) <= 232448, "shared memory of an SM");
@@ -554,7 +565,6 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         const float4* scale = &ctl.scale[E8 ? ip % 3 : 0][0][E8 && !WIDE ? wg * (S::kCols / 4) : 0];
         if (warp_live) {
           const uint32_t sc = lanes + S::kS + buf * S::kSStep + (WIDE ? 0 : wg * S::kCols);
-          const uint32_t pc = lanes + S::kP + buf * S::kPStep + (WIDE ? 0 : wg * S::kCols / 2);
           const bool whole = f.p0 >= lo_hi && f.p0 + kKeys <= f.n && (f.valid[0] & f.valid[1] & f.valid[2] & f.valid[3]) == 0xffffffffu;
           // 64 columns at a time (head_dim 256: 32); code is kept short, for the roles share the instruction cache
           constexpr int kHalves = S::kCols >= 64 ? 2 : 1, kTurns = S::kCols / (32 * kHalves);
@@ -647,7 +657,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             if (kTurns > 1) fetch(turn);
 #pragma unroll
             for (int h = 0; h < kHalves; ++h) {
-              uint32_t pk[16];
+              uint32_t pk[16], low[kLow ? 16 : 1];
 #pragma unroll
               for (int j = 0; j < 32; j += 4) {
                 float2 e[2] = {make_float2(v[h][j], v[h][j + 1]), make_float2(v[h][j + 2], v[h][j + 3])};
@@ -657,10 +667,16 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
                   e[i] = E8 ? __fadd2_rn(e[i], off2) : __ffma2_rn(e[i], cf2, off2);
                   const float2 p = make_float2(exp2_fast(e[i].x), exp2_fast(e[i].y));
                   part = E8 ? __ffma2_rn(p, i ? make_float2(back.z, back.w) : make_float2(back.x, back.y), part) : __fadd2_rn(part, p);
-                  pk[j / 2 + i] = pack2<M>(p.x, p.y);
+                  if constexpr (kLow) {
+                    const float2 rest = high_part<M>(p, pk[j / 2 + i]);
+                    low[j / 2 + i] = pack2<M>(rest.x, rest.y);
+                  } else {
+                    pk[j / 2 + i] = pack2<M>(p.x, p.y);
+                  }
                 }
               }
-              st16(pc + 32 * turn + 16 * h, pk);
+              st16(sc + 64 * turn + 16 * h, pk);
+              if constexpr (kLow) st16(sc + 64 * turn + S::kGroup / 2 + 16 * h, low);
             }
           }
           l += part.x + part.y;
@@ -926,11 +942,15 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       // output of tile t of track x: the weights are there, and the values
       auto outputs = [&](int x, int buf, uint32_t e, bool first) {
         tc::fence_after();
-        const uint32_t vd = uniform((uint32_t)v0 | entry(e)), out = tm + S::kO + x * S::kOStep, p = uniform(tm + S::kP + buf * S::kPStep);
+        const uint32_t vd = uniform((uint32_t)v0 | entry(e)), out = tm + S::kO + x * S::kOStep, p = uniform(tm + S::kS + buf * S::kSStep);
         const uint32_t more = uniform(!first);
+        constexpr int kIn = S::kGroup / 16;
 #pragma unroll
         for (int kk = 0; kk < kKeys / 16; ++kk)
-          mma_ts(out, p + 8 * kk, desc_of(vd + kk * 128, (uint32_t)(v0 >> 32)), kIdO, kk > 0 ? 1u : more, leader);
+#pragma unroll
+          for (int low = 0; low <= kLow; ++low)
+            mma_ts(out, p + kk / kIn * S::kGroup + kk % kIn * 8 + low * (S::kGroup / 2), desc_of(vd + kk * 128, (uint32_t)(v0 >> 32)), kIdO,
+                   kk + low > 0 ? 1u : more, leader);
         commit(&ctl.pv_done[x]);
       };
       auto scores = [&](int x, int buf, int qb, uint32_t e) {
@@ -1383,12 +1403,6 @@ static pe_status go_dim(const TreeArgs& a, void* ws, int32_t* error, const Patie
   if (a.c.head_dim == 64) return wide(64, rows) ? go<T, E8, 64, true>(a, ws, error, p, st) : go<T, E8, 64, false>(a, ws, error, p, st);
   if (a.c.head_dim == 128) return wide(128, rows) ? go<T, E8, 128, true>(a, ws, error, p, st) : go<T, E8, 128, false>(a, ws, error, p, st);
   return go<T, E8, 256, false>(a, ws, error, p, st);
-}
-
-// the flag that a wait of this translation unit's kernels sets when it gives up
-static inline pe_status flag_address(const void* symbol, int32_t** p) {
-  PE_TRY_CUDA(cudaGetSymbolAddress(reinterpret_cast<void**>(p), symbol));
-  return PE_OK;
 }
 
 }  // namespace tree
