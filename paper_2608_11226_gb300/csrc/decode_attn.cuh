@@ -441,7 +441,7 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
       const int e = min(max(vbyte, 63), 247);
       s_scale[team][scale_stage][lane] =
           kbyte < 0 ? make_float4(0.0f, 0.0f, 1.0f, 0.0f)
-                    : make_float4(scale_of(kbyte), vbyte == 255 ? CUDART_NAN_F : (float)(e - 127), __int_as_float((254 - e) << 23), 0.0f);
+                    : make_float4(key_scale(kbyte), vbyte == 255 ? CUDART_NAN_F : (float)(e - 127), __int_as_float((254 - e) << 23), 0.0f);
     }
     scale_stage = -1;
   };
@@ -552,7 +552,7 @@ __global__ void __launch_bounds__(DecodeShape<E8, D, NT, HT>::kThreads, DecodeSh
     else
       asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(32 * HT) : "memory");
   };
-  const float qscale = a.scale * 1.4426950408889634f;  // scores in powers of two
+  const float qscale = a.scale * 1.4426950408889634f * (E8 ? kRowFactor : 1.0f);  // scores in powers of two
   const int g = a.n_q_heads / c.n_heads, group = rows_of<TREE>(a, g);  // query heads, rows of a key head
   uint32_t qf[D / 16][NT][2];
   float o[D / 16][NT][4], m[NT][2], l[NT][2];

@@ -62,9 +62,12 @@ struct DecodeArgs {
   int64_t q_node, o_node, mask_stride;
 };
 
-// scale of a row of an 8-bit cache (pe.h: pe_kv_scales)
-__device__ __forceinline__ float scale_of(int byte) {
-  return __int_as_float(byte == 255 ? 0x7fc00000 : min(max(byte, 63), 247) << 23);
+// Key scale of a row of an 8-bit cache (pe.h: pe_kv_scales) over 2^16, with which a score's row factor is
+// multiplied: codes times queries reach 2^32, scales 2^120, so one factor alone would pass fp32's range ahead of
+// the other's taking it back.
+constexpr float kRowFactor = 65536.0f;
+__device__ __forceinline__ float key_scale(int byte) {
+  return __int_as_float(byte == 255 ? 0x7fc00000 : (min(max(byte, 63), 247) - 16) << 23);
 }
 
 // Attention of one or several new tokens over either kind of cache: the tree's

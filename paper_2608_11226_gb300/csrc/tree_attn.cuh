@@ -512,7 +512,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");  // 256 threads of 160 and 256 of 96: what 512 of 128 had
     const int wg = warp >> 2, row = (warp & 3) * 32 + lane;  // row of the tile, lane of TMEM
     const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-    const float qlog = fabsf(a.scale) * 1.4426950408889634f;
+    const float qlog = fabsf(a.scale) * 1.4426950408889634f * (E8 ? kRowFactor : 1.0f);
     uint32_t sp[2] = {0, 0}, pp = 0, ip = 0;  // phases: scores, outputs, tiles seen
     uint64_t bits = 0;  // the row's mask, of sequence last_b
     int last_b = -1;
@@ -908,7 +908,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         for (int j = 0; j < kMine; ++j) {
           const int r = lane + 32 * j, byte = b[j], ve = min(max(byte, 63), 247);  // (what is not there is masked: any number will do)
           if (which == 0) {
-            to[r] = byte < 0 ? 0.0f : scale_of(byte);
+            to[r] = byte < 0 ? 0.0f : key_scale(byte);
           } else {
             to[r] = byte < 0 ? 0.0f : byte == 255 ? CUDART_NAN_F : (float)(ve - 127);
             to[kKeys + r] = __int_as_float((254 - ve) << 23);

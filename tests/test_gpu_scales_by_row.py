@@ -141,3 +141,27 @@ def test_attended_rows_far_apart(dtype, D, N, G, far):
     ro, rl, to, tl = attend(P, q, lens, D ** -0.5, 0, masks)
     base.close(out, ro, to)
     base.close(lse, rl, tl)
+
+
+@pytest.mark.parametrize("D,N,G", CALLS)
+@pytest.mark.parametrize("power", [-50, 60, 114])
+def test_large_keys_and_small_queries(D, N, G, power):
+    """Keys 2^power times as large, queries as much smaller: the same scores, so the same bits."""
+    page, H, n = 16, 2, 150
+    P = base.Pool(1, 24, page, H, D, BF16, True, "slot", 6)
+    q = 1.0 + torch.rand((1, max(N, 1), G * H, D), generator=base.gen(1), device="cuda")
+    q *= torch.where(torch.rand(q.shape, generator=base.gen(2), device="cuda") < 0.5, -1.0, 1.0)
+    t = torch.tensor([n], dtype=torch.int32, device="cuda")
+    masks = base.tensor_of(base.tree_masks(1, max(N, 1), 3))
+    got = []
+    for k in (0, power):
+        P.ks += k if k >= 0 else 256 + k  # (bytes wrap)
+        x = (q.to(BF16).double() * 2.0 ** -k).to(BF16)
+        out, lse = torch.full_like(x, NAN), torch.full(x.shape[:-1], NAN, device="cuda")
+        if N:
+            pe.tree_attn(P.cache, x, t, masks, out, lse=lse)
+        else:
+            pe.decode_attn(P.cache, x[:, 0], t, out[:, 0], lse=lse)
+        got.append((out, lse))
+    assert torch.isfinite(got[0][0].float()).all()
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
