@@ -99,14 +99,14 @@ struct Shape {
   static constexpr int kQs = WIDE || D == 256 ? 1 : 2;
   static constexpr int kEntries = D == 64 ? (WIDE ? 8 : 6) : E8 ? 3 : 4;
   static constexpr int kStages = !E8 ? 0 : D == 64 ? 4 : 3;  // entries of codes on their way
-  static constexpr int kScales = E8 ? 3 : 0;                 // tiles whose scales are kept: the softmax's two, and the next
+  static constexpr int kScales = !E8 ? 0 : D == 128 ? 4 : 8;  // tiles whose scales are kept, from their codes' copies to the softmax
   // two producer warps for keys and two for values, where each kind has its own places (an odd number
   // of them passes from one kind to the other, and a wait for the one would not see the other's turn)
   static constexpr bool kSplit = kEntries % 2 == 0 && kStages % 2 == 0 && !(E8 && WIDE);
   static constexpr int kBring = kSplit ? kProducers / 2 : kProducers;  // warps that bring an entry
   static constexpr int kTurn = 2;  // tiles that a segment's end is worth in the dealing (it takes 6-9 k clk)
   static constexpr int kQBytes = kRows * D * 2;
-  static constexpr int kNeed = kQs * kQBytes + kEntries * kEntry + kStages * kEntry / 2 + 1024;
+  static constexpr int kNeed = kQs * kQBytes + kEntries * kEntry + kStages * kEntry / 2;
   static constexpr int kSmem = kNeed > kPdlTmemSmem ? kNeed : kPdlTmemSmem + 1024;
   static constexpr int kCols = WIDE ? kKeys : kKeys / 2;  // columns of a thread
   // TMEM columns
@@ -123,15 +123,18 @@ struct Info {  // a tile
 
 template <class S>
 struct Control {
-  uint64_t full[8], empty[8], info[kInfos], paged[8], placed[4], taken[4], staged[4], unstaged[4], q_full[2], q_empty[2], s_full[4], p_full[4], pv_done[2], used[3], fin;
+  uint64_t full[8], empty[8], info[kInfos], paged[8], placed[4], taken[4], staged[4], unstaged[4], q_full[2], q_empty[2], s_full[4], p_full[4], pv_done[2], used[8], fin;
   Info tile[kInfos];
   unsigned long long bad[16][2];  // per segment: nodes, and positions from lo on, with values that are not finite
   int64_t off[4][S::kKeys];      // element offsets of a tile's rows, -1: none
   int page[8][S::kKeys];         // pages of a tile's rows, -1: none
   // of each position of an 8-bit tile: key scale, exponent of the value scale, and 2 to minus that
   float4 scale[S::kScales ? S::kScales : 1][3][S::kScales ? S::kKeys / 4 : 1];
-  int64_t sum[16];
-  float mx[2][2][S::kShared], qf[3][S::kRows];  // maxima (a segment's sums at its end); what is left of a query's scale
+  union {
+    int64_t sum[16];       // of the warps' tiles, at the start
+    float qf[3][S::kRows];  // what is left of a query's scale
+  };
+  float mx[2][2][S::kShared];  // maxima (a segment's sums at its end)
   long long patience;  // of a wait, in clocks
   int where[5];  // sequence, key head and block, tile, length; what the share has of a segment's end ahead of that
   uint32_t tmem;
@@ -394,16 +397,19 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
   using M = typename std::conditional<E8, __half, T>::type;  // type of the products
   constexpr int kKeys = S::kKeys, kChunks = D / 8, kEntries = S::kEntries, kTurn = S::kTurn;
   constexpr bool kLow = !std::is_same<M, __half>::value || std::is_same<T, __half>::value;  // weights have a low part
-  extern __shared__ unsigned char smem_raw[];
+  extern __shared__ __align__(1024) unsigned char smem[];  // (a swizzle's atoms)
   __shared__ __align__(16) Control<S> ctl;
-  static_assert(S::kSmem + sizeof(Control<S>) <= 232448, "shared memory of an SM");
+  static_assert(S::kSmem + (sizeof(Control<S>) + 1023) / 1024 * 1024 <= 232448, "shared memory of an SM");
   const TreeArgs& a = g.a;
   const pe_kv_cache& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t qs = tc::smem_u32(smem), ring = qs + S::kQs * S::kQBytes;
   const int G = a.n_q_heads / c.n_heads, R = a.n_nodes * G, B = c.n_seqs;
 
+  if (qs & 1023) {  // a base that is not what it was declared to be
+    if (tid == 0) atomicExch(g.error, 1);
+    return;
+  }
   if (warp == 8) tc::tmem_alloc(&ctl.tmem, 512);
   if (tid == 0) {
     for (int i = 0; i < 8; ++i) {
@@ -411,7 +417,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       tc::mbar_init(&ctl.empty[i], 1);
     }
     for (int i = 0; i < kInfos; ++i) tc::mbar_init(&ctl.info[i], E8 ? 3 : 1);  // warps: places, scales of keys, of values
-    for (int i = 0; i < 3; ++i) tc::mbar_init(&ctl.used[i], 8);
+    for (int i = 0; i < 8; ++i) tc::mbar_init(&ctl.used[i], 8);
     for (int i = 0; i < 8; ++i) tc::mbar_init(&ctl.paged[i], 1);
     for (int i = 0; i < 4; ++i) {
       tc::mbar_init(&ctl.placed[i], 1);
@@ -537,7 +543,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       float m = -CUDART_INF_F, l = 0.0f, qf = 1.0f;
       auto use = [&](uint32_t tile) {  // the warp has read the tile's scales
         __syncwarp();
-        if (E8 && lane == 0) tc::mbar_arrive(&ctl.used[tile % 3]);
+        if (E8 && lane == 0) tc::mbar_arrive(&ctl.used[tile & (S::kScales - 1)]);
       };
       if (WIDE && wg == 1 && !both) {
         if constexpr (E8)
@@ -562,7 +568,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         // (16 bits: a scale of 0 as the least there is, what is masked stays -inf)
         const float cf = E8 ? qf : fmaxf(qlog, 1e-37f);
         const float2 cf2 = make_float2(cf, cf);
-        const float4* scale = &ctl.scale[E8 ? ip % 3 : 0][0][E8 && !WIDE ? wg * (S::kCols / 4) : 0];
+        const float4* scale = &ctl.scale[E8 ? ip & (S::kScales - 1) : 0][0][E8 && !WIDE ? wg * (S::kCols / 4) : 0];
         if (warp_live) {
           const uint32_t sc = lanes + S::kS + buf * S::kSStep + (WIDE ? 0 : wg * S::kCols);
           const bool whole = f.p0 >= lo_hi && f.p0 + kKeys <= f.n && (f.valid[0] & f.valid[1] & f.valid[2] & f.valid[3]) == 0xffffffffu;
@@ -901,9 +907,10 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tc::smem_u32(&ctl.staged[st])) : "memory");
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&ctl.taken[x & 3]);
-        if (x >= 3) wait(ctl, &ctl.used[x % 3], (x / 3 - 1) & 1);
+        constexpr uint32_t kSlots = S::kScales;
+        if (x >= kSlots) wait(ctl, &ctl.used[x % kSlots], (x / kSlots - 1) & 1);
         __syncwarp();
-        float* to = reinterpret_cast<float*>(ctl.scale[x % 3][which]);
+        float* to = reinterpret_cast<float*>(ctl.scale[x % kSlots][which]);
 #pragma unroll
         for (int j = 0; j < kMine; ++j) {
           const int r = lane + 32 * j, byte = b[j], ve = min(max(byte, 63), 247);  // (what is not there is masked: any number will do)
