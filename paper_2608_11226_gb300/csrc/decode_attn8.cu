@@ -10,7 +10,10 @@ static pe_status go_heads(const DecodeArgs& a, void* ws, cudaStream_t st) {
   const int n = seg_heads(D, a.n_q_heads / a.c.n_heads);
   if (n == 8) return go<T, true, D, 1, 1>(a, ws, st);
   if (n == 16) return go<T, true, D, D == 256 ? 1 : 2, D == 256 ? 2 : 1>(a, ws, st);
-  if constexpr (D < 256) return go<T, true, D, 3, 1>(a, ws, st);  // 24
+  if constexpr (D == 64)
+    if (n == 32) return go<T, true, D, 4, 1>(a, ws, st);
+  if constexpr (D < 256)
+    if (n == 24) return go<T, true, D, 3, 1>(a, ws, st);
   return fail(PE_EINVAL, "too many heads");  // they go to tree_attn_launch
 }
 

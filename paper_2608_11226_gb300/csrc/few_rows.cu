@@ -8,17 +8,18 @@ pe_status few_rows8_launch(const DecodeArgs& a, int dtype, void* ws, cudaStream_
 
 // Which kernel takes a tree: this one up to as many rows as one warp holds (over 8 bits
 // of head_dim 256 two), the one of tiles (tree_attn.cuh) beyond.  Measured with 8 key heads, 8 sequences of
-// 32,640 positions, this against that: 8 bits, head_dim 128, 8 rows 93 against 208
-// us, 16 rows 110, 24 rows 188 (2 sequences of 512: 11.4, 14.4, 17.2 against 16.1);
-// head_dim 64, 24 rows 98 against 166; head_dim 256, 8 rows 172 against 377, 16 rows
-// 209 against 370.
-// 16 bits, head_dim 128, 8 rows 165 against 169, 16 rows 171 against 169 (64
-// sequences of 2,048: 95 against 102), 24 rows 175 against 170 (107 against 102);
-// head_dim 64, 24 rows 96 against 130; head_dim 256, 8 rows 310 against 319.
+// 32,640 positions, this against that: 8 bits, head_dim 128, 8 rows 92 against 230
+// us, 16 rows 112, 24 rows 181 (2 sequences of 512: 9.9, 12.7, 16.2 against 13.8);
+// head_dim 64, 24 rows 98, 32 rows 124 against 208 (64 sequences of 2,048: 73, 98 against 157;
+// 2 of 512: 12.3, 13.9 against 13.1); head_dim 256, 8 rows 171 against 354, 16 rows 211.
+// 16 bits, head_dim 128, 8 rows 165 against 182, 16 rows 171 (64 sequences of 2,048: 96
+// against 117), 24 rows 175 against 181 (111 against 118; 2 of 512: 16.2 against 13.0);
+// head_dim 64, 24 rows 98, 32 rows 111 against 156 (69, 85 against 102; 12.1, 13.3 against
+// 12.0); head_dim 256, 8 rows 319 against 336.
 bool few_rows(const pe_kv_cache& c, int n_nodes, int n_q_heads) {
   const int rows = n_nodes * (n_q_heads / c.n_heads);
   const bool eight = c.dtype == PE_E4M3;
-  return rows <= (c.head_dim == 256 ? (eight ? 16 : 8) : c.head_dim == 64 || eight ? 24 : 16);
+  return rows <= (c.head_dim == 256 ? (eight ? 16 : 8) : c.head_dim == 64 ? 32 : eight ? 24 : 16);
 }
 
 int64_t few_rows_ws_bytes(const pe_kv_cache& c, int n_nodes, int n_q_heads) { return decode_ws_bytes(c, n_nodes * n_q_heads); }

@@ -16,6 +16,8 @@ static pe_status few_go(const DecodeArgs& a, void* ws, cudaStream_t st) {
     if (n == 16) return go<T, E8, D, 2, 1, true>(a, ws, st);
     if constexpr (E8 || D == 64)
       if (n == 24) return go<T, E8, D, 3, 1, true>(a, ws, st);
+    if constexpr (D == 64)
+      if (n == 32) return go<T, E8, D, 4, 1, true>(a, ws, st);
   }
   return fail(PE_EINVAL, "too many rows");  // few_rows() is false for them
 }

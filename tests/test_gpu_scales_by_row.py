@@ -58,7 +58,7 @@ def attend(P, q, lens, scale, window, masks=None):
 
 
 # nodes and heads a key head on either side of every choice of kernel and block
-ROWS = [(64, 24, 1), (64, 25, 1), (64, 43, 3), (128, 24, 1), (128, 25, 1), (128, 43, 3), (256, 16, 1), (256, 17, 1), (256, 43, 3)]
+ROWS = [(64, 24, 1), (64, 32, 1), (64, 33, 1), (64, 43, 3), (128, 24, 1), (128, 25, 1), (128, 43, 3), (256, 16, 1), (256, 17, 1), (256, 43, 3)]
 
 
 @pytest.mark.parametrize("D,N,G", ROWS)

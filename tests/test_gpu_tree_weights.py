@@ -23,6 +23,7 @@ CASES = [  # dtype, 8 bits, D, nodes, heads a key head: few rows, tiles, wide bl
     (BF16, False, 64, 24, 1), (BF16, False, 64, 25, 1), (BF16, False, 64, 43, 3), (BF16, False, 128, 16, 1), (BF16, False, 128, 32, 4),
     (BF16, False, 128, 50, 4), (BF16, False, 256, 8, 1), (BF16, False, 256, 32, 4), (F16, False, 64, 33, 2), (F16, False, 128, 25, 1),
     (F16, False, 128, 64, 4), (F16, False, 256, 17, 2), (F16, True, 64, 25, 2), (F16, True, 128, 20, 1), (F16, True, 128, 32, 4),
+    (BF16, False, 64, 33, 1), (BF16, False, 128, 17, 1), (F16, False, 128, 24, 1), (BF16, False, 64, 8, 4),
     (F16, True, 128, 50, 4), (F16, True, 256, 17, 2), (BF16, True, 128, 32, 4), (BF16, True, 128, 50, 4), (BF16, True, 64, 43, 3)]
 
 
@@ -50,3 +51,31 @@ def test_weights(dtype, eight, D, N, G):
     base.close(out[0], ref, tol)
     error, least = (out[0].double() - ref).norm(), (ref.to(dtype).double() - ref).norm()
     assert error <= 1.05 * least, f"{(error / ref.norm()).item():.3g} for {(least / ref.norm()).item():.3g}"
+
+
+@pytest.mark.parametrize("dtype,eight,lens,N,max_pages,page,Hq,Hkv,layout", [
+    (BF16, True, [900, 0, 31, 257], 8, 30, 32, 8, 2, "slot"), (F16, True, [64, 63, 65, 5], 29, 9, 13, 3, 3, "head"),
+    (BF16, False, [3000], 4, 64, 48, 8, 1, "slot"), (F16, False, [500, 40, 7], 31, 40, 16, 2, 2, "head"),
+    (BF16, True, [20, 8, -3], 32, 3, 8, 1, 1, "slot")])  # the last: nodes beyond the table
+@pytest.mark.parametrize("window", [0, 64, 200])
+def test_four_tiles_of_rows(dtype, eight, lens, N, max_pages, page, Hq, Hkv, layout, window):
+    """25 to 32 rows of head_dim 64, in one warp."""
+    base.test_tree(dtype, eight, lens, N, max_pages, page, Hq, Hkv, 64, layout, window)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("window", [0, 70])
+def test_four_tiles_of_rows_and_values_that_are_no_numbers(eight, window):
+    base.test_few_rows_and_values_that_are_no_numbers(eight, 8, 8, 64, 500, window)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("B,longest", [(90, 300), (3, 9000), (700, 2), (1, 20000)])
+def test_four_tiles_of_rows_of_many_segments(eight, B, longest):
+    base.test_many_segments(eight, 64, 4, 30, B, longest)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("lens,window", [([700, 3, 0], 0), ([9000, 40, 700], 0), ([9000, 40, 700], 1000)])
+def test_one_token_of_32_heads(dtype, lens, window):
+    base.test_decode8(dtype, True, lens, 150, 64, 60, 2, 64, "slot", window)
