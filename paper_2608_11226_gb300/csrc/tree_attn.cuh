@@ -47,11 +47,16 @@
 // warps that widen codes and the softmax set the pace (issue active 33%, a quarter
 // of the stalls for instructions).
 //
-// An 8-bit row is its codes times 2^e.  The products are of the codes themselves, exact in
-// fp16; a key's scale multiplies its column of scores and a value's exponent is added to it,
-// so that the running maximum is that of weight times scale, and the sum of the weights takes
-// the value's scale out again.  A row's scale so counts for that row alone, and for those who
-// attend to it.  Queries become fp16 with a power of two of their own: exact for fp16,
+// An 8-bit row is its codes times 2^e.  Where rows attend differently, or scales lie far
+// apart, the products are of the codes themselves, exact in fp16; a key's scale multiplies its
+// column of scores and a value's exponent is added to it, so that the running maximum is
+// that of weight times scale, and the sum of the weights takes the value's scale out again.  A row's
+// scale so counts for that row alone, and for those who attend to it.  Reading three numbers a
+// column for every row is dear (256 rows, 8 sequences of 32,640 positions: 458 us for 318), so
+// where everyone attends to the whole tile and its exponents are close to the largest, E, codes become
+// fp16 as code * 2^(e - E), which is exact, and 2^E goes into the exponentials' argument: keys within
+// 14 of E, values within 5, because E stands for their exponents in the running maximum.
+// Queries become fp16 with a power of two of their own: exact for fp16,
 // for bf16 down to 2^-31 of the row's largest (the rest is off by 2^-39 of that at most).
 //
 // P enters the second product as a sum of two 16-bit numbers, hi + lo (bf16, or fp16 over
@@ -65,7 +70,7 @@
 // Sums of weights are of the fp32 weights.
 //
 // Weights are relative to a running maximum that follows only when it is passed
-// by 8 (a factor of 256), so the output is seldom rescaled.
+// by 8 (a factor of 256; 8 bits: 5), so the output is seldom rescaled.
 #pragma once
 
 #include <math_constants.h>
@@ -99,7 +104,7 @@ struct Shape {
   static constexpr int kQs = WIDE || D == 256 ? 1 : 2;
   static constexpr int kEntries = D == 64 ? (WIDE ? 8 : 6) : E8 ? 3 : 4;
   static constexpr int kStages = !E8 ? 0 : D == 64 ? 4 : 3;  // entries of codes on their way
-  static constexpr int kScales = !E8 ? 0 : D == 128 ? 4 : 8;  // tiles whose scales are kept, from their codes' copies to the softmax
+  static constexpr int kScales = !E8 ? 0 : D == 128 ? 3 : 8;  // tiles whose columns' scales are kept, from their codes' copies to the softmax
   // two producer warps for keys and two for values, where each kind has its own places (an odd number
   // of them passes from one kind to the other, and a wait for the one would not see the other's turn)
   static constexpr bool kSplit = kEntries % 2 == 0 && kStages % 2 == 0 && !(E8 && WIDE);
@@ -119,6 +124,9 @@ struct Shape {
 struct Info {  // a tile
   uint32_t valid[4];  // its positions that exist: in the sequence's range, on present pages
   int p0, n, lo, flags;  // first position; the sequence's length and lowest position; 1: rows attend to it differently (segment from bit 1 on)
+  // 8 bits: whether columns have scales of their own; else 2^E of the keys (their rows' factor taken out), E of the values
+  int key_columns, value_columns;
+  float ek, ev;
 };
 
 template <class S>
@@ -128,6 +136,7 @@ struct Control {
   unsigned long long bad[16][2];  // per segment: nodes, and positions from lo on, with values that are not finite
   int64_t off[4][S::kKeys];      // element offsets of a tile's rows, -1: none
   int page[8][S::kKeys];         // pages of a tile's rows, -1: none
+  uint8_t fac[4][2][S::kScales ? S::kKeys : 1];  // 2^(e - E) of each row of an 8-bit tile in fp16, its upper byte; 1 with scales by column
   // of each position of an 8-bit tile: key scale, exponent of the value scale, and 2 to minus that
   float4 scale[S::kScales ? S::kScales : 1][3][S::kScales ? S::kKeys / 4 : 1];
   union {
@@ -340,16 +349,20 @@ __device__ __forceinline__ float piece_weight(float m, float mm) {
   return m == -CUDART_INF_F ? (mm == -CUDART_INF_F ? 1.0f : 0.0f) : exp2_fast(m - mm);
 }
 
-// fp16 weights are e^(s - m) 2^6, at most 2^14: what is 2^-30 of the largest is kept
-template <typename M> struct Weights;
-template <> struct Weights<__nv_bfloat16> {
-  static constexpr float kBias = 0.0f;
+// fp16 weights are e^(s - m) 2^kBias, at most 2^(kBias + kLag): what is 2^-30 of the largest is kept
+// (8 bits: 2^-27 of the largest weight times scale, for a tile's E counts for up to 5 more than a row's exponent)
+template <typename M, bool E8> struct Weights;
+template <> struct Weights<__nv_bfloat16, false> {
+  static constexpr float kBias = 0.0f, kLag = 8.0f;
 };
-template <> struct Weights<__half> {
-  static constexpr float kBias = 6.0f;
+template <> struct Weights<__half, false> {
+  static constexpr float kBias = 6.0f, kLag = 8.0f;
 };
-template <typename M> __device__ __forceinline__ float log_sum(float m, float l) {
-  return l == 0.0f ? -CUDART_INF_F : (m == -CUDART_INF_F ? 0.0f : m - Weights<M>::kBias) * 0.69314718f + logf(l);
+template <> struct Weights<__half, true> {
+  static constexpr float kBias = 7.0f, kLag = 8.0f;
+};
+template <typename M, bool E8> __device__ __forceinline__ float log_sum(float m, float l) {
+  return l == 0.0f ? -CUDART_INF_F : (m == -CUDART_INF_F ? 0.0f : m - Weights<M, E8>::kBias) * 0.69314718f + logf(l);
 }
 
 // the first 16-bit part of two weights, packed, and what it leaves of them
@@ -371,7 +384,7 @@ __device__ __forceinline__ uint32_t chunk_at(int r, int ch, int rows) {
 
 // which of elements d .. d + 15 of the marked positions' values (nodes, positions from lo on) are not finite
 template <typename T, bool E8>
-__device__ __forceinline__ uint32_t spoilt_columns(const TreeArgs& a, int b, int hk, int n, int lo, uint64_t nodes, uint64_t ahead, int d) {
+__device__ __noinline__ uint32_t spoilt_columns(const TreeArgs& a, int b, int hk, int n, int lo, uint64_t nodes, uint64_t ahead, int d) {
   const pe_kv_cache& c = a.c;
   uint32_t nan = 0;
 #pragma unroll 1
@@ -387,6 +400,76 @@ __device__ __forceinline__ uint32_t spoilt_columns(const TreeArgs& a, int b, int
       if (E8 ? (((const uint8_t*)c.v)[at + j] & 0x7f) == 0x7f : not_finite<T>(((const uint16_t*)c.v)[at + j], 0)) nan |= 1u << j;
   }
   return nan;
+}
+
+// What is not the same for every column and row, in functions apart from the kernel's body, whose roles' code the
+// instruction cache has to hold.
+
+// Scores of `COLS` columns from `first` of tile f on, in their place: -inf where the row does not attend; over 8
+// bits in powers of two, columns' own scales and their values' exponents in them
+template <bool E8, int COLS, int KEYS>
+__device__ __noinline__ void set_apart(uint32_t sc, const Info& f, int first, int row_lo, uint64_t bits, bool live, const float4* scale, float cs) {
+  const bool keys = E8 && f.key_columns, values = E8 && f.value_columns;
+#pragma unroll 1
+  for (int i = 0; i < COLS / 32; ++i) {
+    const int pw = f.p0 + first + 32 * i;
+    const int below = min(max(f.n - pw, 0), 32), skip = min(max(row_lo - pw, 0), 32);
+    uint32_t ctx = below == 32 ? 0xffffffffu : (1u << below) - 1;
+    ctx &= skip == 32 ? 0u : 0xffffffffu << skip;
+    const int sh = pw - f.n;
+    const uint32_t nodes = sh >= 64 || sh <= -32 ? 0u : sh >= 0 ? (uint32_t)(bits >> sh) : (uint32_t)(bits << -sh);
+    const uint32_t kept = live ? f.valid[(first >> 5) + i] & (ctx | nodes) : 0u;
+    float x[32];
+    ld32(sc + 32 * i, x);
+    ld_wait(x);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t r[16];
+#pragma unroll
+      for (int j = 0; j < 16; j += 4) {
+        float4 k = make_float4(1.0f, 1.0f, 1.0f, 1.0f), e = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (keys) k = scale[8 * i + 4 * h + j / 4];
+        if (values) e = scale[KEYS / 4 + 8 * i + 4 * h + j / 4];
+        float z[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) z[u] = x[16 * h + j + u];
+        if (E8) z[0] = fmaf(z[0] * k.x, cs, e.x), z[1] = fmaf(z[1] * k.y, cs, e.y), z[2] = fmaf(z[2] * k.z, cs, e.z), z[3] = fmaf(z[3] * k.w, cs, e.w);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) r[j + u] = __float_as_uint((kept >> (16 * h + j + u)) & 1 ? z[u] : -CUDART_INF_F);
+      }
+      st16(sc + 32 * i + 16 * h, r);
+    }
+  }
+  st_wait();
+}
+// a lane's bytes as what those take, 32 positions apart (what is not there is masked: any number will do)
+static __device__ __noinline__ void column_scales(float* to, bool values, int keys, int b0, int b1, int b2, int b3) {
+#pragma unroll 1
+  for (int r = 0; r < keys; r += 32) {
+    const int e = min(max(b0, 63), 247);
+    to[r] = b0 < 0 ? 0.0f : !values ? key_scale(b0) : b0 == 255 ? CUDART_NAN_F : (float)(e - 127);
+    if (values) to[keys + r] = __int_as_float((254 - e) << 23);
+    b0 = b1, b1 = b2, b2 = b3;
+  }
+}
+// l and the sum of those columns' weights with the value scales taken out
+template <int COLS, int KEYS>
+__device__ __noinline__ float column_sum(uint32_t sc, const float4* scale, float off, float l) {
+#pragma unroll 1
+  for (int i = 0; i < COLS / 32; ++i) {
+    float x[32];
+    ld32(sc + 32 * i, x);
+    ld_wait(x);
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+      const float4 back = scale[2 * (KEYS / 4) + 8 * i + j / 4];
+      l = fmaf(exp2_fast(x[j] + off), back.x, l);
+      l = fmaf(exp2_fast(x[j + 1] + off), back.y, l);
+      l = fmaf(exp2_fast(x[j + 2] + off), back.z, l);
+      l = fmaf(exp2_fast(x[j + 3] + off), back.w, l);
+    }
+  }
+  return l;
 }
 
 // ---------------------------------------------------------------- the kernel
@@ -416,11 +499,12 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       tc::mbar_init(&ctl.full[i], E8 ? S::kBring : 32 * S::kBring);
       tc::mbar_init(&ctl.empty[i], 1);
     }
-    for (int i = 0; i < kInfos; ++i) tc::mbar_init(&ctl.info[i], E8 ? 3 : 1);  // warps: places, scales of keys, of values
+    constexpr int kPlacers = E8 ? 3 : 1;  // warps: places, scales of keys, of values
+    for (int i = 0; i < kInfos; ++i) tc::mbar_init(&ctl.info[i], kPlacers);
     for (int i = 0; i < 8; ++i) tc::mbar_init(&ctl.used[i], 8);
     for (int i = 0; i < 8; ++i) tc::mbar_init(&ctl.paged[i], 1);
     for (int i = 0; i < 4; ++i) {
-      tc::mbar_init(&ctl.placed[i], 1);
+      tc::mbar_init(&ctl.placed[i], kPlacers);
       tc::mbar_init(&ctl.taken[i], E8 ? S::kProducers + 2 : S::kProducers);
       tc::mbar_init(&ctl.s_full[i], 1);
       tc::mbar_init(&ctl.p_full[i], WIDE ? 4 : 8);
@@ -518,7 +602,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");  // 256 threads of 160 and 256 of 96: what 512 of 128 had
     const int wg = warp >> 2, row = (warp & 3) * 32 + lane;  // row of the tile, lane of TMEM
     const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-    const float qlog = fabsf(a.scale) * 1.4426950408889634f * (E8 ? kRowFactor : 1.0f);
+    const float qlog = fabsf(a.scale) * 1.4426950408889634f;
     uint32_t sp[2] = {0, 0}, pp = 0, ip = 0;  // phases: scores, outputs, tiles seen
     uint64_t bits = 0;  // the row's mask, of sequence last_b
     int last_b = -1;
@@ -543,7 +627,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       float m = -CUDART_INF_F, l = 0.0f, qf = 1.0f;
       auto use = [&](uint32_t tile) {  // the warp has read the tile's scales
         __syncwarp();
-        if (E8 && lane == 0) tc::mbar_arrive(&ctl.used[tile & (S::kScales - 1)]);
+        if (E8 && lane == 0) tc::mbar_arrive(&ctl.used[tile & 7]);
       };
       if (WIDE && wg == 1 && !both) {
         if constexpr (E8)
@@ -564,54 +648,26 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         ++sp[b2];
         __syncwarp();
         tc::fence_after();
-        if (E8 && t == 0) qf = qlog * ctl.qf[w.index % 3][(WIDE ? wg * 128 : 0) + row];
-        // (16 bits: a scale of 0 as the least there is, what is masked stays -inf)
-        const float cf = E8 ? qf : fmaxf(qlog, 1e-37f);
+        if (E8 && t == 0) qf = ctl.qf[w.index % 3][(WIDE ? wg * 128 : 0) + row];
+        const bool kcol = E8 && f.key_columns, vcol = E8 && f.value_columns;
+        const float ev = E8 ? f.ev : 0.0f;
+        const bool whole = f.p0 >= lo_hi && f.p0 + kKeys <= f.n && (f.valid[0] & f.valid[1] & f.valid[2] & f.valid[3]) == 0xffffffffu;
+        const bool apart = !whole || kcol || vcol;
+        // what takes a score to powers of two (a scale of 0 as the least there is, what is masked stays -inf)
+        const float cs = E8 ? qlog * (qf * f.ek) : qlog, cf = E8 && apart ? 1.0f : fmaxf(cs, 1e-37f);
         const float2 cf2 = make_float2(cf, cf);
-        const float4* scale = &ctl.scale[E8 ? ip & (S::kScales - 1) : 0][0][E8 && !WIDE ? wg * (S::kCols / 4) : 0];
+        const float4* scale = &ctl.scale[E8 ? ip % (E8 ? S::kScales : 1) : 0][0][E8 && !WIDE ? wg * (S::kCols / 4) : 0];
         if (warp_live) {
           const uint32_t sc = lanes + S::kS + buf * S::kSStep + (WIDE ? 0 : wg * S::kCols);
-          const bool whole = f.p0 >= lo_hi && f.p0 + kKeys <= f.n && (f.valid[0] & f.valid[1] & f.valid[2] & f.valid[3]) == 0xffffffffu;
           // 64 columns at a time (head_dim 256: 32); code is kept short, for the roles share the instruction cache
           constexpr int kHalves = S::kCols >= 64 ? 2 : 1, kTurns = S::kCols / (32 * kHalves);
-          uint32_t keep[S::kCols / 32];
-          if (__builtin_expect(!whole, 0)) {
-#pragma unroll
-            for (int i = 0; i < S::kCols / 32; ++i) {
-              const int at = i + (WIDE ? 0 : wg * (S::kCols / 32)), pw = f.p0 + 32 * at;
-              const int below = min(max(f.n - pw, 0), 32), skip = min(max(row_lo - pw, 0), 32);
-              uint32_t ctx = below == 32 ? 0xffffffffu : (1u << below) - 1;
-              ctx &= skip == 32 ? 0u : 0xffffffffu << skip;
-              const int sh = pw - f.n;
-              const uint32_t nodes = sh >= 64 || sh <= -32 ? 0u : sh >= 0 ? (uint32_t)(bits >> sh) : (uint32_t)(bits << -sh);
-              keep[i] = live ? f.valid[at] & (ctx | nodes) : 0u;
-            }
-          }
+          if (__builtin_expect(apart, 0)) set_apart<E8, S::kCols, kKeys>(sc, f, WIDE ? 0 : wg * S::kCols, row_lo, bits, live, scale, cs);
           float v[kHalves][32];
           auto fetch = [&](int turn) {
 #pragma unroll
             for (int h = 0; h < kHalves; ++h) ld32(sc + 64 * turn + 32 * h, v[h]);
 #pragma unroll
             for (int h = 0; h < kHalves; ++h) ld_wait(v[h]);
-            if constexpr (E8) {  // in powers of two, the value's exponent in it
-#pragma unroll
-              for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-                for (int j = 0; j < 32; j += 4) {
-                  const float4 k = scale[16 * turn + 8 * h + j / 4], e = scale[kKeys / 4 + 16 * turn + 8 * h + j / 4];
-                  const float2 a = __ffma2_rn(__fmul2_rn(make_float2(v[h][j], v[h][j + 1]), make_float2(k.x, k.y)), cf2, make_float2(e.x, e.y));
-                  const float2 b = __ffma2_rn(__fmul2_rn(make_float2(v[h][j + 2], v[h][j + 3]), make_float2(k.z, k.w)), cf2, make_float2(e.z, e.w));
-                  v[h][j] = a.x, v[h][j + 1] = a.y, v[h][j + 2] = b.x, v[h][j + 3] = b.y;
-                }
-            }
-            if (__builtin_expect(!whole, 0)) {
-#pragma unroll
-              for (int h = 0; h < kHalves; ++h) {
-                const uint32_t k = kTurns == 1 ? keep[h] : turn ? keep[(kTurns - 1) * kHalves + h] : keep[h];
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[h][j] = (k >> j) & 1 ? v[h][j] : -CUDART_INF_F;
-              }
-            }
           };
           // the row's largest score
           float top = -CUDART_INF_F;
@@ -632,8 +688,8 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             bar_sync(1 + (warp & 3), 64);
             top = fmaxf(top, ctl.mx[ip & 1][wg ^ 1][row]);
           }
-          if (!E8) top = top == -CUDART_INF_F ? top : top * cf;
-          const bool over = top > m + 8.0f;
+          top = top == -CUDART_INF_F ? top : fmaf(top, cf, ev);
+          const bool over = top > m + Weights<M, E8>::kLag;
           if (__builtin_expect(__any_sync(0xffffffffu, over), 0)) {
             const float x = over ? top : m;
             const float fr = over ? (m == -CUDART_INF_F ? 0.0f : exp2_fast(m - x)) : 1.0f;
@@ -655,9 +711,10 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
               }
             }
           }
-          const float off = Weights<M>::kBias - (m == -CUDART_INF_F ? 0.0f : m);
+          const float off = ev + Weights<M, E8>::kBias - (m == -CUDART_INF_F ? 0.0f : m);
           const float2 off2 = make_float2(off, off);
           float2 part = make_float2(0.0f, 0.0f);
+          if (E8 && __builtin_expect(vcol, 0)) l = column_sum<S::kCols, kKeys>(sc, scale, off, l);
 #pragma unroll 1
           for (int turn = 0; turn < kTurns; ++turn) {
             if (kTurns > 1) fetch(turn);
@@ -665,27 +722,22 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
             for (int h = 0; h < kHalves; ++h) {
               uint32_t pk[16], low[kLow ? 16 : 1];
 #pragma unroll
-              for (int j = 0; j < 32; j += 4) {
-                float2 e[2] = {make_float2(v[h][j], v[h][j + 1]), make_float2(v[h][j + 2], v[h][j + 3])};
-                const float4 back = E8 ? scale[2 * (kKeys / 4) + 16 * turn + 8 * h + j / 4] : make_float4(1.0f, 1.0f, 1.0f, 1.0f);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                  e[i] = E8 ? __fadd2_rn(e[i], off2) : __ffma2_rn(e[i], cf2, off2);
-                  const float2 p = make_float2(exp2_fast(e[i].x), exp2_fast(e[i].y));
-                  part = E8 ? __ffma2_rn(p, i ? make_float2(back.z, back.w) : make_float2(back.x, back.y), part) : __fadd2_rn(part, p);
-                  if constexpr (kLow) {
-                    const float2 rest = high_part<M>(p, pk[j / 2 + i]);
-                    low[j / 2 + i] = pack2<M>(rest.x, rest.y);
-                  } else {
-                    pk[j / 2 + i] = pack2<M>(p.x, p.y);
-                  }
+              for (int j = 0; j < 32; j += 2) {
+                const float2 e = __ffma2_rn(make_float2(v[h][j], v[h][j + 1]), cf2, off2);
+                const float2 p = make_float2(exp2_fast(e.x), exp2_fast(e.y));
+                part = __fadd2_rn(part, p);
+                if constexpr (kLow) {
+                  const float2 rest = high_part<M>(p, pk[j / 2]);
+                  low[j / 2] = pack2<M>(rest.x, rest.y);
+                } else {
+                  pk[j / 2] = pack2<M>(p.x, p.y);
                 }
               }
               st16(sc + 64 * turn + 16 * h, pk);
               if constexpr (kLow) st16(sc + 64 * turn + S::kGroup / 2 + 16 * h, low);
             }
           }
-          l += part.x + part.y;
+          if (!vcol) l = E8 ? fmaf(part.x + part.y, exp2f(-ev), l) : l + (part.x + part.y);
           st_wait();
         } else if (!WIDE) {
           bar_sync(1 + (warp & 3), 64);
@@ -755,7 +807,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         }
         if (exists && (WIDE || wg == 0)) {
           if (whole) {
-            if (a.lse) a.lse[((int64_t)s.b * a.n_nodes + node) * a.n_q_heads + head] = log_sum<M>(m, l);
+            if (a.lse) a.lse[((int64_t)s.b * a.n_nodes + node) * a.n_q_heads + head] = log_sum<M, E8>(m, l);
           } else {
             piece[S::kRows * D + prow] = m;
             piece[S::kRows * (D + 1) + prow] = l;
@@ -859,8 +911,8 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     }
     if constexpr (E8) if (warp >= 10) {
       // ================================================ scales: of keys, of values
-      // The codes go to a stage: copies wait their turn here, apart from the warps that widen them.  Then the
-      // scales, as the softmax takes them; their bytes are loaded a tile ahead.
+      // What brings a row's scale to the tile's largest, or its own number for the softmax; bytes are loaded a
+      // tile ahead.  The codes go to a stage: copies wait their turn here, apart from the warps that widen them.
       constexpr int kMine = kKeys / 32;
       const int which = warp - 10;
       const uint8_t* base = which ? a.sc.v : a.sc.k;
@@ -887,6 +939,31 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       load(b, 0);
 #pragma unroll 1
       for (uint32_t x = 0;; ++x) {
+        // bytes in [63, 247]; 255 takes no part in the largest and the least
+        auto fit = [](int b) { return min(max(b, 63), 247); };
+        int big = -1, small = 256;
+#pragma unroll
+        for (int j = 0; j < kMine; ++j)
+          if (b[j] >= 0 && b[j] != 255) big = max(big, fit(b[j])), small = min(small, fit(b[j]));
+        big = __reduce_max_sync(0xffffffffu, big);
+        small = __reduce_min_sync(0xffffffffu, small);
+        Info& f = ctl.tile[x % kInfos];
+        const bool columns = (f.flags & 1) || big - small > (which ? 5 : 14);
+        if (big < 0) big = 127;
+        if (x >= 4) wait(ctl, &ctl.taken[x & 3], ((x >> 2) - 1) & 1);
+        if (x >= 8) wait(ctl, &ctl.used[x & 7], ((x >> 3) - 1) & 1);  // so that a wait for a later tile's cannot take one phase for another
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < kMine; ++j)
+          ctl.fac[x & 3][which][lane + 32 * j] = b[j] < 0 ? 0 : columns ? 0x3c : b[j] == 255 ? 0x7e : (15 + fit(b[j]) - big) << 2;
+        if (lane == 0) {
+          if (which)
+            f.ev = columns ? 0.0f : (float)(big - 127), f.value_columns = columns;
+          else
+            f.ek = columns ? kRowFactor : __int_as_float(big << 23), f.key_columns = columns;
+        }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&ctl.placed[x & 3]);
         const bool last = !more;
         load(next, x + 1);
         const uint32_t e = 2 * x + which, st = e % S::kStages;
@@ -907,19 +984,11 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tc::smem_u32(&ctl.staged[st])) : "memory");
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&ctl.taken[x & 3]);
-        constexpr uint32_t kSlots = S::kScales;
-        if (x >= kSlots) wait(ctl, &ctl.used[x % kSlots], (x / kSlots - 1) & 1);
-        __syncwarp();
-        float* to = reinterpret_cast<float*>(ctl.scale[x % kSlots][which]);
-#pragma unroll
-        for (int j = 0; j < kMine; ++j) {
-          const int r = lane + 32 * j, byte = b[j], ve = min(max(byte, 63), 247);  // (what is not there is masked: any number will do)
-          if (which == 0) {
-            to[r] = byte < 0 ? 0.0f : key_scale(byte);
-          } else {
-            to[r] = byte < 0 ? 0.0f : byte == 255 ? CUDART_NAN_F : (float)(ve - 127);
-            to[kKeys + r] = __int_as_float((254 - ve) << 23);
-          }
+        if (__builtin_expect(columns, 0)) {
+          constexpr uint32_t kSlots = E8 ? S::kScales : 1;
+          if (kSlots < 8 && x >= kSlots) wait(ctl, &ctl.used[(x - kSlots) & 7], ((x - kSlots) >> 3) & 1);
+          __syncwarp();
+          column_scales(reinterpret_cast<float*>(ctl.scale[x % kSlots][which]) + lane, which, kKeys, b[0], b[1], b[2 % kMine], b[3 % kMine]);
         }
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&ctl.info[x % kInfos]);
@@ -1227,7 +1296,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         }
         __syncwarp();
       };
-      auto put = [&](uint32_t e, bool check, const Info& f) {
+      auto put = [&](uint32_t e, const uint8_t* fac, bool check, const Info& f) {
         wait(ctl, &ctl.staged[e % kStages], (e / kStages) & 1);
         if (e >= kEntries) wait(ctl, &ctl.empty[e % kEntries], (e / kEntries - 1) & 1);
         __syncwarp();
@@ -1239,21 +1308,27 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         const unsigned char* own = from - pt * 16 + row0 * D + ch * 8;
 #pragma unroll 1
         for (int i0 = 0; i0 < kEach; i0 += kAtOnce) {
+          uint32_t fr[kAtOnce];
           uint2 z[kAtOnce][2];
 #pragma unroll
           for (int i = 0; i < kAtOnce; ++i) {
+            fr[i] = fac[row0 + (i0 + i) * kPass] * 0x01000100u;
             z[i][0] = *reinterpret_cast<const uint2*>(own + (i0 + i) * kPass * D);
             z[i][1] = *reinterpret_cast<const uint2*>(own + (i0 + i) * kPass * D + D / 2);
           }
 #pragma unroll
           for (int i = 0; i < kAtOnce; ++i) {
+            const __half2 ff = *reinterpret_cast<const __half2*>(&fr[i]);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               uint32_t y[4];
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
                 const uint32_t w = j < 2 ? z[i][h].x : z[i][h].y;
-                asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y[j]) : "h"((uint16_t)(w >> (16 * (j & 1)))));
+                uint32_t v;
+                asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(v) : "h"((uint16_t)(w >> (16 * (j & 1)))));
+                const __half2 p = __hmul2(*reinterpret_cast<const __half2*>(&v), ff);
+                y[j] = *reinterpret_cast<const uint32_t*>(&p);
               }
               *reinterpret_cast<uint4*>(dst + chunk_at(row0 + (i0 + i) * kPass, ch + h * kCh, kKeys)) = make_uint4(y[0], y[1], y[2], y[3]);
             }
@@ -1272,7 +1347,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
           placed(tile);
           const Info& f = ctl.tile[tile % kInfos];
 #pragma unroll 1
-          for (int kv = kind; kv < (S::kSplit ? kind + 1 : 2); ++kv) put(2 * tile + kv, kv && (f.flags & 1), f);
+          for (int kv = kind; kv < (S::kSplit ? kind + 1 : 2); ++kv) put(2 * tile + kv, ctl.fac[tile & 3][kv], kv && (f.flags & 1), f);
           arrive(&ctl.taken[tile & 3]);
           // (where they have one place, the first tile is under way before the last segment's are done with)
           if (S::kQs == 1 && t == 0) load_q(w);
@@ -1292,7 +1367,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
 // lanes hold the pieces' maxima and sums, then the output's elements.  Bound by
 // latency, so the first pieces are on their way before their weights are known.
 constexpr int kJoinRows = 8;
-template <typename T, typename M, int D>
+template <typename T, typename M, bool E8, int D>
 __global__ void __launch_bounds__(32 * kJoinRows) join_kernel(Args g, int block_rows) {
   cudaGridDependencySynchronize();
   cudaTriggerProgrammaticLaunchCompletion();
@@ -1366,7 +1441,7 @@ __global__ void __launch_bounds__(32 * kJoinRows) join_kernel(Args g, int block_
     if (sum == 0.0f) x = make_uint2(0, 0);
     *reinterpret_cast<uint2*>(out + 4 * (lane + 32 * v)) = x;
   }
-  if (a.lse && lane == 0) a.lse[((int64_t)s.seq * a.n_nodes + node) * a.n_q_heads + head] = log_sum<M>(mm, sum);
+  if (a.lse && lane == 0) a.lse[((int64_t)s.seq * a.n_nodes + node) * a.n_q_heads + head] = log_sum<M, E8>(mm, sum);
 }
 
 constexpr int64_t kMetaBytes = (kCtas * (int64_t)sizeof(SegMeta) + 255) / 256 * 256;
@@ -1399,7 +1474,7 @@ static pe_status go(const TreeArgs& a, void* ws, int32_t* error, const Patience&
   auto kern = attn_kernel<T, E8, D, WIDE>;
   PE_TRY_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
   PE_TRY_CUDA(launch_pdl(kern, dim3(kCtas), dim3(S::kThreads), S::kSmem, st, true, g));
-  PE_TRY_CUDA(launch_pdl(join_kernel<T, M, D>, dim3(kCtas, ceil_div(rows < S::kRows ? rows : S::kRows, kJoinRows)), dim3(32 * kJoinRows), 0, st,
+  PE_TRY_CUDA(launch_pdl(join_kernel<T, M, E8, D>, dim3(kCtas, ceil_div(rows < S::kRows ? rows : S::kRows, kJoinRows)), dim3(32 * kJoinRows), 0, st,
                          true, g, (int)S::kRows));
   return PE_OK;
 }
