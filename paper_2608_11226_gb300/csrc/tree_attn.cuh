@@ -70,7 +70,7 @@
 // Sums of weights are of the fp32 weights.
 //
 // Weights are relative to a running maximum that follows only when it is passed
-// by 8 (a factor of 256; 8 bits: 5), so the output is seldom rescaled.
+// by 8 (a factor of 256), so the output is seldom rescaled.
 #pragma once
 
 #include <math_constants.h>
@@ -442,6 +442,78 @@ __device__ __noinline__ void set_apart(uint32_t sc, const Info& f, int first, in
   }
   st_wait();
 }
+// an output whose weights' reference has moved
+__device__ __forceinline__ void rescale(uint32_t at, int columns, float f) {
+#pragma unroll 1
+  for (int i = 0; i < columns; i += 16) {
+    float o[16];
+    tc::tmem_ld16(at + i, o);
+    uint32_t r[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(o[j] * f);
+    st16(at + i, r);
+  }
+}
+
+// bit of row r's values, if rows attend to them differently: of a node (which 0), of a position from lo on (1)
+__device__ __forceinline__ uint64_t apart_bit(const Info& f, int r, int window, int n_nodes, int& which) {
+  const int p = f.p0 + r, node = p - f.n;
+  which = 0;
+  if (node >= 0) return node < n_nodes ? 1ull << node : 0;
+  which = 1;
+  return window > 0 && p >= f.lo && p - f.lo < 64 ? 1ull << (p - f.lo) : 0;
+}
+// Values that are not finite, where rows attend to them differently, become zeros and a mark: a thread's chunks of a tile
+template <typename T, int KEYS, int PASS>
+__device__ __noinline__ void clean_values(unsigned char* entry, const Info& f, unsigned long long* bad, int window, int n_nodes, int row0, int ch) {
+  // (nodes' rows alone, where there is no window)
+  const int from = window > 0 ? 0 : max(f.n - f.p0, 0), to = window > 0 ? KEYS : min(KEYS, f.n + n_nodes - f.p0);
+#pragma unroll 1
+  for (int r = row0 + (from - row0 + PASS - 1) / PASS * PASS; r < to; r += PASS) {
+    if (r < from) continue;
+    int which;
+    const uint64_t bit = apart_bit(f, r, window, n_nodes, which);
+    if (!bit || !((f.valid[r >> 5] >> (r & 31)) & 1)) continue;
+    uint4* p = reinterpret_cast<uint4*>(entry + chunk_at(r, ch, KEYS));
+    uint4 x = *p;
+    uint32_t* y = reinterpret_cast<uint32_t*>(&x);
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (not_finite<T>(y[i], 0)) y[i] &= 0xffff0000u, any = true;
+      if (not_finite<T>(y[i], 1)) y[i] &= 0x0000ffffu, any = true;
+    }
+    if (any) {
+      *p = x;
+      atomicOr(&bad[which], bit);
+    }
+  }
+}
+// The same of codes that are no numbers, in their stage (a scale that is none is in its column of scores, masked like those)
+template <int EACH, int PASS, int THREADS>
+__device__ __noinline__ void clean_codes(unsigned char* from, const Info& f, unsigned long long* bad, int window, int n_nodes, int row0) {
+#pragma unroll 1
+  for (int i = 0; i < EACH; ++i) {
+    const int r = row0 + i * PASS;
+    if (window == 0 && (i + 1) * PASS <= f.n - f.p0) continue;  // no nodes there
+    int which;
+    const uint64_t bit = (f.valid[r >> 5] >> (r & 31)) & 1 ? apart_bit(f, r, window, n_nodes, which) : 0;
+    if (!bit) continue;
+    uint4 z = *reinterpret_cast<const uint4*>(from + i * THREADS * 16);
+    uint32_t* y = reinterpret_cast<uint32_t*>(&z);
+    bool any = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int b = 0; b < 32; b += 8)
+        if (((y[j] >> b) & 0x7f) == 0x7f) y[j] &= ~(0xffu << b), any = true;
+    if (any) {
+      *reinterpret_cast<uint4*>(from + i * THREADS * 16) = z;
+      atomicOr(&bad[which], bit);
+    }
+  }
+}
+
 // a lane's bytes as what those take, 32 positions apart (what is not there is masked: any number will do)
 static __device__ __noinline__ void column_scales(float* to, bool values, int keys, int b0, int b1, int b2, int b3) {
 #pragma unroll 1
@@ -699,16 +771,7 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
               wait(ctl, &ctl.pv_done[WIDE ? wg : 0], (pp - 1) & 1);  // the last product into the output
               __syncwarp();
               tc::fence_after();
-              const uint32_t oc = lanes + S::kO + (WIDE ? wg * S::kOStep : wg * (D / 2));
-#pragma unroll 1
-              for (int i = 0; i < (WIDE ? D : D / 2) / 16; ++i) {
-                float o[16];
-                tc::tmem_ld16(oc + 16 * i, o);
-                uint32_t r[16];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(o[j] * fr);
-                st16(oc + 16 * i, r);
-              }
+              rescale(lanes + S::kO + (WIDE ? wg * S::kOStep : wg * (D / 2)), WIDE ? D : D / 2, fr);
             }
           }
           const float off = ev + Weights<M, E8>::kBias - (m == -CUDART_INF_F ? 0.0f : m);
@@ -1185,14 +1248,6 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
         arrive(&ctl.q_full[qb]);
       }
     };
-    // bits of the values that rows attend to differently: (nodes, positions from lo on)
-    auto apart = [&](const Info& f, int r, int& which) -> uint64_t {
-      const int p = f.p0 + r, node = p - f.n;
-      which = 0;
-      if (node >= 0) return node < a.n_nodes ? 1ull << node : 0;
-      which = 1;
-      return a.window > 0 && p >= f.lo && p - f.lo < 64 ? 1ull << (p - f.lo) : 0;
-    };
     Walk<kKeys, kTurn> w(g, ctl.where, share);
     uint32_t tile = 0;  // tiles behind
     auto placed = [&](uint32_t x) {
@@ -1203,36 +1258,6 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
     if constexpr (!E8) {
       constexpr int kPass = kN / kChunks;  // rows of a pass
       const int row0 = pt / kChunks, ch = pt % kChunks;
-      // Values that are not finite, where rows attend to them differently, become zeros and a mark
-      auto spoils = [&](uint32_t e, const Info& f) {
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        const uint32_t at = S::kQs * S::kQBytes + (e % kEntries) * S::kEntry;
-        unsigned long long* bad = ctl.bad[f.flags >> 1];
-        // (nodes' rows alone, where there is no window)
-        const int from = a.window > 0 ? 0 : max(f.n - f.p0, 0), to = a.window > 0 ? kKeys : min(kKeys, f.n + a.n_nodes - f.p0);
-#pragma unroll 1
-        for (int r = row0 + (from - row0 + kPass - 1) / kPass * kPass; r < to; r += kPass) {
-          if (r < from) continue;
-          int which;
-          const uint64_t bit = apart(f, r, which);
-          if (!bit || !((f.valid[r >> 5] >> (r & 31)) & 1)) continue;
-          uint4* p = reinterpret_cast<uint4*>(smem + at + chunk_at(r, ch, kKeys));
-          uint4 x = *p;
-          uint32_t* y = reinterpret_cast<uint32_t*>(&x);
-          bool any = false;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (not_finite<T>(y[i], 0)) y[i] &= 0xffff0000u, any = true;
-            if (not_finite<T>(y[i], 1)) y[i] &= 0x0000ffffu, any = true;
-          }
-          if (any) {
-            *p = x;
-            atomicOr(&bad[which], bit);
-          }
-        }
-        tc::fence_async_smem();
-        tc::mbar_arrive(&ctl.full[e % kEntries]);
-      };
       do {
         for (int t = 0; t < w.cnt; ++t, ++tile) {
           placed(tile);
@@ -1255,7 +1280,10 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
               copy16(dst + chunk_at(row0 + (i0 + i) * kPass, ch, kKeys), src + (o[i] < 0 ? 0 : o[i]), o[i] >= 0);
           }
           if (__builtin_expect(kv && (f.flags & 1), 0)) {
-            spoils(e, f);
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            clean_values<T, kKeys, kPass>(smem + S::kQs * S::kQBytes + (e % kEntries) * S::kEntry, f, ctl.bad[f.flags >> 1], a.window, a.n_nodes, row0, ch);
+            tc::fence_async_smem();
+            tc::mbar_arrive(&ctl.full[e % kEntries]);
           } else {
             // the thread arrives when its copies have landed
             asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tc::smem_u32(&ctl.full[e % kEntries])) : "memory");
@@ -1270,38 +1298,15 @@ __global__ void __launch_bounds__(Shape<D, E8, WIDE>::kThreads, 1) attn_kernel(A
       constexpr int kStages = S::kStages;
       const int row0 = pt / kCh, ch = pt % kCh;
       unsigned char* stages = smem + S::kQs * S::kQBytes + kEntries * S::kEntry + pt * 16;
-      // a value that is no number, where rows attend to it differently, becomes zero and a mark (a scale that is
-      // none is in the column of scores, masked like those)
-      auto spoils = [&](unsigned char* from, const Info& f) {
-        unsigned long long* bad = ctl.bad[f.flags >> 1];
-#pragma unroll 1
-        for (int i = 0; i < kEach; ++i) {
-          const int r = row0 + i * kPass;
-          if (a.window == 0 && (i + 1) * kPass <= f.n - f.p0) continue;  // no nodes there
-          int k;
-          const uint64_t bit = (f.valid[r >> 5] >> (r & 31)) & 1 ? apart(f, r, k) : 0;
-          if (!bit) continue;
-          uint4 z = *reinterpret_cast<const uint4*>(from + i * kN * 16);
-          uint32_t* y = reinterpret_cast<uint32_t*>(&z);
-          bool any = false;
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int b = 0; b < 32; b += 8)
-              if (((y[j] >> b) & 0x7f) == 0x7f) y[j] &= ~(0xffu << b), any = true;
-          if (any) {
-            *reinterpret_cast<uint4*>(from + i * kN * 16) = z;
-            atomicOr(&bad[k], bit);
-          }
-        }
-        __syncwarp();
-      };
       auto put = [&](uint32_t e, const uint8_t* fac, bool check, const Info& f) {
         wait(ctl, &ctl.staged[e % kStages], (e / kStages) & 1);
         if (e >= kEntries) wait(ctl, &ctl.empty[e % kEntries], (e / kEntries - 1) & 1);
         __syncwarp();
         unsigned char* from = stages + (e % kStages) * (S::kEntry / 2);
-        if (__builtin_expect(check, 0)) spoils(from, f);  // (a row's lanes are in one warp)
+        if (__builtin_expect(check, 0)) {
+          clean_codes<kEach, kPass, kN>(from, f, ctl.bad[f.flags >> 1], a.window, a.n_nodes, row0);
+          __syncwarp();  // (a row's lanes are in one warp)
+        }
         unsigned char* dst = smem + S::kQs * S::kQBytes + (e % kEntries) * S::kEntry;
         // 8 codes from each half of the row: their chunks of the ring meet no bank twice
         constexpr int kAtOnce = kEach < 4 ? kEach : 4;
