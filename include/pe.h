@@ -518,7 +518,9 @@ pe_status pe_decode_attn(const pe_kv_cache* cache, const void* q, int64_t q_seq_
  * each row (position and head) of keys and of values, at
  * page * page_stride + slot * slot_stride + head * head_stride.  Byte b stands
  * for 2^(b - 127); 255 for NaN; bytes below 63 count as 63, others above 247 as
- * 247.  A row's elements are its codes times its scale.
+ * 247.  A row's elements are its codes times its scale, and it counts in attention by its own scale,
+ * whatever the others' are; only where the scales of attended values lie more than 2^100
+ * apart, weights of the smaller ones may be missing from a sum.
  * Used by the calls below, which take a 16-bit cache with NULL in its place.
  * An 8-bit cache's k and v are 16-byte aligned and its strides multiples of
  * 16; the calls above refuse it. */
@@ -546,7 +548,11 @@ pe_status pe_kv_append_at(const pe_kv_cache* cache, const pe_kv_scales* scales, 
 
 /* pe_decode_attn over an 8-bit cache; q and out are of `dtype` (PE_BF16 or
  * PE_F16).  A position whose key or value scale is 255 makes the output of the
- * heads that attend to it NaN (a key's the log sum too; a value's may). */
+ * heads that attend to it NaN (a key's the log sum too; a value's may).  Up to 24
+ * heads a key head (head_dim 64: 32; 256: 16) weights enter the sum of values as two
+ * fp16 numbers, beyond that as described at pe_tree_attn.
+ * Errors: PE_EINVAL (beyond those heads also where a CTA's positions could pass 2^31),
+ * PE_ECUDA; beyond those heads a wait on the device that gave up is reported by pe_device_check. */
 int64_t pe_decode_attn8_workspace_bytes(const pe_kv_cache* cache, int32_t n_q_heads);
 pe_status pe_decode_attn8(const pe_kv_cache* cache, const pe_kv_scales* scales, int32_t dtype, const void* q,
                           int64_t q_seq_stride, int64_t q_head_stride, int32_t n_q_heads, const int32_t* lens,
@@ -579,9 +585,10 @@ typedef struct pe_tree_queries {
  * slots that are not attended to as in pe_decode_attn, for each node by
  * itself: a row that does not attend to a node does not see what that holds.
  * Weights enter the sum of values as two numbers of 16 bits (bf16 cache: bf16, others:
- * fp16, where one below 2^-30 of the largest may count as 0), with bf16 queries over
- * an 8-bit cache and more than 24 rows (16 of head_dim 256) of nodes and heads a key head
- * as one fp16 number.  An attended value
+ * fp16, where one below 2^-30 of the largest may count as 0).  Over an 8-bit cache, with more than
+ * 24 rows of nodes and heads a key head (head_dim 64: 32; 256: 16), bf16 queries' weights are one
+ * fp16 number, and one that times its value's scale is below 2^-27 of the largest such product
+ * may count as 0.  An attended value
  * that is not finite leaves its element not finite (an infinite one may become
  * NaN); a scale of 255 makes the node's output NaN.
  *  strides in elements, multiples of 8, 16-byte aligned; window 0 or >= 64.

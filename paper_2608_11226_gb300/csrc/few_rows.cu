@@ -8,14 +8,14 @@ pe_status few_rows8_launch(const DecodeArgs& a, int dtype, void* ws, cudaStream_
 
 // Which kernel takes a tree: this one up to as many rows as one warp holds (over 8 bits
 // of head_dim 256 two), the one of tiles (tree_attn.cuh) beyond.  Measured with 8 key heads, 8 sequences of
-// 32,640 positions, this against that: 8 bits, head_dim 128, 8 rows 92 against 230
-// us, 16 rows 112, 24 rows 181 (2 sequences of 512: 9.9, 12.7, 16.2 against 13.8);
-// head_dim 64, 24 rows 98, 32 rows 124 against 208 (64 sequences of 2,048: 73, 98 against 157;
-// 2 of 512: 12.3, 13.9 against 13.1); head_dim 256, 8 rows 171 against 354, 16 rows 211.
-// 16 bits, head_dim 128, 8 rows 165 against 182, 16 rows 171 (64 sequences of 2,048: 96
-// against 117), 24 rows 175 against 181 (111 against 118; 2 of 512: 16.2 against 13.0);
-// head_dim 64, 24 rows 98, 32 rows 111 against 156 (69, 85 against 102; 12.1, 13.3 against
-// 12.0); head_dim 256, 8 rows 319 against 336.
+// 32,640 positions, this against that: 8 bits, head_dim 128, 8 rows 93 against 228
+// us, 16 rows 112, 24 rows 180 (64 sequences of 2,048: 60, 78, 128 against 158; 2 of 512: 10.0, 13.0,
+// 16.4 against 14.8); head_dim 64, 24 rows 98, 32 rows 123 against 172 (73, 98 against 135; 12.7,
+// 14.4 against 13.7); head_dim 256, 8 rows 172 against 378, 16 rows 210.
+// 16 bits, head_dim 128, 8 rows 166 against 179, 16 rows 171 (64 sequences of 2,048: 91, 96
+// against 112), 24 rows 175 against 181 (111 against 112; 2 of 512: 16.2 against 13.0);
+// head_dim 64, 24 rows 98, 32 rows 112 against 149 (69, 85 against 95; 12.2, 13.5 against
+// 11.7); head_dim 256, 8 rows 316 against 337.
 bool few_rows(const pe_kv_cache& c, int n_nodes, int n_q_heads) {
   const int rows = n_nodes * (n_q_heads / c.n_heads);
   const bool eight = c.dtype == PE_E4M3;

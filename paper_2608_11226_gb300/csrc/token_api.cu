@@ -156,11 +156,11 @@ pe_status pe_tree_attn(const pe_kv_cache* cache, const pe_kv_scales* scales, con
 
 // Whether one token's heads of a key head are enough for tiles of 128 rows.  Measured
 // over 8 bits, 8 key heads, 8 sequences of 32,640 positions, the one-token kernel
-// against tiles: head_dim 128, 16 heads 109 against 229 us, 24 heads 153 against 229,
-// 32 heads 281 against 228, 64 heads 400 against 234; head_dim 64, 24 heads 94 against
-// 204, 32 heads 114 against 204, 64 heads 236 against 213; head_dim 256, 16 heads 209
-// against 356, 24 heads 446 against 352.  (Short sequences are latency: 2 of 512,
-// 32 heads of 128, 12.3 against 13.8.)
+// against tiles: head_dim 128, 16 heads 109 against 227 us, 24 heads 153 against 227,
+// 32 heads 281 against 226, 64 heads 400 against 229; head_dim 64, 24 heads 94 against
+// 170, 32 heads 114 against 170, 64 heads 236 against 171; head_dim 256, 16 heads 208
+// against 378, 24 heads 446 against 377.  (Short sequences are latency: 2 of 512,
+// 32 heads of 128, 12.3 against 13.4.)
 static bool many_heads(const pe_kv_cache& c, int n_q_heads) { return n_q_heads / c.n_heads > (c.head_dim == 256 ? 16 : c.head_dim == 64 ? 32 : 24); }
 
 static int64_t decode8_ws_bytes(const pe_kv_cache& c, int n_q_heads) {

@@ -4,7 +4,7 @@
 // A sequence's new tokens and the query heads of a key head are the rows of one
 // matrix, so keys and values are read once for all of them: S = Q K^T and
 // O += P V are products of 128 rows with tiles of kKeys positions.  Up to 128
-// rows the cache's bytes bound it (bf16, head_dim 128: 1,024 clk of products against
+// rows the cache's bytes bound it (bf16, head_dim 128: 1,536 clk of products against
 // 2,790 of HBM for 128 positions), beyond 256 the products and the exponentials do.
 //
 // One CTA on an SM.  Tiles of all (sequence, key head, block of rows) segments
@@ -27,12 +27,12 @@
 //          stages through registers, where codes become fp16
 // A role's code is kept short: together they pass the instruction cache, which was
 // what cost most (whole tiles without masks, loops not unrolled: 549 to 510 us for 512
-// rows over 8 bits).  Tensor copies of a page's rows in place of cp.async gave nothing
+// rows over 8 bits; what rarely runs in functions of its own: 483 to 416).  Tensor copies of a page's rows in place of cp.async gave nothing
 // for 16 bits; a bulk copy for each row of 8 bits took 36 clk each (524 us for 208 with 32
-// rows and 32,640 positions).  There a tile takes 3.4 k clk: a scale warp's loop, 1.6 k of
+// rows and 32,640 positions).  There a tile takes 3.7 k clk: a scale warp's loop, 1.6 k of
 // it copies at the rate of cp.async (22 clk an instruction of a warp), and next to it
 // 2.9 k of widening.  Up to 64 rows the softmax needs four warps; the others as widening
-// warps (235 us) or copying apart from the scales (229) made it slower, and so did more
+// warps (235 us for 208) or copying apart from the scales (229) made it slower, and so did more
 // copies at once: what they share is the path to shared memory.
 //   Wide (more than 128 rows in a block): each warpgroup has 128 rows of its own,
 //     whose products run while the other works on its weights; P replaces S.  (Tiles of
@@ -42,9 +42,9 @@
 //     each (they exchange the maxima), and S, which P replaces, has two buffers.
 //
 // Measured, 8 sequences of 32,640 positions, 8 key heads: 16 bits, head_dim 128, 128
-// rows a key head 184 us (5.8 TB/s, 86% of the copy rate), 256 rows 242; head_dim 256, 128
-// rows 344 (92%).  8 bits, head_dim 128, 128 rows 239 us, 256 rows 356: there the
-// warps that widen codes and the softmax set the pace (issue active 33%, a quarter
+// rows a key head 194 us (5.5 TB/s, 81% of the copy rate), 256 rows 293; head_dim 256, 128
+// rows 366 (87%).  8 bits, head_dim 128, 128 rows 249 us, 256 rows 315: there the
+// warps that widen codes and the softmax set the pace (issue active 35%, 14%
 // of the stalls for instructions).
 //
 // An 8-bit row is its codes times 2^e.  Where rows attend differently, or scales lie far
@@ -52,7 +52,7 @@
 // column of scores and a value's exponent is added to it, so that the running maximum is
 // that of weight times scale, and the sum of the weights takes the value's scale out again.  A row's
 // scale so counts for that row alone, and for those who attend to it.  Reading three numbers a
-// column for every row is dear (256 rows, 8 sequences of 32,640 positions: 458 us for 318), so
+// column for every row is dear (256 rows, 8 sequences of 32,640 positions: 564 us for 314), so
 // where everyone attends to the whole tile and its exponents are close to the largest, E, codes become
 // fp16 as code * 2^(e - E), which is exact, and 2^E goes into the exponentials' argument: keys within
 // 14 of E, values within 5, because E stands for their exponents in the running maximum.
@@ -63,10 +63,11 @@
 // fp16 and 8 bits), which leave 2^-18 (fp16: 2^-24) of a weight, as on the one-token kernel: the
 // result is as exact as its own rounding for any number of rows.  (One number alone: 2.0e-3
 // in the relative 2-norm for 1.6e-3 in bf16, 2.8e-4 for 2.1e-4 in fp16.)  Both parts lie where the
-// scores of their keys were.  The second product and the splitting cost 2% with 128 rows
-// of head_dim 128 (16 bits, 8 sequences of 32,640 positions), 18% of head_dim 64, 22% with 256 rows.
-// With bf16 queries over 8 bits P is one fp16 number: off by 2^-12 at most, an eighth
-// of what the result's rounding may be off by (a low part would cost 13-22% there).
+// scores of their keys were.  The second product and the splitting cost, with 8 sequences of
+// 32,640 positions and 128 rows over 16 bits, 127 to 153 us (head_dim 64), 184 to 194 (128), 350 to 366
+// (256), and 237 to 293 with 256 rows of 128.
+// With bf16 queries over 8 bits P is one fp16 number: off by 2^-12 of a weight at most, where the
+// result's rounding is off by up to 2^-8 (the low part costs fp16 queries 249 to 299 us, 256 rows 315 to 423).
 // Sums of weights are of the fp32 weights.
 //
 // Weights are relative to a running maximum that follows only when it is passed

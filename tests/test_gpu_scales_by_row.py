@@ -8,9 +8,11 @@ row j, p_j its share of the weights):
     e_j and taking it out again rounds sums of up to 192 (|e| <= 120, |z| <= 72
     here) three times, 2^-17 each in powers of two;
   weights are rounded to fp16, 2^-11, and exponentials and sums are off by 2^-14;
-    of a weight times scale below 2^-30 of the largest, 448 codes may be missing:
+    where a weight times its scale is below 2^-27 of the largest, 448 codes may be missing
+    (fp16 keeps 2^-25 of numbers that start at 2^7; a tile's common factor may exceed a
+    row's scale by 2^5):
     |out - ref| <= u |ref| + (2 ds + 2^-11 + 2^-14 + 3 * 2^-17) sum_j p_j |v_j|
-                   + n 2^-30 448 max_j p_j t_j
+                   + n 2^-27 448 max_j p_j t_j
     |lse - ref| <= ds + 3 * 2^-17 + 2^-18 (1 + |ref|)
 """
 import pytest
@@ -50,7 +52,7 @@ def attend(P, q, lens, scale, window, masks=None):
                 p = torch.softmax(z, -1)
                 lse[b, i, hs], out[b, i, hs] = torch.logsumexp(z, -1), p @ v[:, h]
                 ds = 2.0 ** -20 * abs(scale) * (qs.abs() @ k[:, h].abs().T).amax(-1)
-                lost = len(where) * 2.0 ** -30 * 448 * (p * vs[:, h]).amax(-1)
+                lost = len(where) * 2.0 ** -27 * 448 * (p * vs[:, h]).amax(-1)
                 tol[b, i, hs] = (U[q.dtype] * out[b, i, hs].abs()
                                  + (2 * ds + 2.0 ** -11 + 2.0 ** -14 + 3 * 2.0 ** -17)[:, None] * (p @ v[:, h].abs()) + lost[:, None])
                 ltol[b, i, hs] = ds + 3 * 2.0 ** -17 + 2.0 ** -18 * (1 + lse[b, i, hs].abs())
@@ -165,3 +167,25 @@ def test_large_keys_and_small_queries(D, N, G, power):
         got.append((out, lse))
     assert torch.isfinite(got[0][0].float()).all()
     assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
+@pytest.mark.parametrize("D,N,G", [c for c in CALLS if c[0] * c[2] > 64 or c[1] > 20])
+@pytest.mark.parametrize("keys,values", [(0, 0), (5, 5), (14, 5), (15, 5), (14, 6), (15, 6), (3, 9)])
+def test_spreads_of_scales(D, N, G, keys, values):
+    """Scales within so many powers of two in every tile: either side of where a tile has one factor."""
+    page, H, lens = 16, 2, [300, 129]
+    P = base.Pool(2, 24, page, H, D, BF16, True, "slot", 6)
+    for s, spread in ((P.ks, keys), (P.vs, values)):
+        s.copy_(torch.randint(118 - spread // 2, 119 - spread // 2 + spread, s.shape, generator=base.gen(spread), device="cuda"))
+        s[:, :: page - 1] = torch.tensor([118 - spread // 2, 118 - spread // 2 + spread], device="cuda")[:, None].to(torch.uint8)
+    q = torch.randn((2, max(N, 1), G * H, D), generator=base.gen(1), device="cuda").to(BF16)
+    out, lse = torch.full_like(q, NAN), torch.full(q.shape[:-1], NAN, device="cuda")
+    t = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    masks = base.tree_masks(2, N, 3) if N else None
+    if N:
+        pe.tree_attn(P.cache, q, t, base.tensor_of(masks), out, lse=lse)
+    else:
+        pe.decode_attn(P.cache, q[:, 0], t, out[:, 0], lse=lse)
+    ro, rl, to, tl = attend(P, q, lens, D ** -0.5, 0, masks)
+    base.close(out, ro, to)
+    base.close(lse, rl, tl)
